@@ -46,6 +46,7 @@ extern "C" {
 
 #define STAND_DTYPE_F32 0
 #define STAND_DTYPE_BF16 1
+#define STAND_DTYPE_F16 2 /* stand_tree_attention and stand_kv_commit only */
 
 #define STAND_OK 0
 #define STAND_E_ARG (-1)       /* invalid argument or configuration */
@@ -294,6 +295,152 @@ int stand_profile_stages(stand_ctx* ctx, void* const* events);
  * anything was copied, which is how the tests reach the failure path; a negative value restores the default.
  * Larger values are clamped: a wait cannot be made unbounded. */
 int stand_set_wait_limit(int64_t polls);
+
+/* ---------------------------------------------------------------------------------------------------------
+ * Around the step: a paged cache of keys and values, attention of a draft tree over it, and the processing of
+ * the logits before stand_step.  (The paper runs its target model in a serving system; these are the operators
+ * such a system needs next to the step.)  They need no context.  One step of a decoding loop:
+ *
+ *   stand_tree_attention   per layer: the tree's nodes attend to the cache and to their ancestors
+ *   stand_process_logits   penalties, biases and grammar masks on the nodes' logits
+ *   stand_step             verification, update, drafting
+ *   stand_page_map         pages and slots for the n_emitted tokens whose keys are to be kept
+ *   stand_kv_commit        their keys and values, of all layers, into the cache
+ *
+ * The cache holds the text WITHOUT its last token: that one is the tree's root, whose keys are computed in the
+ * step.  The nodes of the accepted path (stand_last_path; n_emitted of them) then join the cache.
+ *
+ * The cache is a pool of `pages` pages of page_size tokens; block table row b lists the pages of sequence b in
+ * text order (entries past its length may be anything).  Slot s of the pool is token s % page_size of page
+ * s / page_size.  Problems found on the device never fault: see each entry. */
+
+/* The shapes of stand_tree_attention.  Strides are in elements; the innermost dimension (dim) is contiguous.
+ * Queries, keys and values of the nodes may be slices of one projection's output. */
+typedef struct {
+  int32_t B;          /* sequences, >= 1 */
+  int32_t N;          /* nodes per sequence, 1..STAND_MAX_NODES; up to 65536 when the mask is NULL */
+  int32_t heads_q;    /* query heads; query head h reads key head h / (heads_q / heads_kv) */
+  int32_t heads_kv;   /* key heads; divides heads_q */
+  int32_t dim;        /* 1..256 */
+  int32_t dtype;      /* STAND_DTYPE_* of q, k, v, cache and out */
+  int32_t page_size;  /* a multiple of 16, up to 4096 */
+  int32_t pages;      /* pages in the pool, >= 0 */
+  int32_t max_pages;  /* columns of the block table, >= 0 */
+  float scale;        /* scores are scale * q . k */
+  int64_t q_stride[3];      /* sequence, node, head */
+  int64_t kv_stride[3];     /* sequence, node, head (the nodes' keys and values alike) */
+  int64_t cache_stride[3];  /* page, head, token (both caches alike) */
+} stand_attention;
+
+/* Attention of all nodes of B draft trees over the cached text and the nodes' ancestors (Sec. 4.2's tree, Sec. 5:
+ * the target model scores all drafted tokens in one pass).  Row (b, u, h) attends to the first dev_len[b] tokens of
+ * sequence b's pages (dev_table [B, max_pages] int32) and to those nodes v <= u of its own tree whose bit is set in
+ * dev_mask [N, ceil(N/32)] uint32 (bit v % 32 of word v / 32 of row u; mask_stride words between the masks of two
+ * sequences, 0: all share one); dev_mask NULL: all nodes v <= u (a chain of drafted tokens, a prompt).
+ * dev_tree_tokens [B, N] int32 (may be NULL): a node below 0 was not drafted; its row is empty.
+ * Writes dev_out [B, N, heads_q, dim] and, if not NULL, dev_lse [B, N, heads_q] float: the natural log-sum-exp of the
+ * row's scaled scores.  An empty row (no visible key) gets zeros and -inf.  Keys and values that a row does not see
+ * do not enter it, whatever they hold.
+ * Scores, softmax statistics and sums are 32-bit floats.  dev_len is int64; a length below 0 counts as 0, one beyond
+ * max_pages * page_size as that; a table entry outside [0, pages) reads as a page of zeros.  dev_scratch: 256-byte
+ * aligned, stand_tree_attention_scratch_bytes (0: invalid shapes) of it; calls that may overlap need scratch of their
+ * own.  A bounded wait inside a kernel that runs out (never seen) gives NaN in every output. */
+size_t stand_tree_attention_scratch_bytes(const stand_attention* shape);
+int stand_tree_attention(const stand_attention* shape, const void* dev_q, const void* dev_k, const void* dev_v,
+                         const void* dev_cache_k, const void* dev_cache_v, const int32_t* dev_table,
+                         const int64_t* dev_len, const uint32_t* dev_mask, int64_t mask_stride,
+                         const int32_t* dev_tree_tokens, void* dev_scratch, size_t scratch_bytes, void* dev_out,
+                         float* dev_lse, void* cu_stream);
+
+/* The ancestor mask of a static tree, as stand_tree_attention reads it.  Host only.  host_mask [n, ceil(n/32)]:
+ * bit v of row u is set if v is u or lies above it.  STAND_E_ARG if the parent array is not a tree (parent[0] = -1,
+ * 0 <= parent[u] < u). */
+int stand_tree_mask(const int32_t* host_parent, int32_t n, uint32_t* host_mask);
+
+/* Pages and slots for new tokens.  Sequence b holds dev_len[b] tokens (int64) in the first ceil(len / page_size)
+ * entries of its table row and gets dev_new[b] (int32, 0..width) more.  The pages that this takes beyond those it
+ * has come from the free list, a stack of *dev_n_free page numbers in dev_free [capacity]: in the order of the
+ * sequences, then of the text, from the top down.  They are entered into dev_table [B, max_pages].
+ * dev_slots [B, width] int64: the slots of the new tokens, -1 past dev_new[b].
+ * A sequence is refused - its row of slots is -1, its table row and length stay - when dev_new[b] is outside
+ * [0, width], its length is negative, it would need more than max_pages pages, or the pages needed by all sequences
+ * up to and including it (those refused for the reasons before left out) are more than the list has while it needs
+ * one itself.  dev_granted [B] int32: dev_new[b], or -1 where it was refused.
+ * dev_len_out [B] int64, dev_n_free_out [1] int32: lengths and list size after the call.  They must not be the
+ * input arrays (blocks read those while others write); dev_granted, dev_len_out may be NULL. */
+int stand_page_map(const int64_t* dev_len, const int32_t* dev_new, int32_t B, int32_t width, int32_t page_size,
+                   int32_t max_pages, const int32_t* dev_free, int32_t capacity, const int32_t* dev_n_free,
+                   int32_t* dev_table, int64_t* dev_slots, int32_t* dev_granted, int64_t* dev_len_out, int32_t* dev_n_free_out,
+                   void* cu_stream);
+
+/* Gives the pages of finished sequences back: for every b with dev_done[b] != 0 the first ceil(len / page_size)
+ * entries of its table row are pushed on the free list (dev_free has room for `capacity` page numbers), in the order
+ * of the sequences, then of the text, and dev_len_out[b] is 0; other lengths are copied.  Pages that would not fit
+ * the list are dropped (then the list was not this pool's).  Output arrays must not be input arrays. */
+int stand_page_release(const int64_t* dev_len, const int32_t* dev_done, int32_t B, int32_t page_size,
+                       int32_t max_pages, const int32_t* dev_table, int32_t capacity, int32_t* dev_free,
+                       const int32_t* dev_n_free, int64_t* dev_len_out, int32_t* dev_n_free_out, void* cu_stream);
+
+/* The shapes of stand_kv_commit.  Strides are in elements, dim is contiguous; keys and values have the same. */
+typedef struct {
+  int32_t layers, B, N; /* N nodes per sequence in the source */
+  int32_t heads, dim, dtype;
+  int32_t page_size, pages;
+  int32_t width;           /* columns of dev_slots and dev_path */
+  int32_t reserved;        /* must be 0 */
+  int64_t src_stride[4];   /* layer, sequence, node, head */
+  int64_t cache_stride[4]; /* layer, page, head, token */
+} stand_kv_shape;
+
+/* Copies keys and values of chosen nodes into their slots, for all layers: row (l, b, dev_path[b, j], h) of dev_k and
+ * dev_v goes to slot dev_slots[b, j] (int64) of the caches.  dev_path [B, width] int32, or NULL: node j.  Places
+ * with a slot outside [0, pages * page_size) or a node outside [0, N) are skipped (-1 pads).  Slots of one call
+ * must be distinct; the source must not overlap the caches. */
+int stand_kv_commit(const stand_kv_shape* shape, const void* dev_k, const void* dev_v, const int32_t* dev_path,
+                    const int64_t* dev_slots, void* dev_cache_k, void* dev_cache_v, void* cu_stream);
+
+/* The shapes of stand_process_logits. */
+typedef struct {
+  int32_t B, N, V;        /* as in stand_config */
+  int32_t dtype;          /* STAND_DTYPE_F32 or _BF16 */
+  const int32_t* parent;  /* HOST, [N], the tree as in stand_config; read during the call only; NULL with N = 1 */
+  int64_t in_stride;      /* elements between rows of dev_in, >= V */
+  int64_t out_stride;     /* elements between rows of dev_out, >= V */
+  int32_t text_stride;    /* columns of dev_text, >= 0 */
+  int32_t masks;          /* rows of dev_mask */
+  int32_t biases;         /* entries of bias_id and bias_value */
+  int32_t reserved;       /* must be 0 */
+} stand_logits;
+
+/* The inputs of stand_process_logits; any pointer may be NULL (that part is left out). */
+typedef struct {
+  const int32_t* text;       /* [B, text_stride]: prompt and output tokens of each sequence, in order */
+  const int64_t* n_text;     /* [B]: how many of them there are (the last one is the tree's root) */
+  const int64_t* n_prompt;   /* [B]: how many of those belong to the prompt (NULL: none) */
+  const int32_t* tree_tokens; /* [B, N]: the drafted tokens (stand_draft_tree), -1: not drafted */
+  const float* repetition;   /* [B], > 0 */
+  const float* frequency;    /* [B] */
+  const float* presence;     /* [B] */
+  const int32_t* bias_start; /* [B + 1]: sequence b's biases are entries bias_start[b] .. bias_start[b + 1] - 1 */
+  const int32_t* bias_id;    /* tokens; of several entries for one token the last counts */
+  const float* bias_value;
+  const uint32_t* mask;      /* [masks, ceil(V / 32)]: bit t % 32 of word t / 32 set: token t is allowed */
+  const int32_t* mask_row;   /* [B, N]: the mask of each row, -1 (or outside [0, masks)): none */
+} stand_logits_inputs;
+
+/* Processes the logits of every node of every tree before stand_step: dev_in [B * N rows of V] to dev_out (the same
+ * pointer with the same stride: in place).  For token t in row (b, u), with the text of the sequence followed by the
+ * tokens on the path from below the root to u:
+ *   met(t): t occurs in it;  c(t): how often it does, the prompt left out.
+ *   x = met(t) ? (x > 0 ? x / repetition : x * repetition) : x
+ *   x = x - frequency * c(t) - presence * [c(t) > 0]
+ *   x = x + bias(t)
+ *   x = -inf where the row's mask does not allow t
+ * in 32-bit floats, rounded once.  Tokens outside [0, V) are left out of the counts.  A row whose mask allows
+ * nothing comes out as -inf throughout (stand_step then samples nothing meaningful from it).
+ * Masked logits may hold anything; the others are finite or -inf, as for stand_step. */
+int stand_process_logits(const stand_logits* shape, const stand_logits_inputs* inputs, const void* dev_in, void* dev_out,
+                         void* cu_stream);
 
 /* How many kernels the library has launched through this context so far. */
 uint64_t stand_launch_count(const stand_ctx* ctx);

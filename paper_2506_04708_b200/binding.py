@@ -13,7 +13,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libstand.so")
 
 STAND_MAX_TOPK, STAND_MAX_ORDER, STAND_MAX_NODES = 12, 4, 640
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 
 EXPORTS = [
     "stand_workspace_bytes", "stand_init", "stand_destroy", "stand_reset_sequences", "stand_verify_tree",
@@ -23,6 +23,8 @@ EXPORTS = [
     "stand_last_path", "stand_tree_depth", "stand_table_dump", "stand_table_load", "stand_state_dump",
     "stand_state_load", "stand_profile_row_pass", "stand_profile_stages", "stand_node_accepts", "stand_prune_tree",
     "stand_initial_tree", "stand_launch_count", "stand_set_wait_limit", "stand_strerror",
+    "stand_tree_attention_scratch_bytes", "stand_tree_attention", "stand_tree_mask", "stand_page_map",
+    "stand_page_release", "stand_kv_commit", "stand_process_logits",
 ]
 
 
@@ -41,6 +43,36 @@ class StandStats(C.Structure):
         ("drops", C.c_uint64), ("bad_tokens", C.c_uint64), ("lookups", C.c_uint64),
         ("lookup_hits", C.c_uint64 * STAND_MAX_ORDER), ("max_probe_seen", C.c_uint64), ("wait_timeouts", C.c_uint64),
     ]
+
+
+class StandAttention(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("N", C.c_int32), ("heads_q", C.c_int32), ("heads_kv", C.c_int32), ("dim", C.c_int32),
+        ("dtype", C.c_int32), ("page_size", C.c_int32), ("pages", C.c_int32), ("max_pages", C.c_int32),
+        ("scale", C.c_float), ("q_stride", C.c_int64 * 3), ("kv_stride", C.c_int64 * 3), ("cache_stride", C.c_int64 * 3),
+    ]
+
+
+class StandKvShape(C.Structure):
+    _fields_ = [
+        ("layers", C.c_int32), ("B", C.c_int32), ("N", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32),
+        ("dtype", C.c_int32), ("page_size", C.c_int32), ("pages", C.c_int32), ("width", C.c_int32),
+        ("reserved", C.c_int32), ("src_stride", C.c_int64 * 4), ("cache_stride", C.c_int64 * 4),
+    ]
+
+
+class StandLogits(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("N", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32), ("parent", C.c_void_p),
+        ("in_stride", C.c_int64), ("out_stride", C.c_int64), ("text_stride", C.c_int32), ("masks", C.c_int32),
+        ("biases", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
+class StandLogitsInputs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in (
+        "text", "n_text", "n_prompt", "tree_tokens", "repetition", "frequency", "presence", "bias_start", "bias_id",
+        "bias_value", "mask", "mask_row")]
 
 
 class StandError(RuntimeError):
@@ -108,6 +140,20 @@ def lib():
     L.stand_set_wait_limit.restype = C.c_int
     L.stand_strerror.argtypes = [C.c_int]
     L.stand_strerror.restype = C.c_char_p
+    L.stand_tree_attention_scratch_bytes.restype = C.c_size_t
+    L.stand_tree_attention_scratch_bytes.argtypes = [C.POINTER(StandAttention)]
+    L.stand_tree_attention.restype = C.c_int
+    L.stand_tree_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, C.c_size_t, vp, vp, vp]
+    L.stand_tree_mask.restype = C.c_int
+    L.stand_tree_mask.argtypes = [vp, i32, vp]
+    L.stand_page_map.restype = C.c_int
+    L.stand_page_map.argtypes = [vp, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.stand_page_release.restype = C.c_int
+    L.stand_page_release.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]
+    L.stand_kv_commit.restype = C.c_int
+    L.stand_kv_commit.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    L.stand_process_logits.restype = C.c_int
+    L.stand_process_logits.argtypes = [vp, vp, vp, vp, vp]
     for name in ["stand_init", "stand_destroy", "stand_reset_sequences", "stand_verify_tree", "stand_ngram_update",
                  "stand_ngram_update_bulk", "stand_draft_tree", "stand_step", "stand_step_host", "stand_row_stats",
                  "stand_get_stats", "stand_last_path", "stand_table_dump", "stand_table_load", "stand_state_dump",

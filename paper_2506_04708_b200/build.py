@@ -25,7 +25,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and up_to_date():
         return LIB
     cmd = [NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-           "--fmad=true", "-Xcompiler", "-fPIC", "-shared", "-o", LIB] + sources()
+           "--fmad=true", "--threads", "0", "-Xcompiler", "-fPIC", "-shared", "-o", LIB] + sources()
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")

@@ -1,0 +1,57 @@
+// Attention of draft trees over a paged cache: what the kernels share.
+//
+// Row r of a (sequence b, key head g) pair is node u = r / G under query head g * G + r % G, G = heads_q / heads_kv:
+// all rows of the pair read the same keys and values, so they are read once for all of them.  The keys in order are
+// the len cached positions, then the tree's nodes; node u sees all of the former and, of the latter, those its mask
+// names.  With s = scale * log2(e) * q.k the softmax is carried as the running maximum m and the sums l = sum 2^(s-m)
+// and o = sum 2^(s-m) v, all in fp32, so that pieces of the keys can be joined: with M = max m_i,
+// o = sum 2^(m_i - M) o_i, l likewise; the result is o / l and lse = ln 2 (M + log2 l).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace stand {
+
+struct AttnParams {
+  const char* q;
+  const char* k;
+  const char* v;
+  const char* cache_k;
+  const char* cache_v;
+  const int* table;
+  const long long* len;
+  const uint32_t* mask;
+  long long mask_stride;
+  const int* tree;
+  char* out;
+  float* lse;
+  int B, N, heads_q, heads_kv, group, dim, page, pages, cols, mask_words;
+  float scale2;  // scale * log2(e)
+  long long q_stride[3], kv_stride[3], cache_stride[3];  // elements
+};
+
+template <typename T> __device__ __forceinline__ float to_float(T v);
+template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_float<__half>(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+// Cached tokens of sequence b that count.
+__device__ __forceinline__ long long attn_len(const AttnParams& p, int b) {
+  const long long n = p.len[b], most = (long long)p.cols * p.page;
+  return n < 0 ? 0 : (n > most ? most : n);
+}
+
+// Does node u of sequence b see node v?
+__device__ __forceinline__ bool attn_sees(const AttnParams& p, int b, int u, int v) {
+  if (v > u) return false;
+  return !p.mask || (p.mask[b * p.mask_stride + (long long)u * p.mask_words + (v >> 5)] >> (v & 31) & 1u);
+}
+
+}  // namespace stand

@@ -16,6 +16,7 @@
 // takes one chunk of every tile.  The inner loop has no branches: packed bf16 max, packed fp32 FMA/ADD,
 // one ex2 per entry.
 #pragma once
+#include "async.cuh"
 #include "common.cuh"
 
 namespace stand {
@@ -31,7 +32,6 @@ template <int DT> constexpr int k1_stage_bytes() { return K1Shape<DT>::CW * CHUN
 template <int DT> constexpr int k1_smem_bytes() {
   return (2 * K1_SMEM_DATA / K1_CTAS / k1_stage_bytes<DT>()) * k1_stage_bytes<DT>();
 }
-constexpr unsigned SPIN_LIMIT = 1u << 22;                  // bounded waits: about a second, then the kernel gives up
 
 constexpr int COMPACT_AT = 64;              // candidate count that triggers a compaction
 constexpr int CAND_CAP = COMPACT_AT + 256;  // a warp adds at most 32 lanes x 8 entries between checks
@@ -173,37 +173,7 @@ __device__ __forceinline__ float2 reduce_chunk(const uint4 (&v)[NV], float c) {
   return make_float2(warp_sum_f(a + b), cm);
 }
 
-// ---- mbarrier / bulk-copy primitives ---------------------------------------------
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded wait; false if the limit ran out or another thread of the CTA already gave up.
-__device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity, const volatile int* abort_flag,
-                                                  unsigned limit = SPIN_LIMIT) {
-  for (unsigned spin = 0; spin < limit; ++spin) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
-  }
-  return false;
-}
+// ---- bulk-copy primitives ----------------------------------------------------------
 __device__ __forceinline__ unsigned long long l2_evict_first_policy() {
   unsigned long long pol;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));

@@ -11,6 +11,7 @@
 
 #include "common.cuh"
 #include "draft.cuh"
+#include "launch.cuh"
 #include "row_pass.cuh"
 #include "table.cuh"
 #include "tail.cuh"
@@ -127,18 +128,12 @@ struct stand_ctx {
 
 namespace {
 
-int cuda_ok(cudaError_t e) { return e == cudaSuccess ? STAND_OK : STAND_E_CUDA; }
-int launch_ok() { return cuda_ok(cudaGetLastError()); }
-
 float log2e_over_T(float T) { return (float)(1.4426950408889634 / (double)T); }
 
 bool rows_aligned(const void* base, int V, int dtype) {
   const size_t es = esize_of(dtype);
   return ((uintptr_t)base % 16 == 0) && (((size_t)V * es) % 16 == 0);
 }
-
-template <typename P>
-int launch_dependent(void (*kernel)(P), unsigned grid, unsigned block, cudaStream_t st, const P& params, size_t smem = 0);
 
 // The streaming kernel needs more dynamic shared memory than the default limit: raise it once per device.
 constexpr int MAX_DEVICES = 64;
@@ -224,24 +219,7 @@ int launch_row_pass(const void* logits, long long rows, int V, int dtype, int n_
   return launch_ok();
 }
 
-// Launch with programmatic stream serialisation: the kernel may be scheduled while its predecessor in the
-// stream is still running; it calls pdl_wait() before it touches the predecessor's results.
-template <typename P>
-int launch_dependent(void (*kernel)(P), unsigned grid, unsigned block, cudaStream_t st, const P& params, size_t smem) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cuda_ok(cudaLaunchKernelEx(&cfg, kernel, params));
-}
-
-// The same, as one thread-block cluster of `grid` blocks.
+// launch_dependent, as one thread-block cluster of `grid` blocks.
 template <typename P>
 int launch_dependent_cluster(void (*kernel)(P), unsigned grid, unsigned block, cudaStream_t st, const P& params, size_t smem) {
   cudaLaunchConfig_t cfg = {};
