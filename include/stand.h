@@ -291,7 +291,7 @@ int stand_profile_stages(stand_ctx* ctx, void* const* events);
  * runs out the kernel records it, lets its copies in flight land and returns, and the host sees
  * stand_stats.wait_timeouts (or NaN / -1 results from stand_row_stats): the GPU context stays usable.  This
  * call sets, for the whole process, how many polls the kernel's loader spends waiting for a free stage of its
- * shared-memory ring: 1 .. 2^22 (the default, about a second); 0 makes its very first wait give up before
+ * shared-memory ring, and every wait of stand_tree_attention: 1 .. 2^22 (the default, about a second); 0 makes its very first wait give up before
  * anything was copied, which is how the tests reach the failure path; a negative value restores the default.
  * Larger values are clamped: a wait cannot be made unbounded. */
 int stand_set_wait_limit(int64_t polls);
@@ -325,8 +325,8 @@ typedef struct {
   int32_t dtype;      /* STAND_DTYPE_* of q, k, v, cache and out */
   int32_t page_size;  /* a multiple of 16, up to 4096 */
   int32_t pages;      /* pages in the pool, >= 0 */
-  int32_t max_pages;  /* columns of the block table, >= 0 */
-  float scale;        /* scores are scale * q . k */
+  int32_t max_pages;  /* columns of the block table, >= 0; max_pages * page_size <= 2^30 */
+  float scale;        /* scores are scale * q . k; > 0 */
   int64_t q_stride[3];      /* sequence, node, head */
   int64_t kv_stride[3];     /* sequence, node, head (the nodes' keys and values alike) */
   int64_t cache_stride[3];  /* page, head, token (both caches alike) */
@@ -344,7 +344,8 @@ typedef struct {
  * Scores, softmax statistics and sums are 32-bit floats.  dev_len is int64; a length below 0 counts as 0, one beyond
  * max_pages * page_size as that; a table entry outside [0, pages) reads as a page of zeros.  dev_scratch: 256-byte
  * aligned, stand_tree_attention_scratch_bytes (0: invalid shapes) of it; calls that may overlap need scratch of their
- * own.  A bounded wait inside a kernel that runs out (never seen) gives NaN in every output. */
+ * own.  If a bounded wait inside the kernel runs out (never seen; stand_set_wait_limit), every output that depended on
+ * it is NaN. */
 size_t stand_tree_attention_scratch_bytes(const stand_attention* shape);
 int stand_tree_attention(const stand_attention* shape, const void* dev_q, const void* dev_k, const void* dev_v,
                          const void* dev_cache_k, const void* dev_cache_v, const int32_t* dev_table,

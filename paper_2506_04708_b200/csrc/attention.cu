@@ -2,11 +2,13 @@
 #include "../../include/stand.h"
 
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdint.h>
 #include <string.h>
 
 #include "attention.cuh"
 #include "attention_plain.cuh"
+#include "attention_tensor.cuh"
 #include "launch.cuh"
 
 using namespace stand;
@@ -19,7 +21,7 @@ bool attention_valid(const stand_attention* c) {
   if (!c || c->B < 1 || c->N < 1 || c->N > MOST_CHAIN || c->heads_kv < 1 || c->heads_q < 1 || c->heads_q % c->heads_kv != 0) return false;
   if (c->dim < 1 || c->dim > ATTN_DIM_MAX || c->dtype < STAND_DTYPE_F32 || c->dtype > STAND_DTYPE_F16) return false;
   if (c->page_size < 16 || c->page_size > 4096 || c->page_size % 16 != 0 || c->pages < 0 || c->max_pages < 0) return false;
-  if (!(c->scale == c->scale) || c->heads_q > 65535) return false;
+  if (!(c->scale > 0.0f && c->scale < INFINITY) || c->heads_q > 65535 || (long long)c->max_pages * c->page_size > (1ll << 30)) return false;
   if ((long long)c->N * (c->heads_q / c->heads_kv) >= (1ll << 20) || (long long)c->B * c->heads_kv > (1ll << 24)) return false;
   for (int i = 0; i < 3; ++i)
     if (c->q_stride[i] < 0 || c->kv_stride[i] < 0 || c->cache_stride[i] < 0) return false;
@@ -32,7 +34,7 @@ extern "C" {
 
 size_t stand_tree_attention_scratch_bytes(const stand_attention* c) {
   if (!attention_valid(c)) return 0;
-  return 256;
+  return tensor_scratch_bytes(c->N * (c->heads_q / c->heads_kv), c->dim);
 }
 
 int stand_tree_attention(const stand_attention* c, const void* dev_q, const void* dev_k, const void* dev_v, const void* dev_cache_k,
@@ -52,6 +54,18 @@ int stand_tree_attention(const stand_attention* c, const void* dev_q, const void
   p.scale2 = (float)((double)c->scale * 1.4426950408889634);
   for (int i = 0; i < 3; ++i) { p.q_stride[i] = c->q_stride[i]; p.kv_stride[i] = c->kv_stride[i]; p.cache_stride[i] = c->cache_stride[i]; }
   cudaStream_t st = (cudaStream_t)cu_stream;
+  if (tensor_takes(p, c->dtype)) {
+    int dev = -1, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return STAND_E_CUDA;
+    const int dp = tensor_dim(p.dim);
+    const bool bf = c->dtype == STAND_DTYPE_BF16;
+    const unsigned limit = wait_limit();
+    int rc;
+    if (dp == 64) rc = bf ? launch_tensor_attention<64, true>(p, dev_scratch, sms, limit, st) : launch_tensor_attention<64, false>(p, dev_scratch, sms, limit, st);
+    else if (dp == 128) rc = bf ? launch_tensor_attention<128, true>(p, dev_scratch, sms, limit, st) : launch_tensor_attention<128, false>(p, dev_scratch, sms, limit, st);
+    else rc = bf ? launch_tensor_attention<256, true>(p, dev_scratch, sms, limit, st) : launch_tensor_attention<256, false>(p, dev_scratch, sms, limit, st);
+    if (rc != STAND_E_ARG) return rc;  // strides that the copy unit cannot take: the other kernel
+  }
   if (c->dtype == STAND_DTYPE_F32) return launch_plain_attention<float>(p, st);
   if (c->dtype == STAND_DTYPE_BF16) return launch_plain_attention<__nv_bfloat16>(p, st);
   return launch_plain_attention<__half>(p, st);

@@ -10,6 +10,8 @@ namespace stand {
 inline int cuda_ok(cudaError_t e) { return e == cudaSuccess ? STAND_OK : STAND_E_CUDA; }
 inline int launch_ok() { return cuda_ok(cudaGetLastError()); }
 
+unsigned wait_limit();  // polls of a bounded wait (stand_set_wait_limit)
+
 // Raises a kernel's limit of dynamic shared memory, once per device.
 struct SmemLimit {
   static constexpr int DEVICES = 64;

@@ -500,6 +500,10 @@ __global__ void export_records_entry(const ExportParams q) {
 
 }  // namespace
 
+namespace stand {
+unsigned wait_limit() { return g_empty_wait_limit.load(std::memory_order_relaxed); }
+}  // namespace stand
+
 extern "C" {
 
 size_t stand_workspace_bytes(const stand_config* cfg) {

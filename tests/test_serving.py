@@ -775,3 +775,17 @@ def test_logits_binding_refuses_wrong_tensors():
                dict(tree_tokens=torch.zeros((2, 5), dtype=torch.int32, device="cuda:0"))):
         with pytest.raises(binding.StandError):
             op(x, **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("f16", 64), ("bf16", 256)])
+def test_a_wait_that_runs_out_gives_nan_and_leaves_the_gpu_usable(dtype, dim):
+    """The safe form: every wait of the kernel gives up before anything was copied.  The next call is right again."""
+    c = _attention_case(81, dtype, [0, 700, 64], 8, 8, 2, dim, 16, parent=inputs.topology(8, 4, 2))
+    binding.set_wait_limit(0)
+    try:
+        out, lse = _run_attention(c)
+    finally:
+        binding.set_wait_limit(-1)
+    assert np.isnan(out).all() and np.isnan(lse).all()
+    _check_attention(c, _run_attention(c))
