@@ -56,7 +56,6 @@ struct alignas(64) TaParams {
   int groups;
   int min_tiles;      // fewest tiles worth a group of their own
   int box_rows;       // rows of a page that one copy takes
-  int k_steps;        // steps of 16 over the head size
   int part_rows;      // rows of a piece in scratch
   long long tree_tiles;  // sum over the row blocks of a pair
   TaRecord* records;
@@ -77,14 +76,27 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ uint32_t elect_one() {  // 1 in one lane of the (whole) warp
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
 }
-// D (tensor memory, fp32) = or += A (tensor memory, 16 bit) * B (shared memory)
-__device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+// The whole warp calls these two, the elected lane acts: the operands then sit in uniform registers, where the unit wants
+// them.  (In a branch of one lane each product took 60 cycles to issue, most of it moving five operands there.)
+__device__ __forceinline__ void tc_commit(uint32_t bar, uint32_t elected) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+      "{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %1, 0;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(elected)
+      : "memory");
+}
+// D (tensor memory, fp32) = or += A (tensor memory, 16 bit) * B (shared memory).  The descriptor of B in two words: only
+// the low one changes, by an addition; one thread issues all products, so each instruction that it spends counts.
+__device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate,
+                                       uint32_t elected) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b64 b;\n\tmov.b64 b, {%2, %3};\n\tsetp.ne.u32 p, %5, 0;\n\tsetp.ne.u32 e, %6, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc),
+      "r"(accumulate), "r"(elected)
       : "memory");
 }
 // 32 columns of this warp's 32 lanes: one row per thread
@@ -114,9 +126,9 @@ __device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32]) 
 //   keys as rows (K: the head size is the summed dimension): stride 1024 between groups of eight keys;
 //   keys as the summed dimension (V: rows are the head size): stride 1024 between groups of eight keys, and `chunk`
 //   bytes between chunks of 64 of the head size.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t chunk) {
-  return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(chunk >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+// Low word: address and `chunk`, both in units of 16 bytes; high word: the stride, the version, the swizzle.
+__device__ __forceinline__ uint32_t smem_desc_lo(uint32_t addr, uint32_t chunk) { return (addr & 0x3FFFF) >> 4 | (chunk >> 4) << 16; }
+constexpr uint32_t SMEM_DESC_HI = (1024 >> 4) | 1u << 14 | 2u << 29;
 // Instruction descriptor: fp32 accumulator, both operands of type `bf16` or half, M = 128.
 __host__ __device__ constexpr uint32_t mma_desc(bool bf16, bool b_transposed, int n) {
   return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (b_transposed ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
@@ -131,6 +143,11 @@ __device__ __forceinline__ float ta_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 template <bool BF16> __device__ __forceinline__ uint32_t ta_pack(float lo, float hi) {
   uint32_t r;
@@ -312,21 +329,24 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
     }
   }
   const uint32_t tmem = s_tmem;
-  const volatile int* abort_flag = &s_abort;
-  auto wait = [&](const uint64_t& bar, uint32_t parity) {
-    if (mbar_wait_bounded(smem_addr(&bar), parity, abort_flag, p.wait_limit)) return true;
-    *const_cast<volatile int*>(abort_flag) = 1;
+  volatile int* abort_flag = &s_abort;
+  const unsigned limit = p.wait_limit;
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (limit && mbar_try_wait(bar, parity)) return true;
+    if (mbar_wait_bounded(bar, parity, abort_flag, limit)) return true;
+    *abort_flag = 1;
     return false;
   };
-
-  auto wait_warp = [&](const uint64_t& bar, uint32_t parity) { return (bool)__all_sync(FULL, wait(bar, parity)); };
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(FULL, wait(bar, parity)); };
+  const uint32_t bar_full = smem_addr(s_full), bar_empty = smem_addr(s_empty), bar_q = smem_addr(&s_q), bar_s = smem_addr(&s_s),
+                 bar_p = smem_addr(&s_p), bar_o = smem_addr(&s_o);
 
   if (warp == 4) {
     // ---- copies: a lane per box (rows of one page x 64 elements) -------------------------
     const int n_boxes = KT / p.box_rows;
     const int half = lane % HALVES, box = lane / HALVES;
     TaSeg s;
-    unsigned it = 0;
+    unsigned it = 0, slot = 0, phase = 1;  // phase: parity of the wait for the slot's last use
     bool ok = true;
     while (ok && walk.next(p, s)) {
       auto page_of = [&](int j) {  // the page that this lane's box of tile j lies in; -1: none
@@ -350,10 +370,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
         const int in_page = tree ? 0 : (j * KT + row) % p.a.page;
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv, ++it) {
-          const unsigned slot = it % Sh::SLOTS;
-          ok = wait_warp(s_empty[slot], ((it / Sh::SLOTS) & 1u) ^ 1u);
+          ok = wait_warp(bar_empty + 8 * slot, phase);
           if (!ok) break;
-          const uint32_t bar = smem_addr(&s_full[slot]);
+          const uint32_t bar = bar_full + 8 * slot;
           if (lane == 0) mbar_expect_tx(bar, bytes);
           __syncwarp();
           const uint32_t dst = ring + slot * Sh::SLOT + half * (KT * 128);
@@ -362,6 +381,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
           } else if (page >= 0) {
             tma_load_4d(dst + row * 128, kv ? &p.cache_v : &p.cache_k, bar, half * 64, in_page, s.g, page);
           }
+          if (++slot == Sh::SLOTS) slot = 0, phase ^= 1u;
         }
       }
     }
@@ -372,84 +392,105 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
     __syncwarp();
   } else if (warp == 5) {
     // ---- products -----------------------------------------------------------------------
-    if (lane == 0) {
-      constexpr uint32_t IDESC_S = mma_desc(BF16, false, KT), IDESC_O = mma_desc(BF16, true, DP);
-      TaSeg s;
-      unsigned it = 0, n = 0, n_seg = 0;
-      bool ok = true;
-      while (ok && walk.next(p, s)) {
-        if (s.begin >= s.end) continue;
-        ok = wait(s_q, n_seg & 1u);
-        for (int j = s.begin; ok && j < s.end; ++j, ++n) {
-          unsigned slot = it % Sh::SLOTS;
-          ok = wait(s_full[slot], (it / Sh::SLOTS) & 1u);
-          if (!ok) break;
-          tc_fence_after();
-          for (int k = 0; k < p.k_steps; ++k)
-            tc_mma(tmem + Sh::COL_S, tmem + Sh::COL_Q + k * 8, smem_desc(ring + slot * Sh::SLOT + (k >> 2) * (KT * 128) + (k & 3) * 32, 16),
-                   IDESC_S, k > 0);
-          tc_commit(smem_addr(&s_empty[slot]));
-          tc_commit(smem_addr(&s_s));
-          ++it;
-          slot = it % Sh::SLOTS;
-          ok = wait(s_p, n & 1u) && wait(s_full[slot], (it / Sh::SLOTS) & 1u);
-          if (!ok) break;
-          tc_fence_after();
+    constexpr uint32_t IDESC_S = mma_desc(BF16, false, KT), IDESC_O = mma_desc(BF16, true, DP);
+    TaSeg s;
+    uint32_t slot = 0, phase = 0, tile_phase = 0, seg_phase = 0;
+    const uint32_t elected = elect_one(), base = __shfl_sync(FULL, tmem, 0);
+    const uint32_t k_desc = smem_desc_lo(ring, 16), v_desc = smem_desc_lo(ring, KT * 128);
+    const uint32_t d_s = base + Sh::COL_S, d_o = base + Sh::COL_O, a_q = base + Sh::COL_Q;
+    bool ok = true;
+    while (ok && walk.next(p, s)) {
+      const int tiles = __shfl_sync(FULL, s.end - s.begin, 0);
+      if (tiles <= 0) continue;
+      ok = wait_warp(bar_q, seg_phase);
+      seg_phase ^= 1u;
+      for (int j = 0; ok && j < tiles; ++j, tile_phase ^= 1u) {
+        ok = wait_warp(bar_full + 8 * slot, phase);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t bk = k_desc + slot * (Sh::SLOT >> 4);
 #pragma unroll
-          for (int k = 0; k < KT / 16; ++k)
-            tc_mma(tmem + Sh::COL_O, tmem + Sh::COL_S + k * 8, smem_desc(ring + slot * Sh::SLOT + k * 2048, KT * 128), IDESC_O,
-                   j > s.begin || k > 0);
-          tc_commit(smem_addr(&s_empty[slot]));
-          ++it;
-          if (j + 1 == s.end) tc_commit(smem_addr(&s_o));
-        }
-        ++n_seg;
+        for (int k = 0; k < DP / 16; ++k)
+          tc_mma(d_s, a_q + k * 8, bk + (((k >> 2) * (KT * 128) + (k & 3) * 32) >> 4), SMEM_DESC_HI, IDESC_S, k > 0, elected);
+        tc_commit(bar_s, elected);
+        tc_commit(bar_empty + 8 * slot, elected);
+        if (++slot == Sh::SLOTS) slot = 0, phase ^= 1u;
+        ok = wait_warp(bar_full + 8 * slot, phase) && wait_warp(bar_p, tile_phase);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t bv = v_desc + slot * (Sh::SLOT >> 4);
+#pragma unroll
+        for (int k = 0; k < KT / 16; ++k) tc_mma(d_o, d_s + k * 8, bv + k * (2048 >> 4), SMEM_DESC_HI, IDESC_O, k > 0 || j > 0, elected);
+        if (j + 1 == tiles) tc_commit(bar_o, elected);
+        tc_commit(bar_empty + 8 * slot, elected);
+        if (++slot == Sh::SLOTS) slot = 0, phase ^= 1u;
       }
-      if (!ok) {  // products in flight end before tensor memory is given back
-        tc_commit(smem_addr(&s_drain));
-        for (unsigned spin = 0; spin < SPIN_LIMIT && !mbar_try_wait(smem_addr(&s_drain), 0); ++spin) {}
-      }
+    }
+    if (!ok) {  // products in flight end before tensor memory is given back
+      tc_commit(smem_addr(&s_drain), elected);
+      for (unsigned spin = 0; spin < SPIN_LIMIT && !mbar_try_wait(smem_addr(&s_drain), 0); ++spin) {}
     }
     __syncwarp();
   } else {
     // ---- softmax: thread = row ------------------------------------------------------------
     const uint32_t my = tmem + ((uint32_t)(warp * 32) << 16);
     const float scale2 = p.a.scale2;
-    TaSeg s;
+    // The next piece's rows are read into tensor memory as soon as this piece's last scores are there, before its result
+    // is written: so the first product of the next piece runs beside that.
+    TaSeg s, s_next;
     unsigned n = 0, n_seg = 0;
     bool ok = true;
-    while (walk.next(p, s)) {
-      if (!s.rows) continue;
+    auto row_of = [&](const TaSeg& s, int& u, int& h) {
       const int r = s.row0 + tid;
       const bool in = r < p.rows;
+      u = in ? r / p.a.group : 0;
+      h = s.g * p.a.group + (in ? r - u * p.a.group : 0);
+      return in;
+    };
+    auto next_piece = [&](TaSeg& s) {  // the next one with keys
+      while (walk.next(p, s)) {
+        if (!s.rows) continue;
+        if (s.begin < s.end) return true;
+        const long long part = ((long long)blockIdx.x * 2 + s.which) * p.part_rows + tid;
+        if (s.row0 + tid < p.rows) p.part_ml[part] = make_float2(-INFINITY, 0.0f);  // a piece of others that this CTA's rows do not see
+      }
+      return false;
+    };
+    auto load_q = [&](const TaSeg& s) {
+      if (s.row0 + warp * 32 < p.rows) {
+        int u, h;
+        const bool in = row_of(s, u, h);
+        const uint4* src = reinterpret_cast<const uint4*>(
+            p.a.q + 2 * ((long long)s.b * p.a.q_stride[0] + (long long)u * p.a.q_stride[1] + (long long)h * p.a.q_stride[2]));
+#pragma unroll
+        for (int hh = 0; hh < HALVES; ++hh) {
+          uint32_t w[32];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (in && hh * 64 + c * 8 < p.a.dim) v = __ldg(src + hh * 8 + c);
+            w[4 * c] = v.x;
+            w[4 * c + 1] = v.y;
+            w[4 * c + 2] = v.z;
+            w[4 * c + 3] = v.w;
+          }
+          tc_st32(my + Sh::COL_Q + hh * 32, w);
+        }
+        tc_wait_st();
+      }
+      tc_fence_before();
+      mbar_arrive(bar_q);
+    };
+    bool more = next_piece(s);
+    if (more) load_q(s);
+    for (; more; s = s_next) {
+      int u, h;
+      const bool in = row_of(s, u, h);
       const bool warp_in = s.row0 + warp * 32 < p.rows;
-      const int u = in ? r / p.a.group : 0, h = s.g * p.a.group + (in ? r - u * p.a.group : 0);
       const bool live = in && !(p.a.tree && p.a.tree[(long long)s.b * p.a.N + u] < 0);
       float m = -INFINITY, l = 0.0f;
       bool odd = false;
-      if (ok && s.begin < s.end) {
-        if (warp_in) {
-          const uint4* src = reinterpret_cast<const uint4*>(
-              p.a.q + 2 * ((long long)s.b * p.a.q_stride[0] + (long long)u * p.a.q_stride[1] + (long long)h * p.a.q_stride[2]));
-#pragma unroll
-          for (int hh = 0; hh < HALVES; ++hh) {
-            uint32_t w[32];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              uint4 v = make_uint4(0, 0, 0, 0);
-              if (in && hh * 64 + c * 8 < p.a.dim) v = __ldg(src + hh * 8 + c);
-              w[4 * c] = v.x;
-              w[4 * c + 1] = v.y;
-              w[4 * c + 2] = v.z;
-              w[4 * c + 3] = v.w;
-            }
-            tc_st32(my + Sh::COL_Q + hh * 32, w);
-          }
-          tc_wait_st();
-        }
-        tc_fence_before();
-        mbar_arrive(smem_addr(&s_q));
-
+      if (ok) {
         for (int j = s.begin; j < s.end; ++j, ++n) {
           const bool tree = j >= s.p_tiles;
           const int left = s.len - j * KT;  // cached tokens from this tile on
@@ -459,7 +500,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
             // become zero.  In the tree some rows may see what others do not: there, elements that are not finite become
             // zero and are added at the end to the rows that do see them.
             const unsigned iv = 2 * n + 1, slot = iv % Sh::SLOTS;
-            ok = wait_warp(s_full[slot], (iv / Sh::SLOTS) & 1u);
+            ok = wait_warp(bar_full + 8 * slot, (iv / Sh::SLOTS) & 1u);
             if (!ok) break;
             char* v0 = ta_smem + (ring - smem_addr(ta_smem)) + slot * Sh::SLOT;
             if (partial) {
@@ -468,7 +509,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
                 for (int hh = 0; hh < HALVES; ++hh) *reinterpret_cast<uint4*>(v0 + hh * (KT * 128) + i * 16) = make_uint4(0, 0, 0, 0);
             } else {
               constexpr uint32_t EXP = BF16 ? 0x7F80u : 0x7C00u;
-              for (int i = tid; i < HALVES * KT * 8; i += TA_ROWS) {
+              const int nodes = p.a.N - (j - s.p_tiles) * KT, pieces = (nodes < KT ? nodes : KT) * 8;  // the rest are zeros
+              for (int k = tid; k < HALVES * pieces; k += TA_ROWS) {
+                const int i = k + (HALVES > 1 ? k / pieces * (KT * 8 - pieces) : 0);
                 uint4 v = *reinterpret_cast<uint4*>(v0 + i * 16);
                 uint32_t* e = reinterpret_cast<uint32_t*>(&v);
                 bool odd = false;
@@ -485,7 +528,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
-          ok = wait_warp(s_s, n & 1u);
+          ok = wait_warp(bar_s, n & 1u);
           if (!ok) break;
           tc_fence_after();
           if (warp_in) {
@@ -510,12 +553,15 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
                 for (int i = 0; i < 32; ++i) x[c][i] = seen >> i & 1u ? x[c][i] : 0xFF800000u;
               }
             }
-            float top = -INFINITY;
+            float top = -INFINITY, top1 = -INFINITY;
 #pragma unroll
             for (int c = 0; c < KT / 32; ++c)
 #pragma unroll
-              for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(x[c][i]));
-            top *= scale2;
+              for (int i = 0; i < 32; i += 4) {
+                top = max3(top, __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
+                top1 = max3(top1, __uint_as_float(x[c][i + 2]), __uint_as_float(x[c][i + 3]));
+              }
+            top = fmaxf(top, top1) * scale2;
             // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores
             // pass it by TA_SLACK, so that o is seldom read, scaled and written (weights up to 2^8 lose nothing in
             // either 16-bit type, sums are fp32).
@@ -556,16 +602,19 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
             tc_wait_st();
           }
           tc_fence_before();
-          mbar_arrive(smem_addr(&s_p));
+          mbar_arrive(bar_p);
         }
-        if (ok) ok = wait_warp(s_o, n_seg & 1u);
+      }
+      more = next_piece(s_next);
+      if (ok) {
+        if (more) load_q(s_next);
+        ok = wait_warp(bar_o, n_seg & 1u);
         tc_fence_after();
         odd = ok && s_odd[n_seg & 1] == n_seg + 1;
         ++n_seg;
       }
       if (!warp_in) continue;
       // ---- the piece's result ---------------------------------------------------------------
-      const bool some = s.begin < s.end;
       if (!ok) l = NAN;  // a wait ran out: nothing of this piece is to be trusted
       const long long row = ((long long)s.b * p.a.N + u) * p.a.heads_q + h;
       const long long part = ((long long)blockIdx.x * 2 + s.which) * p.part_rows + tid;
@@ -575,11 +624,10 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
         if (!s.whole) p.part_ml[part] = live || !ok ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
         else if (p.a.lse) p.a.lse[row] = !ok ? NAN : (empty ? -INFINITY : 0.6931471805599453f * (m + log2f(l)));
       }
-      if (!s.whole && !some && ok) continue;  // no keys here: the joining kernel does not read o
 #pragma unroll 1
       for (int c = 0; c < DP / 32; ++c) {
         uint32_t o[32];
-        if (some && ok) {
+        if (ok) {
           tc_ld32(o, my + Sh::COL_O + c * 32);
           tc_wait_ld();
         } else {
@@ -751,7 +799,6 @@ template <int DP, bool BF16> int launch_tensor_attention(const AttnParams& a, vo
   if (p.groups > (most + p.min_tiles - 1) / p.min_tiles) p.groups = (int)((most + p.min_tiles - 1) / p.min_tiles);
   p.box_rows = 16;
   while (p.box_rows < Sh::KT && a.page % (p.box_rows * 2) == 0) p.box_rows *= 2;
-  p.k_steps = (a.dim + 15) / 16;
   p.part_rows = rows < TA_ROWS ? (int)rows : TA_ROWS;
   p.wait_limit = wait_limit;
 

@@ -36,18 +36,23 @@ class _Op:
         self.dev = torch.device(device)
         if self.dev.index is None:
             self.dev = torch.device(self.dev.type, torch.cuda.current_device())
-        self._current_stream = torch.cuda.current_stream
+        self._index = self.dev.index
+        self._raw_stream, self._current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
         self._lib = lib()
 
-    def _stream(self, stream):
-        return (stream if stream is not None else self._current_stream(self.dev)).cuda_stream
-
-    def _on_device(self):
-        """The device of the operator, current for the launch."""
-        return self.torch.cuda.device(self.dev)
+    def _launch(self, stream, name, *args):
+        """One library call on `stream` (or the device's current one), with the operator's device current."""
+        st = self._raw_stream(self._index) if stream is None else stream.cuda_stream
+        if self._current_device() == self._index:
+            rc = getattr(self._lib, name)(*args, st)
+        else:
+            with self.torch.cuda.device(self.dev):
+                rc = getattr(self._lib, name)(*args, st)
+        if rc:
+            _check(rc, name)
 
     def _ints(self, t, dtype, shape, what):
-        if t.dtype is not dtype or t.shape != shape or t.device != self.dev or not t.is_contiguous():
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
             raise StandError(f"{what}: wants a contiguous {dtype} tensor {tuple(shape)} on {self.dev}, "
                              f"got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
@@ -99,10 +104,10 @@ class TreeAttention(_Op):
         self._scratch_bytes = need
         self.out = t.empty(self._q_shape, dtype=dtype, device=self.dev)
         self.lse = t.empty((B, N, heads_q), dtype=t.float32, device=self.dev)
-        self._cfg_ptr = C.addressof(self.cfg)
+        self._cfg_ptr, self._strides = C.addressof(self.cfg), None
 
     def _floats(self, x, shape, what):
-        if x.dtype is not self.dtype or x.shape != shape or x.device != self.dev or x.stride(3) != 1:
+        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index or x.stride(3) != 1:
             raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev} with a contiguous last dimension, "
                              f"got {x.dtype} {tuple(x.shape)} on {x.device}")
         return x.data_ptr()
@@ -118,9 +123,10 @@ class TreeAttention(_Op):
         ks, cs = k.stride(), cache_k.stride()
         if v.stride() != ks or cache_v.stride() != cs:
             raise StandError("TreeAttention: keys and values have the same strides")
-        c.q_stride[:] = q.stride()[:3]
-        c.kv_stride[:] = ks[:3]
-        c.cache_stride[:] = cs[:3]
+        qs = q.stride()
+        if (qs, ks, cs) != self._strides:
+            c.q_stride[:], c.kv_stride[:], c.cache_stride[:] = qs[:3], ks[:3], cs[:3]
+            self._strides = (qs, ks, cs)
         ptab = self._ints(table, t.int32, self._table_shape, "table")
         plen = self._ints(length, t.int64, self._len_shape, "length")
         ptree = self._opt(tree_tokens, t.int32, self._tree_shape, "tree_tokens")
@@ -131,12 +137,8 @@ class TreeAttention(_Op):
         if lse is None:
             lse = self.lse
         plse = self._ints(lse, t.float32, self.lse.shape, "lse")
-        with self._on_device():
-            rc = self._lib.stand_tree_attention(self._cfg_ptr, pq, pk, pv, pck, pcv, ptab, plen, self._mask_ptr, self.mask_stride,
-                                                ptree, self._scratch, self._scratch_bytes, out.data_ptr(), plse,
-                                                self._stream(stream))
-        if rc:
-            _check(rc, "stand_tree_attention")
+        self._launch(stream, "stand_tree_attention", self._cfg_ptr, pq, pk, pv, pck, pcv, ptab, plen, self._mask_ptr,
+                     self.mask_stride, ptree, self._scratch, self._scratch_bytes, out.data_ptr(), plse)
         return out, lse
 
 
@@ -172,10 +174,7 @@ class PageMap(_Op):
                 self.page_size, self.max_pages, self._ints(free, t.int32, self._list, "free"), self.capacity,
                 self._ints(n_free, t.int32, self._one, "n_free"), self._ints(table, t.int32, self._table, "table"),
                 self.slots.data_ptr(), self.granted.data_ptr(), len_out.data_ptr(), n_out.data_ptr())
-        with self._on_device():
-            rc = self._lib.stand_page_map(*args, self._stream(stream))
-        if rc:
-            _check(rc, "stand_page_map")
+        self._launch(stream, "stand_page_map", *args)
         return self.slots, self.granted, len_out, n_out
 
     def release(self, length, done, table, free, n_free, stream=None):
@@ -186,10 +185,7 @@ class PageMap(_Op):
                 self.page_size, self.max_pages, self._ints(table, t.int32, self._table, "table"), self.capacity,
                 self._ints(free, t.int32, self._list, "free"), self._ints(n_free, t.int32, self._one, "n_free"),
                 len_out.data_ptr(), n_out.data_ptr())
-        with self._on_device():
-            rc = self._lib.stand_page_release(*args, self._stream(stream))
-        if rc:
-            _check(rc, "stand_page_release")
+        self._launch(stream, "stand_page_release", *args)
         return len_out, n_out
 
 
@@ -202,10 +198,10 @@ class KvCommit(_Op):
         self.dtype = dtype
         self._src, self._cache = (layers, B, N, heads, dim), (layers, pages, heads, page_size, dim)
         self._places = (B, width)
-        self._cfg_ptr = C.addressof(self.cfg)
+        self._cfg_ptr, self._strides = C.addressof(self.cfg), None
 
     def _floats(self, x, shape, what):
-        if x.dtype is not self.dtype or x.shape != shape or x.device != self.dev or x.stride(4) != 1:
+        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index or x.stride(4) != 1:
             raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev} with a contiguous last dimension, "
                              f"got {x.dtype} {tuple(x.shape)} on {x.device}")
         return x.data_ptr()
@@ -219,15 +215,12 @@ class KvCommit(_Op):
         ks, cs = k.stride(), cache_k.stride()
         if v.stride() != ks or cache_v.stride() != cs:
             raise StandError("KvCommit: keys and values have the same strides")
-        c.src_stride[:] = ks[:4]
-        # the C interface's order is layer, page, head, token
-        c.cache_stride[:] = cs[:4]
+        if (ks, cs) != self._strides:
+            c.src_stride[:], c.cache_stride[:] = ks[:4], cs[:4]
+            self._strides = (ks, cs)
         ps = self._ints(slots, t.int64, self._places, "slots")
         pp = self._opt(path, t.int32, self._places, "path")
-        with self._on_device():
-            rc = self._lib.stand_kv_commit(self._cfg_ptr, pk, pv, pp, ps, pck, pcv, self._stream(stream))
-        if rc:
-            _check(rc, "stand_kv_commit")
+        self._launch(stream, "stand_kv_commit", self._cfg_ptr, pk, pv, pp, ps, pck, pcv)
 
 
 class LogitsProcessor(_Op):
@@ -251,7 +244,7 @@ class LogitsProcessor(_Op):
     def _logits(self, x, what):
         """Address and row stride of [B, N, V] logits whose rows are evenly spaced."""
         B, N, V = self._shape
-        if x.dtype is not self.dtype or x.shape != self._shape or x.device != self.dev:
+        if x.dtype is not self.dtype or x.shape != self._shape or x.get_device() != self._index:
             raise StandError(f"{what}: wants a {self.dtype} tensor {self._shape} on {self.dev}")
         sb, sn, sv = x.stride()
         row = sn if N > 1 else (sb if B > 1 else V)
@@ -305,8 +298,5 @@ class LogitsProcessor(_Op):
         else:
             _need(mask_row is None, "mask_row goes with mask")
             x.mask = x.mask_row = None
-        with self._on_device():
-            rc = self._lib.stand_process_logits(self._cfg_ptr, self._in_ptr, src, dst, self._stream(stream))
-        if rc:
-            _check(rc, "stand_process_logits")
+        self._launch(stream, "stand_process_logits", self._cfg_ptr, self._in_ptr, src, dst)
         return out
