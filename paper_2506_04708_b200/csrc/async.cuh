@@ -36,5 +36,15 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
   }
   return false;
 }
+// A wait bounded by time: a poll may itself be suspended for long, so polls alone bound little.  `limit` counts units of
+// 512 clock cycles (SPIN_LIMIT: about a second); 0 gives up at once.
+__device__ __forceinline__ bool mbar_wait_timed(uint32_t bar, uint32_t parity, const volatile int* abort_flag, unsigned limit) {
+  const long long end = clock64() + (long long)limit * 512;
+  while (limit && clock64() < end) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (abort_flag && *abort_flag) return false;
+  }
+  return false;
+}
 
 }  // namespace stand

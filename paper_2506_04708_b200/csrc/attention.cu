@@ -34,7 +34,7 @@ extern "C" {
 
 size_t stand_tree_attention_scratch_bytes(const stand_attention* c) {
   if (!attention_valid(c)) return 0;
-  return tensor_scratch_bytes(c->N * (c->heads_q / c->heads_kv), c->dim);
+  return tensor_scratch_bytes(c->N, c->heads_q / c->heads_kv, c->dim);
 }
 
 int stand_tree_attention(const stand_attention* c, const void* dev_q, const void* dev_k, const void* dev_v, const void* dev_cache_k,
@@ -61,9 +61,9 @@ int stand_tree_attention(const stand_attention* c, const void* dev_q, const void
     const bool bf = c->dtype == STAND_DTYPE_BF16;
     const unsigned limit = wait_limit();
     int rc;
-    if (dp == 64) rc = bf ? launch_tensor_attention<64, true>(p, dev_scratch, sms, limit, st) : launch_tensor_attention<64, false>(p, dev_scratch, sms, limit, st);
-    else if (dp == 128) rc = bf ? launch_tensor_attention<128, true>(p, dev_scratch, sms, limit, st) : launch_tensor_attention<128, false>(p, dev_scratch, sms, limit, st);
-    else rc = bf ? launch_tensor_attention<256, true>(p, dev_scratch, sms, limit, st) : launch_tensor_attention<256, false>(p, dev_scratch, sms, limit, st);
+    if (dp == 64) rc = bf ? launch_tensor_parts<64, true>(p, dev_scratch, sms, limit, st) : launch_tensor_parts<64, false>(p, dev_scratch, sms, limit, st);
+    else if (dp == 128) rc = bf ? launch_tensor_parts<128, true>(p, dev_scratch, sms, limit, st) : launch_tensor_parts<128, false>(p, dev_scratch, sms, limit, st);
+    else rc = bf ? launch_tensor_parts<256, true>(p, dev_scratch, sms, limit, st) : launch_tensor_parts<256, false>(p, dev_scratch, sms, limit, st);
     if (rc != STAND_E_ARG) return rc;  // strides that the copy unit cannot take: the other kernel
   }
   if (c->dtype == STAND_DTYPE_F32) return launch_plain_attention<float>(p, st);

@@ -1,14 +1,20 @@
 // Tree attention on the tensor cores (tcgen05, sm_100a): bfloat16 and half, head sizes that are a multiple of 8, 16-byte
-// aligned rows.
+// aligned rows, up to 128 query heads per key head.
 //
-// A block (CTA) of six warps works on 128 rows of one (sequence, key head) pair and walks over its keys in tiles:
+// A block (CTA) of six warps works on up to 128 rows of one (sequence, key head) pair and walks over its keys in tiles of
+// 64:
 //   warp 4  copies tiles of keys and of values from the pages (and from the tree's own keys) with TMA into a ring,
-//   warp 5  issues the matrix products S = Q K^T and O += P V, one thread for all,
+//   warp 5  issues the matrix products S = Q K^T and O += P V, and copies the rows Q,
 //   warps 0-3  own one row per thread: read S, keep the running maximum and sum, write P, finally write O / l.
-// Q, S and O live in tensor memory (a row is a lane): Q as the first operand of the first product, P, in 16 bits and in
-// the place of S, as that of the second, so that shared memory holds nothing but the ring of keys and values and is read
-// once per product.  What a tile costs in sequence (product, softmax, product) is hidden by the second CTA of the SM: the
-// two take 256 of the 512 columns of tensor memory and half of the shared memory each (head size 256: one CTA per SM).
+// S and O live in tensor memory (a row is a lane).  P, in 16 bits, takes the place of S as the first operand of the second
+// product.  There are two places for S, so the scores of the next tile are computed while the softmax works on this
+// one, and the softmax waits for nothing but its own arithmetic; O is only touched by it when the maximum has risen a
+// good deal.  Two CTAs share an SM (256 of the 512 columns of tensor memory and half of the shared memory each; head
+// size 256: one CTA).
+//
+// With at most 32 (64) rows the four (two) parts of the lanes hold the same rows: each part takes a quarter (half) of a
+// tile's keys, has its own maximum, sum and O, and they are joined at the end.  The product computes 128 rows anyway;
+// the exponentials of a tile then take all four warps instead of one.
 //
 // The keys of all pairs, laid end to end in tiles, are cut into as many equal ranges as there are CTAs (or groups of
 // CTAs: the row tiles of a pair with more than 128 rows go to neighbours that walk over the same keys at the same time,
@@ -28,17 +34,24 @@ constexpr int TA_ROWS = 128;              // rows of a CTA: lanes of tensor memo
 constexpr int TA_THREADS = 192;
 constexpr int TA_SMS = 148;               // B200; scratch is laid out for that many
 constexpr int TA_GROUP = 4;               // row tiles that walk together, at most
+constexpr int TA_KT = 64;                 // keys per tile
+constexpr int TA_PIECE_COST = 3;          // what beginning and ending a piece costs, in tiles
+constexpr int TA_MIN_TILES = 4;           // fewest tiles (that cost included) worth a range of their own
 constexpr float TA_SLACK = 8.0f;          // the maximum is raised only when scores pass it by 2^8 (below)
+constexpr int TA_XCOLS = 16;              // columns of O that the parts exchange at a time
 
-template <int DP> struct TaShape {
-  static constexpr int KT = DP == 64 ? 128 : 64;              // keys per tile
+template <int DP, int C> struct TaShape {
   static constexpr int CTAS = DP == 256 ? 1 : 2;              // per SM
-  static constexpr int SLOT = KT * DP * 2;                    // bytes of a tile of keys or values
-  static constexpr int SLOTS = 6;
-  static constexpr int COL_O = 0, COL_S = DP, COL_Q = DP + KT;
+  static constexpr int SLOT = TA_KT * DP * 2;                 // bytes of a tile of keys or values
+  static constexpr int SLOTS = DP == 64 ? (C > 1 ? 10 : 12) : (C > 1 ? 4 : 5);
+  static constexpr int Q = TA_ROWS * DP * 2;
+  static constexpr int COL_O = 0, COL_S = DP;                 // two places for S
   static constexpr int COLS = DP == 256 ? 512 : 256;          // tensor memory columns allocated
-  static constexpr int SMEM = SLOTS * SLOT + 1024;            // and room to align the ring
-  static_assert(COL_Q + DP / 2 <= COLS, "tensor memory");
+  static constexpr int X = C > 1 ? TA_ROWS * (TA_XCOLS + 1) * 4 : 0;  // exchange between the parts
+  static constexpr int SHARED = C > 1 ? 1536 : 512;           // barriers and the like
+  static constexpr int SMEM = Q + SLOTS * SLOT + X + SHARED;
+  static_assert(COL_S + 2 * TA_KT <= COLS, "tensor memory");
+  static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory");
 };
 
 struct TaRecord {  // what the joining kernel has to do for the last pair that a group began
@@ -48,15 +61,14 @@ struct TaRecord {  // what the joining kernel has to do for the last pair that a
 };
 
 struct alignas(64) TaParams {
-  CUtensorMap cache_k, cache_v, tree_k, tree_v;
+  CUtensorMap cache_k, cache_v, tree_k, tree_v, q;
   AttnParams a;
-  int rows;           // N * group
+  int tile_nodes;     // nodes of a row tile
+  int part_rows;      // its rows: rows of a piece in scratch
   int row_blocks;     // groups of row tiles
   int group_ctas;     // row tiles per group
   int groups;
-  int min_tiles;      // fewest tiles worth a group of their own
   int box_rows;       // rows of a page that one copy takes
-  int part_rows;      // rows of a piece in scratch
   long long tree_tiles;  // sum over the row blocks of a pair
   TaRecord* records;
   float2* part_ml;
@@ -99,8 +111,37 @@ __device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint32_t b_lo, ui
       "r"(accumulate), "r"(elected)
       : "memory");
 }
-// 32 columns of this warp's 32 lanes: one row per thread
-__device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr) {
+// The same with A in shared memory.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate,
+                                          uint32_t elected) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\tsetp.ne.u32 p, %5, 0;\n\t"
+      "setp.ne.u32 e, %6, 0;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi),
+      "r"(idesc), "r"(accumulate), "r"(elected)
+      : "memory");
+}
+// 16 or 32 columns of this warp's 32 lanes: one row per thread
+__device__ __forceinline__ void tc_ld16(uint32_t* r, uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_st8(uint32_t addr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+      "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tc_ld32(uint32_t* r, uint32_t addr) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
       "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -111,7 +152,7 @@ __device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr) {
       : "r"(addr)
       : "memory");
 }
-__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
       "%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
@@ -156,67 +197,81 @@ template <bool BF16> __device__ __forceinline__ uint32_t ta_pack(float lo, float
   return r;
 }
 
+// Stores W / 2 words as the P of this part's W keys, and zeros as that of the other parts' keys.
+template <int C> __device__ __forceinline__ void store_p(uint32_t addr, int part, const uint32_t* w) {
+  if constexpr (C == 1) {
+    tc_st32(addr, w);
+  } else if constexpr (C == 2) {
+    const uint32_t zero[16] = {};
+    tc_st16(addr + part * 16, w);
+    tc_st16(addr + (part ^ 1) * 16, zero);
+  } else {
+    const uint32_t zero[8] = {};
+    tc_st8(addr + part * 8, w);
+#pragma unroll
+    for (int c = 1; c < 4; ++c) tc_st8(addr + ((part + c) & 3) * 8, zero);
+  }
+}
+
 // ---- the walk over a group's range of tiles -----------------------------------------
 struct TaSeg {
-  int b, g, rb, row0;      // pair, row block, first row of this CTA
+  int b, g, rb, node0;     // pair, row block, first node of this CTA
   int len, p_tiles;        // cached tokens, their tiles
   int begin, end;          // this CTA's tiles of the pair (cached ones, then the tree's)
-  bool whole, rows;        // the range covers the pair; the CTA has rows in this block
+  int whole;               // the range covers the pair
+  int rows;                // the CTA has rows in this block
   int which;               // the group's first piece or a later one
+  int starts, units;       // the pair begins in this group's range; its length there (cost and tiles)
 };
 
-template <int KT> struct TaWalk {
+struct TaWalk {
   long long t, hi, b_start;
   int b;
   bool first;
 
-  // tree tiles that rows before row_end see
-  __device__ static __forceinline__ int tree_tiles(const TaParams& p, long long row_end) {
-    const long long last = (row_end < p.rows ? row_end : p.rows) - 1;
-    return (int)(last / p.a.group) / KT + 1;
+  // tree tiles that nodes before node_end see
+  __device__ static __forceinline__ int tree_tiles(const TaParams& p, int node_end) {
+    return ((node_end < p.a.N ? node_end : p.a.N) - 1) / TA_KT + 1;
   }
-  __device__ static __forceinline__ long long tiles_of(const TaParams& p, int b) {
-    const long long tiles = (attn_len(p.a, b) + KT - 1) / KT;
-    return p.a.heads_kv * (p.row_blocks * tiles + p.tree_tiles);
+  // length of all pairs and row blocks of a (sequence, key head), in tiles, a piece's fixed cost included
+  __device__ static __forceinline__ long long per_head(const TaParams& p, long long len) {
+    return p.row_blocks * ((len + TA_KT - 1) / TA_KT + TA_PIECE_COST) + p.tree_tiles;
   }
+  __device__ static __forceinline__ long long length_of(const TaParams& p, int b) { return p.a.heads_kv * per_head(p, attn_len(p.a, b)); }
   __device__ __forceinline__ bool next(const TaParams& p, TaSeg& s) {
     while (t < hi) {
       s.len = (int)attn_len(p.a, b);
-      s.p_tiles = (s.len + KT - 1) / KT;
-      const long long per_head = (long long)p.row_blocks * s.p_tiles + p.tree_tiles;
+      s.p_tiles = (s.len + TA_KT - 1) / TA_KT;
+      const long long head = per_head(p, s.len);
       long long off = t - b_start;
-      if (off >= p.a.heads_kv * per_head) {
-        b_start += p.a.heads_kv * per_head;
+      if (off >= p.a.heads_kv * head) {
+        b_start += p.a.heads_kv * head;
         ++b;
         continue;
       }
       s.b = b;
-      s.g = (int)(off / per_head);
-      off -= s.g * per_head;
+      s.g = head <= 0x7FFFFFFF && off <= 0x7FFFFFFF ? (int)((uint32_t)off / (uint32_t)head) : (int)(off / head);
+      off -= s.g * head;
       s.rb = 0;
-      int n;
       while (true) {
-        n = s.p_tiles + tree_tiles(p, (long long)(s.rb + 1) * p.group_ctas * TA_ROWS);
-        if (off < n) break;
-        off -= n;
+        s.units = TA_PIECE_COST + s.p_tiles + tree_tiles(p, (s.rb + 1) * p.group_ctas * p.tile_nodes);
+        if (off < s.units) break;
+        off -= s.units;
         ++s.rb;
       }
-      s.begin = (int)off;
-      s.end = n - s.begin < hi - t ? n : (int)(s.begin + (hi - t));
-      s.whole = s.begin == 0 && s.end == n;
+      const int from = (int)off, to = s.units - from < hi - t ? s.units : (int)(from + (hi - t));
+      s.starts = from == 0;
+      s.whole = from == 0 && to == s.units;
       s.which = first ? 0 : 1;
       first = false;
-      t += s.end - s.begin;
-      const long long row0 = ((long long)s.rb * p.group_ctas + blockIdx.x % p.group_ctas) * TA_ROWS;
-      s.rows = row0 < p.rows;
-      s.row0 = (int)row0;
-      if (s.rows) {
-        const int own = s.p_tiles + tree_tiles(p, row0 + TA_ROWS);  // later tree tiles are above all of this CTA's rows
-        if (s.end > own) s.end = own;
-        if (s.end < s.begin) s.end = s.begin;
-      } else {
-        s.end = s.begin;
-      }
+      t += to - from;
+      s.begin = from > TA_PIECE_COST ? from - TA_PIECE_COST : 0;
+      s.end = to > TA_PIECE_COST ? to - TA_PIECE_COST : 0;
+      s.node0 = (s.rb * p.group_ctas + blockIdx.x % p.group_ctas) * p.tile_nodes;
+      s.rows = s.node0 < p.a.N;
+      const int own = s.rows ? s.p_tiles + tree_tiles(p, s.node0 + p.tile_nodes) : 0;  // later tree tiles are above all of this CTA's rows
+      if (s.end > own) s.end = own;
+      if (s.end < s.begin) s.end = s.begin;
       return true;
     }
     return false;
@@ -224,73 +279,84 @@ template <int KT> struct TaWalk {
 };
 
 // ---- the kernel -----------------------------------------------------------------------
-template <int DP, bool BF16>
-__global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
-  using Sh = TaShape<DP>;
-  constexpr int KT = Sh::KT, HALVES = DP / 64;
-  extern __shared__ char ta_smem[];
-  __shared__ alignas(8) uint64_t s_full[Sh::SLOTS], s_empty[Sh::SLOTS], s_q, s_s, s_p, s_o, s_drain;
-  __shared__ uint32_t s_tmem;
-  __shared__ int s_abort;
-  __shared__ unsigned s_odd[2];  // 1 + the last piece (even ones, odd ones) whose tree has values that are not finite
-  __shared__ long long s_sum[TA_THREADS / 32], s_b_start;
-  __shared__ int s_b;
+template <int DP, int C, bool BF16>
+__global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
+  using Sh = TaShape<DP, C>;
+  constexpr int KT = TA_KT, HALVES = DP / 64, SLOTS = Sh::SLOTS;
+  constexpr int PART_ROWS = TA_ROWS / C, W = KT / C;  // rows of a part; keys of a tile that it takes
+  extern __shared__ __align__(1024) char ta_smem[];
+  struct Shared {
+    uint64_t full[SLOTS], empty[SLOTS], q, s[2], p[2], o[2], x, drain;  // s, p, o: by the place of a tile's scores
+    long long sum[TA_THREADS / 32], b_start, lo, hi;
+    float2 ml[C > 1 ? TA_ROWS : 1];
+    TaSeg seg;         // the piece that the rows in shared memory belong to; b < 0: no more
+    unsigned odd[2];   // 1 + the last piece (even ones, odd ones) whose tree has values that are not finite
+    uint32_t tmem;
+    int b, abort;
+  };
+  static_assert(sizeof(Shared) <= Sh::SHARED, "barriers");
+  float* const exchange = reinterpret_cast<float*>(ta_smem + Sh::Q + SLOTS * Sh::SLOT);  // [TA_ROWS][TA_XCOLS + 1]
+  Shared& sh = *reinterpret_cast<Shared*>(ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t ring = (smem_addr(ta_smem) + 1023u) & ~1023u;
+  const uint32_t q_smem = smem_addr(ta_smem), ring = q_smem + Sh::Q;
   pdl_trigger();
   if (warp == 5) {
-    tc_alloc(smem_addr(&s_tmem), Sh::COLS);
+    tc_alloc(smem_addr(&sh.tmem), Sh::COLS);
   } else if (tid == 0) {
-    for (int i = 0; i < Sh::SLOTS; ++i) {
-      mbar_init(smem_addr(&s_full[i]), 1);
-      mbar_init(smem_addr(&s_empty[i]), 1);
+    for (int i = 0; i < SLOTS; ++i) {
+      mbar_init(smem_addr(&sh.full[i]), 1);
+      mbar_init(smem_addr(&sh.empty[i]), 1);
     }
-    mbar_init(smem_addr(&s_q), TA_ROWS);
-    mbar_init(smem_addr(&s_s), 1);
-    mbar_init(smem_addr(&s_p), TA_ROWS);
-    mbar_init(smem_addr(&s_o), 1);
-    mbar_init(smem_addr(&s_drain), 1);
+    mbar_init(smem_addr(&sh.q), 1);
+    mbar_init(smem_addr(&sh.s[0]), 1);
+    mbar_init(smem_addr(&sh.s[1]), 1);
+    mbar_init(smem_addr(&sh.p[0]), TA_ROWS);
+    mbar_init(smem_addr(&sh.p[1]), TA_ROWS);
+    mbar_init(smem_addr(&sh.o[0]), 1);
+    mbar_init(smem_addr(&sh.o[1]), 1);
+    mbar_init(smem_addr(&sh.x), TA_ROWS);
+    mbar_init(smem_addr(&sh.drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    s_abort = 0;
-    s_odd[0] = s_odd[1] = 0;
-    s_b = 0;
-    s_b_start = 0;
+    sh.abort = (q_smem & 1023) != 0;  // the swizzle goes by address bits
+    sh.odd[0] = sh.odd[1] = 0;
+    sh.b = 0;
+    sh.b_start = 0;
   }
   pdl_wait();
 
-  // this group's range of tiles, and the sequence in which it begins
-  TaWalk<KT> walk;
+  // this group's range, and the sequence in which it begins
+  TaWalk walk;
   const int group = blockIdx.x / p.group_ctas;
   {
     const int per = (p.a.B + TA_THREADS - 1) / TA_THREADS;
     const int b0 = tid * per, b1 = b0 + per < p.a.B ? b0 + per : p.a.B;
     long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += TaWalk<KT>::tiles_of(p, b);
+    for (int b = b0; b < b1; ++b) mine += TaWalk::length_of(p, b);
     long long upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long v = __shfl_up_sync(FULL, upto, o);
       if (lane >= o) upto += v;
     }
-    if (lane == 31) s_sum[warp] = upto;
+    if (lane == 31) sh.sum[warp] = upto;
     __syncthreads();
     long long total = 0;
     for (int w = 0; w < TA_THREADS / 32; ++w) {
-      if (w < warp) upto += s_sum[w];
-      total += s_sum[w];
+      if (w < warp) upto += sh.sum[w];
+      total += sh.sum[w];
     }
-    long long groups = (total + p.min_tiles - 1) / p.min_tiles;
+    long long groups = (total + TA_MIN_TILES - 1) / TA_MIN_TILES;
     if (groups > p.groups) groups = p.groups;
     const long long lo = group < groups ? total * group / groups : total;
     const long long hi = group < groups ? total * (group + 1) / groups : total;
     if (lo < hi && upto - mine <= lo && lo < upto) {
       long long at = upto - mine;
       for (int b = b0; b < b1; ++b) {
-        const long long n = TaWalk<KT>::tiles_of(p, b);
+        const long long n = TaWalk::length_of(p, b);
         if (lo < at + n) {
-          s_b = b;
-          s_b_start = at;
+          sh.b = b;
+          sh.b_start = at;
           break;
         }
         at += n;
@@ -301,8 +367,8 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
     tc_fence_after();
     walk.t = lo;
     walk.hi = hi;
-    walk.b = s_b;
-    walk.b_start = s_b_start;
+    walk.b = sh.b;
+    walk.b_start = sh.b_start;
     walk.first = true;
     if (tid == 0 && blockIdx.x % p.group_ctas == 0) {
       // the pair in which the range ends, if it began here and goes on in the next groups
@@ -310,13 +376,12 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
       r.n_parts = 0;
       r.first_which = r.b = r.g = r.rb = 0;
       if (lo < hi && group + 1 < groups) {
-        TaWalk<KT> w = walk;
+        TaWalk w = walk;
         TaSeg s;
         long long from = w.t;
         while (w.next(p, s)) {
-          const int n = s.p_tiles + TaWalk<KT>::tree_tiles(p, (long long)(s.rb + 1) * p.group_ctas * TA_ROWS);
-          if (w.t == hi && s.begin == 0 && hi - from < n) {
-            r.n_parts = (int)(((from + n) * groups - 1) / total) - group + 1;
+          if (w.t == hi && s.starts && hi - from < s.units) {
+            r.n_parts = (int)(((from + s.units) * groups - 1) / total) - group + 1;
             r.first_which = s.which;
             r.b = s.b;
             r.g = s.g;
@@ -328,351 +393,431 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP>::CTAS) tensor_attentio
       p.records[group] = r;
     }
   }
-  const uint32_t tmem = s_tmem;
-  volatile int* abort_flag = &s_abort;
+  const uint32_t tmem = sh.tmem;
+  volatile int* abort_flag = &sh.abort;
   const unsigned limit = p.wait_limit;
-  auto wait = [&](uint32_t bar, uint32_t parity) {
-    if (limit && mbar_try_wait(bar, parity)) return true;
-    if (mbar_wait_bounded(bar, parity, abort_flag, limit)) return true;
-    *abort_flag = 1;
-    return false;
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) {  // the whole warp calls it; false: gave up, as all others soon will
+    bool there = limit && mbar_try_wait(bar, parity);
+    if (!there) there = mbar_wait_timed(bar, parity, abort_flag, limit);
+    there = __all_sync(FULL, there);
+    if (!there) *abort_flag = 1;
+    return there;
   };
-  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return (bool)__all_sync(FULL, wait(bar, parity)); };
-  const uint32_t bar_full = smem_addr(s_full), bar_empty = smem_addr(s_empty), bar_q = smem_addr(&s_q), bar_s = smem_addr(&s_s),
-                 bar_p = smem_addr(&s_p), bar_o = smem_addr(&s_o);
+  const uint32_t bar_full = smem_addr(sh.full), bar_empty = smem_addr(sh.empty), bar_q = smem_addr(&sh.q), bar_s = smem_addr(sh.s),
+                 bar_p = smem_addr(sh.p), bar_o = smem_addr(sh.o), bar_x = smem_addr(&sh.x);
+  // scratch row of this CTA's piece
+  auto part_row = [&](const TaSeg& s, int row) { return ((long long)blockIdx.x * 2 + s.which) * p.part_rows + row; };
 
   if (warp == 4) {
-    // ---- copies: a lane per box (rows of one page x 64 elements) -------------------------
+    // ---- keys and values: a lane per box (rows of one page x 64 elements) -----------------
+    // in the order of their use: K0 K1 V0 K2 V1 ... (the scores are one tile ahead)
     const int n_boxes = KT / p.box_rows;
-    const int half = lane % HALVES, box = lane / HALVES;
+    const int half = lane % HALVES, box = lane / HALVES, row = box * p.box_rows;
     TaSeg s;
-    unsigned it = 0, slot = 0, phase = 1;  // phase: parity of the wait for the slot's last use
-    bool ok = true;
+    uint32_t slot = 0, phase = 1, used = 0;  // phase: parity of the wait for the slot's last use
+    bool ok = *abort_flag == 0;
     while (ok && walk.next(p, s)) {
+      if (s.begin >= s.end) {
+        if (s.rows && !s.whole)  // a piece of others that this CTA's rows do not see
+          for (int i = lane; i < p.part_rows; i += 32) p.part_ml[part_row(s, i)] = make_float2(-INFINITY, 0.0f);
+        continue;
+      }
       auto page_of = [&](int j) {  // the page that this lane's box of tile j lies in; -1: none
-        const int pos = j * KT + box * p.box_rows;
-        if (j >= s.p_tiles || box >= n_boxes || pos >= s.len) return -1;
+        const int pos = j * KT + row;
+        if (j >= s.p_tiles || j >= s.end || box >= n_boxes || pos >= s.len) return -1;
         const int page = __ldg(p.a.table + (long long)s.b * p.a.cols + pos / p.a.page);
         return page >= 0 && page < p.a.pages ? page : p.a.pages;  // past the pool: the copy unit fills in zeros
       };
-      int page_next = s.begin < s.end ? page_of(s.begin) : -1;
-      for (int j = s.begin; ok && j < s.end; ++j) {
-        const int page = page_next;
-        if (j + 1 < s.end) page_next = page_of(j + 1);
+      auto copy = [&](int j, int page, bool value) {
+        if (!wait_warp(bar_empty + 8 * slot, phase)) return false;
         const bool tree = j >= s.p_tiles;
-        int boxes = 1;
-        if (!tree) {
-          const int left = s.len - j * KT;
-          boxes = left >= KT ? n_boxes : (left + p.box_rows - 1) / p.box_rows;
+        const uint32_t bar = bar_full + 8 * slot, dst = ring + slot * Sh::SLOT + half * (KT * 128);
+        if (lane == 0) {
+          const int left = s.len - j * KT, boxes = left >= KT ? n_boxes : (left + p.box_rows - 1) / p.box_rows;
+          mbar_expect_tx(bar, tree ? Sh::SLOT : (uint32_t)(boxes * HALVES * p.box_rows * 128));
         }
-        const uint32_t bytes = tree ? Sh::SLOT : (uint32_t)(boxes * HALVES * p.box_rows * 128);
-        const int row = box * p.box_rows;
-        const int in_page = tree ? 0 : (j * KT + row) % p.a.page;
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv, ++it) {
-          ok = wait_warp(bar_empty + 8 * slot, phase);
-          if (!ok) break;
-          const uint32_t bar = bar_full + 8 * slot;
-          if (lane == 0) mbar_expect_tx(bar, bytes);
-          __syncwarp();
-          const uint32_t dst = ring + slot * Sh::SLOT + half * (KT * 128);
-          if (tree) {
-            if (lane < HALVES) tma_load_4d(dst, kv ? &p.tree_v : &p.tree_k, bar, half * 64, (j - s.p_tiles) * KT, s.g, s.b);
-          } else if (page >= 0) {
-            tma_load_4d(dst + row * 128, kv ? &p.cache_v : &p.cache_k, bar, half * 64, in_page, s.g, page);
-          }
-          if (++slot == Sh::SLOTS) slot = 0, phase ^= 1u;
+        __syncwarp();
+        if (tree) {
+          if (lane < HALVES) tma_load_4d(dst, value ? &p.tree_v : &p.tree_k, bar, half * 64, (j - s.p_tiles) * KT, s.g, s.b);
+        } else if (page >= 0) {
+          tma_load_4d(dst + row * 128, value ? &p.cache_v : &p.cache_k, bar, half * 64, (j * KT + row) % p.a.page, s.g, page);
         }
+        ++used;
+        if (++slot == SLOTS) slot = 0, phase ^= 1u;
+        return true;
+      };
+      int page = page_of(s.begin), page_next = page_of(s.begin + 1);
+      ok = copy(s.begin, page, false);
+      for (int j = s.begin; ok && j < s.end; ++j) {
+        const int page_after = page_of(j + 2);
+        if (j + 1 < s.end) ok = copy(j + 1, page_next, false);
+        ok = ok && copy(j, page, true);
+        page = page_next;
+        page_next = page_after;
       }
     }
     if (!ok && lane == 0) {  // copies in flight land before the block ends
-      for (unsigned i = it > Sh::SLOTS ? it - Sh::SLOTS : 0; i < it; ++i)
-        for (unsigned spin = 0; spin < SPIN_LIMIT && !mbar_try_wait(smem_addr(&s_full[i % Sh::SLOTS]), (i / Sh::SLOTS) & 1u); ++spin) {}
+      for (unsigned i = used > SLOTS ? used - SLOTS : 0; i < used; ++i)
+        mbar_wait_timed(bar_full + 8 * (i % SLOTS), (i / SLOTS) & 1u, nullptr, SPIN_LIMIT);
     }
     __syncwarp();
   } else if (warp == 5) {
     // ---- products -----------------------------------------------------------------------
     constexpr uint32_t IDESC_S = mma_desc(BF16, false, KT), IDESC_O = mma_desc(BF16, true, DP);
     TaSeg s;
-    uint32_t slot = 0, phase = 0, tile_phase = 0, seg_phase = 0;
+    uint32_t slot = 0, phase = 0, n = 0, q_phase = 0, buf = 0;  // n: tiles so far
     const uint32_t elected = elect_one(), base = __shfl_sync(FULL, tmem, 0);
-    const uint32_t k_desc = smem_desc_lo(ring, 16), v_desc = smem_desc_lo(ring, KT * 128);
-    const uint32_t d_s = base + Sh::COL_S, d_o = base + Sh::COL_O, a_q = base + Sh::COL_Q;
-    bool ok = true;
-    while (ok && walk.next(p, s)) {
-      const int tiles = __shfl_sync(FULL, s.end - s.begin, 0);
-      if (tiles <= 0) continue;
-      ok = wait_warp(bar_q, seg_phase);
-      seg_phase ^= 1u;
-      for (int j = 0; ok && j < tiles; ++j, tile_phase ^= 1u) {
-        ok = wait_warp(bar_full + 8 * slot, phase);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t bk = k_desc + slot * (Sh::SLOT >> 4);
+    const uint32_t q_desc = smem_desc_lo(q_smem, 16), k_desc = smem_desc_lo(ring, 16), v_desc = smem_desc_lo(ring, KT * 128);
+    const uint32_t d_s = base + Sh::COL_S, d_o = base + Sh::COL_O;
+    bool ok = *abort_flag == 0, copying = false;
+    auto next_piece = [&](TaSeg& s) {  // the next one with keys
+      while (walk.next(p, s))
+        if (s.begin < s.end) return true;
+      return false;
+    };
+    // the piece's rows into shared memory, and its description to the softmax warps, which wait for the same barrier
+    auto load_q = [&](const TaSeg& s, bool more) {
+      if (lane == 0) {
+        sh.seg = s;
+        if (!more) sh.seg.b = -1;
+        if (more) mbar_expect_tx(bar_q, C * HALVES * p.part_rows * 128);
+        else mbar_arrive(bar_q);
+      }
+      __syncwarp();
+      if (more && lane < C * HALVES) {
+        const int part = lane / HALVES, half = lane % HALVES;
+        tma_load_4d(q_smem + half * (TA_ROWS * 128) + part * (PART_ROWS * 128), &p.q, bar_q, half * 64, s.g * p.a.group, s.node0, s.b);
+      }
+      copying = more;
+    };
+    auto scores = [&]() {  // S of the tile whose keys are in the ring's next slot
+      if (!wait_warp(bar_full + 8 * slot, phase)) return false;
+      tc_fence_after();
+      const uint32_t bk = k_desc + slot * (Sh::SLOT >> 4);
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-          tc_mma(d_s, a_q + k * 8, bk + (((k >> 2) * (KT * 128) + (k & 3) * 32) >> 4), SMEM_DESC_HI, IDESC_S, k > 0, elected);
-        tc_commit(bar_s, elected);
-        tc_commit(bar_empty + 8 * slot, elected);
-        if (++slot == Sh::SLOTS) slot = 0, phase ^= 1u;
-        ok = wait_warp(bar_full + 8 * slot, phase) && wait_warp(bar_p, tile_phase);
+      for (int k = 0; k < DP / 16; ++k)
+        tc_mma_ss(d_s + buf * KT, q_desc + (((k >> 2) * (TA_ROWS * 128) + (k & 3) * 32) >> 4),
+                  bk + (((k >> 2) * (KT * 128) + (k & 3) * 32) >> 4), SMEM_DESC_HI, IDESC_S, k > 0, elected);
+      tc_commit(bar_s + 8 * buf, elected);
+      tc_commit(bar_empty + 8 * slot, elected);
+      if (++slot == SLOTS) slot = 0, phase ^= 1u;
+      buf ^= 1u;
+      return true;
+    };
+    bool more = next_piece(s);
+    if (ok) load_q(s, more);
+    while (ok && more) {
+      const int tiles = __shfl_sync(FULL, s.end - s.begin, 0);
+      ok = wait_warp(bar_q, q_phase);
+      if (!ok) break;
+      copying = false;
+      q_phase ^= 1u;
+      tc_fence_after();
+      ok = scores();
+      for (int j = 0; ok && j < tiles; ++j, ++n) {
+        // The scores' place was that of tile j - 1, whose P V is issued: products run in order.
+        if (j + 1 < tiles) ok = scores();
+        else more = next_piece(s);
+        const uint32_t d_p = d_s + (n & 1) * KT;
+        ok = ok && wait_warp(bar_full + 8 * slot, phase) && wait_warp(bar_p + 8 * (n & 1), (n >> 1) & 1u);
         if (!ok) break;
         tc_fence_after();
         const uint32_t bv = v_desc + slot * (Sh::SLOT >> 4);
 #pragma unroll
-        for (int k = 0; k < KT / 16; ++k) tc_mma(d_o, d_s + k * 8, bv + k * (2048 >> 4), SMEM_DESC_HI, IDESC_O, k > 0 || j > 0, elected);
-        if (j + 1 == tiles) tc_commit(bar_o, elected);
+        for (int k = 0; k < KT / 16; ++k) tc_mma(d_o, d_p + k * 8, bv + k * (2048 >> 4), SMEM_DESC_HI, IDESC_O, k > 0 || j > 0, elected);
+        tc_commit(bar_o + 8 * (n & 1), elected);
         tc_commit(bar_empty + 8 * slot, elected);
-        if (++slot == Sh::SLOTS) slot = 0, phase ^= 1u;
+        if (++slot == SLOTS) slot = 0, phase ^= 1u;
+        if (j + 1 == tiles) load_q(s, more);  // P of the last tile is there, so the scores are done with these rows
       }
     }
-    if (!ok) {  // products in flight end before tensor memory is given back
-      tc_commit(smem_addr(&s_drain), elected);
-      for (unsigned spin = 0; spin < SPIN_LIMIT && !mbar_try_wait(smem_addr(&s_drain), 0); ++spin) {}
+    if (!ok) {  // what is in flight ends before the block does
+      if (copying) mbar_wait_timed(bar_q, q_phase, nullptr, SPIN_LIMIT);
+      __syncwarp();
+      tc_commit(smem_addr(&sh.drain), elected);
+      mbar_wait_timed(smem_addr(&sh.drain), 0, nullptr, SPIN_LIMIT);
     }
     __syncwarp();
   } else {
-    // ---- softmax: thread = row ------------------------------------------------------------
+    // ---- softmax: thread = row (of a part) -------------------------------------------------
     const uint32_t my = tmem + ((uint32_t)(warp * 32) << 16);
+    const int part = tid / PART_ROWS, row = tid % PART_ROWS;  // a warp lies in one part
+    const bool in_tile = row < p.part_rows, warp_in = (warp * 32) % PART_ROWS < p.part_rows;
+    const int up = in_tile ? row / p.a.group : 0, head = in_tile ? row - up * p.a.group : 0;
     const float scale2 = p.a.scale2;
-    // The next piece's rows are read into tensor memory as soon as this piece's last scores are there, before its result
-    // is written: so the first product of the next piece runs beside that.
-    TaSeg s, s_next;
-    unsigned n = 0, n_seg = 0;
-    bool ok = true;
-    auto row_of = [&](const TaSeg& s, int& u, int& h) {
-      const int r = s.row0 + tid;
-      const bool in = r < p.rows;
-      u = in ? r / p.a.group : 0;
-      h = s.g * p.a.group + (in ? r - u * p.a.group : 0);
-      return in;
+    unsigned n = 0, n_seg = 0, base_it = 0, x_phase = 0;  // tiles, pieces and copies so far
+    bool ok = *abort_flag == 0;
+    auto sync_rows = [&]() {  // all rows' threads
+      mbar_arrive(bar_x);
+      ok = wait_warp(bar_x, x_phase) && ok;
+      x_phase ^= 1u;
     };
-    auto next_piece = [&](TaSeg& s) {  // the next one with keys
-      while (walk.next(p, s)) {
-        if (!s.rows) continue;
-        if (s.begin < s.end) return true;
-        const long long part = ((long long)blockIdx.x * 2 + s.which) * p.part_rows + tid;
-        if (s.row0 + tid < p.rows) p.part_ml[part] = make_float2(-INFINITY, 0.0f);  // a piece of others that this CTA's rows do not see
-      }
-      return false;
-    };
-    auto load_q = [&](const TaSeg& s) {
-      if (s.row0 + warp * 32 < p.rows) {
-        int u, h;
-        const bool in = row_of(s, u, h);
-        const uint4* src = reinterpret_cast<const uint4*>(
-            p.a.q + 2 * ((long long)s.b * p.a.q_stride[0] + (long long)u * p.a.q_stride[1] + (long long)h * p.a.q_stride[2]));
-#pragma unroll
-        for (int hh = 0; hh < HALVES; ++hh) {
-          uint32_t w[32];
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (in && hh * 64 + c * 8 < p.a.dim) v = __ldg(src + hh * 8 + c);
-            w[4 * c] = v.x;
-            w[4 * c + 1] = v.y;
-            w[4 * c + 2] = v.z;
-            w[4 * c + 3] = v.w;
-          }
-          tc_st32(my + Sh::COL_Q + hh * 32, w);
-        }
-        tc_wait_st();
-      }
-      tc_fence_before();
-      mbar_arrive(bar_q);
-    };
-    bool more = next_piece(s);
-    if (more) load_q(s);
-    for (; more; s = s_next) {
-      int u, h;
-      const bool in = row_of(s, u, h);
-      const bool warp_in = s.row0 + warp * 32 < p.rows;
+    while (ok) {
+      ok = wait_warp(bar_q, n_seg & 1u);
+      if (!ok) break;
+      const TaSeg s = sh.seg;
+      if (s.b < 0) break;
+      const int u = s.node0 + up, h = s.g * p.a.group + head;
+      const bool in = in_tile && u < p.a.N;
       const bool live = in && !(p.a.tree && p.a.tree[(long long)s.b * p.a.N + u] < 0);
       float m = -INFINITY, l = 0.0f;
-      bool odd = false;
-      if (ok) {
-        for (int j = s.begin; j < s.end; ++j, ++n) {
-          const bool tree = j >= s.p_tiles;
-          const int left = s.len - j * KT;  // cached tokens from this tile on
-          const bool partial = !tree && left < KT;
-          if (tree || partial) {
-            // Values that no row sees must not enter the product, 0 times them included: those past the text's end
-            // become zero.  In the tree some rows may see what others do not: there, elements that are not finite become
-            // zero and are added at the end to the rows that do see them.
-            const unsigned iv = 2 * n + 1, slot = iv % Sh::SLOTS;
-            ok = wait_warp(bar_full + 8 * slot, (iv / Sh::SLOTS) & 1u);
-            if (!ok) break;
-            char* v0 = ta_smem + (ring - smem_addr(ta_smem)) + slot * Sh::SLOT;
-            if (partial) {
-              for (int i = left * 8 + tid; i < KT * 8; i += TA_ROWS)
+      for (int j = s.begin; j < s.end; ++j, ++n) {
+        const bool tree = j >= s.p_tiles;
+        const int left = s.len - j * KT;  // cached tokens from this tile on
+        const bool partial = !tree && left < KT;
+        ok = wait_warp(bar_s + 8 * (n & 1), (n >> 1) & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        if (warp_in) {
+          const uint32_t s_addr = my + Sh::COL_S + (n & 1) * KT;
+          uint32_t x[W];
+          if constexpr (C == 4) {
+            tc_ld16(x, s_addr + part * W);
+          } else {
 #pragma unroll
-                for (int hh = 0; hh < HALVES; ++hh) *reinterpret_cast<uint4*>(v0 + hh * (KT * 128) + i * 16) = make_uint4(0, 0, 0, 0);
-            } else {
-              constexpr uint32_t EXP = BF16 ? 0x7F80u : 0x7C00u;
-              const int nodes = p.a.N - (j - s.p_tiles) * KT, pieces = (nodes < KT ? nodes : KT) * 8;  // the rest are zeros
-              for (int k = tid; k < HALVES * pieces; k += TA_ROWS) {
-                const int i = k + (HALVES > 1 ? k / pieces * (KT * 8 - pieces) : 0);
-                uint4 v = *reinterpret_cast<uint4*>(v0 + i * 16);
-                uint32_t* e = reinterpret_cast<uint32_t*>(&v);
-                bool odd = false;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  if ((e[c] & EXP) == EXP) { e[c] &= 0xFFFF0000u; odd = true; }
-                  if ((e[c] & (EXP << 16)) == (EXP << 16)) { e[c] &= 0xFFFFu; odd = true; }
-                }
-                if (odd) {
-                  *reinterpret_cast<uint4*>(v0 + i * 16) = v;
-                  s_odd[n_seg & 1] = n_seg + 1;
-                }
-              }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            for (int c = 0; c < W / 32; ++c) tc_ld32(x + c * 32, s_addr + part * W + c * 32);
           }
-          ok = wait_warp(bar_s, n & 1u);
-          if (!ok) break;
-          tc_fence_after();
-          if (warp_in) {
-            uint32_t x[KT / 32][32];
+          tc_wait_ld();
+          if (tree || partial) {
 #pragma unroll
-            for (int c = 0; c < KT / 32; ++c) tc_ld32(x[c], my + Sh::COL_S + c * 32);
-            tc_wait_ld();
-            if (tree || partial) {
-#pragma unroll
-              for (int c = 0; c < KT / 32; ++c) {
-                uint32_t seen;
-                if (tree) {
-                  const int first = (j - s.p_tiles) * KT + c * 32, below = u + 1 - first;  // nodes first .. u
-                  seen = below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
-                  if (p.a.mask && seen)
-                    seen &= __ldg(p.a.mask + (long long)s.b * p.a.mask_stride + (long long)u * p.a.mask_words + (first >> 5));
-                } else {
-                  const int below = left - c * 32;
-                  seen = below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
-                }
-#pragma unroll
-                for (int i = 0; i < 32; ++i) x[c][i] = seen >> i & 1u ? x[c][i] : 0xFF800000u;
+            for (int c = 0; c < (W + 31) / 32; ++c) {
+              const int key = part * W + c * 32;  // of the tile
+              uint32_t seen;
+              if (tree) {
+                const int first = (j - s.p_tiles) * KT + key, below = u + 1 - first;  // nodes first .. u
+                seen = below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
+                if (p.a.mask && seen)
+                  seen &= __ldg(p.a.mask + (long long)s.b * p.a.mask_stride + (long long)u * p.a.mask_words + (first >> 5)) >> (first & 31);
+              } else {
+                const int below = left - key;
+                seen = below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
               }
+#pragma unroll
+              for (int i = 0; i < (W < 32 ? W : 32); ++i) x[c * 32 + i] = seen >> i & 1u ? x[c * 32 + i] : 0xFF800000u;
             }
-            float top = -INFINITY, top1 = -INFINITY;
+          }
+          float top = -INFINITY, top1 = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < KT / 32; ++c)
-#pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                top = max3(top, __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
-                top1 = max3(top1, __uint_as_float(x[c][i + 2]), __uint_as_float(x[c][i + 3]));
-              }
-            top = fmaxf(top, top1) * scale2;
-            // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores
-            // pass it by TA_SLACK, so that o is seldom read, scaled and written (weights up to 2^8 lose nothing in
-            // either 16-bit type, sums are fp32).
-            if (__any_sync(FULL, top > m + TA_SLACK)) {
-              const float raised = fmaxf(m, top);
-              const float keep = raised == -INFINITY ? 1.0f : ta_ex2(m - raised);
-              m = raised;
-              l *= keep;
-              if (j > s.begin) {
+          for (int i = 0; i < W; i += 4) {
+            top = max3(top, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+            top1 = max3(top1, __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
+          }
+          top = fmaxf(top, top1) * scale2;
+          // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores pass
+          // it by TA_SLACK, so that o is seldom read, scaled and written (weights up to 2^8 lose nothing in either 16-bit
+          // type, sums are fp32).
+          __syncwarp();
+          if (__any_sync(FULL, top > m + TA_SLACK)) {
+            const float raised = fmaxf(m, top);
+            const float keep = raised == -INFINITY ? 1.0f : ta_ex2(m - raised);
+            m = raised;
+            l *= keep;
+            if (j > s.begin) {
+              ok = wait_warp(bar_o + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1u);  // P V of the tile before
+              if (!ok) break;
+              tc_fence_after();
 #pragma unroll 1
-                for (int c = 0; c < DP / 32; ++c) {
-                  uint32_t o[32];
-                  tc_ld32(o, my + Sh::COL_O + c * 32);
-                  tc_wait_ld();
+              for (int c = 0; c < DP / 32; ++c) {
+                uint32_t o[32];
+                tc_ld32(o, my + Sh::COL_O + c * 32);
+                tc_wait_ld();
 #pragma unroll
-                  for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
-                  tc_st32(my + Sh::COL_O + c * 32, o);
-                }
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
+                tc_st32(my + Sh::COL_O + c * 32, o);
               }
             }
-            const float base = m == -INFINITY ? 0.0f : m;
-            float sum0 = 0.0f, sum1 = 0.0f;
+          }
+          const float base = m == -INFINITY ? 0.0f : m;
+          float sum0 = 0.0f, sum1 = 0.0f;
+          uint32_t w[W / 2];
 #pragma unroll
-            for (int c = 0; c < KT / 64; ++c) {
-              uint32_t w[32];
+          for (int i = 0; i < W / 2; ++i) {
+            const float a = ta_ex2(fmaf(__uint_as_float(x[2 * i]), scale2, -base));
+            const float b = ta_ex2(fmaf(__uint_as_float(x[2 * i + 1]), scale2, -base));
+            sum0 += a;
+            sum1 += b;
+            w[i] = ta_pack<BF16>(a, b);
+          }
+          store_p<C>(s_addr, part, w);
+          l += sum0 + sum1;
+          tc_wait_st();
+        }
+        if (tree || partial) {
+          // Values that no row sees must not enter the product, 0 times them included: those past the text's end become
+          // zero.  In the tree some rows may see what others do not: there, elements that are not finite become zero and
+          // are added at the end to the rows that do see them.
+          // (Not before the scores are there: until then the slot may still await the tile before the last.)
+          const int t = j - s.begin;
+          const unsigned iv = base_it + (j + 1 < s.end ? 2 * t + 2 : 2 * t + 1), slot = iv % SLOTS;
+          ok = wait_warp(bar_full + 8 * slot, (iv / SLOTS) & 1u);
+          if (!ok) break;
+          char* v0 = ta_smem + Sh::Q + slot * Sh::SLOT;
+          if (partial) {
+            for (int i = left * 8 + tid; i < KT * 8; i += TA_ROWS)
+#pragma unroll
+              for (int hh = 0; hh < HALVES; ++hh) *reinterpret_cast<uint4*>(v0 + hh * (KT * 128) + i * 16) = make_uint4(0, 0, 0, 0);
+          } else {
+            constexpr uint32_t EXP = BF16 ? 0x7F80u : 0x7C00u;
+            const int nodes = p.a.N - (j - s.p_tiles) * KT, pieces = (nodes < KT ? nodes : KT) * 8;  // the rest are zeros
+            for (int k = tid; k < HALVES * pieces; k += TA_ROWS) {
+              const int i = k + (HALVES > 1 ? k / pieces * (KT * 8 - pieces) : 0);
+              uint4 v = *reinterpret_cast<uint4*>(v0 + i * 16);
+              uint32_t* e = reinterpret_cast<uint32_t*>(&v);
+              bool odd = false;
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                if ((e[c] & EXP) == EXP) { e[c] &= 0xFFFF0000u; odd = true; }
+                if ((e[c] & (EXP << 16)) == (EXP << 16)) { e[c] &= 0xFFFFu; odd = true; }
+              }
+              if (odd) {
+                *reinterpret_cast<uint4*>(v0 + i * 16) = v;
+                sh.odd[n_seg & 1] = n_seg + 1;
+              }
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        tc_fence_before();
+        mbar_arrive(bar_p + 8 * (n & 1));
+      }
+      if (!ok) break;
+      ok = wait_warp(bar_o + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1u);
+      if (!ok) break;
+      tc_fence_after();
+      const bool odd = sh.odd[n_seg & 1] == n_seg + 1;
+      base_it += 2 * (s.end - s.begin);
+      ++n_seg;
+
+      // ---- the piece's result ---------------------------------------------------------------
+      float factor = 1.0f;  // of this part's o
+      if constexpr (C > 1) {
+        sh.ml[tid] = make_float2(m, l);
+        sync_rows();
+        if (!ok) break;
+        float top = m, total = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) top = fmaxf(top, sh.ml[c * PART_ROWS + row].x);
+        const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const float2 v = sh.ml[c * PART_ROWS + row];
+          total += v.y * ta_ex2(v.x - base);
+        }
+        factor = ta_ex2(m - base);
+        m = top;
+        l = total;
+      }
+      const long long out_row = ((long long)s.b * p.a.N + u) * p.a.heads_q + h, at = part_row(s, row);
+      const bool empty = !live || l == 0.0f;
+      const float inv = empty ? 0.0f : 1.0f / l;
+      if (in && part == 0) {
+        if (!s.whole) p.part_ml[at] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
+        else if (p.a.lse) p.a.lse[out_row] = empty ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
+      }
+      // columns col .. col + E - 1 of this thread's row, of which it has the sums
+      auto add_odd = [&](float& o, int col) {
+        if (col >= p.a.dim) return;
+        const int n0 = (s.begin > s.p_tiles ? s.begin - s.p_tiles : 0) * KT, n1 = s.end > s.p_tiles ? (s.end - s.p_tiles) * KT : 0;
+        for (int v = n0; v < n1 && v <= u; ++v) {
+          if (!attn_sees(p.a, s.b, u, v)) continue;
+          const unsigned short raw = reinterpret_cast<const unsigned short*>(
+              p.a.v)[(long long)s.b * p.a.kv_stride[0] + (long long)v * p.a.kv_stride[1] + (long long)s.g * p.a.kv_stride[2] + col];
+          const float f = BF16 ? __uint_as_float((uint32_t)raw << 16) : __half2float(__ushort_as_half(raw));
+          if (!isfinite(f)) o += f;
+        }
+      };
+      if constexpr (C == 1) {
+        if (warp_in) {
+#pragma unroll 1
+          for (int c = 0; c < DP / 32; ++c) {
+            uint32_t o[32];
+            __syncwarp();  // rows that do not exist have gone another way
+            tc_ld32(o, my + Sh::COL_O + c * 32);
+            tc_wait_ld();
+            if (!in) continue;
+            if (odd && live) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
-                const int at = 2 * i;
-                const float a = ta_ex2(fmaf(__uint_as_float(x[2 * c + at / 32][at % 32]), scale2, -base));
-                const float b = ta_ex2(fmaf(__uint_as_float(x[2 * c + at / 32][at % 32 + 1]), scale2, -base));
-                sum0 += a;
-                sum1 += b;
-                w[i] = ta_pack<BF16>(a, b);
+                float v = __uint_as_float(o[i]);
+                add_odd(v, c * 32 + i);
+                o[i] = __float_as_uint(v);
               }
-              tc_st32(my + Sh::COL_S + c * 32, w);
             }
-            l += sum0 + sum1;
-            tc_wait_st();
+            if (!s.whole) {
+              float4* dst = reinterpret_cast<float4*>(p.part_o + at * DP + c * 32);
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                dst[i] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]),
+                                     __uint_as_float(o[4 * i + 3]));
+            } else {
+              uint4* dst = reinterpret_cast<uint4*>(p.a.out + 2 * (out_row * p.a.dim + c * 32));
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  w[e] = empty ? 0u : ta_pack<BF16>(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
+                if (c * 32 + i * 8 < p.a.dim) dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+              }
+            }
           }
-          tc_fence_before();
-          mbar_arrive(bar_p);
         }
-      }
-      more = next_piece(s_next);
-      if (ok) {
-        if (more) load_q(s_next);
-        ok = wait_warp(bar_o, n_seg & 1u);
-        tc_fence_after();
-        odd = ok && s_odd[n_seg & 1] == n_seg + 1;
-        ++n_seg;
-      }
-      if (!warp_in) continue;
-      // ---- the piece's result ---------------------------------------------------------------
-      if (!ok) l = NAN;  // a wait ran out: nothing of this piece is to be trusted
-      const long long row = ((long long)s.b * p.a.N + u) * p.a.heads_q + h;
-      const long long part = ((long long)blockIdx.x * 2 + s.which) * p.part_rows + tid;
-      const bool empty = !live || l == 0.0f;
-      const float inv = !ok ? NAN : (empty ? 0.0f : 1.0f / l);
-      if (in) {
-        if (!s.whole) p.part_ml[part] = live || !ok ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
-        else if (p.a.lse) p.a.lse[row] = !ok ? NAN : (empty ? -INFINITY : 0.6931471805599453f * (m + log2f(l)));
-      }
+      } else {
+        // TA_XCOLS columns at a time through shared memory; then each part sums its share of them over the parts
+        constexpr int E = TA_XCOLS / C;
 #pragma unroll 1
-      for (int c = 0; c < DP / 32; ++c) {
-        uint32_t o[32];
-        if (ok) {
-          tc_ld32(o, my + Sh::COL_O + c * 32);
-          tc_wait_ld();
-        } else {
+        for (int c = 0; c < DP / TA_XCOLS; ++c) {
+          if (warp_in) {
+            uint32_t o[TA_XCOLS];
+            __syncwarp();
+            tc_ld16(o, my + Sh::COL_O + c * TA_XCOLS);
+            tc_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = 0;
-        }
-        if (!in) continue;
-        if (odd && live) {
-          const int n0 = (s.begin > s.p_tiles ? s.begin - s.p_tiles : 0) * KT;
-          const int n1 = s.end > s.p_tiles ? (s.end - s.p_tiles) * KT : 0;
-          for (int v = n0; v < n1 && v <= u; ++v) {
-            if (!attn_sees(p.a, s.b, u, v)) continue;
-            const unsigned short* src = reinterpret_cast<const unsigned short*>(p.a.v) + (long long)s.b * p.a.kv_stride[0] +
-                                        (long long)v * p.a.kv_stride[1] + (long long)s.g * p.a.kv_stride[2] + c * 32;
+            for (int i = 0; i < TA_XCOLS; ++i) exchange[tid * (TA_XCOLS + 1) + i] = factor == 0.0f ? 0.0f : __uint_as_float(o[i]) * factor;
+          }
+          sync_rows();
+          if (!ok) break;
+          if (in) {
+            float v[E];
+            const int col = c * TA_XCOLS + part * E;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              if (c * 32 + i >= p.a.dim) break;
-              const unsigned short raw = src[i];
-              const float f = BF16 ? __uint_as_float((uint32_t)raw << 16) : __half2float(__ushort_as_half(raw));
-              if (!isfinite(f)) o[i] = __float_as_uint(__uint_as_float(o[i]) + f);
+            for (int e = 0; e < E; ++e) {
+              v[e] = 0.0f;
+#pragma unroll
+              for (int k = 0; k < C; ++k) v[e] += exchange[(k * PART_ROWS + row) * (TA_XCOLS + 1) + part * E + e];
+              if (odd && live) add_odd(v[e], col + e);
+            }
+            if (!s.whole) {
+              float4* dst = reinterpret_cast<float4*>(p.part_o + at * DP + col);
+#pragma unroll
+              for (int e = 0; e < E; e += 4) dst[e / 4] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+            } else if (col < p.a.dim) {
+              uint32_t w[E / 2];
+#pragma unroll
+              for (int e = 0; e < E; e += 2) w[e / 2] = empty ? 0u : ta_pack<BF16>(v[e] * inv, v[e + 1] * inv);
+              char* dst = p.a.out + 2 * (out_row * p.a.dim + col);
+              if constexpr (C == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+              else *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
             }
           }
+          sync_rows();
+          if (!ok) break;
         }
-        if (!s.whole) {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + part * DP + c * 32);
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            dst[i] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]),
-                                 __uint_as_float(o[4 * i + 3]));
-        } else {
-          uint4* dst = reinterpret_cast<uint4*>(p.a.out + 2 * (row * p.a.dim + c * 32));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float lo = empty && ok ? 0.0f : __uint_as_float(o[8 * i + 2 * e]) * inv;
-              const float hi = empty && ok ? 0.0f : __uint_as_float(o[8 * i + 2 * e + 1]) * inv;
-              w[e] = ta_pack<BF16>(lo, hi);
-            }
-            if (c * 32 + i * 8 < p.a.dim) dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        }
+        if (!ok) break;
       }
       tc_fence_before();
+    }
+    if (!ok) {  // a wait ran out: nothing that this block had to do is to be trusted
+      TaSeg s;
+      while (walk.next(p, s)) {
+        const int u = s.node0 + up, h = s.g * p.a.group + head;
+        if (!in_tile || part != 0 || u >= p.a.N) continue;
+        p.part_ml[part_row(s, row)] = make_float2(0.0f, NAN);
+        if (!s.whole) continue;
+        const long long out_row = ((long long)s.b * p.a.N + u) * p.a.heads_q + h;
+        if (p.a.lse) p.a.lse[out_row] = NAN;
+        for (int d = 0; d < p.a.dim; ++d) reinterpret_cast<unsigned short*>(p.a.out)[out_row * p.a.dim + d] = 0x7FFFu;  // NaN in both types
+      }
     }
   }
   __syncthreads();
@@ -693,8 +838,8 @@ template <int DP, bool BF16> __global__ void __launch_bounds__(TJ_WARPS * 32) jo
   if (rec.n_parts == 0) return;
   const int tiles_y = (p.part_rows + TJ_WARPS - 1) / TJ_WARPS;
   const int rt = blockIdx.y / tiles_y, in_tile = (blockIdx.y % tiles_y) * TJ_WARPS + warp;
-  const long long r = ((long long)rec.rb * p.group_ctas + rt) * TA_ROWS + in_tile;
-  if (in_tile >= p.part_rows || r >= p.rows) return;
+  const int up = in_tile / p.a.group, u = (rec.rb * p.group_ctas + rt) * p.tile_nodes + up, h = rec.g * p.a.group + in_tile - up * p.a.group;
+  if (in_tile >= p.part_rows || u >= p.a.N) return;
   auto at = [&](int i) {  // row of piece i in scratch
     const long long cta = (long long)(blockIdx.x + i) * p.group_ctas + rt;
     return (cta * 2 + (i == 0 ? rec.first_which : 0)) * p.part_rows + in_tile;
@@ -729,7 +874,6 @@ template <int DP, bool BF16> __global__ void __launch_bounds__(TJ_WARPS * 32) jo
       }
     }
   }
-  const int u = (int)(r / p.a.group), h = rec.g * p.a.group + (int)(r % p.a.group);
   const long long row = ((long long)rec.b * p.a.N + u) * p.a.heads_q + h;
   const bool empty = total == 0.0f;
   const float inv = empty ? 0.0f : 1.0f / total;
@@ -755,51 +899,52 @@ inline EncodeTiled encode_tiled() {
   return fn;
 }
 
-// A tensor [w][z][y][dim] of 16-bit elements (strides in elements) that is copied `rows` y at a time, 64 of dim wide.
-inline bool encode_map(CUtensorMap* map, const void* base, bool bf16, int dim, const long long (&n)[3], const long long (&stride)[3], int rows) {
+// A tensor [w][z][y][dim] of 16-bit elements (strides in elements) that is copied ny x nz rows at a time, 64 elements wide.
+inline bool encode_map(CUtensorMap* map, const void* base, bool bf16, int dim, const long long (&n)[3], const long long (&stride)[3], int ny,
+                       int nz) {
   cuuint64_t dims[4] = {(cuuint64_t)dim, 1, 1, 1}, strides[3];
   for (int i = 0; i < 3; ++i) {
     dims[i + 1] = (cuuint64_t)n[i];
-    strides[i] = n[i] == 1 ? 16 : (cuuint64_t)stride[i] * 2;
+    strides[i] = n[i] == 1 ? 16 : (cuuint64_t)stride[i] * 2;  // a dimension of extent 1 may have any stride
     if (strides[i] == 0 || (strides[i] & 15) != 0 || strides[i] >= (1ull << 40)) return false;
   }
-  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {64, (cuuint32_t)ny, (cuuint32_t)nz, 1}, step[4] = {1, 1, 1, 1};
   return encode_tiled()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), dims, strides,
                         box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 inline int tensor_dim(int dim) { return dim <= 64 ? 64 : (dim <= 128 ? 128 : 256); }
-inline size_t tensor_scratch_bytes(int rows, int dim) {
-  const size_t dp = tensor_dim(dim), ctas = dp == 256 ? TA_SMS : 2 * TA_SMS, part_rows = rows < TA_ROWS ? rows : TA_ROWS;
-  const size_t pieces = ctas * 2 * part_rows;
+// Row tiles hold whole nodes, so that one copy brings a tile's rows.
+inline int tile_nodes(int n, int group) { return n * group <= TA_ROWS ? n : TA_ROWS / group; }
+inline size_t tensor_scratch_bytes(int n, int group, int dim) {
+  if (group > TA_ROWS) return 256;
+  const size_t dp = tensor_dim(dim), ctas = dp == 256 ? TA_SMS : 2 * TA_SMS, pieces = ctas * 2 * tile_nodes(n, group) * group;
   return ctas * sizeof(TaRecord) + ((pieces * sizeof(float2) + 255) & ~(size_t)255) + pieces * dp * sizeof(float);
 }
 
-// STAND_E_ARG: not a call for these kernels (alignment, or what the copy unit cannot address); nothing was launched.
-template <int DP, bool BF16> int launch_tensor_attention(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
-  using Sh = TaShape<DP>;
+// STAND_E_ARG: not a call for these kernels (what the copy unit cannot address); nothing was launched.
+template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
+  using Sh = TaShape<DP, C>;
   TaParams p;
   p.a = a;
-  const long long rows = (long long)a.N * a.group;
-  p.rows = (int)rows;
-  const int row_tiles = (int)((rows + TA_ROWS - 1) / TA_ROWS);
+  p.tile_nodes = tile_nodes(a.N, a.group);
+  p.part_rows = p.tile_nodes * a.group;
+  const int row_tiles = (a.N + p.tile_nodes - 1) / p.tile_nodes;
   p.row_blocks = (row_tiles + TA_GROUP - 1) / TA_GROUP;
   p.group_ctas = (row_tiles + p.row_blocks - 1) / p.row_blocks;
   p.row_blocks = (row_tiles + p.group_ctas - 1) / p.group_ctas;
   p.tree_tiles = 0;
   for (int rb = 0; rb < p.row_blocks; ++rb) {
-    long long end = (long long)(rb + 1) * p.group_ctas * TA_ROWS;
-    if (end > rows) end = rows;
-    p.tree_tiles += (end - 1) / a.group / Sh::KT + 1;
+    const long long end = (long long)(rb + 1) * p.group_ctas * p.tile_nodes;
+    p.tree_tiles += ((end < a.N ? end : a.N) - 1) / TA_KT + 1;
   }
-  p.min_tiles = 4;
   p.groups = (sms < TA_SMS ? sms : TA_SMS) * Sh::CTAS / p.group_ctas;
-  const long long most = (long long)a.B * a.heads_kv * (p.row_blocks * (((long long)a.cols * a.page + Sh::KT - 1) / Sh::KT) + p.tree_tiles);
-  if (p.groups > (most + p.min_tiles - 1) / p.min_tiles) p.groups = (int)((most + p.min_tiles - 1) / p.min_tiles);
+  const long long most = (long long)a.B * a.heads_kv *
+                         (p.row_blocks * (((long long)a.cols * a.page + TA_KT - 1) / TA_KT + TA_PIECE_COST) + p.tree_tiles);
+  if (p.groups > (most + TA_MIN_TILES - 1) / TA_MIN_TILES) p.groups = (int)((most + TA_MIN_TILES - 1) / TA_MIN_TILES);
   p.box_rows = 16;
-  while (p.box_rows < Sh::KT && a.page % (p.box_rows * 2) == 0) p.box_rows *= 2;
-  p.part_rows = rows < TA_ROWS ? (int)rows : TA_ROWS;
+  while (p.box_rows < TA_KT && a.page % (p.box_rows * 2) == 0) p.box_rows *= 2;
   p.wait_limit = wait_limit;
 
   char* at = (char*)scratch;
@@ -811,36 +956,42 @@ template <int DP, bool BF16> int launch_tensor_attention(const AttnParams& a, vo
   p.part_o = (float*)at;
 
   const long long tree_n[3] = {a.N, a.heads_kv, a.B}, tree_stride[3] = {a.kv_stride[1], a.kv_stride[2], a.kv_stride[0]};
-  if (!encode_map(&p.tree_k, a.k, BF16, a.dim, tree_n, tree_stride, Sh::KT) || !encode_map(&p.tree_v, a.v, BF16, a.dim, tree_n, tree_stride, Sh::KT))
+  const long long q_n[3] = {a.heads_q, a.N, a.B}, q_stride[3] = {a.q_stride[2], a.q_stride[1], a.q_stride[0]};
+  if (!encode_map(&p.q, a.q, BF16, a.dim, q_n, q_stride, a.group, p.tile_nodes) ||
+      !encode_map(&p.tree_k, a.k, BF16, a.dim, tree_n, tree_stride, TA_KT, 1) ||
+      !encode_map(&p.tree_v, a.v, BF16, a.dim, tree_n, tree_stride, TA_KT, 1))
     return STAND_E_ARG;
   if (a.cols > 0) {
     const long long n[3] = {a.page, a.heads_kv, a.pages}, stride[3] = {a.cache_stride[2], a.cache_stride[1], a.cache_stride[0]};
-    if (a.pages < 1 || !encode_map(&p.cache_k, a.cache_k, BF16, a.dim, n, stride, p.box_rows) ||
-        !encode_map(&p.cache_v, a.cache_v, BF16, a.dim, n, stride, p.box_rows))
+    if (a.pages < 1 || !encode_map(&p.cache_k, a.cache_k, BF16, a.dim, n, stride, p.box_rows, 1) ||
+        !encode_map(&p.cache_v, a.cache_v, BF16, a.dim, n, stride, p.box_rows, 1))
       return STAND_E_ARG;
   } else {  // no cache: never read
     p.cache_k = p.tree_k;
     p.cache_v = p.tree_v;
   }
   static SmemLimit limit;
-  int rc = limit.raise(tensor_attention_kernel<DP, BF16>, Sh::SMEM);
+  int rc = limit.raise(tensor_attention_kernel<DP, C, BF16>, Sh::SMEM);
   if (rc) return STAND_E_CUDA;
-  rc = launch_dependent(tensor_attention_kernel<DP, BF16>, dim3((unsigned)(p.groups * p.group_ctas)), TA_THREADS, st, p, Sh::SMEM);
+  rc = launch_dependent(tensor_attention_kernel<DP, C, BF16>, dim3((unsigned)(p.groups * p.group_ctas)), TA_THREADS, st, p, Sh::SMEM);
   if (rc) return rc;
   const unsigned tiles_y = (unsigned)((p.part_rows + TJ_WARPS - 1) / TJ_WARPS);
   return launch_dependent(join_attention_kernel<DP, BF16>, dim3((unsigned)p.groups, tiles_y * p.group_ctas), TJ_WARPS * 32, st, p);
 }
 
-// Rows and strides of 16-byte pieces; a dimension of extent 1 may have any stride.
+template <int DP, bool BF16> int launch_tensor_parts(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
+  const int rows = tile_nodes(a.N, a.group) * a.group;
+  if (rows <= TA_ROWS / 4) return launch_tensor_attention<DP, 4, BF16>(a, scratch, sms, wait_limit, st);
+  if (rows <= TA_ROWS / 2) return launch_tensor_attention<DP, 2, BF16>(a, scratch, sms, wait_limit, st);
+  return launch_tensor_attention<DP, 1, BF16>(a, scratch, sms, wait_limit, st);
+}
+
+// Rows of 16-byte pieces (strides are looked at when they are encoded).
 inline bool tensor_takes(const AttnParams& a, int dtype) {
-  if (dtype == STAND_DTYPE_F32 || a.dim % 8 != 0 || !encode_tiled()) return false;
+  if (dtype == STAND_DTYPE_F32 || a.dim % 8 != 0 || a.group > TA_ROWS || !encode_tiled()) return false;
   uintptr_t bits = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.out;
   if (a.cols > 0) bits |= (uintptr_t)a.cache_k | (uintptr_t)a.cache_v;
-  if (bits & 15) return false;
-  const long long n[3] = {a.B, a.N, a.heads_q};
-  for (int i = 0; i < 3; ++i)
-    if (n[i] > 1 && a.q_stride[i] % 8 != 0) return false;
-  return true;
+  return (bits & 15) == 0;
 }
 
 }  // namespace stand
