@@ -1,9 +1,9 @@
 // Tree attention on the tensor cores (tcgen05, sm_100a): bfloat16 and half, head sizes that are a multiple of 8, 16-byte
 // aligned rows, up to 128 query heads per key head.
 //
-// A block (CTA) of six warps works on up to 128 rows of one (sequence, key head) pair and walks over its keys in tiles of
+// A block (CTA) of seven warps works on up to 128 rows of one (sequence, key head) pair and walks over its keys in tiles of
 // 64:
-//   warp 4  copies tiles of keys and of values from the pages (and from the tree's own keys) with TMA into a ring,
+//   warps 4 and 6  copy tiles of keys and of values from the pages (and from the tree's own) with TMA, each into a ring,
 //   warp 5  issues the matrix products S = Q K^T and O += P V, and copies the rows Q,
 //   warps 0-3  own one row per thread: read S, keep the running maximum and sum, write P, finally write O / l.
 // S and O live in tensor memory (a row is a lane).  P, in 16 bits, takes the place of S as the first operand of the second
@@ -31,7 +31,7 @@
 namespace stand {
 
 constexpr int TA_ROWS = 128;              // rows of a CTA: lanes of tensor memory
-constexpr int TA_THREADS = 192;
+constexpr int TA_THREADS = 224;
 constexpr int TA_SMS = 148;               // B200; scratch is laid out for that many
 constexpr int TA_GROUP = 4;               // row tiles that walk together, at most
 constexpr int TA_KT = 64;                 // keys per tile
@@ -43,7 +43,8 @@ constexpr int TA_XCOLS = 16;              // columns of O that the parts exchang
 template <int DP, int C> struct TaShape {
   static constexpr int CTAS = DP == 256 ? 1 : 2;              // per SM
   static constexpr int SLOT = TA_KT * DP * 2;                 // bytes of a tile of keys or values
-  static constexpr int SLOTS = DP == 64 ? (C > 1 ? 10 : 12) : (C > 1 ? 4 : 5);
+  static constexpr int K_SLOTS = DP == 64 ? (C > 1 ? 5 : 6) : 2, V_SLOTS = DP == 64 ? K_SLOTS : (C > 1 ? 2 : 3);
+  static constexpr int SLOTS = K_SLOTS + V_SLOTS;
   static constexpr int Q = TA_ROWS * DP * 2;
   static constexpr int COL_O = 0, COL_S = DP;                 // two places for S
   static constexpr int COLS = DP == 256 ? 512 : 256;          // tensor memory columns allocated
@@ -93,7 +94,7 @@ __device__ __forceinline__ uint32_t elect_one() {  // 1 in one lane of the (whol
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
   return r;
 }
-// The whole warp calls these two, the elected lane acts: the operands then sit in uniform registers, where the unit wants
+// The whole warp calls these (and the copies below), the elected lane acts: the operands then sit in uniform registers, where the unit wants
 // them.  (In a branch of one lane each product took 60 cycles to issue, most of it moving five operands there.)
 __device__ __forceinline__ void tc_commit(uint32_t bar, uint32_t elected) {
   asm volatile(
@@ -175,11 +176,14 @@ __host__ __device__ constexpr uint32_t mma_desc(bool bf16, bool b_transposed, in
   return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (b_transposed ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
 }
 
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z, int w) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
-               "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
-               : "memory");
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z, int w, uint32_t elected) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %7, 0;\n\t"
+      "@e cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];\n\t}" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w), "r"(elected)
+      : "memory");
 }
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(FULL, v, 0); }  // the compiler then knows that it is
 __device__ __forceinline__ float ta_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -197,20 +201,14 @@ template <bool BF16> __device__ __forceinline__ uint32_t ta_pack(float lo, float
   return r;
 }
 
-// Stores W / 2 words as the P of this part's W keys, and zeros as that of the other parts' keys.
-template <int C> __device__ __forceinline__ void store_p(uint32_t addr, int part, const uint32_t* w) {
-  if constexpr (C == 1) {
-    tc_st32(addr, w);
-  } else if constexpr (C == 2) {
-    const uint32_t zero[16] = {};
-    tc_st16(addr + part * 16, w);
-    tc_st16(addr + (part ^ 1) * 16, zero);
-  } else {
-    const uint32_t zero[8] = {};
-    tc_st8(addr + part * 8, w);
-#pragma unroll
-    for (int c = 1; c < 4; ++c) tc_st8(addr + ((part + c) & 3) * 8, zero);
-  }
+template <int N> __device__ __forceinline__ void tc_ld(uint32_t* r, uint32_t addr) {
+  if constexpr (N == 32) tc_ld32(r, addr);
+  else tc_ld16(r, addr);
+}
+template <int N> __device__ __forceinline__ void tc_st(uint32_t addr, const uint32_t* r) {
+  if constexpr (N == 32) tc_st32(addr, r);
+  else if constexpr (N == 16) tc_st16(addr, r);
+  else tc_st8(addr, r);
 }
 
 // ---- the walk over a group's range of tiles -----------------------------------------
@@ -278,12 +276,20 @@ struct TaWalk {
   }
 };
 
+// The rest of a wait that did not end at once; out of line, since each role's code should stay small: the roles share the
+// instruction caches, and a warp whose code is fetched anew takes several cycles per instruction.
+__device__ __noinline__ bool ta_wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned limit) {
+  const bool there = __all_sync(FULL, mbar_wait_timed(bar, parity, abort_flag, limit));
+  if (!there) *abort_flag = 1;
+  return there;
+}
+
 // ---- the kernel -----------------------------------------------------------------------
 template <int DP, int C, bool BF16>
 __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
   using Sh = TaShape<DP, C>;
-  constexpr int KT = TA_KT, HALVES = DP / 64, SLOTS = Sh::SLOTS;
-  constexpr int PART_ROWS = TA_ROWS / C, W = KT / C;  // rows of a part; keys of a tile that it takes
+  constexpr int KT = TA_KT, HALVES = DP / 64, SLOTS = Sh::SLOTS, K_SLOTS = Sh::K_SLOTS, V_SLOTS = Sh::V_SLOTS;
+  constexpr int PART_ROWS = TA_ROWS / C, W = KT / C, CH = W < 32 ? W : 32;  // rows of a part; keys of a tile that it takes
   extern __shared__ __align__(1024) char ta_smem[];
   struct Shared {
     uint64_t full[SLOTS], empty[SLOTS], q, s[2], p[2], o[2], x, drain;  // s, p, o: by the place of a tile's scores
@@ -295,7 +301,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     int b, abort;
   };
   static_assert(sizeof(Shared) <= Sh::SHARED, "barriers");
-  float* const exchange = reinterpret_cast<float*>(ta_smem + Sh::Q + SLOTS * Sh::SLOT);  // [TA_ROWS][TA_XCOLS + 1]
+  float* const exchange = reinterpret_cast<float*>(ta_smem + Sh::Q + SLOTS * Sh::SLOT);
   Shared& sh = *reinterpret_cast<Shared*>(ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -318,7 +324,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     mbar_init(smem_addr(&sh.x), TA_ROWS);
     mbar_init(smem_addr(&sh.drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    sh.abort = (q_smem & 1023) != 0;  // the swizzle goes by address bits
+    sh.abort = (q_smem & 1023) != 0 || p.wait_limit == 0;  // the swizzle goes by address bits; no waiting allowed
     sh.odd[0] = sh.odd[1] = 0;
     sh.b = 0;
     sh.b_start = 0;
@@ -397,138 +403,128 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
   volatile int* abort_flag = &sh.abort;
   const unsigned limit = p.wait_limit;
   auto wait_warp = [&](uint32_t bar, uint32_t parity) {  // the whole warp calls it; false: gave up, as all others soon will
-    bool there = limit && mbar_try_wait(bar, parity);
-    if (!there) there = mbar_wait_timed(bar, parity, abort_flag, limit);
-    there = __all_sync(FULL, there);
-    if (!there) *abort_flag = 1;
-    return there;
+    if (__all_sync(FULL, mbar_try_wait(bar, parity))) return true;
+    return ta_wait_on(bar, parity, abort_flag, limit);
   };
   const uint32_t bar_full = smem_addr(sh.full), bar_empty = smem_addr(sh.empty), bar_q = smem_addr(&sh.q), bar_s = smem_addr(sh.s),
                  bar_p = smem_addr(sh.p), bar_o = smem_addr(sh.o), bar_x = smem_addr(&sh.x);
   // scratch row of this CTA's piece
   auto part_row = [&](const TaSeg& s, int row) { return ((long long)blockIdx.x * 2 + s.which) * p.part_rows + row; };
 
-  if (warp == 4) {
-    // ---- keys and values: a lane per box (rows of one page x 64 elements) -----------------
-    // in the order of their use: K0 K1 V0 K2 V1 ... (the scores are one tile ahead)
+  if (warp == 4 || warp == 6) {
+    // ---- keys (warp 4), values (warp 6) --------------------------------------------------
+    // A tile is copied in boxes of box_rows rows of one page; lane i keeps the place of the tile's i-th box and reads its
+    // page's number a tile ahead.
+    const bool value = warp == 6;
+    const CUtensorMap* cache_map = value ? &p.cache_v : &p.cache_k;
+    const CUtensorMap* tree_map = value ? &p.tree_v : &p.tree_k;
+    const uint32_t slot0 = value ? K_SLOTS : 0, slots = value ? V_SLOTS : K_SLOTS;
     const int n_boxes = KT / p.box_rows;
-    const int half = lane % HALVES, box = lane / HALVES, row = box * p.box_rows;
+    const uint32_t elected = elect_one();
     TaSeg s;
     uint32_t slot = 0, phase = 1, used = 0;  // phase: parity of the wait for the slot's last use
     bool ok = *abort_flag == 0;
     while (ok && walk.next(p, s)) {
       if (s.begin >= s.end) {
-        if (s.rows && !s.whole)  // a piece of others that this CTA's rows do not see
+        if (s.rows && !s.whole && !value)  // a piece of others that this CTA's rows do not see
           for (int i = lane; i < p.part_rows; i += 32) p.part_ml[part_row(s, i)] = make_float2(-INFINITY, 0.0f);
         continue;
       }
-      auto page_of = [&](int j) {  // the page that this lane's box of tile j lies in; -1: none
-        const int pos = j * KT + row;
-        if (j >= s.p_tiles || j >= s.end || box >= n_boxes || pos >= s.len) return -1;
-        const int page = __ldg(p.a.table + (long long)s.b * p.a.cols + pos / p.a.page);
-        return page >= 0 && page < p.a.pages ? page : p.a.pages;  // past the pool: the copy unit fills in zeros
-      };
-      auto copy = [&](int j, int page, bool value) {
-        if (!wait_warp(bar_empty + 8 * slot, phase)) return false;
-        const bool tree = j >= s.p_tiles;
-        const uint32_t bar = bar_full + 8 * slot, dst = ring + slot * Sh::SLOT + half * (KT * 128);
-        if (lane == 0) {
-          const int left = s.len - j * KT, boxes = left >= KT ? n_boxes : (left + p.box_rows - 1) / p.box_rows;
-          mbar_expect_tx(bar, tree ? Sh::SLOT : (uint32_t)(boxes * HALVES * p.box_rows * 128));
-        }
-        __syncwarp();
-        if (tree) {
-          if (lane < HALVES) tma_load_4d(dst, value ? &p.tree_v : &p.tree_k, bar, half * 64, (j - s.p_tiles) * KT, s.g, s.b);
-        } else if (page >= 0) {
-          tma_load_4d(dst + row * 128, value ? &p.cache_v : &p.cache_k, bar, half * 64, (j * KT + row) % p.a.page, s.g, page);
+      const int b = uniform(s.b), g = uniform(s.g), len = uniform(s.len), p_tiles = uniform(s.p_tiles), begin = uniform(s.begin), end = uniform(s.end);
+      int pos = begin * KT + lane * p.box_rows, col = pos / p.a.page, in_page = pos - col * p.a.page;
+      const int* table = p.a.table + (long long)b * p.a.cols;
+      int next = lane < n_boxes && pos < len ? __ldg(table + col) : 0;
+      for (int tile = begin; tile < end; ++tile) {
+        const int page = next >= 0 && next < p.a.pages ? next : p.a.pages, at = in_page;  // past the pool: the copy unit fills in zeros
+        pos += KT;
+        for (in_page += KT; in_page >= p.a.page; in_page -= p.a.page) ++col;
+        if (lane < n_boxes && pos < len) next = __ldg(table + col);
+        if (!(ok = wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
+        const uint32_t bar = bar_full + 8 * (slot0 + slot), dst = ring + (slot0 + slot) * Sh::SLOT;
+        if (tile < p_tiles) {
+          const int left = len - tile * KT, boxes = left >= KT ? n_boxes : (left + p.box_rows - 1) / p.box_rows;
+          if (elected) mbar_expect_tx(bar, boxes * HALVES * p.box_rows * 128);
+          int from[KT / 16], row[KT / 16];
+#pragma unroll
+          for (int i = 0; i < KT / 16; ++i) from[i] = __shfl_sync(FULL, page, i), row[i] = __shfl_sync(FULL, at, i);
+#pragma unroll
+          for (int i = 0; i < KT / 16; ++i) {
+            if (i >= boxes) break;
+#pragma unroll
+            for (int half = 0; half < HALVES; ++half)
+              tma_load_4d(dst + half * (KT * 128) + i * p.box_rows * 128, cache_map, bar, half * 64, row[i], g, from[i], elected);
+          }
+        } else {
+          if (elected) mbar_expect_tx(bar, Sh::SLOT);
+#pragma unroll
+          for (int half = 0; half < HALVES; ++half)
+            tma_load_4d(dst + half * (KT * 128), tree_map, bar, half * 64, (tile - p_tiles) * KT, g, b, elected);
         }
         ++used;
-        if (++slot == SLOTS) slot = 0, phase ^= 1u;
-        return true;
-      };
-      int page = page_of(s.begin), page_next = page_of(s.begin + 1);
-      ok = copy(s.begin, page, false);
-      for (int j = s.begin; ok && j < s.end; ++j) {
-        const int page_after = page_of(j + 2);
-        if (j + 1 < s.end) ok = copy(j + 1, page_next, false);
-        ok = ok && copy(j, page, true);
-        page = page_next;
-        page_next = page_after;
+        if (++slot == slots) slot = 0, phase ^= 1u;
       }
     }
     if (!ok && lane == 0) {  // copies in flight land before the block ends
-      for (unsigned i = used > SLOTS ? used - SLOTS : 0; i < used; ++i)
-        mbar_wait_timed(bar_full + 8 * (i % SLOTS), (i / SLOTS) & 1u, nullptr, SPIN_LIMIT);
+      for (unsigned i = used > slots ? used - slots : 0; i < used; ++i)
+        mbar_wait_timed(bar_full + 8 * (slot0 + i % slots), (i / slots) & 1u, nullptr, SPIN_LIMIT);
     }
     __syncwarp();
   } else if (warp == 5) {
     // ---- products -----------------------------------------------------------------------
     constexpr uint32_t IDESC_S = mma_desc(BF16, false, KT), IDESC_O = mma_desc(BF16, true, DP);
     TaSeg s;
-    uint32_t slot = 0, phase = 0, n = 0, q_phase = 0, buf = 0;  // n: tiles so far
+    uint32_t k_slot = 0, k_phase = 0, v_slot = 0, v_phase = 0, n = 0, q_phase = 0, buf = 0;  // n: tiles so far
     const uint32_t elected = elect_one(), base = __shfl_sync(FULL, tmem, 0);
     const uint32_t q_desc = smem_desc_lo(q_smem, 16), k_desc = smem_desc_lo(ring, 16), v_desc = smem_desc_lo(ring, KT * 128);
     const uint32_t d_s = base + Sh::COL_S, d_o = base + Sh::COL_O;
     bool ok = *abort_flag == 0, copying = false;
-    auto next_piece = [&](TaSeg& s) {  // the next one with keys
-      while (walk.next(p, s))
-        if (s.begin < s.end) return true;
-      return false;
-    };
-    // the piece's rows into shared memory, and its description to the softmax warps, which wait for the same barrier
-    auto load_q = [&](const TaSeg& s, bool more) {
-      if (lane == 0) {
+    while (ok) {
+      bool more;
+      do more = walk.next(p, s);  // the next piece with keys
+      while (more && s.begin >= s.end);
+      // Its rows into shared memory, and its description to the softmax warps, which wait for the same barrier.  They
+      // have written P of the last tile before, so its scores are done with the rows that lie there.
+      if (elected) {
         sh.seg = s;
         if (!more) sh.seg.b = -1;
         if (more) mbar_expect_tx(bar_q, C * HALVES * p.part_rows * 128);
         else mbar_arrive(bar_q);
       }
-      __syncwarp();
-      if (more && lane < C * HALVES) {
-        const int part = lane / HALVES, half = lane % HALVES;
-        tma_load_4d(q_smem + half * (TA_ROWS * 128) + part * (PART_ROWS * 128), &p.q, bar_q, half * 64, s.g * p.a.group, s.node0, s.b);
-      }
-      copying = more;
-    };
-    auto scores = [&]() {  // S of the tile whose keys are in the ring's next slot
-      if (!wait_warp(bar_full + 8 * slot, phase)) return false;
-      tc_fence_after();
-      const uint32_t bk = k_desc + slot * (Sh::SLOT >> 4);
+      if (!more) break;
+      copying = true;
+      const int head = uniform(s.g * p.a.group), node0 = uniform(s.node0), b = uniform(s.b);
 #pragma unroll
-      for (int k = 0; k < DP / 16; ++k)
-        tc_mma_ss(d_s + buf * KT, q_desc + (((k >> 2) * (TA_ROWS * 128) + (k & 3) * 32) >> 4),
-                  bk + (((k >> 2) * (KT * 128) + (k & 3) * 32) >> 4), SMEM_DESC_HI, IDESC_S, k > 0, elected);
-      tc_commit(bar_s + 8 * buf, elected);
-      tc_commit(bar_empty + 8 * slot, elected);
-      if (++slot == SLOTS) slot = 0, phase ^= 1u;
-      buf ^= 1u;
-      return true;
-    };
-    bool more = next_piece(s);
-    if (ok) load_q(s, more);
-    while (ok && more) {
-      const int tiles = __shfl_sync(FULL, s.end - s.begin, 0);
-      ok = wait_warp(bar_q, q_phase);
-      if (!ok) break;
+      for (int i = 0; i < C * HALVES; ++i)
+        tma_load_4d(q_smem + i % HALVES * (TA_ROWS * 128) + i / HALVES * (PART_ROWS * 128), &p.q, bar_q, i % HALVES * 64, head, node0, b, elected);
+      const int tiles = uniform(s.end - s.begin);
+      if (!(ok = wait_warp(bar_q, q_phase))) break;
       copying = false;
       q_phase ^= 1u;
-      tc_fence_after();
-      ok = scores();
-      for (int j = 0; ok && j < tiles; ++j, ++n) {
-        // The scores' place was that of tile j - 1, whose P V is issued: products run in order.
-        if (j + 1 < tiles) ok = scores();
-        else more = next_piece(s);
-        const uint32_t d_p = d_s + (n & 1) * KT;
-        ok = ok && wait_warp(bar_full + 8 * slot, phase) && wait_warp(bar_p + 8 * (n & 1), (n >> 1) & 1u);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t bv = v_desc + slot * (Sh::SLOT >> 4);
+      for (int j = -1; j < tiles; ++j) {
+        if (j + 1 < tiles) {  // S of tile j + 1.  Its place was that of tile j - 1, whose P V is issued: products run in order.
+          if (!(ok = wait_warp(bar_full + 8 * k_slot, k_phase))) break;
+          tc_fence_after();
+          const uint32_t bk = k_desc + k_slot * (Sh::SLOT >> 4);
 #pragma unroll
-        for (int k = 0; k < KT / 16; ++k) tc_mma(d_o, d_p + k * 8, bv + k * (2048 >> 4), SMEM_DESC_HI, IDESC_O, k > 0 || j > 0, elected);
-        tc_commit(bar_o + 8 * (n & 1), elected);
-        tc_commit(bar_empty + 8 * slot, elected);
-        if (++slot == SLOTS) slot = 0, phase ^= 1u;
-        if (j + 1 == tiles) load_q(s, more);  // P of the last tile is there, so the scores are done with these rows
+          for (int k = 0; k < DP / 16; ++k)
+            tc_mma_ss(d_s + buf * KT, q_desc + (((k >> 2) * (TA_ROWS * 128) + (k & 3) * 32) >> 4),
+                      bk + (((k >> 2) * (KT * 128) + (k & 3) * 32) >> 4), SMEM_DESC_HI, IDESC_S, k > 0, elected);
+          tc_commit(bar_s + 8 * buf, elected);
+          tc_commit(bar_empty + 8 * k_slot, elected);
+          if (++k_slot == K_SLOTS) k_slot = 0, k_phase ^= 1u;
+          buf ^= 1u;
+        }
+        if (j >= 0) {  // O += P V of tile j
+          if (!(ok = wait_warp(bar_full + 8 * (K_SLOTS + v_slot), v_phase) && wait_warp(bar_p + 8 * (n & 1), (n >> 1) & 1u))) break;
+          tc_fence_after();
+          const uint32_t bv = v_desc + (K_SLOTS + v_slot) * (Sh::SLOT >> 4), d_p = d_s + (n & 1) * KT;
+#pragma unroll
+          for (int k = 0; k < KT / 16; ++k) tc_mma(d_o, d_p + k * 8, bv + k * (2048 >> 4), SMEM_DESC_HI, IDESC_O, k > 0 || j > 0, elected);
+          tc_commit(bar_o + 8 * (n & 1), elected);
+          tc_commit(bar_empty + 8 * (K_SLOTS + v_slot), elected);
+          if (++v_slot == V_SLOTS) v_slot = 0, v_phase ^= 1u;
+          ++n;
+        }
       }
     }
     if (!ok) {  // what is in flight ends before the block does
@@ -545,7 +541,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     const bool in_tile = row < p.part_rows, warp_in = (warp * 32) % PART_ROWS < p.part_rows;
     const int up = in_tile ? row / p.a.group : 0, head = in_tile ? row - up * p.a.group : 0;
     const float scale2 = p.a.scale2;
-    unsigned n = 0, n_seg = 0, base_it = 0, x_phase = 0;  // tiles, pieces and copies so far
+    unsigned n = 0, n_seg = 0, x_phase = 0;  // tiles and pieces so far
     bool ok = *abort_flag == 0;
     auto sync_rows = [&]() {  // all rows' threads
       mbar_arrive(bar_x);
@@ -569,44 +565,43 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
         if (!ok) break;
         tc_fence_after();
         if (warp_in) {
-          const uint32_t s_addr = my + Sh::COL_S + (n & 1) * KT;
-          uint32_t x[W];
-          if constexpr (C == 4) {
-            tc_ld16(x, s_addr + part * W);
-          } else {
-#pragma unroll
-            for (int c = 0; c < W / 32; ++c) tc_ld32(x + c * 32, s_addr + part * W + c * 32);
-          }
-          tc_wait_ld();
-          if (tree || partial) {
-#pragma unroll
-            for (int c = 0; c < (W + 31) / 32; ++c) {
-              const int key = part * W + c * 32;  // of the tile
-              uint32_t seen;
-              if (tree) {
-                const int first = (j - s.p_tiles) * KT + key, below = u + 1 - first;  // nodes first .. u
-                seen = below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
-                if (p.a.mask && seen)
-                  seen &= __ldg(p.a.mask + (long long)s.b * p.a.mask_stride + (long long)u * p.a.mask_words + (first >> 5)) >> (first & 31);
-              } else {
-                const int below = left - key;
-                seen = below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
-              }
-#pragma unroll
-              for (int i = 0; i < (W < 32 ? W : 32); ++i) x[c * 32 + i] = seen >> i & 1u ? x[c * 32 + i] : 0xFF800000u;
-            }
-          }
+          // Twice over the scores, 32 (or all W) at a time, from tensor memory both times: little code, few registers.
+          const uint32_t s_addr = my + Sh::COL_S + (n & 1) * KT + part * W;
           float top = -INFINITY, top1 = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < W / CH; ++c) {
+            uint32_t x[CH];
+            tc_ld<CH>(x, s_addr + c * CH);
+            tc_wait_ld();
+            if (tree || partial) {
+              const int key = part * W + c * CH;  // of the tile
+              int below;                          // this row sees keys before that, or none after it
+              uint32_t seen = FULL;
+              if (tree) {
+                const int first = (j - s.p_tiles) * KT + key;
+                below = u + 1 - first;            // nodes first .. u
+                if (p.a.mask && below > 0)
+                  seen = __ldg(p.a.mask + (long long)s.b * p.a.mask_stride + (long long)u * p.a.mask_words + (first >> 5)) >> (first & 31);
+              } else {
+                below = left - key;
+              }
+              seen &= below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
 #pragma unroll
-          for (int i = 0; i < W; i += 4) {
-            top = max3(top, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-            top1 = max3(top1, __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
+              for (int i = 0; i < CH; ++i) x[i] = seen >> i & 1u ? x[i] : 0xFF800000u;
+              __syncwarp();
+              tc_st<CH>(s_addr + c * CH, x);
+              tc_wait_st();
+            }
+#pragma unroll
+            for (int i = 0; i < CH; i += 4) {
+              top = max3(top, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+              top1 = max3(top1, __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
+            }
           }
           top = fmaxf(top, top1) * scale2;
           // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores pass
           // it by TA_SLACK, so that o is seldom read, scaled and written (weights up to 2^8 lose nothing in either 16-bit
           // type, sums are fp32).
-          __syncwarp();
           if (__any_sync(FULL, top > m + TA_SLACK)) {
             const float raised = fmaxf(m, top);
             const float keep = raised == -INFINITY ? 1.0f : ta_ex2(m - raised);
@@ -628,17 +623,31 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
             }
           }
           const float base = m == -INFINITY ? 0.0f : m;
-          float sum0 = 0.0f, sum1 = 0.0f;
-          uint32_t w[W / 2];
+          const unsigned long long scale_2 = pack2(scale2, scale2), base_2 = pack2(-base, -base);
+          unsigned long long sum_2 = pack2(0.0f, 0.0f);
+#pragma unroll 1
+          for (int c = 0; c < W / CH; ++c) {
+            uint32_t x[CH], w[CH / 2];
+            tc_ld<CH>(x, s_addr + c * CH);
+            tc_wait_ld();
 #pragma unroll
-          for (int i = 0; i < W / 2; ++i) {
-            const float a = ta_ex2(fmaf(__uint_as_float(x[2 * i]), scale2, -base));
-            const float b = ta_ex2(fmaf(__uint_as_float(x[2 * i + 1]), scale2, -base));
-            sum0 += a;
-            sum1 += b;
-            w[i] = ta_pack<BF16>(a, b);
+            for (int i = 0; i < CH / 2; ++i) {
+              float a, b;
+              unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), scale_2, base_2), a, b);
+              a = ta_ex2(a);
+              b = ta_ex2(b);
+              sum_2 = add2(sum_2, pack2(a, b));
+              w[i] = ta_pack<BF16>(a, b);
+            }
+            tc_st<CH / 2>(s_addr - part * W + part * (W / 2) + c * (CH / 2), w);
           }
-          store_p<C>(s_addr, part, w);
+          if constexpr (C > 1) {  // the other parts' keys have no weight in these lanes
+            const uint32_t zero[W / 2] = {};
+#pragma unroll
+            for (int k = 1; k < C; ++k) tc_st<W / 2>(s_addr - part * W + (part + k) % C * (W / 2), zero);
+          }
+          float sum0, sum1;
+          unpack2(sum_2, sum0, sum1);
           l += sum0 + sum1;
           tc_wait_st();
         }
@@ -646,10 +655,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           // Values that no row sees must not enter the product, 0 times them included: those past the text's end become
           // zero.  In the tree some rows may see what others do not: there, elements that are not finite become zero and
           // are added at the end to the rows that do see them.
-          // (Not before the scores are there: until then the slot may still await the tile before the last.)
-          const int t = j - s.begin;
-          const unsigned iv = base_it + (j + 1 < s.end ? 2 * t + 2 : 2 * t + 1), slot = iv % SLOTS;
-          ok = wait_warp(bar_full + 8 * slot, (iv / SLOTS) & 1u);
+          // (Not before the scores are there: until then the slot may still await the values of two tiles before.)
+          const unsigned slot = K_SLOTS + n % V_SLOTS;
+          ok = wait_warp(bar_full + 8 * slot, (n / V_SLOTS) & 1u);
           if (!ok) break;
           char* v0 = ta_smem + Sh::Q + slot * Sh::SLOT;
           if (partial) {
@@ -685,7 +693,6 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
       if (!ok) break;
       tc_fence_after();
       const bool odd = sh.odd[n_seg & 1] == n_seg + 1;
-      base_it += 2 * (s.end - s.begin);
       ++n_seg;
 
       // ---- the piece's result ---------------------------------------------------------------
@@ -706,6 +713,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
         factor = ta_ex2(m - base);
         m = top;
         l = total;
+        sync_rows();  // all have read
+        if (!ok) break;
+        if (part == 0) sh.ml[row] = make_float2(!live || l == 0.0f ? 0.0f : 1.0f / l, live ? 1.0f : 0.0f);
       }
       const long long out_row = ((long long)s.b * p.a.N + u) * p.a.heads_q + h, at = part_row(s, row);
       const bool empty = !live || l == 0.0f;
@@ -714,8 +724,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
         if (!s.whole) p.part_ml[at] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
         else if (p.a.lse) p.a.lse[out_row] = empty ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
       }
-      // columns col .. col + E - 1 of this thread's row, of which it has the sums
-      auto add_odd = [&](float& o, int col) {
+      auto add_odd = [&](float& o, int col, int u) {
         if (col >= p.a.dim) return;
         const int n0 = (s.begin > s.p_tiles ? s.begin - s.p_tiles : 0) * KT, n1 = s.end > s.p_tiles ? (s.end - s.p_tiles) * KT : 0;
         for (int v = n0; v < n1 && v <= u; ++v) {
@@ -739,7 +748,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
                 float v = __uint_as_float(o[i]);
-                add_odd(v, c * 32 + i);
+                add_odd(v, c * 32 + i, u);
                 o[i] = __float_as_uint(v);
               }
             }
@@ -763,41 +772,49 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           }
         }
       } else {
-        // TA_XCOLS columns at a time through shared memory; then each part sums its share of them over the parts
-        constexpr int E = TA_XCOLS / C;
+        // Some columns at a time through shared memory, as many as fit (with few rows all of them); then each thread
+        // sums four columns of a row over the parts.
+        const int rows = p.part_rows;
+        int cols = TA_XCOLS;
+        while (cols < DP && C * rows * (2 * cols + 1) <= TA_ROWS * (TA_XCOLS + 1)) cols *= 2;
+        const int pitch = cols + 1;
 #pragma unroll 1
-        for (int c = 0; c < DP / TA_XCOLS; ++c) {
+        for (int c0 = 0; c0 < DP; c0 += cols) {
           if (warp_in) {
-            uint32_t o[TA_XCOLS];
-            __syncwarp();
-            tc_ld16(o, my + Sh::COL_O + c * TA_XCOLS);
-            tc_wait_ld();
+#pragma unroll 1
+            for (int c = 0; c < cols; c += 16) {
+              uint32_t o[16];
+              __syncwarp();
+              tc_ld16(o, my + Sh::COL_O + c0 + c);
+              tc_wait_ld();
+              if (in_tile) {
 #pragma unroll
-            for (int i = 0; i < TA_XCOLS; ++i) exchange[tid * (TA_XCOLS + 1) + i] = factor == 0.0f ? 0.0f : __uint_as_float(o[i]) * factor;
+                for (int i = 0; i < 16; ++i)
+                  exchange[(part * rows + row) * pitch + c + i] = factor == 0.0f ? 0.0f : __uint_as_float(o[i]) * factor;
+              }
+            }
           }
           sync_rows();
           if (!ok) break;
-          if (in) {
-            float v[E];
-            const int col = c * TA_XCOLS + part * E;
+          const int quads = cols / 4;
+          for (int i = tid; i < rows * quads; i += TA_ROWS) {
+            const int r = i / quads, q = i - r * quads, col = c0 + q * 4;
+            const int ru = s.node0 + r / p.a.group, rh = s.g * p.a.group + r % p.a.group;
+            if (ru >= p.a.N) continue;
+            float v[4] = {};
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              v[e] = 0.0f;
+            for (int k = 0; k < C; ++k)
 #pragma unroll
-              for (int k = 0; k < C; ++k) v[e] += exchange[(k * PART_ROWS + row) * (TA_XCOLS + 1) + part * E + e];
-              if (odd && live) add_odd(v[e], col + e);
-            }
+              for (int e = 0; e < 4; ++e) v[e] += exchange[(k * rows + r) * pitch + q * 4 + e];
+            const float2 ml = sh.ml[r];  // 1 / l, and whether the row is there at all
+            if (odd && ml.y != 0.0f)
+              for (int e = 0; e < 4; ++e) add_odd(v[e], col + e, ru);
             if (!s.whole) {
-              float4* dst = reinterpret_cast<float4*>(p.part_o + at * DP + col);
-#pragma unroll
-              for (int e = 0; e < E; e += 4) dst[e / 4] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+              *reinterpret_cast<float4*>(p.part_o + part_row(s, r) * DP + col) = make_float4(v[0], v[1], v[2], v[3]);
             } else if (col < p.a.dim) {
-              uint32_t w[E / 2];
-#pragma unroll
-              for (int e = 0; e < E; e += 2) w[e / 2] = empty ? 0u : ta_pack<BF16>(v[e] * inv, v[e + 1] * inv);
-              char* dst = p.a.out + 2 * (out_row * p.a.dim + col);
-              if constexpr (C == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-              else *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+              const bool none = ml.x == 0.0f;
+              *reinterpret_cast<uint2*>(p.a.out + 2 * ((((long long)s.b * p.a.N + ru) * p.a.heads_q + rh) * p.a.dim + col)) =
+                  make_uint2(none ? 0u : ta_pack<BF16>(v[0] * ml.x, v[1] * ml.x), none ? 0u : ta_pack<BF16>(v[2] * ml.x, v[3] * ml.x));
             }
           }
           sync_rows();
