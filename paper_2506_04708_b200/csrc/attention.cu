@@ -34,7 +34,11 @@ extern "C" {
 
 size_t stand_tree_attention_scratch_bytes(const stand_attention* c) {
   if (!attention_valid(c)) return 0;
-  return tensor_scratch_bytes(c->N, c->heads_q / c->heads_kv, c->dim);
+  const int group = c->heads_q / c->heads_kv;
+  const size_t plain = ta_scratch_bytes(plain_tile_rows(c->N * group), c->dim, plain_ctas(c->dim));
+  if (c->dtype == STAND_DTYPE_F32 || group > TA_ROWS) return plain;
+  const size_t tensor = ta_scratch_bytes(tensor_tile_rows(c->N, group), c->dim, tensor_ctas(c->dim));
+  return tensor > plain ? tensor : plain;  // alignment decides, and that is not known here
 }
 
 int stand_tree_attention(const stand_attention* c, const void* dev_q, const void* dev_k, const void* dev_v, const void* dev_cache_k,
@@ -54,9 +58,9 @@ int stand_tree_attention(const stand_attention* c, const void* dev_q, const void
   p.scale2 = (float)((double)c->scale * 1.4426950408889634);
   for (int i = 0; i < 3; ++i) { p.q_stride[i] = c->q_stride[i]; p.kv_stride[i] = c->kv_stride[i]; p.cache_stride[i] = c->cache_stride[i]; }
   cudaStream_t st = (cudaStream_t)cu_stream;
+  int dev = -1, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return STAND_E_CUDA;
   if (tensor_takes(p, c->dtype)) {
-    int dev = -1, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return STAND_E_CUDA;
     const int dp = tensor_dim(p.dim);
     const bool bf = c->dtype == STAND_DTYPE_BF16;
     const unsigned limit = wait_limit();
@@ -66,9 +70,9 @@ int stand_tree_attention(const stand_attention* c, const void* dev_q, const void
     else rc = bf ? launch_tensor_parts<256, true>(p, dev_scratch, sms, limit, st) : launch_tensor_parts<256, false>(p, dev_scratch, sms, limit, st);
     if (rc != STAND_E_ARG) return rc;  // strides that the copy unit cannot take: the other kernel
   }
-  if (c->dtype == STAND_DTYPE_F32) return launch_plain_attention<float>(p, st);
-  if (c->dtype == STAND_DTYPE_BF16) return launch_plain_attention<__nv_bfloat16>(p, st);
-  return launch_plain_attention<__half>(p, st);
+  if (c->dtype == STAND_DTYPE_F32) return launch_plain_attention<float>(p, dev_scratch, sms, st);
+  if (c->dtype == STAND_DTYPE_BF16) return launch_plain_attention<__nv_bfloat16>(p, dev_scratch, sms, st);
+  return launch_plain_attention<__half>(p, dev_scratch, sms, st);
 }
 
 int stand_tree_mask(const int32_t* host_parent, int32_t n, uint32_t* host_mask) {

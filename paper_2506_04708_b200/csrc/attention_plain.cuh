@@ -1,144 +1,294 @@
-// Tree attention without matrix instructions: any type, any strides, any head size up to ATTN_DIM_MAX.
+// Tree attention without matrix instructions: any type (single precision among them), any strides, any head size up to
+// ATTN_DIM_MAX.
+//
+// A block takes up to RT rows of a pair and walks over its tiles of 64 keys (attention_split.cuh), two tiles of keys and
+// values in shared memory (single precision: cp.async; 16-bit types are converted on the way).  A warp has RT / 8 rows; for
+// the scores a lane has two keys, for the sums its share of the head size.  So every value from shared memory is used for
+// RT / 8 rows, no sum crosses a warp, and the products run near the rate of the fused multiply-adds (RT = 32: 12 shared-memory
+// passes for 32 of them in the scores, 20 for 64 in the sums).  With at most 8 rows RT = 8 leaves no thread without a row.
 #pragma once
-#include "attention.cuh"
+#include "async.cuh"
+#include "attention_split.cuh"
 #include "launch.cuh"
 
 namespace stand {
 
 constexpr int ATTN_DIM_MAX = 256;
-constexpr int PA_WARPS = 4, PA_ROWS = 4;       // rows per warp
-constexpr int PA_BLOCK_ROWS = PA_WARPS * PA_ROWS;
-constexpr int PA_KEYS = 32;                    // keys per tile, one per lane
-constexpr int PA_OUT = ATTN_DIM_MAX / 32;      // output elements of a row per lane
+constexpr int PA_WARPS = 8, PA_THREADS = PA_WARPS * 32;
 
-inline size_t plain_smem_bytes(int dim) { return sizeof(float) * (size_t)(PA_KEYS * (dim + 1) + PA_KEYS * dim + PA_BLOCK_ROWS * dim); }
+template <int DP> struct PaShape {
+  static constexpr int STAGES = DP == 256 ? 1 : 2;
+  static constexpr int KP = DP + 4;                                     // floats between keys: no bank conflicts
+  static constexpr int STAGE = TA_KT * KP + TA_KT * DP;                 // floats of a tile of keys and of values
+  template <int RT> static constexpr int smem() { return (STAGES * STAGE + RT * KP + RT * TA_KT) * 4; }
+};
+// Blocks per SM that the split counts on.
+inline int plain_ctas(int dim) { return tensor_dim(dim) == 64 ? 2 : 1; }
+inline int plain_tile_rows(int rows) { return rows <= 8 ? 8 : 32; }
 
-template <typename T>
-__global__ void __launch_bounds__(PA_WARPS * 32) plain_attention_kernel(const AttnParams p) {
+template <typename T> __device__ __forceinline__ float4 load4(const T* p, bool wide) {
+  if constexpr (sizeof(T) == 2) {
+    if (wide) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      const T* e = reinterpret_cast<const T*>(&v);
+      return make_float4(to_float(e[0]), to_float(e[1]), to_float(e[2]), to_float(e[3]));
+    }
+  } else if (wide) {
+    return *reinterpret_cast<const float4*>(p);
+  }
+  return make_float4(to_float(p[0]), to_float(p[1]), to_float(p[2]), to_float(p[3]));
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// wide: bases and strides allow 4 elements at a time
+template <typename T, int DP, int RT>
+__global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __grid_constant__ TaSplit p, const bool wide) {
+  using Sh = PaShape<DP>;
+  constexpr int KT = TA_KT, KP = Sh::KP, STAGES = Sh::STAGES, R = RT / PA_WARPS, E = DP / 32;
+  constexpr int EV = E < 4 ? E : 4;  // elements of the head size that lie together: lane * EV + 128 * i
   extern __shared__ float pa_smem[];
-  __shared__ const T* s_key[PA_KEYS];
-  __shared__ const T* s_value[PA_KEYS];
-  const int D = p.dim, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  float* sk = pa_smem;                       // [PA_KEYS][D + 1]
-  float* sv = sk + PA_KEYS * (D + 1);        // [PA_KEYS][D]
-  float* sq = sv + PA_KEYS * D;              // [PA_BLOCK_ROWS][D]
+  __shared__ const T* s_src[3][2][KT];  // where keys and values of a tile lie; null: zeros
+  __shared__ TaRange<PA_THREADS> s_range;
+  float* const sq = pa_smem + STAGES * Sh::STAGE;                      // [RT][KP]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.dim, D4 = (D + 3) & ~3;
+  float* const sp = sq + RT * KP + warp * R * KT;                      // [R][KT] of this warp
   pdl_trigger();
   pdl_wait();
-  const int R = p.N * p.group;
-  const int b = (int)(blockIdx.x / p.heads_kv), g = (int)(blockIdx.x % p.heads_kv);
-  const int r0 = blockIdx.y * PA_BLOCK_ROWS;
-  const int n_rows = R - r0 < PA_BLOCK_ROWS ? R - r0 : PA_BLOCK_ROWS;
-  const long long len = attn_len(p, b);
-  const int last_node = (r0 + n_rows - 1) / p.group;
-  const long long n_keys = len + last_node + 1;
-
-  for (int i = tid; i < PA_BLOCK_ROWS * D; i += PA_WARPS * 32) {
-    const int r = r0 + i / D, d = i % D;
-    float v = 0.0f;
-    if (r < R) {
-      const int u = r / p.group, h = g * p.group + r % p.group;
-      v = to_float(reinterpret_cast<const T*>(p.q)[b * p.q_stride[0] + u * p.q_stride[1] + h * p.q_stride[2] + d]);
-    }
-    sq[i] = v;
-  }
-  int node[PA_ROWS];
-  bool live[PA_ROWS];
-  float m[PA_ROWS], l[PA_ROWS], o[PA_ROWS][PA_OUT];
-#pragma unroll
-  for (int i = 0; i < PA_ROWS; ++i) {
-    const int r = r0 + warp * PA_ROWS + i;
-    node[i] = r / p.group;
-    live[i] = r < R && !(p.tree && p.tree[(long long)b * p.N + node[i]] < 0);
-    m[i] = -INFINITY;
-    l[i] = 0.0f;
-#pragma unroll
-    for (int e = 0; e < PA_OUT; ++e) o[i][e] = 0.0f;
+  TaWalk walk;
+  ta_begin<PA_THREADS>(p, walk, s_range, [] {}, [] {});
+  // what a row has beyond the head size counts as zeros
+  for (int i = tid; i < STAGES * KT * (D4 - D); i += PA_THREADS) {
+    const int row = i / (D4 - D);
+    pa_smem[row / KT * Sh::STAGE + row % KT * KP + D + i % (D4 - D)] = 0.0f;
   }
 
-  for (long long k0 = 0; k0 < n_keys; k0 += PA_KEYS) {
-    __syncthreads();  // the tile before has been used
-    if (tid < PA_KEYS) {
-      const long long pos = k0 + tid;
-      const T *key = nullptr, *value = nullptr;
-      if (pos < len) {
-        const long long c = pos / p.page;
-        const int page = p.table[(long long)b * p.cols + c];
-        if (page >= 0 && page < p.pages) {
-          const long long at = page * p.cache_stride[0] + g * p.cache_stride[1] + (pos - c * p.page) * p.cache_stride[2];
-          key = reinterpret_cast<const T*>(p.cache_k) + at;
-          value = reinterpret_cast<const T*>(p.cache_v) + at;
+  TaSeg s;
+  while (walk.next(p, s)) {
+    if (!s.rows) continue;
+    const T* kv[2] = {reinterpret_cast<const T*>(p.a.k), reinterpret_cast<const T*>(p.a.v)};
+    const T* cache[2] = {reinterpret_cast<const T*>(p.a.cache_k), reinterpret_cast<const T*>(p.a.cache_v)};
+    auto find = [&](int tile) {  // where the rows of a tile are
+      if (tid < 2 * KT && tile < s.end) {
+        const int key = tid % KT, which = tid / KT;
+        const T* src = nullptr;
+        if (tile < s.p_tiles) {
+          const int pos = tile * KT + key, c = pos / p.a.page;
+          if (pos < s.len) {
+            const int page = p.a.table[(long long)s.b * p.a.cols + c];
+            if (page >= 0 && page < p.a.pages)
+              src = cache[which] + page * p.a.cache_stride[0] + s.g * p.a.cache_stride[1] + (long long)(pos - c * p.a.page) * p.a.cache_stride[2];
+          }
+        } else {
+          const int node = (tile - s.p_tiles) * KT + key;
+          if (node < p.a.N) src = kv[which] + s.b * p.a.kv_stride[0] + node * p.a.kv_stride[1] + s.g * p.a.kv_stride[2];
         }
-      } else if (pos < n_keys) {
-        const long long at = b * p.kv_stride[0] + (pos - len) * p.kv_stride[1] + g * p.kv_stride[2];
-        key = reinterpret_cast<const T*>(p.k) + at;
-        value = reinterpret_cast<const T*>(p.v) + at;
+        s_src[tile % 3][which][key] = src;
       }
-      s_key[tid] = key;
-      s_value[tid] = value;
+    };
+    auto fetch = [&](int tile) {
+      if (tile < s.end) {
+        float* const base = pa_smem + (tile % STAGES) * Sh::STAGE;
+        if (wide) {
+          const int quads = D / 4;
+          for (int i = tid; i < 2 * KT * quads; i += PA_THREADS) {
+            const int row = i / quads, q = i - row * quads, key = row % KT;
+            const T* src = s_src[tile % 3][row / KT][key];
+            float* dst = row < KT ? base + key * KP + q * 4 : base + KT * KP + key * DP + q * 4;
+            if (!src) *reinterpret_cast<float4*>(dst) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            else if constexpr (sizeof(T) == 4) cp_async16(smem_addr(dst), src + q * 4);
+            else *reinterpret_cast<float4*>(dst) = load4(src + q * 4, true);
+          }
+        } else {
+          for (int i = tid; i < 2 * KT * D; i += PA_THREADS) {
+            const int row = i / D, d = i - row * D, key = row % KT;
+            const T* src = s_src[tile % 3][row / KT][key];
+            float* dst = row < KT ? base + key * KP + d : base + KT * KP + key * DP + d;
+            if (!src) *dst = 0.0f;
+            else if constexpr (sizeof(T) == 4) cp_async4(smem_addr(dst), src + d);
+            else *dst = to_float(src[d]);
+          }
+        }
+      }
+      cp_commit();
+    };
+
+    __syncthreads();  // the piece before has been read
+    for (int i = tid; i < RT * D4; i += PA_THREADS) {
+      const int row = i / D4, d = i - row * D4, r = s.row0 + row;
+      float v = 0.0f;
+      if (row < p.tile_rows && r < p.rows && d < D) {
+        const int u = r / p.a.group, h = s.g * p.a.group + r - u * p.a.group;
+        v = to_float(reinterpret_cast<const T*>(p.a.q)[s.b * p.a.q_stride[0] + u * p.a.q_stride[1] + h * p.a.q_stride[2] + d]);
+      }
+      sq[row * KP + d] = v;
     }
+    int node[R];
+    bool live[R];
+    float m[R], l[R], o[R][E];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int row = warp * R + i, r = s.row0 + row;
+      node[i] = r / p.a.group;
+      live[i] = row < p.tile_rows && r < p.rows && !(p.a.tree && p.a.tree[(long long)s.b * p.a.N + node[i]] < 0);
+      m[i] = -INFINITY;
+      l[i] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[i][e] = 0.0f;
+    }
+    find(s.begin);
+    find(s.begin + 1);
     __syncthreads();
-    for (int i = tid; i < PA_KEYS * D; i += PA_WARPS * 32) {
-      const int j = i / D, d = i % D;
-      sk[j * (D + 1) + d] = s_key[j] ? to_float(s_key[j][d]) : 0.0f;
-      sv[j * D + d] = s_value[j] ? to_float(s_value[j][d]) : 0.0f;
+    if (STAGES == 2) fetch(s.begin);
+
+    for (int j = s.begin; j < s.end; ++j) {
+      if (STAGES == 2) {
+        fetch(j + 1);
+        find(j + 2);
+        cp_wait<1>();
+      } else {
+        fetch(j);
+        find(j + 2);
+        cp_wait<0>();
+      }
+      __syncthreads();
+      const float* sk = pa_smem + (j % STAGES) * Sh::STAGE;
+      const float* sv = sk + KT * KP;
+      float x[R][2];
+#pragma unroll
+      for (int i = 0; i < R; ++i) x[i][0] = x[i][1] = 0.0f;
+      const float* q0 = sq + warp * R * KP;
+#pragma unroll 4
+      for (int d = 0; d < D4; d += 4) {
+        const float4 k0 = *reinterpret_cast<const float4*>(sk + lane * KP + d), k1 = *reinterpret_cast<const float4*>(sk + (lane + 32) * KP + d);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const float4 q = *reinterpret_cast<const float4*>(q0 + i * KP + d);
+          x[i][0] = fmaf(q.x, k0.x, fmaf(q.y, k0.y, fmaf(q.z, k0.z, fmaf(q.w, k0.w, x[i][0]))));
+          x[i][1] = fmaf(q.x, k1.x, fmaf(q.y, k1.y, fmaf(q.z, k1.z, fmaf(q.w, k1.w, x[i][1]))));
+        }
+      }
+      const bool tree = j >= s.p_tiles, partial = !tree && s.len - j * KT < KT;
+      uint32_t seen[R][2];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int key = lane + 32 * c;
+          bool sees = live[i];
+          if (partial) sees = sees && key < s.len - j * KT;
+          else if (tree) {
+            const int v = (j - s.p_tiles) * KT + key;
+            sees = sees && v < p.a.N && attn_sees(p.a, s.b, node[i], v);
+          }
+          seen[i][c] = __ballot_sync(FULL, sees);
+          x[i][c] = sees ? x[i][c] * p.a.scale2 : -INFINITY;
+        }
+        const float top = fmaxf(m[i], warp_max_f(fmaxf(x[i][0], x[i][1])));
+        const float base = top == -INFINITY ? 0.0f : top, keep = exp2f(m[i] - base);
+        float w[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          w[c] = seen[i][c] >> lane & 1u ? exp2f(x[i][c] - base) : 0.0f;
+          sp[i * KT + lane + 32 * c] = w[c];
+        }
+        m[i] = top;
+        l[i] = l[i] * keep + warp_sum_f(w[0] + w[1]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[i][e] *= keep;
+      }
+      __syncwarp();
+      if (!tree && !partial) {
+#pragma unroll 2
+        for (int k = 0; k < KT; k += 4) {
+          float4 w[R];
+#pragma unroll
+          for (int i = 0; i < R; ++i) w[i] = *reinterpret_cast<const float4*>(sp + i * KT + k);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            float v[E];
+#pragma unroll
+            for (int e = 0; e < E; e += EV) {
+              const float* src = sv + (k + kk) * DP + lane * EV + e / EV * 128;
+              if constexpr (EV == 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(src);
+              else *reinterpret_cast<float2*>(v + e) = *reinterpret_cast<const float2*>(src);
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const float wk = kk == 0 ? w[i].x : (kk == 1 ? w[i].y : (kk == 2 ? w[i].z : w[i].w));
+#pragma unroll
+              for (int e = 0; e < E; ++e) o[i][e] = fmaf(wk, v[e], o[i][e]);
+            }
+          }
+        }
+      } else {  // an unseen value may be anything, 0 times it too: row by row, only what it sees
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            for (uint32_t left = seen[i][c]; left; left &= left - 1) {
+              const int k = 32 * c + __ffs(left) - 1;
+              const float wk = sp[i * KT + k];
+#pragma unroll
+              for (int e = 0; e < E; ++e) o[i][e] = fmaf(wk, sv[k * DP + lane * EV + e / EV * 128 + e % EV], o[i][e]);
+            }
+      }
+      __syncthreads();  // the tile has been read
     }
-    __syncthreads();
-    float s[PA_ROWS];
+
 #pragma unroll
-    for (int i = 0; i < PA_ROWS; ++i) s[i] = 0.0f;
-    const float* q0 = sq + warp * PA_ROWS * D;
-    for (int d = 0; d < D; ++d) {
-      const float kd = sk[lane * (D + 1) + d];
+    for (int i = 0; i < R; ++i) {
+      const int row = warp * R + i, r = s.row0 + row;
+      if (row >= p.tile_rows || r >= p.rows) continue;
+      const int h = s.g * p.a.group + r - node[i] * p.a.group;
+      const long long out = ((long long)s.b * p.a.N + node[i]) * p.a.heads_q + h, at = ta_part_row(p, s, row);
+      const bool empty = !live[i] || l[i] == 0.0f;
+      if (lane == 0) {
+        if (!s.whole) p.part_ml[at] = live[i] ? make_float2(m[i], l[i]) : make_float2(-INFINITY, 0.0f);
+        else if (p.a.lse) p.a.lse[out] = empty ? -INFINITY : 0.6931471805599453f * (m[i] + log2f(l[i]));
+      }
 #pragma unroll
-      for (int i = 0; i < PA_ROWS; ++i) s[i] = fmaf(q0[i * D + d], kd, s[i]);
-    }
-    const long long pos = k0 + lane;
-#pragma unroll
-    for (int i = 0; i < PA_ROWS; ++i) {
-      bool sees = live[i] && pos < n_keys;
-      if (sees && pos >= len) sees = attn_sees(p, b, node[i], (int)(pos - len));
-      const uint32_t seen = __ballot_sync(FULL, sees);
-      if (seen == 0) continue;
-      const float x = sees ? s[i] * p.scale2 : -INFINITY;
-      const float top = fmaxf(m[i], warp_max_f(x));
-      const float base = top == -INFINITY ? 0.0f : top;
-      const float w = sees ? exp2f(x - base) : 0.0f;
-      const float keep = exp2f(m[i] - base);
-      m[i] = top;
-      l[i] = l[i] * keep + warp_sum_f(w);
-#pragma unroll
-      for (int e = 0; e < PA_OUT; ++e) o[i][e] *= keep;
-      for (int j = 0; j < PA_KEYS; ++j) {
-        if (!(seen >> j & 1u)) continue;  // an unseen value may be anything, 0 times it too
-        const float wj = __shfl_sync(FULL, w, j);
-#pragma unroll
-        for (int e = 0; e < PA_OUT; ++e)
-          if (e * 32 + lane < D) o[i][e] = fmaf(wj, sv[j * D + e * 32 + lane], o[i][e]);
+      for (int e = 0; e < E; ++e) {
+        const int d = lane * EV + e / EV * 128 + e % EV;
+        if (!s.whole) p.part_o[at * DP + d] = o[i][e];
+        else if (d < D) reinterpret_cast<T*>(p.a.out)[out * D + d] = from_float<T>(empty ? 0.0f : o[i][e] / l[i]);
       }
     }
-  }
-#pragma unroll
-  for (int i = 0; i < PA_ROWS; ++i) {
-    const int r = r0 + warp * PA_ROWS + i;
-    if (r >= R) continue;
-    const int u = r / p.group, h = g * p.group + r % p.group;
-    const long long row = ((long long)b * p.N + u) * p.heads_q + h;
-    const bool empty = l[i] == 0.0f;
-#pragma unroll
-    for (int e = 0; e < PA_OUT; ++e)
-      if (e * 32 + lane < D) reinterpret_cast<T*>(p.out)[row * D + e * 32 + lane] = from_float<T>(empty ? 0.0f : o[i][e] / l[i]);
-    if (p.lse && lane == 0) p.lse[row] = empty ? -INFINITY : 0.6931471805599453f * (m[i] + log2f(l[i]));
   }
 }
 
-template <typename T> int launch_plain_attention(const AttnParams& p, cudaStream_t st) {
-  const size_t smem = plain_smem_bytes(p.dim);
+template <typename T, int DP, int RT> int launch_plain_rows(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
+  TaSplit p;
+  ta_split(p, a, RT, DP, sms, plain_ctas(DP), 2, scratch);
+  const size_t al = 4 * sizeof(T);
+  uintptr_t bits = (uintptr_t)a.k | (uintptr_t)a.v | (a.cols > 0 ? (uintptr_t)a.cache_k | (uintptr_t)a.cache_v : 0);
+  for (int i = 0; i < 3; ++i) bits |= (uintptr_t)(a.kv_stride[i] * sizeof(T)) | (a.cols > 0 ? (uintptr_t)(a.cache_stride[i] * sizeof(T)) : 0);
+  const bool wide = bits % al == 0 && a.dim % 4 == 0;
   static SmemLimit limit;
-  int rc = limit.raise(plain_attention_kernel<T>, plain_smem_bytes(ATTN_DIM_MAX));
+  const int smem = PaShape<DP>::template smem<RT>();
+  int rc = limit.raise(plain_attention_kernel<T, DP, RT>, smem);
   if (rc) return rc;
-  const int R = p.N * p.group;
-  const dim3 grid((unsigned)(p.B * p.heads_kv), (unsigned)((R + PA_BLOCK_ROWS - 1) / PA_BLOCK_ROWS));
-  return launch_dependent(plain_attention_kernel<T>, grid, PA_WARPS * 32, st, p, smem);
+  rc = launch_dependent2(plain_attention_kernel<T, DP, RT>, dim3((unsigned)(p.groups * p.group_ctas)), PA_THREADS, st, (size_t)smem, p, wide);
+  if (rc) return rc;
+  return launch_join<DP, T>(p, st);
+}
+
+template <typename T> int launch_plain_attention(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
+  const int dp = tensor_dim(a.dim);
+  if (plain_tile_rows(a.N * a.group) == 8) {
+    if (dp == 64) return launch_plain_rows<T, 64, 8>(a, scratch, sms, st);
+    if (dp == 128) return launch_plain_rows<T, 128, 8>(a, scratch, sms, st);
+    return launch_plain_rows<T, 256, 8>(a, scratch, sms, st);
+  }
+  if (dp == 64) return launch_plain_rows<T, 64, 32>(a, scratch, sms, st);
+  if (dp == 128) return launch_plain_rows<T, 128, 32>(a, scratch, sms, st);
+  return launch_plain_rows<T, 256, 32>(a, scratch, sms, st);
 }
 
 }  // namespace stand

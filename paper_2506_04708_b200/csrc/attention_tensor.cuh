@@ -25,18 +25,13 @@
 #include <cuda.h>
 
 #include "async.cuh"
-#include "attention.cuh"
+#include "attention_split.cuh"
 #include "launch.cuh"
 
 namespace stand {
 
 constexpr int TA_ROWS = 128;              // rows of a CTA: lanes of tensor memory
 constexpr int TA_THREADS = 224;
-constexpr int TA_SMS = 148;               // B200; scratch is laid out for that many
-constexpr int TA_GROUP = 4;               // row tiles that walk together, at most
-constexpr int TA_KT = 64;                 // keys per tile
-constexpr int TA_PIECE_COST = 3;          // what beginning and ending a piece costs, in tiles
-constexpr int TA_MIN_TILES = 4;           // fewest tiles (that cost included) worth a range of their own
 constexpr float TA_SLACK = 8.0f;          // the maximum is raised only when scores pass it by 2^8 (below)
 constexpr int TA_XCOLS = 16;              // columns of O that the parts exchange at a time
 
@@ -55,25 +50,10 @@ template <int DP, int C> struct TaShape {
   static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory");
 };
 
-struct TaRecord {  // what the joining kernel has to do for the last pair that a group began
-  int n_parts;     // 0: nothing (that pair ends within the group)
-  int first_which, b, g, rb;
-  int pad[3];
-};
-
 struct alignas(64) TaParams {
   CUtensorMap cache_k, cache_v, tree_k, tree_v, q;
-  AttnParams a;
-  int tile_nodes;     // nodes of a row tile
-  int part_rows;      // its rows: rows of a piece in scratch
-  int row_blocks;     // groups of row tiles
-  int group_ctas;     // row tiles per group
-  int groups;
+  TaSplit s;
   int box_rows;       // rows of a page that one copy takes
-  long long tree_tiles;  // sum over the row blocks of a pair
-  TaRecord* records;
-  float2* part_ml;
-  float* part_o;
   unsigned wait_limit;
 };
 
@@ -211,71 +191,6 @@ template <int N> __device__ __forceinline__ void tc_st(uint32_t addr, const uint
   else tc_st8(addr, r);
 }
 
-// ---- the walk over a group's range of tiles -----------------------------------------
-struct TaSeg {
-  int b, g, rb, node0;     // pair, row block, first node of this CTA
-  int len, p_tiles;        // cached tokens, their tiles
-  int begin, end;          // this CTA's tiles of the pair (cached ones, then the tree's)
-  int whole;               // the range covers the pair
-  int rows;                // the CTA has rows in this block
-  int which;               // the group's first piece or a later one
-  int starts, units;       // the pair begins in this group's range; its length there (cost and tiles)
-};
-
-struct TaWalk {
-  long long t, hi, b_start;
-  int b;
-  bool first;
-
-  // tree tiles that nodes before node_end see
-  __device__ static __forceinline__ int tree_tiles(const TaParams& p, int node_end) {
-    return ((node_end < p.a.N ? node_end : p.a.N) - 1) / TA_KT + 1;
-  }
-  // length of all pairs and row blocks of a (sequence, key head), in tiles, a piece's fixed cost included
-  __device__ static __forceinline__ long long per_head(const TaParams& p, long long len) {
-    return p.row_blocks * ((len + TA_KT - 1) / TA_KT + TA_PIECE_COST) + p.tree_tiles;
-  }
-  __device__ static __forceinline__ long long length_of(const TaParams& p, int b) { return p.a.heads_kv * per_head(p, attn_len(p.a, b)); }
-  __device__ __forceinline__ bool next(const TaParams& p, TaSeg& s) {
-    while (t < hi) {
-      s.len = (int)attn_len(p.a, b);
-      s.p_tiles = (s.len + TA_KT - 1) / TA_KT;
-      const long long head = per_head(p, s.len);
-      long long off = t - b_start;
-      if (off >= p.a.heads_kv * head) {
-        b_start += p.a.heads_kv * head;
-        ++b;
-        continue;
-      }
-      s.b = b;
-      s.g = head <= 0x7FFFFFFF && off <= 0x7FFFFFFF ? (int)((uint32_t)off / (uint32_t)head) : (int)(off / head);
-      off -= s.g * head;
-      s.rb = 0;
-      while (true) {
-        s.units = TA_PIECE_COST + s.p_tiles + tree_tiles(p, (s.rb + 1) * p.group_ctas * p.tile_nodes);
-        if (off < s.units) break;
-        off -= s.units;
-        ++s.rb;
-      }
-      const int from = (int)off, to = s.units - from < hi - t ? s.units : (int)(from + (hi - t));
-      s.starts = from == 0;
-      s.whole = from == 0 && to == s.units;
-      s.which = first ? 0 : 1;
-      first = false;
-      t += to - from;
-      s.begin = from > TA_PIECE_COST ? from - TA_PIECE_COST : 0;
-      s.end = to > TA_PIECE_COST ? to - TA_PIECE_COST : 0;
-      s.node0 = (s.rb * p.group_ctas + blockIdx.x % p.group_ctas) * p.tile_nodes;
-      s.rows = s.node0 < p.a.N;
-      const int own = s.rows ? s.p_tiles + tree_tiles(p, s.node0 + p.tile_nodes) : 0;  // later tree tiles are above all of this CTA's rows
-      if (s.end > own) s.end = own;
-      if (s.end < s.begin) s.end = s.begin;
-      return true;
-    }
-    return false;
-  }
-};
-
 // The rest of a wait that did not end at once; out of line, since each role's code should stay small: the roles share the
 // instruction caches, and a warp whose code is fetched anew takes several cycles per instruction.
 __device__ __noinline__ bool ta_wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned limit) {
@@ -293,12 +208,12 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
   extern __shared__ __align__(1024) char ta_smem[];
   struct Shared {
     uint64_t full[SLOTS], empty[SLOTS], q, s[2], p[2], o[2], x, drain;  // s, p, o: by the place of a tile's scores
-    long long sum[TA_THREADS / 32], b_start, lo, hi;
+    TaRange<TA_THREADS> range;
     float2 ml[C > 1 ? TA_ROWS : 1];
     TaSeg seg;         // the piece that the rows in shared memory belong to; b < 0: no more
     unsigned odd[2];   // 1 + the last piece (even ones, odd ones) whose tree has values that are not finite
     uint32_t tmem;
-    int b, abort;
+    int abort;
   };
   static_assert(sizeof(Shared) <= Sh::SHARED, "barriers");
   float* const exchange = reinterpret_cast<float*>(ta_smem + Sh::Q + SLOTS * Sh::SLOT);
@@ -317,88 +232,20 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     mbar_init(smem_addr(&sh.q), 1);
     mbar_init(smem_addr(&sh.s[0]), 1);
     mbar_init(smem_addr(&sh.s[1]), 1);
-    mbar_init(smem_addr(&sh.p[0]), TA_ROWS);
-    mbar_init(smem_addr(&sh.p[1]), TA_ROWS);
+    mbar_init(smem_addr(&sh.p[0]), 4);  // a lane of each warp arrives for it
+    mbar_init(smem_addr(&sh.p[1]), 4);
     mbar_init(smem_addr(&sh.o[0]), 1);
     mbar_init(smem_addr(&sh.o[1]), 1);
-    mbar_init(smem_addr(&sh.x), TA_ROWS);
+    mbar_init(smem_addr(&sh.x), 4);
     mbar_init(smem_addr(&sh.drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.abort = (q_smem & 1023) != 0 || p.wait_limit == 0;  // the swizzle goes by address bits; no waiting allowed
     sh.odd[0] = sh.odd[1] = 0;
-    sh.b = 0;
-    sh.b_start = 0;
   }
   pdl_wait();
 
-  // this group's range, and the sequence in which it begins
   TaWalk walk;
-  const int group = blockIdx.x / p.group_ctas;
-  {
-    const int per = (p.a.B + TA_THREADS - 1) / TA_THREADS;
-    const int b0 = tid * per, b1 = b0 + per < p.a.B ? b0 + per : p.a.B;
-    long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += TaWalk::length_of(p, b);
-    long long upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long v = __shfl_up_sync(FULL, upto, o);
-      if (lane >= o) upto += v;
-    }
-    if (lane == 31) sh.sum[warp] = upto;
-    __syncthreads();
-    long long total = 0;
-    for (int w = 0; w < TA_THREADS / 32; ++w) {
-      if (w < warp) upto += sh.sum[w];
-      total += sh.sum[w];
-    }
-    long long groups = (total + TA_MIN_TILES - 1) / TA_MIN_TILES;
-    if (groups > p.groups) groups = p.groups;
-    const long long lo = group < groups ? total * group / groups : total;
-    const long long hi = group < groups ? total * (group + 1) / groups : total;
-    if (lo < hi && upto - mine <= lo && lo < upto) {
-      long long at = upto - mine;
-      for (int b = b0; b < b1; ++b) {
-        const long long n = TaWalk::length_of(p, b);
-        if (lo < at + n) {
-          sh.b = b;
-          sh.b_start = at;
-          break;
-        }
-        at += n;
-      }
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    walk.t = lo;
-    walk.hi = hi;
-    walk.b = sh.b;
-    walk.b_start = sh.b_start;
-    walk.first = true;
-    if (tid == 0 && blockIdx.x % p.group_ctas == 0) {
-      // the pair in which the range ends, if it began here and goes on in the next groups
-      TaRecord r;
-      r.n_parts = 0;
-      r.first_which = r.b = r.g = r.rb = 0;
-      if (lo < hi && group + 1 < groups) {
-        TaWalk w = walk;
-        TaSeg s;
-        long long from = w.t;
-        while (w.next(p, s)) {
-          if (w.t == hi && s.starts && hi - from < s.units) {
-            r.n_parts = (int)(((from + s.units) * groups - 1) / total) - group + 1;
-            r.first_which = s.which;
-            r.b = s.b;
-            r.g = s.g;
-            r.rb = s.rb;
-          }
-          from = w.t;
-        }
-      }
-      p.records[group] = r;
-    }
-  }
+  ta_begin<TA_THREADS>(p.s, walk, sh.range, [] { tc_fence_before(); }, [] { tc_fence_after(); });
   const uint32_t tmem = sh.tmem;
   volatile int* abort_flag = &sh.abort;
   const unsigned limit = p.wait_limit;
@@ -408,8 +255,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
   };
   const uint32_t bar_full = smem_addr(sh.full), bar_empty = smem_addr(sh.empty), bar_q = smem_addr(&sh.q), bar_s = smem_addr(sh.s),
                  bar_p = smem_addr(sh.p), bar_o = smem_addr(sh.o), bar_x = smem_addr(&sh.x);
-  // scratch row of this CTA's piece
-  auto part_row = [&](const TaSeg& s, int row) { return ((long long)blockIdx.x * 2 + s.which) * p.part_rows + row; };
+  auto part_row = [&](const TaSeg& s, int row) { return ta_part_row(p.s, s, row); };
 
   if (warp == 4 || warp == 6) {
     // ---- keys (warp 4), values (warp 6) --------------------------------------------------
@@ -424,20 +270,20 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     TaSeg s;
     uint32_t slot = 0, phase = 1, used = 0;  // phase: parity of the wait for the slot's last use
     bool ok = *abort_flag == 0;
-    while (ok && walk.next(p, s)) {
+    while (ok && walk.next(p.s, s)) {
       if (s.begin >= s.end) {
         if (s.rows && !s.whole && !value)  // a piece of others that this CTA's rows do not see
-          for (int i = lane; i < p.part_rows; i += 32) p.part_ml[part_row(s, i)] = make_float2(-INFINITY, 0.0f);
+          for (int i = lane; i < p.s.tile_rows; i += 32) p.s.part_ml[part_row(s, i)] = make_float2(-INFINITY, 0.0f);
         continue;
       }
       const int b = uniform(s.b), g = uniform(s.g), len = uniform(s.len), p_tiles = uniform(s.p_tiles), begin = uniform(s.begin), end = uniform(s.end);
-      int pos = begin * KT + lane * p.box_rows, col = pos / p.a.page, in_page = pos - col * p.a.page;
-      const int* table = p.a.table + (long long)b * p.a.cols;
+      int pos = begin * KT + lane * p.box_rows, col = pos / p.s.a.page, in_page = pos - col * p.s.a.page;
+      const int* table = p.s.a.table + (long long)b * p.s.a.cols;
       int next = lane < n_boxes && pos < len ? __ldg(table + col) : 0;
       for (int tile = begin; tile < end; ++tile) {
-        const int page = next >= 0 && next < p.a.pages ? next : p.a.pages, at = in_page;  // past the pool: the copy unit fills in zeros
+        const int page = next >= 0 && next < p.s.a.pages ? next : p.s.a.pages, at = in_page;  // past the pool: the copy unit fills in zeros
         pos += KT;
-        for (in_page += KT; in_page >= p.a.page; in_page -= p.a.page) ++col;
+        for (in_page += KT; in_page >= p.s.a.page; in_page -= p.s.a.page) ++col;
         if (lane < n_boxes && pos < len) next = __ldg(table + col);
         if (!(ok = wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
         const uint32_t bar = bar_full + 8 * (slot0 + slot), dst = ring + (slot0 + slot) * Sh::SLOT;
@@ -480,19 +326,19 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     bool ok = *abort_flag == 0, copying = false;
     while (ok) {
       bool more;
-      do more = walk.next(p, s);  // the next piece with keys
+      do more = walk.next(p.s, s);  // the next piece with keys
       while (more && s.begin >= s.end);
       // Its rows into shared memory, and its description to the softmax warps, which wait for the same barrier.  They
       // have written P of the last tile before, so its scores are done with the rows that lie there.
       if (elected) {
         sh.seg = s;
         if (!more) sh.seg.b = -1;
-        if (more) mbar_expect_tx(bar_q, C * HALVES * p.part_rows * 128);
+        if (more) mbar_expect_tx(bar_q, C * HALVES * p.s.tile_rows * 128);
         else mbar_arrive(bar_q);
       }
       if (!more) break;
       copying = true;
-      const int head = uniform(s.g * p.a.group), node0 = uniform(s.node0), b = uniform(s.b);
+      const int head = uniform(s.g * p.s.a.group), node0 = uniform(s.row0 / p.s.a.group), b = uniform(s.b);
 #pragma unroll
       for (int i = 0; i < C * HALVES; ++i)
         tma_load_4d(q_smem + i % HALVES * (TA_ROWS * 128) + i / HALVES * (PART_ROWS * 128), &p.q, bar_q, i % HALVES * 64, head, node0, b, elected);
@@ -538,13 +384,14 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     // ---- softmax: thread = row (of a part) -------------------------------------------------
     const uint32_t my = tmem + ((uint32_t)(warp * 32) << 16);
     const int part = tid / PART_ROWS, row = tid % PART_ROWS;  // a warp lies in one part
-    const bool in_tile = row < p.part_rows, warp_in = (warp * 32) % PART_ROWS < p.part_rows;
-    const int up = in_tile ? row / p.a.group : 0, head = in_tile ? row - up * p.a.group : 0;
-    const float scale2 = p.a.scale2;
+    const bool in_tile = row < p.s.tile_rows, warp_in = (warp * 32) % PART_ROWS < p.s.tile_rows;
+    const int up = in_tile ? row / p.s.a.group : 0, head = in_tile ? row - up * p.s.a.group : 0;
+    const float scale2 = p.s.a.scale2;
     unsigned n = 0, n_seg = 0, x_phase = 0;  // tiles and pieces so far
     bool ok = *abort_flag == 0;
     auto sync_rows = [&]() {  // all rows' threads
-      mbar_arrive(bar_x);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_x);
       ok = wait_warp(bar_x, x_phase) && ok;
       x_phase ^= 1u;
     };
@@ -553,9 +400,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
       if (!ok) break;
       const TaSeg s = sh.seg;
       if (s.b < 0) break;
-      const int u = s.node0 + up, h = s.g * p.a.group + head;
-      const bool in = in_tile && u < p.a.N;
-      const bool live = in && !(p.a.tree && p.a.tree[(long long)s.b * p.a.N + u] < 0);
+      const int u = s.row0 / p.s.a.group + up, h = s.g * p.s.a.group + head;
+      const bool in = in_tile && u < p.s.a.N;
+      const bool live = in && !(p.s.a.tree && p.s.a.tree[(long long)s.b * p.s.a.N + u] < 0);
       float m = -INFINITY, l = 0.0f;
       for (int j = s.begin; j < s.end; ++j, ++n) {
         const bool tree = j >= s.p_tiles;
@@ -580,8 +427,8 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
               if (tree) {
                 const int first = (j - s.p_tiles) * KT + key;
                 below = u + 1 - first;            // nodes first .. u
-                if (p.a.mask && below > 0)
-                  seen = __ldg(p.a.mask + (long long)s.b * p.a.mask_stride + (long long)u * p.a.mask_words + (first >> 5)) >> (first & 31);
+                if (p.s.a.mask && below > 0)
+                  seen = __ldg(p.s.a.mask + (long long)s.b * p.s.a.mask_stride + (long long)u * p.s.a.mask_words + (first >> 5)) >> (first & 31);
               } else {
                 below = left - key;
               }
@@ -666,7 +513,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
               for (int hh = 0; hh < HALVES; ++hh) *reinterpret_cast<uint4*>(v0 + hh * (KT * 128) + i * 16) = make_uint4(0, 0, 0, 0);
           } else {
             constexpr uint32_t EXP = BF16 ? 0x7F80u : 0x7C00u;
-            const int nodes = p.a.N - (j - s.p_tiles) * KT, pieces = (nodes < KT ? nodes : KT) * 8;  // the rest are zeros
+            const int nodes = p.s.a.N - (j - s.p_tiles) * KT, pieces = (nodes < KT ? nodes : KT) * 8;  // the rest are zeros
             for (int k = tid; k < HALVES * pieces; k += TA_ROWS) {
               const int i = k + (HALVES > 1 ? k / pieces * (KT * 8 - pieces) : 0);
               uint4 v = *reinterpret_cast<uint4*>(v0 + i * 16);
@@ -686,7 +533,8 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         tc_fence_before();
-        mbar_arrive(bar_p + 8 * (n & 1));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p + 8 * (n & 1));
       }
       if (!ok) break;
       ok = wait_warp(bar_o + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1u);
@@ -717,20 +565,20 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
         if (!ok) break;
         if (part == 0) sh.ml[row] = make_float2(!live || l == 0.0f ? 0.0f : 1.0f / l, live ? 1.0f : 0.0f);
       }
-      const long long out_row = ((long long)s.b * p.a.N + u) * p.a.heads_q + h, at = part_row(s, row);
+      const long long out_row = ((long long)s.b * p.s.a.N + u) * p.s.a.heads_q + h, at = part_row(s, row);
       const bool empty = !live || l == 0.0f;
       const float inv = empty ? 0.0f : 1.0f / l;
       if (in && part == 0) {
-        if (!s.whole) p.part_ml[at] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
-        else if (p.a.lse) p.a.lse[out_row] = empty ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
+        if (!s.whole) p.s.part_ml[at] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
+        else if (p.s.a.lse) p.s.a.lse[out_row] = empty ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
       }
       auto add_odd = [&](float& o, int col, int u) {
-        if (col >= p.a.dim) return;
+        if (col >= p.s.a.dim) return;
         const int n0 = (s.begin > s.p_tiles ? s.begin - s.p_tiles : 0) * KT, n1 = s.end > s.p_tiles ? (s.end - s.p_tiles) * KT : 0;
         for (int v = n0; v < n1 && v <= u; ++v) {
-          if (!attn_sees(p.a, s.b, u, v)) continue;
+          if (!attn_sees(p.s.a, s.b, u, v)) continue;
           const unsigned short raw = reinterpret_cast<const unsigned short*>(
-              p.a.v)[(long long)s.b * p.a.kv_stride[0] + (long long)v * p.a.kv_stride[1] + (long long)s.g * p.a.kv_stride[2] + col];
+              p.s.a.v)[(long long)s.b * p.s.a.kv_stride[0] + (long long)v * p.s.a.kv_stride[1] + (long long)s.g * p.s.a.kv_stride[2] + col];
           const float f = BF16 ? __uint_as_float((uint32_t)raw << 16) : __half2float(__ushort_as_half(raw));
           if (!isfinite(f)) o += f;
         }
@@ -753,20 +601,20 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
               }
             }
             if (!s.whole) {
-              float4* dst = reinterpret_cast<float4*>(p.part_o + at * DP + c * 32);
+              float4* dst = reinterpret_cast<float4*>(p.s.part_o + at * DP + c * 32);
 #pragma unroll
               for (int i = 0; i < 8; ++i)
                 dst[i] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]),
                                      __uint_as_float(o[4 * i + 3]));
             } else {
-              uint4* dst = reinterpret_cast<uint4*>(p.a.out + 2 * (out_row * p.a.dim + c * 32));
+              uint4* dst = reinterpret_cast<uint4*>(p.s.a.out + 2 * (out_row * p.s.a.dim + c * 32));
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                   w[e] = empty ? 0u : ta_pack<BF16>(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
-                if (c * 32 + i * 8 < p.a.dim) dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                if (c * 32 + i * 8 < p.s.a.dim) dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
               }
             }
           }
@@ -774,7 +622,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
       } else {
         // Some columns at a time through shared memory, as many as fit (with few rows all of them); then each thread
         // sums four columns of a row over the parts.
-        const int rows = p.part_rows;
+        const int rows = p.s.tile_rows;
         int cols = TA_XCOLS;
         while (cols < DP && C * rows * (2 * cols + 1) <= TA_ROWS * (TA_XCOLS + 1)) cols *= 2;
         const int pitch = cols + 1;
@@ -799,8 +647,8 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           const int quads = cols / 4;
           for (int i = tid; i < rows * quads; i += TA_ROWS) {
             const int r = i / quads, q = i - r * quads, col = c0 + q * 4;
-            const int ru = s.node0 + r / p.a.group, rh = s.g * p.a.group + r % p.a.group;
-            if (ru >= p.a.N) continue;
+            const int ru = s.row0 / p.s.a.group + r / p.s.a.group, rh = s.g * p.s.a.group + r % p.s.a.group;
+            if (ru >= p.s.a.N) continue;
             float v[4] = {};
 #pragma unroll
             for (int k = 0; k < C; ++k)
@@ -810,10 +658,10 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
             if (odd && ml.y != 0.0f)
               for (int e = 0; e < 4; ++e) add_odd(v[e], col + e, ru);
             if (!s.whole) {
-              *reinterpret_cast<float4*>(p.part_o + part_row(s, r) * DP + col) = make_float4(v[0], v[1], v[2], v[3]);
-            } else if (col < p.a.dim) {
+              *reinterpret_cast<float4*>(p.s.part_o + part_row(s, r) * DP + col) = make_float4(v[0], v[1], v[2], v[3]);
+            } else if (col < p.s.a.dim) {
               const bool none = ml.x == 0.0f;
-              *reinterpret_cast<uint2*>(p.a.out + 2 * ((((long long)s.b * p.a.N + ru) * p.a.heads_q + rh) * p.a.dim + col)) =
+              *reinterpret_cast<uint2*>(p.s.a.out + 2 * ((((long long)s.b * p.s.a.N + ru) * p.s.a.heads_q + rh) * p.s.a.dim + col)) =
                   make_uint2(none ? 0u : ta_pack<BF16>(v[0] * ml.x, v[1] * ml.x), none ? 0u : ta_pack<BF16>(v[2] * ml.x, v[3] * ml.x));
             }
           }
@@ -826,79 +674,19 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     }
     if (!ok) {  // a wait ran out: nothing that this block had to do is to be trusted
       TaSeg s;
-      while (walk.next(p, s)) {
-        const int u = s.node0 + up, h = s.g * p.a.group + head;
-        if (!in_tile || part != 0 || u >= p.a.N) continue;
-        p.part_ml[part_row(s, row)] = make_float2(0.0f, NAN);
+      while (walk.next(p.s, s)) {
+        const int u = s.row0 / p.s.a.group + up, h = s.g * p.s.a.group + head;
+        if (!in_tile || part != 0 || u >= p.s.a.N) continue;
+        p.s.part_ml[part_row(s, row)] = make_float2(0.0f, NAN);
         if (!s.whole) continue;
-        const long long out_row = ((long long)s.b * p.a.N + u) * p.a.heads_q + h;
-        if (p.a.lse) p.a.lse[out_row] = NAN;
-        for (int d = 0; d < p.a.dim; ++d) reinterpret_cast<unsigned short*>(p.a.out)[out_row * p.a.dim + d] = 0x7FFFu;  // NaN in both types
+        const long long out_row = ((long long)s.b * p.s.a.N + u) * p.s.a.heads_q + h;
+        if (p.s.a.lse) p.s.a.lse[out_row] = NAN;
+        for (int d = 0; d < p.s.a.dim; ++d) reinterpret_cast<unsigned short*>(p.s.a.out)[out_row * p.s.a.dim + d] = 0x7FFFu;  // NaN in both types
       }
     }
   }
   __syncthreads();
   if (warp == 5) tc_dealloc(tmem, Sh::COLS);
-}
-
-// ---- joining the pieces ---------------------------------------------------------------
-constexpr int TJ_WARPS = 8;
-
-// One warp per row: the factors 2^(m_i - M) of the pieces by lane, then the sum over the pieces of factor * o, each lane
-// DP / 32 elements.  The pieces were written just before and come from L2.
-template <int DP, bool BF16> __global__ void __launch_bounds__(TJ_WARPS * 32) join_attention_kernel(const __grid_constant__ TaParams p) {
-  constexpr int E = DP / 32;
-  pdl_trigger();
-  pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const TaRecord rec = p.records[blockIdx.x];
-  if (rec.n_parts == 0) return;
-  const int tiles_y = (p.part_rows + TJ_WARPS - 1) / TJ_WARPS;
-  const int rt = blockIdx.y / tiles_y, in_tile = (blockIdx.y % tiles_y) * TJ_WARPS + warp;
-  const int up = in_tile / p.a.group, u = (rec.rb * p.group_ctas + rt) * p.tile_nodes + up, h = rec.g * p.a.group + in_tile - up * p.a.group;
-  if (in_tile >= p.part_rows || u >= p.a.N) return;
-  auto at = [&](int i) {  // row of piece i in scratch
-    const long long cta = (long long)(blockIdx.x + i) * p.group_ctas + rt;
-    return (cta * 2 + (i == 0 ? rec.first_which : 0)) * p.part_rows + in_tile;
-  };
-  float top = -INFINITY;
-  for (int i = lane; i < rec.n_parts; i += 32) top = fmaxf(top, p.part_ml[at(i)].x);
-  top = warp_max_f(top);
-  const float base = top == -INFINITY ? 0.0f : top;
-  float total = 0.0f, o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.0f;
-  for (int i0 = 0; i0 < rec.n_parts; i0 += 32) {
-    const int n = rec.n_parts - i0 < 32 ? rec.n_parts - i0 : 32;
-    float w = 0.0f, l = 0.0f;
-    if (lane < n) {
-      const float2 ml = p.part_ml[at(i0 + lane)];
-      w = ta_ex2(ml.x - base);
-      l = ml.y * w;
-      if (ml.y == 0.0f) w = 0.0f;
-    }
-    total += warp_sum_f(l);
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const float wi = __shfl_sync(FULL, w, i);
-      if (wi == 0.0f) continue;  // no weight; a piece without keys has written no o
-      const float* src = p.part_o + at(i0 + i) * DP + lane * E;
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float2 v = *reinterpret_cast<const float2*>(src + e);
-        o[e] = fmaf(wi, v.x, o[e]);
-        o[e + 1] = fmaf(wi, v.y, o[e + 1]);
-      }
-    }
-  }
-  const long long row = ((long long)rec.b * p.a.N + u) * p.a.heads_q + h;
-  const bool empty = total == 0.0f;
-  const float inv = empty ? 0.0f : 1.0f / total;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(p.a.out + 2 * row * p.a.dim);
-#pragma unroll
-  for (int e = 0; e < E; e += 2)
-    if (lane * E + e < p.a.dim) dst[(lane * E + e) >> 1] = empty ? 0u : ta_pack<BF16>(o[e] * inv, o[e + 1] * inv);
-  if (p.a.lse && lane == 0) p.a.lse[row] = empty ? -INFINITY : 0.6931471805599453f * (top + log2f(total));
 }
 
 // ---- launch ------------------------------------------------------------------------------
@@ -931,50 +719,22 @@ inline bool encode_map(CUtensorMap* map, const void* base, bool bf16, int dim, c
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-inline int tensor_dim(int dim) { return dim <= 64 ? 64 : (dim <= 128 ? 128 : 256); }
 // Row tiles hold whole nodes, so that one copy brings a tile's rows.
-inline int tile_nodes(int n, int group) { return n * group <= TA_ROWS ? n : TA_ROWS / group; }
-inline size_t tensor_scratch_bytes(int n, int group, int dim) {
-  if (group > TA_ROWS) return 256;
-  const size_t dp = tensor_dim(dim), ctas = dp == 256 ? TA_SMS : 2 * TA_SMS, pieces = ctas * 2 * tile_nodes(n, group) * group;
-  return ctas * sizeof(TaRecord) + ((pieces * sizeof(float2) + 255) & ~(size_t)255) + pieces * dp * sizeof(float);
-}
+inline int tensor_tile_rows(int n, int group) { return (long long)n * group <= TA_ROWS ? n * group : TA_ROWS / group * group; }
+inline int tensor_ctas(int dim) { return tensor_dim(dim) == 256 ? 1 : 2; }
 
 // STAND_E_ARG: not a call for these kernels (what the copy unit cannot address); nothing was launched.
 template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
   using Sh = TaShape<DP, C>;
   TaParams p;
-  p.a = a;
-  p.tile_nodes = tile_nodes(a.N, a.group);
-  p.part_rows = p.tile_nodes * a.group;
-  const int row_tiles = (a.N + p.tile_nodes - 1) / p.tile_nodes;
-  p.row_blocks = (row_tiles + TA_GROUP - 1) / TA_GROUP;
-  p.group_ctas = (row_tiles + p.row_blocks - 1) / p.row_blocks;
-  p.row_blocks = (row_tiles + p.group_ctas - 1) / p.group_ctas;
-  p.tree_tiles = 0;
-  for (int rb = 0; rb < p.row_blocks; ++rb) {
-    const long long end = (long long)(rb + 1) * p.group_ctas * p.tile_nodes;
-    p.tree_tiles += ((end < a.N ? end : a.N) - 1) / TA_KT + 1;
-  }
-  p.groups = (sms < TA_SMS ? sms : TA_SMS) * Sh::CTAS / p.group_ctas;
-  const long long most = (long long)a.B * a.heads_kv *
-                         (p.row_blocks * (((long long)a.cols * a.page + TA_KT - 1) / TA_KT + TA_PIECE_COST) + p.tree_tiles);
-  if (p.groups > (most + TA_MIN_TILES - 1) / TA_MIN_TILES) p.groups = (int)((most + TA_MIN_TILES - 1) / TA_MIN_TILES);
+  ta_split(p.s, a, tensor_tile_rows(a.N, a.group), DP, sms, Sh::CTAS, DP == 64 ? 8 : 5, scratch);
   p.box_rows = 16;
   while (p.box_rows < TA_KT && a.page % (p.box_rows * 2) == 0) p.box_rows *= 2;
   p.wait_limit = wait_limit;
 
-  char* at = (char*)scratch;
-  const size_t ctas = DP == 256 ? TA_SMS : 2 * TA_SMS, pieces = ctas * 2 * p.part_rows;
-  p.records = (TaRecord*)at;
-  at += ctas * sizeof(TaRecord);
-  p.part_ml = (float2*)at;
-  at += (pieces * sizeof(float2) + 255) & ~(size_t)255;
-  p.part_o = (float*)at;
-
   const long long tree_n[3] = {a.N, a.heads_kv, a.B}, tree_stride[3] = {a.kv_stride[1], a.kv_stride[2], a.kv_stride[0]};
   const long long q_n[3] = {a.heads_q, a.N, a.B}, q_stride[3] = {a.q_stride[2], a.q_stride[1], a.q_stride[0]};
-  if (!encode_map(&p.q, a.q, BF16, a.dim, q_n, q_stride, a.group, p.tile_nodes) ||
+  if (!encode_map(&p.q, a.q, BF16, a.dim, q_n, q_stride, a.group, p.s.tile_rows / a.group) ||
       !encode_map(&p.tree_k, a.k, BF16, a.dim, tree_n, tree_stride, TA_KT, 1) ||
       !encode_map(&p.tree_v, a.v, BF16, a.dim, tree_n, tree_stride, TA_KT, 1))
     return STAND_E_ARG;
@@ -990,14 +750,13 @@ template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams
   static SmemLimit limit;
   int rc = limit.raise(tensor_attention_kernel<DP, C, BF16>, Sh::SMEM);
   if (rc) return STAND_E_CUDA;
-  rc = launch_dependent(tensor_attention_kernel<DP, C, BF16>, dim3((unsigned)(p.groups * p.group_ctas)), TA_THREADS, st, p, Sh::SMEM);
+  rc = launch_dependent(tensor_attention_kernel<DP, C, BF16>, dim3((unsigned)(p.s.groups * p.s.group_ctas)), TA_THREADS, st, p, Sh::SMEM);
   if (rc) return rc;
-  const unsigned tiles_y = (unsigned)((p.part_rows + TJ_WARPS - 1) / TJ_WARPS);
-  return launch_dependent(join_attention_kernel<DP, BF16>, dim3((unsigned)p.groups, tiles_y * p.group_ctas), TJ_WARPS * 32, st, p);
+  return launch_join<DP, typename std::conditional<BF16, __nv_bfloat16, __half>::type>(p.s, st);
 }
 
 template <int DP, bool BF16> int launch_tensor_parts(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
-  const int rows = tile_nodes(a.N, a.group) * a.group;
+  const int rows = tensor_tile_rows(a.N, a.group);
   if (rows <= TA_ROWS / 4) return launch_tensor_attention<DP, 4, BF16>(a, scratch, sms, wait_limit, st);
   if (rows <= TA_ROWS / 2) return launch_tensor_attention<DP, 2, BF16>(a, scratch, sms, wait_limit, st);
   return launch_tensor_attention<DP, 1, BF16>(a, scratch, sms, wait_limit, st);

@@ -29,8 +29,8 @@ struct SmemLimit {
 
 // Launch with programmatic stream serialisation: the kernel may be scheduled while its predecessor in the
 // stream is still running; it calls pdl_wait() before it touches the predecessor's results.
-template <typename P>
-int launch_dependent(void (*kernel)(P), dim3 grid, unsigned block, cudaStream_t st, const P& params, size_t smem = 0) {
+template <typename... P>
+int launch_dependent2(void (*kernel)(P...), dim3 grid, unsigned block, cudaStream_t st, size_t smem, const P&... params) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
@@ -41,7 +41,12 @@ int launch_dependent(void (*kernel)(P), dim3 grid, unsigned block, cudaStream_t 
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cuda_ok(cudaLaunchKernelEx(&cfg, kernel, params));
+  return cuda_ok(cudaLaunchKernelEx(&cfg, kernel, params...));
+}
+
+template <typename P>
+int launch_dependent(void (*kernel)(P), dim3 grid, unsigned block, cudaStream_t st, const P& params, size_t smem = 0) {
+  return launch_dependent2(kernel, grid, block, st, smem, params);
 }
 
 }  // namespace stand
