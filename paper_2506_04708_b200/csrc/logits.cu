@@ -12,7 +12,9 @@ using namespace stand;
 namespace {
 
 constexpr int LG_THREADS = 256;
-constexpr int LG_CHUNK = 4096;     // tokens of the vocabulary per block, at most
+constexpr int LG_CHUNK = 4096;     // tokens of the vocabulary per block in a large batch
+constexpr int LG_BLOCKS = 5;       // blocks per multiprocessor
+constexpr int LG_CHUNK_MAX = 5120; // so many of them still fit its shared memory
 constexpr int LG_VECS = 4;         // 16-byte pieces a lane has in flight
 constexpr uint32_t PROMPT_BIT = 0x80000000u, DRAFT_BIT = 0x40000000u;  // of a token's count: in the prompt; drafted somewhere
 
@@ -176,7 +178,7 @@ __device__ __forceinline__ void stream_row(const char* in, char* out, int t0, in
 // gone by (after the whole rows it took 936 us instead of 600 for 256 x 24 rows: their lines had left L2).  HBM-bound: every logit is read
 // and written once.
 template <int DT>
-__global__ void __launch_bounds__(LG_THREADS, 5) logits_kernel(const __grid_constant__ LogitsParams p) {
+__global__ void __launch_bounds__(LG_THREADS, LG_BLOCKS) logits_kernel(const __grid_constant__ LogitsParams p) {
   extern __shared__ uint32_t lg_smem[];
   __shared__ short s_node[NODES_MAX];  // the drafted token of each node, as a place in the chunk; -1: none there
   const int chunk = p.chunk;
@@ -188,10 +190,28 @@ __global__ void __launch_bounds__(LG_THREADS, 5) logits_kernel(const __grid_cons
   for (int i = tid; i < chunk + chunk / 32 + 1; i += LG_THREADS) s_count[i] = 0;
   if (p.bias_start)
     for (int i = tid; i < chunk; i += LG_THREADS) s_bias[i] = 0;
-  pdl_wait();
-  __syncthreads();
   const int b = blockIdx.x / p.n_chunks, c0 = (blockIdx.x % p.n_chunks) * chunk;
   const int width = p.V - c0 < chunk ? p.V - c0 : chunk;
+  const int n_sub = (width + p.sub - 1) / p.sub;
+  const int tasks = p.N * n_sub;
+  pdl_wait();
+  // all that later steps wait for, asked for at once; and the first piece of each warp's rows on its way to L2
+  long long have = 0, first = 0;
+  int bias_from = 0, bias_to = 0;
+  Penalty q;
+  if (p.text) have = p.n_text[b];
+  if (p.n_prompt) first = p.n_prompt[b];
+  if (p.bias_start) bias_from = max(p.bias_start[b], 0), bias_to = min(p.bias_start[b + 1], p.biases);
+  q.r = p.repetition ? p.repetition[b] : 1.0f;
+  q.f = p.frequency ? p.frequency[b] : 0.0f;
+  q.p = p.presence ? p.presence[b] : 0.0f;
+  if (warp < tasks && p.in != p.out) {
+    const int u = warp / n_sub, lo = (warp - u * n_sub) * p.sub;
+    const long long bytes = (long long)(width - lo < p.sub ? width - lo : p.sub) * (DT == 0 ? 4 : 2);
+    const char* row = p.in + ((long long)b * p.N + u) * p.in_stride + (long long)(c0 + lo) * (DT == 0 ? 4 : 2);
+    for (long long at = lane * 128; at < bytes; at += 32 * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + at));
+  }
+  __syncthreads();
   auto touch = [&](uint32_t i) { atomicOr(&s_bits[i >> 5], 1u << (i & 31)); };
   if (p.tree)
     for (int v = tid; v < p.N; v += LG_THREADS) {
@@ -204,9 +224,7 @@ __global__ void __launch_bounds__(LG_THREADS, 5) logits_kernel(const __grid_cons
       }
     }
   if (p.text) {
-    const long long have = p.n_text[b];
     const int n = have < 0 ? 0 : (have > p.text_stride ? p.text_stride : (int)have);
-    const long long first = p.n_prompt ? p.n_prompt[b] : 0;
     const int* row = p.text + (long long)b * p.text_stride;
     auto count = [&](int t, int i) {
       const uint32_t at = (uint32_t)t - (uint32_t)c0;
@@ -236,8 +254,7 @@ __global__ void __launch_bounds__(LG_THREADS, 5) logits_kernel(const __grid_cons
     if (i < n) count(row[i], i);
   }
   if (p.bias_start) {
-    const int from = max(p.bias_start[b], 0), to = min(p.bias_start[b + 1], p.biases);
-    for (int i = from + tid; i < to; i += LG_THREADS) {
+    for (int i = bias_from + tid; i < bias_to; i += LG_THREADS) {
       const uint32_t at = (uint32_t)p.bias_id[i] - (uint32_t)c0;
       if (at >= (uint32_t)width) continue;
       atomicMax(&s_bias[at], i + 1);
@@ -247,13 +264,7 @@ __global__ void __launch_bounds__(LG_THREADS, 5) logits_kernel(const __grid_cons
 
   __syncthreads();
 
-  Penalty q;
-  q.r = p.repetition ? p.repetition[b] : 1.0f;
   q.r_inv = 1.0f / q.r;
-  q.f = p.frequency ? p.frequency[b] : 0.0f;
-  q.p = p.presence ? p.presence[b] : 0.0f;
-  const int n_sub = (width + p.sub - 1) / p.sub;
-  const int tasks = p.N * n_sub;
   for (int task = warp; task < tasks; task += LG_THREADS / 32) {
     const int u = task / n_sub, lo = c0 + (task - u * n_sub) * p.sub;
     const int hi = lo + p.sub < c0 + width ? lo + p.sub : c0 + width;
@@ -315,10 +326,18 @@ extern "C" int stand_process_logits(const stand_logits* c, const stand_logits_in
   // scanned once per chunk, so a large one is not.
   p.chunk = LG_CHUNK;
   while (p.chunk > 512 && (long long)c->B * ((c->V + p.chunk - 1) / p.chunk) < 2 * 148) p.chunk /= 2;
+  // between one and two rounds of blocks: larger chunks, if that makes it one
+  const long long round = 148 * LG_BLOCKS;
+  if (p.chunk == LG_CHUNK && (long long)c->B * ((c->V + LG_CHUNK - 1) / LG_CHUNK) > round)
+    for (int ch = LG_CHUNK + 512; ch <= LG_CHUNK_MAX; ch += 512)
+      if ((long long)c->B * ((c->V + ch - 1) / ch) <= round) {
+        p.chunk = ch;
+        break;
+      }
   p.n_chunks = (c->V + p.chunk - 1) / p.chunk;
   // few nodes are cut into more pieces: four or so for each warp
   p.sub = p.chunk;
-  while (p.sub > 512 && c->N * (p.chunk / p.sub) < LG_THREADS / 8) p.sub /= 2;
+  while (p.sub >= 1024 && c->N * (p.chunk / p.sub) < LG_THREADS / 8) p.sub = (p.sub / 2 + 31) & ~31;
   const long long blocks = (long long)c->B * p.n_chunks;
   if (blocks > 0x7FFFFFFFll) return STAND_E_ARG;
   const size_t smem = (size_t)p.chunk * (sizeof(int) + (x->bias_start ? sizeof(int) : 0)) + p.chunk / 8 + sizeof(int);
