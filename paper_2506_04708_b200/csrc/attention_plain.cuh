@@ -4,8 +4,8 @@
 // A block takes up to RT rows of a pair and walks over its tiles of 64 keys (attention_split.cuh), two tiles of keys and
 // values in shared memory (single precision: cp.async; 16-bit types are converted on the way).  A warp has RT / 8 rows; for
 // the scores a lane has two keys, for the sums its share of the head size.  So every value from shared memory is used for
-// RT / 8 rows, no sum crosses a warp, and the products run near the rate of the fused multiply-adds (RT = 32: 12 shared-memory
-// passes for 32 of them in the scores, 20 for 64 in the sums).  With at most 8 rows RT = 8 leaves no thread without a row.
+// RT / 8 rows, and no sum crosses a warp.  What bounds it is shared memory: with RT = 64 a warp reads 16 passes for 32 packed
+// multiply-adds in the scores.
 #pragma once
 #include "async.cuh"
 #include "attention_split.cuh"
@@ -15,6 +15,7 @@ namespace stand {
 
 constexpr int ATTN_DIM_MAX = 256;
 constexpr int PA_WARPS = 8, PA_THREADS = PA_WARPS * 32;
+static_assert(PA_THREADS == 4 * TA_KT, "a thread per row of two tiles");
 
 template <int DP> struct PaShape {
   static constexpr int STAGES = DP == 256 ? 1 : 2;
@@ -70,27 +71,28 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
   }
 
   TaSeg s;
+  TaNote note(walk);
   while (walk.next(p, s)) {
+    if (tid == 0) note.piece(walk, s, s_range.total, s_range.groups, blockIdx.x / p.group_ctas);
     if (!s.rows) continue;
     const T* kv[2] = {reinterpret_cast<const T*>(p.a.k), reinterpret_cast<const T*>(p.a.v)};
     const T* cache[2] = {reinterpret_cast<const T*>(p.a.cache_k), reinterpret_cast<const T*>(p.a.cache_v)};
-    auto find = [&](int tile) {  // where the rows of a tile are
-      if (tid < 2 * KT && tile < s.end) {
-        const int key = tid % KT, which = tid / KT;
-        const T* src = nullptr;
-        if (tile < s.p_tiles) {
-          const int pos = tile * KT + key, c = pos / p.a.page;
-          if (pos < s.len) {
-            const int page = p.a.table[(long long)s.b * p.a.cols + c];
-            if (page >= 0 && page < p.a.pages)
-              src = cache[which] + page * p.a.cache_stride[0] + s.g * p.a.cache_stride[1] + (long long)(pos - c * p.a.page) * p.a.cache_stride[2];
-          }
-        } else {
-          const int node = (tile - s.p_tiles) * KT + key;
-          if (node < p.a.N) src = kv[which] + s.b * p.a.kv_stride[0] + node * p.a.kv_stride[1] + s.g * p.a.kv_stride[2];
+    auto find = [&](int tile, int i) {  // where row i of a tile's keys (i < KT) or values is
+      if (tile >= s.end) return;
+      const int key = i % KT, which = i / KT;
+      const T* src = nullptr;
+      if (tile < s.p_tiles) {
+        const int pos = tile * KT + key, c = pos / p.a.page;
+        if (pos < s.len) {
+          const int page = p.a.table[(long long)s.b * p.a.cols + c];
+          if (page >= 0 && page < p.a.pages)
+            src = cache[which] + page * p.a.cache_stride[0] + s.g * p.a.cache_stride[1] + (long long)(pos - c * p.a.page) * p.a.cache_stride[2];
         }
-        s_src[tile % 3][which][key] = src;
+      } else {
+        const int node = (tile - s.p_tiles) * KT + key;
+        if (node < p.a.N) src = kv[which] + s.b * p.a.kv_stride[0] + node * p.a.kv_stride[1] + s.g * p.a.kv_stride[2];
       }
+      s_src[tile % 3][which][key] = src;
     };
     auto fetch = [&](int tile) {
       if (tile < s.end) {
@@ -120,14 +122,18 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
     };
 
     __syncthreads();  // the piece before has been read
-    for (int i = tid; i < RT * D4; i += PA_THREADS) {
-      const int row = i / D4, d = i - row * D4, r = s.row0 + row;
-      float v = 0.0f;
-      if (row < p.tile_rows && r < p.rows && d < D) {
-        const int u = r / p.a.group, h = s.g * p.a.group + r - u * p.a.group;
-        v = to_float(reinterpret_cast<const T*>(p.a.q)[s.b * p.a.q_stride[0] + u * p.a.q_stride[1] + h * p.a.q_stride[2] + d]);
+    find(s.begin + tid / (2 * KT), tid % (2 * KT));
+    // a warp's rows, by that warp alone
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int row = warp * R + i, r = s.row0 + row, u = r / p.a.group;
+      const bool in = row < p.tile_rows && r < p.rows;
+      const T* src = reinterpret_cast<const T*>(p.a.q) + s.b * p.a.q_stride[0] + u * p.a.q_stride[1] + (s.g * p.a.group + r - u * p.a.group) * p.a.q_stride[2];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int d = lane + 32 * e;
+        if (d < D4) sq[row * KP + d] = in && d < D ? to_float(src[d]) : 0.0f;
       }
-      sq[row * KP + d] = v;
     }
     int node[R];
     bool live[R];
@@ -142,92 +148,135 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
 #pragma unroll
       for (int e = 0; e < E; ++e) o[i][e] = 0.0f;
     }
-    find(s.begin);
-    find(s.begin + 1);
     __syncthreads();
     if (STAGES == 2) fetch(s.begin);
 
     for (int j = s.begin; j < s.end; ++j) {
       if (STAGES == 2) {
         fetch(j + 1);
-        find(j + 2);
+        if (tid < 2 * KT) find(j + 2, tid);
         cp_wait<1>();
       } else {
         fetch(j);
-        find(j + 2);
+        if (tid < 2 * KT) find(j + 2, tid);
         cp_wait<0>();
       }
       __syncthreads();
       const float* sk = pa_smem + (j % STAGES) * Sh::STAGE;
       const float* sv = sk + KT * KP;
-      float x[R][2];
+      // products of neighbours in pairs: half the instructions, two sums that are added at the end
+      unsigned long long x2[R][2];
 #pragma unroll
-      for (int i = 0; i < R; ++i) x[i][0] = x[i][1] = 0.0f;
+      for (int i = 0; i < R; ++i) x2[i][0] = x2[i][1] = pack2(0.0f, 0.0f);
       const float* q0 = sq + warp * R * KP;
-#pragma unroll 4
+#pragma unroll 2
       for (int d = 0; d < D4; d += 4) {
-        const float4 k0 = *reinterpret_cast<const float4*>(sk + lane * KP + d), k1 = *reinterpret_cast<const float4*>(sk + (lane + 32) * KP + d);
+        const ulonglong2 k0 = *reinterpret_cast<const ulonglong2*>(sk + lane * KP + d), k1 = *reinterpret_cast<const ulonglong2*>(sk + (lane + 32) * KP + d);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-          const float4 q = *reinterpret_cast<const float4*>(q0 + i * KP + d);
-          x[i][0] = fmaf(q.x, k0.x, fmaf(q.y, k0.y, fmaf(q.z, k0.z, fmaf(q.w, k0.w, x[i][0]))));
-          x[i][1] = fmaf(q.x, k1.x, fmaf(q.y, k1.y, fmaf(q.z, k1.z, fmaf(q.w, k1.w, x[i][1]))));
+          const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(q0 + i * KP + d);
+          x2[i][0] = fma2(q.y, k0.y, fma2(q.x, k0.x, x2[i][0]));
+          x2[i][1] = fma2(q.y, k1.y, fma2(q.x, k1.x, x2[i][1]));
         }
       }
+      float x[R][2];
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float lo, hi;
+          unpack2(x2[i][c], lo, hi);
+          x[i][c] = lo + hi;
+        }
+      // What no row sees of a text's last tile lies there as zeros.  In the tree, what one row does not see another may:
+      // a value that is not finite must then not enter the first one's sum, 0 times it included.
       const bool tree = j >= s.p_tiles, partial = !tree && s.len - j * KT < KT;
-      uint32_t seen[R][2];
+      bool odd = false;
+      if (tree) {
+        const int nodes = p.a.N - (j - s.p_tiles) * KT;
+        for (int i = tid; i < (nodes < KT ? nodes : KT) * D; i += PA_THREADS) odd = odd || !isfinite(sv[i / D * DP + i % D]);
+        odd = __syncthreads_or(odd);
+      }
+      uint32_t seen[R][2];  // the tile's keys that a row sees: bits, by halves
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t bits = live[i] ? FULL : 0u;
+          int below = KT;
+          if (partial) below = s.len - j * KT - 32 * c;
+          if (tree) {
+            const int first = (j - s.p_tiles) * KT + 32 * c;
+            below = node[i] + 1 - first;
+            if (p.a.mask && below > 0) bits &= __ldg(p.a.mask + (long long)s.b * p.a.mask_stride + (long long)node[i] * p.a.mask_words + (first >> 5));
+          }
+          seen[i][c] = below >= 32 ? bits : (below > 0 ? bits & ((1u << below) - 1) : 0u);
+        }
+      // row by row in step: the rows' shuffles and exponentials overlap
+      float top[R], keep[R], sum[R];
 #pragma unroll
       for (int i = 0; i < R; ++i) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int key = lane + 32 * c;
-          bool sees = live[i];
-          if (partial) sees = sees && key < s.len - j * KT;
-          else if (tree) {
-            const int v = (j - s.p_tiles) * KT + key;
-            sees = sees && v < p.a.N && attn_sees(p.a, s.b, node[i], v);
-          }
-          seen[i][c] = __ballot_sync(FULL, sees);
-          x[i][c] = sees ? x[i][c] * p.a.scale2 : -INFINITY;
-        }
-        const float top = fmaxf(m[i], warp_max_f(fmaxf(x[i][0], x[i][1])));
-        const float base = top == -INFINITY ? 0.0f : top, keep = exp2f(m[i] - base);
+        for (int c = 0; c < 2; ++c) x[i][c] = seen[i][c] >> lane & 1u ? x[i][c] * p.a.scale2 : -INFINITY;
+        top[i] = fmaxf(x[i][0], x[i][1]);
+      }
+#pragma unroll
+      for (int w = 16; w > 0; w >>= 1)
+#pragma unroll
+        for (int i = 0; i < R; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(FULL, top[i], w));
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        top[i] = fmaxf(top[i], m[i]);
+        const float base = top[i] == -INFINITY ? 0.0f : top[i];
+        keep[i] = exp2f(m[i] - base);
+        m[i] = top[i];
         float w[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           w[c] = seen[i][c] >> lane & 1u ? exp2f(x[i][c] - base) : 0.0f;
           sp[i * KT + lane + 32 * c] = w[c];
         }
-        m[i] = top;
-        l[i] = l[i] * keep + warp_sum_f(w[0] + w[1]);
+        sum[i] = w[0] + w[1];
+      }
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[i][e] *= keep;
+      for (int w = 16; w > 0; w >>= 1)
+#pragma unroll
+        for (int i = 0; i < R; ++i) sum[i] += __shfl_xor_sync(FULL, sum[i], w);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        l[i] = l[i] * keep[i] + sum[i];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[i][e] *= keep[i];
       }
       __syncwarp();
-      if (!tree && !partial) {
-#pragma unroll 2
+      if (!odd) {
+#pragma unroll 1
         for (int k = 0; k < KT; k += 4) {
           float4 w[R];
 #pragma unroll
           for (int i = 0; i < R; ++i) w[i] = *reinterpret_cast<const float4*>(sp + i * KT + k);
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
-            float v[E];
+            unsigned long long v[E / 2];
 #pragma unroll
             for (int e = 0; e < E; e += EV) {
               const float* src = sv + (k + kk) * DP + lane * EV + e / EV * 128;
-              if constexpr (EV == 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(src);
-              else *reinterpret_cast<float2*>(v + e) = *reinterpret_cast<const float2*>(src);
+              if constexpr (EV == 4) *reinterpret_cast<ulonglong2*>(v + e / 2) = *reinterpret_cast<const ulonglong2*>(src);
+              else v[e / 2] = *reinterpret_cast<const unsigned long long*>(src);
             }
 #pragma unroll
             for (int i = 0; i < R; ++i) {
               const float wk = kk == 0 ? w[i].x : (kk == 1 ? w[i].y : (kk == 2 ? w[i].z : w[i].w));
+              const unsigned long long wk2 = pack2(wk, wk);
 #pragma unroll
-              for (int e = 0; e < E; ++e) o[i][e] = fmaf(wk, v[e], o[i][e]);
+              for (int e = 0; e < E; e += 2) {
+                const unsigned long long r = fma2(wk2, v[e / 2], pack2(o[i][e], o[i][e + 1]));
+                unpack2(r, o[i][e], o[i][e + 1]);
+              }
             }
           }
         }
-      } else {  // an unseen value may be anything, 0 times it too: row by row, only what it sees
+      } else {  // row by row, only what it sees
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
@@ -261,11 +310,12 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
       }
     }
   }
+  if (tid == 0 && blockIdx.x % p.group_ctas == 0) p.records[blockIdx.x / p.group_ctas] = note.r;
 }
 
 template <typename T, int DP, int RT> int launch_plain_rows(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
   TaSplit p;
-  ta_split(p, a, RT, DP, sms, plain_ctas(DP), 2, scratch);
+  ta_split(p, a, RT, DP, sms, plain_ctas(DP), 3, scratch);
   const size_t al = 4 * sizeof(T);
   uintptr_t bits = (uintptr_t)a.k | (uintptr_t)a.v | (a.cols > 0 ? (uintptr_t)a.cache_k | (uintptr_t)a.cache_v : 0);
   for (int i = 0; i < 3; ++i) bits |= (uintptr_t)(a.kv_stride[i] * sizeof(T)) | (a.cols > 0 ? (uintptr_t)(a.cache_stride[i] * sizeof(T)) : 0);
@@ -286,9 +336,14 @@ template <typename T> int launch_plain_attention(const AttnParams& a, void* scra
     if (dp == 128) return launch_plain_rows<T, 128, 8>(a, scratch, sms, st);
     return launch_plain_rows<T, 256, 8>(a, scratch, sms, st);
   }
-  if (dp == 64) return launch_plain_rows<T, 64, 32>(a, scratch, sms, st);
-  if (dp == 128) return launch_plain_rows<T, 128, 32>(a, scratch, sms, st);
-  return launch_plain_rows<T, 256, 32>(a, scratch, sms, st);
+  if (plain_tile_rows(a.N * a.group) == 32) {
+    if (dp == 64) return launch_plain_rows<T, 64, 32>(a, scratch, sms, st);
+    if (dp == 128) return launch_plain_rows<T, 128, 32>(a, scratch, sms, st);
+    return launch_plain_rows<T, 256, 32>(a, scratch, sms, st);
+  }
+  if (dp == 64) return launch_plain_rows<T, 64, 64>(a, scratch, sms, st);
+  if (dp == 128) return launch_plain_rows<T, 128, 64>(a, scratch, sms, st);
+  return launch_plain_rows<T, 256, 64>(a, scratch, sms, st);
 }
 
 }  // namespace stand

@@ -106,12 +106,31 @@ __device__ __forceinline__ long long ta_part_row(const TaSplit& p, const TaSeg& 
 }
 
 template <int THREADS> struct TaRange {
-  long long sum[THREADS / 32], b_start;
-  int b;
+  long long sum[THREADS / 32], b_start, total;
+  int b, groups;
 };
 
-// This group's range and the sequence in which it begins; writes the group's record.  All threads call it; `before` and
-// `after` run around the second of its two barriers.
+// Whoever walks over all pieces of a group's first CTA keeps its record: what has to be joined is the pair in which the
+// range ends, if it began in the range and goes on in the next groups.
+struct TaNote {
+  long long from;  // where the piece to come begins
+  TaRecord r;
+
+  __device__ __forceinline__ explicit TaNote(const TaWalk& walk) : from(walk.t) { r.n_parts = r.first_which = r.b = r.g = r.rb = 0; }
+  __device__ __forceinline__ void piece(const TaWalk& walk, const TaSeg& s, long long total, int groups, int group) {
+    if (walk.t == walk.hi && s.starts && walk.hi - from < s.units) {
+      r.n_parts = (int)(((from + s.units) * groups - 1) / total) - group + 1;
+      r.first_which = s.which;
+      r.b = s.b;
+      r.g = s.g;
+      r.rb = s.rb;
+    }
+    from = walk.t;
+  }
+};
+
+// This group's range and the sequence in which it begins.  All threads call it; `before` and `after` run around the second
+// of its two barriers.
 template <int THREADS, typename F, typename G>
 __device__ __forceinline__ void ta_begin(const TaSplit& p, TaWalk& walk, TaRange<THREADS>& sh, F before, G after) {
   const int group = blockIdx.x / p.group_ctas, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -164,27 +183,9 @@ __device__ __forceinline__ void ta_begin(const TaSplit& p, TaWalk& walk, TaRange
   walk.b_start = sh.b_start;
   walk.first = true;
   walk.cost = cost;
-  if (tid == 0 && blockIdx.x % p.group_ctas == 0) {
-    // the pair in which the range ends, if it began here and goes on in the next groups
-    TaRecord r;
-    r.n_parts = 0;
-    r.first_which = r.b = r.g = r.rb = 0;
-    if (lo < hi && group + 1 < groups) {
-      TaWalk w = walk;
-      TaSeg s;
-      long long from = w.t;
-      while (w.next(p, s)) {
-        if (w.t == hi && s.starts && hi - from < s.units) {
-          r.n_parts = (int)(((from + s.units) * groups - 1) / total) - group + 1;
-          r.first_which = s.which;
-          r.b = s.b;
-          r.g = s.g;
-          r.rb = s.rb;
-        }
-        from = w.t;
-      }
-    }
-    p.records[group] = r;
+  if (tid == 0) {
+    sh.total = total;
+    sh.groups = (int)groups;
   }
 }
 

@@ -270,7 +270,10 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     TaSeg s;
     uint32_t slot = 0, phase = 1, used = 0;  // phase: parity of the wait for the slot's last use
     bool ok = *abort_flag == 0;
-    while (ok && walk.next(p.s, s)) {
+    TaNote note(walk);
+    while (walk.next(p.s, s)) {
+      if (!value) note.piece(walk, s, sh.range.total, sh.range.groups, blockIdx.x / p.s.group_ctas);
+      if (!ok) continue;  // gave up: only the record is still to be found
       if (s.begin >= s.end) {
         if (s.rows && !s.whole && !value)  // a piece of others that this CTA's rows do not see
           for (int i = lane; i < p.s.tile_rows; i += 32) p.s.part_ml[part_row(s, i)] = make_float2(-INFINITY, 0.0f);
@@ -310,6 +313,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
         if (++slot == slots) slot = 0, phase ^= 1u;
       }
     }
+    if (!value && lane == 0 && blockIdx.x % p.s.group_ctas == 0) p.s.records[blockIdx.x / p.s.group_ctas] = note.r;
     if (!ok && lane == 0) {  // copies in flight land before the block ends
       for (unsigned i = used > slots ? used - slots : 0; i < used; ++i)
         mbar_wait_timed(bar_full + 8 * (slot0 + i % slots), (i / slots) & 1u, nullptr, SPIN_LIMIT);
