@@ -363,6 +363,12 @@ class Stand:
                "stand_state_dump")
         return out
 
+    def path_device(self, out, stream=None):
+        """Copies the last verification's accepted paths into `out` (int32 [B, D+1], device; -1 past a path)."""
+        assert out.is_cuda and out.dtype == self.torch.int32 and out.is_contiguous() and out.numel() == self.B * (self.D + 1)
+        _check(lib().stand_last_path(self.h, _ptr(out), None, None, _stream(stream)), "stand_last_path")
+        return out
+
     def launch_count(self):
         return lib().stand_launch_count(self.h)
 
