@@ -40,16 +40,16 @@ class _Op:
         self._raw_stream, self._current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
         self._lib = lib()
 
-    def _launch(self, stream, name, *args):
+    def _launch(self, stream, call, *args):
         """One library call on `stream` (or the device's current one), with the operator's device current."""
         st = self._raw_stream(self._index) if stream is None else stream.cuda_stream
         if self._current_device() == self._index:
-            rc = getattr(self._lib, name)(*args, st)
+            rc = call(*args, st)
         else:
             with self.torch.cuda.device(self.dev):
-                rc = getattr(self._lib, name)(*args, st)
+                rc = call(*args, st)
         if rc:
-            _check(rc, name)
+            _check(rc, call.__name__)
 
     def _ints(self, t, dtype, shape, what):
         if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
@@ -107,8 +107,8 @@ class TreeAttention(_Op):
         self._cfg_ptr, self._strides = C.addressof(self.cfg), None
 
     def _floats(self, x, shape, what):
-        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index or x.stride(3) != 1:
-            raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev} with a contiguous last dimension, "
+        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index:
+            raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev}, "
                              f"got {x.dtype} {tuple(x.shape)} on {x.device}")
         return x.data_ptr()
 
@@ -120,13 +120,13 @@ class TreeAttention(_Op):
         pq, pk, pv = self._floats(q, self._q_shape, "q"), self._floats(k, self._kv_shape, "k"), self._floats(v, self._kv_shape, "v")
         pck = self._floats(cache_k, self._cache_shape, "cache_k")
         pcv = self._floats(cache_v, self._cache_shape, "cache_v")
-        ks, cs = k.stride(), cache_k.stride()
-        if v.stride() != ks or cache_v.stride() != cs:
-            raise StandError("TreeAttention: keys and values have the same strides")
-        qs = q.stride()
-        if (qs, ks, cs) != self._strides:
+        strides = q.stride(), k.stride(), v.stride(), cache_k.stride(), cache_v.stride()
+        if strides != self._strides:
+            qs, ks, vs, cs, cvs = strides
+            if vs != ks or cvs != cs or qs[3] != 1 or ks[3] != 1 or cs[3] != 1:
+                raise StandError("TreeAttention: keys and values have the same strides, and a contiguous last dimension as q has")
             c.q_stride[:], c.kv_stride[:], c.cache_stride[:] = qs[:3], ks[:3], cs[:3]
-            self._strides = (qs, ks, cs)
+            self._strides = strides
         ptab = self._ints(table, t.int32, self._table_shape, "table")
         plen = self._ints(length, t.int64, self._len_shape, "length")
         ptree = self._opt(tree_tokens, t.int32, self._tree_shape, "tree_tokens")
@@ -137,7 +137,7 @@ class TreeAttention(_Op):
         if lse is None:
             lse = self.lse
         plse = self._ints(lse, t.float32, self.lse.shape, "lse")
-        self._launch(stream, "stand_tree_attention", self._cfg_ptr, pq, pk, pv, pck, pcv, ptab, plen, self._mask_ptr,
+        self._launch(stream, self._lib.stand_tree_attention, self._cfg_ptr, pq, pk, pv, pck, pcv, ptab, plen, self._mask_ptr,
                      self.mask_stride, ptree, self._scratch, self._scratch_bytes, out.data_ptr(), plse)
         return out, lse
 
@@ -174,7 +174,7 @@ class PageMap(_Op):
                 self.page_size, self.max_pages, self._ints(free, t.int32, self._list, "free"), self.capacity,
                 self._ints(n_free, t.int32, self._one, "n_free"), self._ints(table, t.int32, self._table, "table"),
                 self.slots.data_ptr(), self.granted.data_ptr(), len_out.data_ptr(), n_out.data_ptr())
-        self._launch(stream, "stand_page_map", *args)
+        self._launch(stream, self._lib.stand_page_map, *args)
         return self.slots, self.granted, len_out, n_out
 
     def release(self, length, done, table, free, n_free, stream=None):
@@ -185,7 +185,7 @@ class PageMap(_Op):
                 self.page_size, self.max_pages, self._ints(table, t.int32, self._table, "table"), self.capacity,
                 self._ints(free, t.int32, self._list, "free"), self._ints(n_free, t.int32, self._one, "n_free"),
                 len_out.data_ptr(), n_out.data_ptr())
-        self._launch(stream, "stand_page_release", *args)
+        self._launch(stream, self._lib.stand_page_release, *args)
         return len_out, n_out
 
 
@@ -201,8 +201,8 @@ class KvCommit(_Op):
         self._cfg_ptr, self._strides = C.addressof(self.cfg), None
 
     def _floats(self, x, shape, what):
-        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index or x.stride(4) != 1:
-            raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev} with a contiguous last dimension, "
+        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index:
+            raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev}, "
                              f"got {x.dtype} {tuple(x.shape)} on {x.device}")
         return x.data_ptr()
 
@@ -212,15 +212,16 @@ class KvCommit(_Op):
         t, c = self.torch, self.cfg
         pk, pv = self._floats(k, self._src, "k"), self._floats(v, self._src, "v")
         pck, pcv = self._floats(cache_k, self._cache, "cache_k"), self._floats(cache_v, self._cache, "cache_v")
-        ks, cs = k.stride(), cache_k.stride()
-        if v.stride() != ks or cache_v.stride() != cs:
-            raise StandError("KvCommit: keys and values have the same strides")
-        if (ks, cs) != self._strides:
+        strides = k.stride(), v.stride(), cache_k.stride(), cache_v.stride()
+        if strides != self._strides:
+            ks, vs, cs, cvs = strides
+            if vs != ks or cvs != cs or ks[4] != 1 or cs[4] != 1:
+                raise StandError("KvCommit: keys and values have the same strides and a contiguous last dimension")
             c.src_stride[:], c.cache_stride[:] = ks[:4], cs[:4]
-            self._strides = (ks, cs)
+            self._strides = strides
         ps = self._ints(slots, t.int64, self._places, "slots")
         pp = self._opt(path, t.int32, self._places, "path")
-        self._launch(stream, "stand_kv_commit", self._cfg_ptr, pk, pv, pp, ps, pck, pcv)
+        self._launch(stream, self._lib.stand_kv_commit, self._cfg_ptr, pk, pv, pp, ps, pck, pcv)
 
 
 class LogitsProcessor(_Op):
@@ -298,5 +299,5 @@ class LogitsProcessor(_Op):
         else:
             _need(mask_row is None, "mask_row goes with mask")
             x.mask = x.mask_row = None
-        self._launch(stream, "stand_process_logits", self._cfg_ptr, self._in_ptr, src, dst)
+        self._launch(stream, self._lib.stand_process_logits, self._cfg_ptr, self._in_ptr, src, dst)
         return out
