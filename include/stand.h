@@ -358,7 +358,7 @@ int stand_tree_attention(const stand_attention* shape, const void* dev_q, const 
  * 0 <= parent[u] < u). */
 int stand_tree_mask(const int32_t* host_parent, int32_t n, uint32_t* host_mask);
 
-/* Pages and slots for new tokens.  Sequence b holds dev_len[b] tokens (int64) in the first ceil(len / page_size)
+/* Pages and slots for new tokens (width and page_size up to 2^27).  Sequence b holds dev_len[b] tokens (int64) in the first ceil(len / page_size)
  * entries of its table row and gets dev_new[b] (int32, 0..width) more.  The pages that this takes beyond those it
  * has come from the free list, a stack of *dev_n_free page numbers in dev_free [capacity]: in the order of the
  * sequences, then of the text, from the top down.  They are entered into dev_table [B, max_pages].

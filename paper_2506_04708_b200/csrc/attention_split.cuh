@@ -209,8 +209,11 @@ template <int DP, typename T> __global__ void __launch_bounds__(TJ_WARPS * 32) j
     const long long cta = (long long)(blockIdx.x + i) * p.group_ctas + rt;
     return (cta * 2 + (i == 0 ? rec.first_which : 0)) * p.tile_rows + in_tile;
   };
-  float top = -INFINITY;
-  for (int i = lane; i < rec.n_parts; i += 32) top = fmaxf(top, p.part_ml[at(i)].x);
+  // up to 32 pieces: one read of their m and l
+  float2 mine = make_float2(-INFINITY, 0.0f);
+  if (lane < rec.n_parts) mine = p.part_ml[at(lane)];
+  float top = mine.x;
+  for (int i = lane + 32; i < rec.n_parts; i += 32) top = fmaxf(top, p.part_ml[at(i)].x);
   top = warp_max_f(top);
   const float base = top == -INFINITY ? 0.0f : top;
   float total = 0.0f, o[E];
@@ -218,25 +221,30 @@ template <int DP, typename T> __global__ void __launch_bounds__(TJ_WARPS * 32) j
   for (int e = 0; e < E; ++e) o[e] = 0.0f;
   for (int i0 = 0; i0 < rec.n_parts; i0 += 32) {
     const int n = rec.n_parts - i0 < 32 ? rec.n_parts - i0 : 32;
-    float w = 0.0f, l = 0.0f;
-    if (lane < n) {
-      const float2 ml = p.part_ml[at(i0 + lane)];
-      w = exp2f(ml.x - base);
-      l = ml.y * w;
-      if (ml.y == 0.0f) w = 0.0f;
-    }
-    total += warp_sum_f(l);
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const float wi = __shfl_sync(FULL, w, i);
-      if (wi == 0.0f) continue;  // no weight; a piece without keys has written no o
-      const float* src = p.part_o + at(i0 + i) * DP + lane * E;
+    if (i0 > 0) mine = lane < n ? p.part_ml[at(i0 + lane)] : make_float2(-INFINITY, 0.0f);
+    float w = exp2f(mine.x - base);
+    total += warp_sum_f(mine.y * w);
+    if (mine.y == 0.0f) w = 0.0f;  // a piece without keys has written no o
+    constexpr int AT_ONCE = E > 4 ? 4 : 8;  // pieces whose o is asked for together
+    for (int i = 0; i < n; i += AT_ONCE) {
+      float wi[AT_ONCE], v[AT_ONCE][E];
 #pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float2 v = *reinterpret_cast<const float2*>(src + e);
-        o[e] = fmaf(wi, v.x, o[e]);
-        o[e + 1] = fmaf(wi, v.y, o[e + 1]);
+      for (int k = 0; k < AT_ONCE; ++k) {
+        wi[k] = __shfl_sync(FULL, w, i + k < n ? i + k : i);
+        if (i + k >= n) wi[k] = 0.0f;
+        const float* src = p.part_o + at(i0 + i + k) * DP + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          float2 t = make_float2(0.0f, 0.0f);
+          if (wi[k] != 0.0f) t = *reinterpret_cast<const float2*>(src + e);
+          v[k][e] = t.x;
+          v[k][e + 1] = t.y;
+        }
       }
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(wi[k], v[k][e], o[e]);
     }
   }
   const long long row = ((long long)rec.b * p.a.N + u) * p.a.heads_q + h;

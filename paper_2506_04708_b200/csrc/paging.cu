@@ -65,7 +65,8 @@ __device__ __forceinline__ long long block_sum(long long v, long long* s_part) {
 // at these sizes the time is that of a launch and three dependent reads (lengths, free list or table, slots).
 __global__ void __launch_bounds__(MAP_THREADS) page_map_kernel(const MapParams p) {
   __shared__ long long s_part[MAP_THREADS / 32];
-  __shared__ long long s_len[MAP_SEQS], s_have[MAP_SEQS], s_want[MAP_SEQS], s_at[MAP_SEQS];
+  __shared__ long long s_col[MAP_SEQS], s_have[MAP_SEQS], s_want[MAP_SEQS], s_at[MAP_SEQS];  // s_col, s_off: where the first new token goes
+  __shared__ unsigned s_off[MAP_SEQS];
   __shared__ int s_new[MAP_SEQS];
   pdl_trigger();
   pdl_wait();
@@ -97,7 +98,8 @@ __global__ void __launch_bounds__(MAP_THREADS) page_map_kernel(const MapParams p
     upto += before;
     const bool served = fits && (need == 0 || upto <= n_free);
     if (mine) {
-      s_len[tid] = len;
+      s_col[tid] = len > 0 ? len / p.page : 0;
+      s_off[tid] = len > 0 ? (unsigned)(len - s_col[tid] * p.page) : 0u;
       s_have[tid] = have;
       s_want[tid] = served ? want : have;
       s_at[tid] = n_free - 1 - (upto - need);  // index of this sequence's first page in the free list
@@ -127,14 +129,16 @@ __global__ void __launch_bounds__(MAP_THREADS) page_map_kernel(const MapParams p
   }
   // slots: the page of a position is an old table entry or comes from the free list, never from what another
   // thread of this launch writes
-  const long long items = (long long)n_own * p.width;
-  for (long long i = (long long)part * MAP_THREADS + tid; i < items; i += (long long)p.split * MAP_THREADS) {
-    const int s = (int)(i / p.width), j = (int)(i - (long long)s * p.width);
+  const int items = n_own * p.width;
+  for (int i = part * MAP_THREADS + tid; i < items; i += p.split * MAP_THREADS) {
+    const int s = p.per_block == 1 ? 0 : i / p.width, j = i - s * p.width;
     long long slot = -1;
     if (j < s_new[s]) {
-      const long long pos = s_len[s] + j, c = pos / p.page;
-      const int page = c < s_have[s] ? p.table[(long long)(first + s) * p.cols + c] : p.free_list[s_at[s] - (c - s_have[s])];
-      if (page >= 0) slot = (long long)page * p.page + (pos - c * p.page);
+      // 32-bit arithmetic from the first new token's place on: the long division is done once per sequence
+      const unsigned off = s_off[s] + (unsigned)j, c = off / (unsigned)p.page;
+      const long long col = s_col[s] + c;
+      const int page = col < s_have[s] ? p.table[(long long)(first + s) * p.cols + col] : p.free_list[s_at[s] - (col - s_have[s])];
+      if (page >= 0) slot = (long long)page * p.page + (off - c * (unsigned)p.page);
     }
     p.slots[(long long)first * p.width + i] = slot;
   }
@@ -253,7 +257,7 @@ extern "C" {
 int stand_page_map(const int64_t* dev_len, const int32_t* dev_new, int32_t B, int32_t width, int32_t page_size, int32_t max_pages,
                    const int32_t* dev_free, int32_t capacity, const int32_t* dev_n_free, int32_t* dev_table, int64_t* dev_slots,
                    int32_t* dev_granted, int64_t* dev_len_out, int32_t* dev_n_free_out, void* cu_stream) {
-  if (B < 1 || width < 1 || page_size < 1 || max_pages < 0 || capacity < 0) return STAND_E_ARG;
+  if (B < 1 || width < 1 || width > (1 << 27) || page_size < 1 || page_size > (1 << 27) || max_pages < 0 || capacity < 0) return STAND_E_ARG;
   if (!dev_len || !dev_new || !dev_n_free || !dev_slots || !dev_n_free_out) return STAND_E_ARG;
   if ((max_pages > 0 && !dev_table) || (capacity > 0 && !dev_free)) return STAND_E_ARG;
   if (dev_len_out == dev_len || dev_n_free_out == dev_n_free) return STAND_E_ARG;
