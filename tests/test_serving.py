@@ -789,3 +789,95 @@ def test_a_wait_that_runs_out_gives_nan_and_leaves_the_gpu_usable(dtype, dim):
         binding.set_wait_limit(-1)
     assert np.isnan(out).all() and np.isnan(lse).all()
     _check_attention(c, _run_attention(c))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ALL_TYPES)
+@pytest.mark.parametrize("B", [193, 700])
+def test_batches_of_more_sequences_than_threads(dtype, B):
+    """Many short texts, among them empty ones: a range of tiles covers dozens of sequences."""
+    rng = np.random.default_rng(B)
+    lens = [int(n) for n in np.where(rng.random(B) < 0.2, 0, rng.integers(1, 90, B))]
+    lens[B // 2] = 1200
+    c = _attention_case(B, dtype, lens, 3, 4, 2, 64, 16, parent=inputs.topology(3, 2, 2), nan=False)
+    _check_attention(c, _run_attention(c))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ALL_TYPES)
+@pytest.mark.parametrize("N,hq,hkv,dim,page", [(1, 130, 1, 64, 16), (2, 300, 2, 128, 32), (3, 4, 2, 20, 16), (9, 6, 3, 36, 16), (4, 2, 1, 7, 48), (5, 128, 1, 128, 64)])
+def test_head_layouts_beside_the_common_ones(dtype, N, hq, hkv, dim, page):
+    """More query heads to a key head than a tile has rows; head sizes that are no multiple of 8."""
+    c = _attention_case(N * hq, dtype, [0, 5, 70, 200], N, hq, hkv, dim, page, parent=inputs.topology(N, min(2, N - 1), 3))
+    _check_attention(c, _run_attention(c))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ALL_TYPES)
+def test_no_cache_at_all_and_pages_of_the_largest_size(dtype):
+    import torch
+    from paper_2506_04708_b200 import serving
+    c = _attention_case(5, dtype, [0, 0], 70, 4, 2, 64, 16)
+    qkv = c["qkv"].to("cuda:0")
+    none = torch.empty((0, 2, 16, 64), dtype=_dtype(dtype), device="cuda:0")
+    plan = serving.TreeAttention(2, 70, 4, 2, 64, _dtype(dtype), 16, 0, 0)
+    out, lse = plan(qkv[:, :, :4], qkv[:, :, 4:6], qkv[:, :, 6:], none, none, torch.empty((2, 0), dtype=torch.int32, device="cuda:0"),
+                    torch.zeros(2, dtype=torch.int64, device="cuda:0"))
+    _check_attention(c, (out.double().cpu().numpy(), lse.double().cpu().numpy()))
+    c = _attention_case(6, dtype, [3000, 4096, 4097], 5, 4, 2, 64, 4096, parent=inputs.topology(5, 2, 2))
+    _check_attention(c, _run_attention(c))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ALL_TYPES)
+def test_broadcast_keys_and_queries(dtype):
+    """Strides of zero: one key head's rows for all heads, one query row for all heads."""
+    import torch
+    c = _attention_case(91, dtype, [0, 130], 8, 8, 4, 64, 16, parent=inputs.topology(8, 4, 2), nan=False)
+    x = c["qkv"]
+    x[:, :, :8] = x[:, :, :1]
+    x[:, :, 8:12] = x[:, :, 8:9]
+    x[:, :, 12:] = x[:, :, 12:13]
+
+    def move(q, k, v, ck, cv):
+        wide = lambda t, n: t[:, :, :1].contiguous().expand(-1, -1, n, -1)  # noqa: E731
+        return wide(q, 8), wide(k, 4), wide(v, 4), ck, cv
+
+    _check_attention(c, _run_attention(c, move=move))
+
+
+@pytest.mark.gpu
+def test_operators_in_a_graph_follow_the_lengths():
+    """Captured once, replayed after lengths, counts and texts have changed in place."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    c = _attention_case(95, "bf16", [600, 40, 333], 24, 8, 2, 128, 16, parent=inputs.topology(24, 6, 3), nan=False)
+    dev = "cuda:0"
+    qkv, ck, cv = c["qkv"].to(dev), c["ck"].to(dev), c["cv"].to(dev)
+    table, length = torch.from_numpy(np.clip(c["table"], 0, ck.shape[0] - 1)).to(dev), torch.from_numpy(c["len"]).to(dev)
+    c["table"] = table.cpu().numpy()
+    plan = serving.TreeAttention(3, 24, 8, 2, 128, torch.bfloat16, 16, ck.shape[0], table.shape[1], parent=c["parent"])
+    args = (qkv[:, :, :8], qkv[:, :, 8:10], qkv[:, :, 10:], ck, cv, table, length)
+    x = torch.randn((3, 1, 5000), device=dev)
+    text = torch.randint(0, 5000, (3, 300), dtype=torch.int32, device=dev)
+    n_text, presence = torch.full((3,), 300, dtype=torch.int64, device=dev), torch.full((3,), 0.5, device=dev)
+    op = serving.LogitsProcessor(3, 1, 5000, torch.float32)
+    plan(*args)
+    op(x, text, n_text, presence=presence)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out, lse = plan(*args)
+        y = op(x, text, n_text, presence=presence)
+    for lens, n in (([600, 40, 333], 300), ([1, 0, 700], 7), ([64, 640, 128], 0)):
+        lens = np.minimum(lens, table.shape[1] * 16)
+        length.copy_(torch.from_numpy(np.array(lens, np.int64)))
+        n_text.fill_(n)
+        g.replay()
+        torch.cuda.synchronize()
+        c["len"] = np.array(lens, np.int64)
+        _check_attention(c, (out.double().cpu().numpy(), lse.double().cpu().numpy()))
+        want = x.clone()
+        for b in range(3):
+            want[b, 0, text[b, :n].long().unique()] -= 0.5
+        assert torch.equal(y, want)
