@@ -35,7 +35,7 @@ extern "C" {
 size_t stand_tree_attention_scratch_bytes(const stand_attention* c) {
   if (!attention_valid(c)) return 0;
   const int group = c->heads_q / c->heads_kv;
-  const size_t plain = ta_scratch_bytes(plain_tile_rows(c->N * group), c->dim, plain_ctas(c->dim));
+  const size_t plain = ta_scratch_bytes(PA_ROWS, c->dim, plain_ctas(c->dim));
   if (c->dtype == STAND_DTYPE_F32 || group > TA_ROWS) return plain;
   const size_t tensor = ta_scratch_bytes(tensor_tile_rows(c->N, group), c->dim, tensor_ctas(c->dim));
   return tensor > plain ? tensor : plain;  // alignment decides, and that is not known here

@@ -1,11 +1,14 @@
 // Tree attention without matrix instructions: any type (single precision among them), any strides, any head size up to
 // ATTN_DIM_MAX.
 //
-// A block takes up to RT rows of a pair and walks over its tiles of 64 keys (attention_split.cuh), two tiles of keys and
-// values in shared memory (single precision: cp.async; 16-bit types are converted on the way).  A warp has RT / 8 rows; for
-// the scores a lane has two keys, for the sums its share of the head size.  So every value from shared memory is used for
-// RT / 8 rows, and no sum crosses a warp.  What bounds it is shared memory: with RT = 64 a warp reads 16 passes for 32 packed
-// multiply-adds in the scores.
+// A block takes up to 32 rows of a pair and walks over its tiles of 64 keys (attention_split.cuh), two tiles of keys and
+// values in shared memory (single precision: cp.async; 16-bit types are converted on the way).  A warp has four rows; for the
+// scores a lane has two keys, for the sums its share of the head size.  So every value from shared memory is used for four
+// rows, and no sum crosses a warp.
+// Measured, single precision, 8 x 16 nodes of 16 / 4 heads of 64, texts of 50 - 1,500: 39 us; one node each over texts of
+// 100 - 4,000: 45 us (8 rows a block there: the same; 64 rows a block need 230 registers, one block per SM: 65 instead of 42).
+// What bounds it: shared memory within a tile (3,200 cycles of passes with two blocks per SM), and with few tiles per
+// block the latency of beginning a piece.
 #pragma once
 #include "async.cuh"
 #include "attention_split.cuh"
@@ -14,18 +17,17 @@
 namespace stand {
 
 constexpr int ATTN_DIM_MAX = 256;
-constexpr int PA_WARPS = 8, PA_THREADS = PA_WARPS * 32;
+constexpr int PA_WARPS = 8, PA_THREADS = PA_WARPS * 32, PA_ROWS = 32;  // rows of a block
 static_assert(PA_THREADS == 4 * TA_KT, "a thread per row of two tiles");
 
 template <int DP> struct PaShape {
   static constexpr int STAGES = DP == 256 ? 1 : 2;
   static constexpr int KP = DP + 4;                                     // floats between keys: no bank conflicts
   static constexpr int STAGE = TA_KT * KP + TA_KT * DP;                 // floats of a tile of keys and of values
-  template <int RT> static constexpr int smem() { return (STAGES * STAGE + RT * KP + RT * TA_KT) * 4; }
+  static constexpr int SMEM = (STAGES * STAGE + PA_ROWS * KP + PA_ROWS * TA_KT) * 4;
 };
 // Blocks per SM that the split counts on.
 inline int plain_ctas(int dim) { return tensor_dim(dim) == 64 ? 2 : 1; }
-inline int plain_tile_rows(int rows) { return rows <= 8 ? 8 : 32; }
 
 template <typename T> __device__ __forceinline__ float4 load4(const T* p, bool wide) {
   if constexpr (sizeof(T) == 2) {
@@ -49,17 +51,17 @@ __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_grou
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // wide: bases and strides allow 4 elements at a time
-template <typename T, int DP, int RT>
+template <typename T, int DP>
 __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __grid_constant__ TaSplit p, const bool wide) {
   using Sh = PaShape<DP>;
-  constexpr int KT = TA_KT, KP = Sh::KP, STAGES = Sh::STAGES, R = RT / PA_WARPS, E = DP / 32;
+  constexpr int KT = TA_KT, KP = Sh::KP, STAGES = Sh::STAGES, R = PA_ROWS / PA_WARPS, E = DP / 32;
   constexpr int EV = E < 4 ? E : 4;  // elements of the head size that lie together: lane * EV + 128 * i
   extern __shared__ float pa_smem[];
   __shared__ const T* s_src[3][2][KT];  // where keys and values of a tile lie; null: zeros
   __shared__ TaRange<PA_THREADS> s_range;
-  float* const sq = pa_smem + STAGES * Sh::STAGE;                      // [RT][KP]
+  float* const sq = pa_smem + STAGES * Sh::STAGE;                      // [PA_ROWS][KP]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.dim, D4 = (D + 3) & ~3;
-  float* const sp = sq + RT * KP + warp * R * KT;                      // [R][KT] of this warp
+  float* const sp = sq + PA_ROWS * KP + warp * R * KT;                      // [R][KT] of this warp
   pdl_trigger();
   pdl_wait();
   TaWalk walk;
@@ -313,37 +315,27 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
   if (tid == 0 && blockIdx.x % p.group_ctas == 0) p.records[blockIdx.x / p.group_ctas] = note.r;
 }
 
-template <typename T, int DP, int RT> int launch_plain_rows(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
+template <typename T, int DP> int launch_plain_rows(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
   TaSplit p;
-  ta_split(p, a, RT, DP, sms, plain_ctas(DP), 3, scratch);
+  ta_split(p, a, PA_ROWS, DP, sms, plain_ctas(DP), 3, scratch);
   const size_t al = 4 * sizeof(T);
   uintptr_t bits = (uintptr_t)a.k | (uintptr_t)a.v | (a.cols > 0 ? (uintptr_t)a.cache_k | (uintptr_t)a.cache_v : 0);
   for (int i = 0; i < 3; ++i) bits |= (uintptr_t)(a.kv_stride[i] * sizeof(T)) | (a.cols > 0 ? (uintptr_t)(a.cache_stride[i] * sizeof(T)) : 0);
   const bool wide = bits % al == 0 && a.dim % 4 == 0;
   static SmemLimit limit;
-  const int smem = PaShape<DP>::template smem<RT>();
-  int rc = limit.raise(plain_attention_kernel<T, DP, RT>, smem);
+  const int smem = PaShape<DP>::SMEM;
+  int rc = limit.raise(plain_attention_kernel<T, DP>, smem);
   if (rc) return rc;
-  rc = launch_dependent2(plain_attention_kernel<T, DP, RT>, dim3((unsigned)(p.groups * p.group_ctas)), PA_THREADS, st, (size_t)smem, p, wide);
+  rc = launch_dependent2(plain_attention_kernel<T, DP>, dim3((unsigned)(p.groups * p.group_ctas)), PA_THREADS, st, (size_t)smem, p, wide);
   if (rc) return rc;
   return launch_join<DP, T>(p, st);
 }
 
 template <typename T> int launch_plain_attention(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
   const int dp = tensor_dim(a.dim);
-  if (plain_tile_rows(a.N * a.group) == 8) {
-    if (dp == 64) return launch_plain_rows<T, 64, 8>(a, scratch, sms, st);
-    if (dp == 128) return launch_plain_rows<T, 128, 8>(a, scratch, sms, st);
-    return launch_plain_rows<T, 256, 8>(a, scratch, sms, st);
-  }
-  if (plain_tile_rows(a.N * a.group) == 32) {
-    if (dp == 64) return launch_plain_rows<T, 64, 32>(a, scratch, sms, st);
-    if (dp == 128) return launch_plain_rows<T, 128, 32>(a, scratch, sms, st);
-    return launch_plain_rows<T, 256, 32>(a, scratch, sms, st);
-  }
-  if (dp == 64) return launch_plain_rows<T, 64, 64>(a, scratch, sms, st);
-  if (dp == 128) return launch_plain_rows<T, 128, 64>(a, scratch, sms, st);
-  return launch_plain_rows<T, 256, 64>(a, scratch, sms, st);
+  if (dp == 64) return launch_plain_rows<T, 64>(a, scratch, sms, st);
+  if (dp == 128) return launch_plain_rows<T, 128>(a, scratch, sms, st);
+  return launch_plain_rows<T, 256>(a, scratch, sms, st);
 }
 
 }  // namespace stand

@@ -12,15 +12,21 @@
 // good deal.  Two CTAs share an SM (256 of the 512 columns of tensor memory and half of the shared memory each; head
 // size 256: one CTA).
 //
-// With at most 32 (64) rows the four (two) parts of the lanes hold the same rows: each part takes a quarter (half) of a
-// tile's keys, has its own maximum, sum and O, and they are joined at the end.  The product computes 128 rows anyway;
-// the exponentials of a tile then take all four warps instead of one.
+// Head sizes up to 64 with at most 32 (64) rows: the four (two) parts of the lanes hold the same rows, each takes a
+// quarter (half) of a tile's keys, has its own maximum, sum and O, and they are joined at the end.  The product computes 128
+// rows anyway; the exponentials of a tile then take all four warps instead of one.
 //
 // The keys of all pairs, laid end to end in tiles, are cut into as many equal ranges as there are CTAs (or groups of
 // CTAs: the row tiles of a pair with more than 128 rows go to neighbours that walk over the same keys at the same time,
 // so that those come from memory once and from L2 after that).  A range may begin and end inside a pair: such pieces
 // leave (m, l, O) in scratch and a second, small kernel joins them.  So long texts with few rows fill the GPU, and so do
 // batches of ragged lengths, without the host knowing a length.
+//
+// Measured (keys and values read once, over the time): 256 sequences x 24 nodes, texts of 130 - 4,100, 32 / 8 heads of 128:
+// 390 - 404 us in short bursts = 5.8 - 6.0 TB/s (0.89 - 0.92 of the copy bandwidth), 460 - 480 us in loops of seconds, where the
+// board's power limit holds the clock at 1.24 - 1.4 GHz; 64 nodes over 32,001 tokens, 28 / 4 heads of 128: 51 us = 0.57 PFLOP/s;
+// one token over 700: 11 us.  No unit is near its limit then (tensor pipe 36 %, exponentials 27 %, issue 29 %, memory 81 % of
+// a copy): what bounds a tile is the chain scores - maximum - exponentials - product, about 2,200 cycles, which two CTAs overlap.
 #pragma once
 #include <cuda.h>
 
@@ -731,6 +737,8 @@ inline int tensor_ctas(int dim) { return tensor_dim(dim) == 256 ? 1 : 2; }
 template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
   using Sh = TaShape<DP, C>;
   TaParams p;
+  // A piece's fixed cost in tiles, measured by trying 3 to 9: 16 sequences of 1 - 8,190 tokens with heads of 64 take 81, 71, 59,
+  // 58 us with 3, 5, 7, 9; 256 sequences of 130 - 4,100 with heads of 128 take 393, 389, 391, 398.
   ta_split(p.s, a, tensor_tile_rows(a.N, a.group), DP, sms, Sh::CTAS, DP == 64 ? 8 : 5, scratch);
   p.box_rows = 16;
   while (p.box_rows < TA_KT && a.page % (p.box_rows * 2) == 0) p.box_rows *= 2;
@@ -760,9 +768,14 @@ template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams
 }
 
 template <int DP, bool BF16> int launch_tensor_parts(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
-  const int rows = tensor_tile_rows(a.N, a.group);
-  if (rows <= TA_ROWS / 4) return launch_tensor_attention<DP, 4, BF16>(a, scratch, sms, wait_limit, st);
-  if (rows <= TA_ROWS / 2) return launch_tensor_attention<DP, 2, BF16>(a, scratch, sms, wait_limit, st);
+  // Few rows of small heads in four (two) parts.  Measured, parts / none: 16 sequences of 1 - 8,190 tokens, 16 / 16 heads of
+  // 64, with 1 node 52 / 63 us, 32 nodes 59 / 66, 48 nodes 68 / 80.  Not for larger heads, whose tiles wait for memory and not
+  // for the softmax, and where the exchange takes room from the rings: head size 128, 48 rows, 129 / 108; 16 rows, 193 / 184.
+  if constexpr (DP == 64) {
+    const int rows = tensor_tile_rows(a.N, a.group);
+    if (rows <= TA_ROWS / 4) return launch_tensor_attention<DP, 4, BF16>(a, scratch, sms, wait_limit, st);
+    if (rows <= TA_ROWS / 2) return launch_tensor_attention<DP, 2, BF16>(a, scratch, sms, wait_limit, st);
+  }
   return launch_tensor_attention<DP, 1, BF16>(a, scratch, sms, wait_limit, st);
 }
 

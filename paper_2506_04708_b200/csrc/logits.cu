@@ -176,7 +176,9 @@ __device__ __forceinline__ void stream_row(const char* in, char* out, int t0, in
 // chunk once in shared memory and marks them, the biased and the drafted ones in a bit map; then its warps stream the
 // nodes' rows through.  Nearly all logits are only copied; those marked are changed as soon as their pieces have
 // gone by (after the whole rows it took 936 us instead of 600 for 256 x 24 rows: their lines had left L2).  HBM-bound: every logit is read
-// and written once.
+// and written once.  Measured: 256 x 24 rows of 151,936 bf16 with biases and masks 603 us = 6.2 TB/s, 0.95 of the copy
+// bandwidth (a plain copy of the same bytes 572 - 580); 8 rows of 32,000 4.0 us; 64 rows of 50,257 with texts of 6,000 - 12,000
+// 17 us, bound by the chain text - counts - rows.
 template <int DT>
 __global__ void __launch_bounds__(LG_THREADS, LG_BLOCKS) logits_kernel(const __grid_constant__ LogitsParams p) {
   extern __shared__ uint32_t lg_smem[];
@@ -322,11 +324,11 @@ extern "C" int stand_process_logits(const stand_logits* c, const stand_logits_in
   p.text_stride = c->text_stride; p.text = x->text; p.n_text = (const long long*)x->n_text; p.n_prompt = (const long long*)x->n_prompt;
   p.tree = x->tree_tokens; p.repetition = x->repetition; p.frequency = x->frequency; p.presence = x->presence;
   p.bias_start = x->bias_start; p.bias_id = x->bias_id; p.bias_value = x->bias_value; p.mask = x->mask; p.mask_row = x->mask_row;
-  // A small batch is cut finer, so that it reaches all multiprocessors (two blocks each) down to 512 tokens; a text is
-  // scanned once per chunk, so a large one is not.
+  // A small batch is cut finer, so that it reaches all multiprocessors (two blocks each) down to 512 tokens (8 rows of 32,000:
+  // 4.0 us instead of 9.2); a text is scanned once per chunk, so a large one is not.
   p.chunk = LG_CHUNK;
   while (p.chunk > 512 && (long long)c->B * ((c->V + p.chunk - 1) / p.chunk) < 2 * 148) p.chunk /= 2;
-  // between one and two rounds of blocks: larger chunks, if that makes it one
+  // between one and two rounds of blocks: larger chunks, if that makes it one (64 rows of 50,257: part of 21 -> 17 us)
   const long long round = 148 * LG_BLOCKS;
   if (p.chunk == LG_CHUNK && (long long)c->B * ((c->V + LG_CHUNK - 1) / LG_CHUNK) > round)
     for (int ch = LG_CHUNK + 512; ch <= LG_CHUNK_MAX; ch += 512)
