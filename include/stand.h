@@ -291,7 +291,8 @@ int stand_profile_stages(stand_ctx* ctx, void* const* events);
  * runs out the kernel records it, lets its copies in flight land and returns, and the host sees
  * stand_stats.wait_timeouts (or NaN / -1 results from stand_row_stats): the GPU context stays usable.  This
  * call sets, for the whole process, how many polls the kernel's loader spends waiting for a free stage of its
- * shared-memory ring, and every wait of stand_tree_attention: 1 .. 2^22 (the default, about a second); 0 makes its very first wait give up before
+ * shared-memory ring, and, in units of 512 clock cycles, how long every wait of
+ * stand_tree_attention may last: 1 .. 2^22 (the default, about a second); 0 makes its very first wait give up before
  * anything was copied, which is how the tests reach the failure path; a negative value restores the default.
  * Larger values are clamped: a wait cannot be made unbounded. */
 int stand_set_wait_limit(int64_t polls);

@@ -3,7 +3,8 @@
 `TreeAttention`, `PageMap`, `KvCommit` and `LogitsProcessor` hold what stays the same from step to step - shapes, the
 tree, workspaces, result tensors - and are called with the step's device tensors.  Argument marshalling only: the work
 runs in the CUDA kernels of libstand.so.  Calls only enqueue work on the current stream (or `stream`) and return; the
-result tensors of an object are overwritten by its next call unless the caller passes its own.
+result tensors of an object are overwritten by its next call unless the caller passes its own.  An object, and tensors given
+to it, must live until the work on the stream is done; calls of one object that may overlap need an order of their own.
 """
 import ctypes as C
 import math
