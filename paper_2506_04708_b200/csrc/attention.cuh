@@ -48,6 +48,16 @@ __device__ __forceinline__ long long attn_len(const AttnParams& p, int b) {
   return n < 0 ? 0 : (n > most ? most : n);
 }
 
+// The nodes first .. first + 31 that node u of sequence b sees, as bits; of the last word of a mask, from bit first % 32
+// on.  The last row tile of a pair may have rows beyond the last node: they see nothing, and no mask is read for them.
+__host__ __device__ __forceinline__ uint32_t attn_nodes_seen(const AttnParams& p, int b, int u, int first) {
+  const int below = u + 1 - first;  // nodes first .. u
+  if (u >= p.N || below <= 0) return 0u;
+  uint32_t bits = FULL;
+  if (p.mask) bits = p.mask[(long long)b * p.mask_stride + (long long)u * p.mask_words + (first >> 5)] >> (first & 31);
+  return below >= 32 ? bits : bits & ((1u << below) - 1);
+}
+
 // Does node u of sequence b see node v?
 __device__ __forceinline__ bool attn_sees(const AttnParams& p, int b, int u, int v) {
   if (v > u) return false;

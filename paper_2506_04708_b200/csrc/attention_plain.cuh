@@ -204,15 +204,14 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
       for (int i = 0; i < R; ++i)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          uint32_t bits = live[i] ? FULL : 0u;
-          int below = KT;
-          if (partial) below = s.len - j * KT - 32 * c;
+          uint32_t bits = FULL;
           if (tree) {
-            const int first = (j - s.p_tiles) * KT + 32 * c;
-            below = node[i] + 1 - first;
-            if (p.a.mask && below > 0) bits &= __ldg(p.a.mask + (long long)s.b * p.a.mask_stride + (long long)node[i] * p.a.mask_words + (first >> 5));
+            bits = attn_nodes_seen(p.a, s.b, node[i], (j - s.p_tiles) * KT + 32 * c);
+          } else if (partial) {
+            const int below = s.len - j * KT - 32 * c;
+            bits = below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
           }
-          seen[i][c] = below >= 32 ? bits : (below > 0 ? bits & ((1u << below) - 1) : 0u);
+          seen[i][c] = live[i] ? bits : 0u;
         }
       // row by row in step: the rows' shuffles and exponentials overlap
       float top[R], keep[R], sum[R];

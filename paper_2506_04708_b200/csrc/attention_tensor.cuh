@@ -432,17 +432,13 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
             tc_wait_ld();
             if (tree || partial) {
               const int key = part * W + c * CH;  // of the tile
-              int below;                          // this row sees keys before that, or none after it
-              uint32_t seen = FULL;
+              uint32_t seen;                      // by this row
               if (tree) {
-                const int first = (j - s.p_tiles) * KT + key;
-                below = u + 1 - first;            // nodes first .. u
-                if (p.s.a.mask && below > 0)
-                  seen = __ldg(p.s.a.mask + (long long)s.b * p.s.a.mask_stride + (long long)u * p.s.a.mask_words + (first >> 5)) >> (first & 31);
+                seen = attn_nodes_seen(p.s.a, s.b, u, (j - s.p_tiles) * KT + key);
               } else {
-                below = left - key;
+                const int below = left - key;
+                seen = below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
               }
-              seen &= below >= 32 ? FULL : (below > 0 ? (1u << below) - 1 : 0u);
 #pragma unroll
               for (int i = 0; i < CH; ++i) x[i] = seen >> i & 1u ? x[i] : 0xFF800000u;
               __syncwarp();
