@@ -133,8 +133,9 @@ class TreeAttention(_Op):
         ptree = self._opt(tree_tokens, t.int32, self._tree_shape, "tree_tokens")
         if out is None:
             out = self.out
-        elif out.dtype is not self.dtype or out.shape != self._q_shape or not out.is_contiguous():
-            raise StandError("out: wants a contiguous tensor of q's shape and type")
+        else:
+            self._floats(out, self._q_shape, "out")
+            _need(out.is_contiguous(), "out: wants a contiguous tensor")
         if lse is None:
             lse = self.lse
         plse = self._ints(lse, t.float32, self.lse.shape, "lse")

@@ -30,3 +30,83 @@ def test_the_mask_is_read_for_existing_nodes_only(bounds_program, N, group, own)
     for masked in (1, 0):
         run = subprocess.run([bounds_program, str(N), str(group), "3", str(own), str(masked)], capture_output=True, text=True, timeout=60)
         assert run.returncode == 0, (run.returncode, run.stdout)
+
+
+# ---------------------------------------------------------------- result tensors
+class _Tensor:
+    """What the binding asks of a tensor, without a device."""
+
+    def __init__(self, shape, dtype, device=0, contiguous=True, stride=None):
+        steps = [1]
+        for n in reversed(shape[1:]):
+            steps.insert(0, steps[0] * n)
+        self.shape, self.dtype, self.device, self._d, self._c, self._s = tuple(shape), dtype, device, device, contiguous, stride or tuple(steps)
+
+    def get_device(self):
+        return self._d
+
+    def is_contiguous(self):
+        return self._c
+
+    def stride(self):
+        return self._s
+
+    def data_ptr(self):
+        return 0x1000
+
+
+def _hostless_attention(B=1, N=4, hq=2, hkv=2, dim=64, page=16, pages=4, cols=4):
+    """A TreeAttention whose launches are counted, not made, and the arguments of a call that it takes."""
+    import ctypes as C
+
+    import torch
+    from paper_2506_04708_b200 import serving
+    bf = torch.bfloat16
+    p = object.__new__(serving.TreeAttention)
+    p.torch, p.dtype, p.dev, p._index = torch, bf, "cuda:0", 0
+    p.cfg = binding.StandAttention(B, N, hq, hkv, dim, binding.DTYPE_BF16, page, pages, cols, 0.125)
+    p._cfg_ptr, p._strides, p._mask_ptr, p.mask_stride, p._scratch, p._scratch_bytes = C.addressof(p.cfg), None, None, 0, 0, 0
+    p._q_shape, p._kv_shape, p._cache_shape = (B, N, hq, dim), (B, N, hkv, dim), (pages, hkv, page, dim)
+    p._table_shape, p._len_shape, p._tree_shape = (B, cols), (B,), (B, N)
+    p.out, p.lse = _Tensor(p._q_shape, bf), _Tensor((B, N, hq), torch.float32)
+    p._lib = type("Lib", (), {"stand_tree_attention": None})
+    p.launches = 0
+
+    def launch(*a):
+        p.launches += 1
+    p._launch = launch
+    args = [_Tensor(p._q_shape, bf)] + [_Tensor(p._kv_shape, bf) for _ in range(2)] + [_Tensor(p._cache_shape, bf) for _ in range(2)]
+    return p, args + [_Tensor((B, cols), torch.int32), _Tensor((B,), torch.int64)]
+
+
+def test_results_go_to_this_device_only():
+    """An `out` or `lse` on the CPU or another GPU, of another type or shape, or with gaps is refused before a launch."""
+    import torch
+    p, args = _hostless_attention()
+    bf, f32, q, rows = torch.bfloat16, torch.float32, p._q_shape, (1, 4, 2)
+    p(*args)
+    p(*args, out=_Tensor(q, bf), lse=_Tensor(rows, f32))
+    assert p.launches == 2
+    for bad in (dict(out=_Tensor(q, bf, device=-1)), dict(out=_Tensor(q, bf, device=1)), dict(out=_Tensor(q, torch.float16)),
+                dict(out=_Tensor((1, 4, 2, 32), bf)), dict(out=_Tensor(q, bf, contiguous=False)), dict(lse=_Tensor(rows, f32, device=-1)),
+                dict(lse=_Tensor(rows, f32, device=1)), dict(lse=_Tensor(rows, bf)), dict(lse=_Tensor((1, 4), f32)),
+                dict(lse=_Tensor(rows, f32, contiguous=False))):
+        with pytest.raises(binding.StandError):
+            p(*args, **bad)
+    assert p.launches == 2
+
+
+@pytest.mark.gpu
+def test_results_on_the_host_are_refused():
+    import torch
+    from paper_2506_04708_b200 import serving
+    dev = "cuda:0"
+    plan = serving.TreeAttention(1, 4, 2, 2, 64, torch.bfloat16, 16, 4, 4)
+    q, cache = torch.zeros((1, 4, 2, 64), dtype=torch.bfloat16, device=dev), torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16, device=dev)
+    args = q, q, q, cache, cache, torch.zeros((1, 4), dtype=torch.int32, device=dev), torch.zeros(1, dtype=torch.int64, device=dev)
+    for bad in (dict(out=torch.empty(q.shape, dtype=q.dtype)), dict(out=torch.empty(q.shape, device=dev)), dict(lse=torch.empty((1, 4, 2)))):
+        with pytest.raises(binding.StandError):
+            plan(*args, **bad)
+    mine = torch.full_like(q, 7)
+    out, _ = plan(*args, out=mine)
+    assert out is mine and not mine.any()
