@@ -341,7 +341,8 @@ typedef struct {
  * dev_tree_tokens [B, N] int32 (may be NULL): a node below 0 was not drafted; its row is empty.
  * Writes dev_out [B, N, heads_q, dim] and, if not NULL, dev_lse [B, N, heads_q] float: the natural log-sum-exp of the
  * row's scaled scores.  An empty row (no visible key) gets zeros and -inf.  Keys and values that a row does not see
- * do not enter it, whatever they hold.
+ * do not enter it, whatever they hold.  A value that it sees and that is not finite makes its element of the row +inf, -inf or
+ * NaN as a sum of such values does, however small its weight.
  * Scores, softmax statistics and sums are 32-bit floats.  dev_len is int64; a length below 0 counts as 0, one beyond
  * max_pages * page_size as that; a table entry outside [0, pages) reads as a page of zeros.  dev_scratch: 256-byte
  * aligned, stand_tree_attention_scratch_bytes (0: invalid shapes) of it; calls that may overlap need scratch of their

@@ -299,6 +299,18 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
       const int h = s.g * p.a.group + r - node[i] * p.a.group;
       const long long out = ((long long)s.b * p.a.N + node[i]) * p.a.heads_q + h, at = ta_part_row(p, s, row);
       const bool empty = !live[i] || l[i] == 0.0f;
+      float zero = 0.0f;  // NaN if one of them is not finite
+#pragma unroll
+      for (int e = 0; e < E; ++e) zero = fmaf(o[i][e], 0.0f, zero);
+      if (isnan(zero) && live[i] && isfinite(l[i])) {
+        const int k1 = s.end * KT, n0 = s.begin > s.p_tiles ? s.begin - s.p_tiles : 0, n1 = s.end > s.p_tiles ? s.end - s.p_tiles : 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int d = lane * EV + e / EV * 128 + e % EV;
+          if (isnan(o[i][e]) && d < D)
+            o[i][e] = attn_settle<T>(p.a, s.b, s.g, node[i], d, s.begin * KT, k1 < s.len ? k1 : s.len, n0 * KT, n1 * KT, o[i][e], true);
+        }
+      }
       if (lane == 0) {
         if (!s.whole) p.part_ml[at] = live[i] ? make_float2(m[i], l[i]) : make_float2(-INFINITY, 0.0f);
         else if (p.a.lse) p.a.lse[out] = empty ? -INFINITY : 0.6931471805599453f * (m[i] + log2f(l[i]));

@@ -225,7 +225,8 @@ template <int DP, typename T> __global__ void __launch_bounds__(TJ_WARPS * 32) j
     if (i0 > 0) mine = lane < n ? p.part_ml[at(i0 + lane)] : make_float2(-INFINITY, 0.0f);
     float w = exp2f(mine.x - base);
     total += warp_sum_f(mine.y * w);
-    if (mine.y == 0.0f) w = 0.0f;  // a piece without keys has written no o
+    // A piece without keys has written no o.  Another's weight may be too small for its type: its o may still hold infinities.
+    w = mine.y == 0.0f ? 0.0f : fmaxf(w, 1.4e-45f);
     constexpr int AT_ONCE = E > 4 ? 4 : 8;  // pieces whose o is asked for together
     for (int i = 0; i < n; i += AT_ONCE) {
       float wi[AT_ONCE], v[AT_ONCE][E];

@@ -578,16 +578,13 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
         if (!s.whole) p.s.part_ml[at] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
         else if (p.s.a.lse) p.s.a.lse[out_row] = empty ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
       }
-      auto add_odd = [&](float& o, int col, int u) {
-        if (col >= p.s.a.dim) return;
-        const int n0 = (s.begin > s.p_tiles ? s.begin - s.p_tiles : 0) * KT, n1 = s.end > s.p_tiles ? (s.end - s.p_tiles) * KT : 0;
-        for (int v = n0; v < n1 && v <= u; ++v) {
-          if (!attn_sees(p.s.a, s.b, u, v)) continue;
-          const unsigned short raw = reinterpret_cast<const unsigned short*>(
-              p.s.a.v)[(long long)s.b * p.s.a.kv_stride[0] + (long long)v * p.s.a.kv_stride[1] + (long long)s.g * p.s.a.kv_stride[2] + col];
-          const float f = BF16 ? __uint_as_float((uint32_t)raw << 16) : __half2float(__ushort_as_half(raw));
-          if (!isfinite(f)) o += f;
-        }
+      // o of a row whose sum of weights is in order (`sound`)
+      auto settle = [&](float o, int col, int u, bool sound) {
+        const bool lost = isnan(o) && sound;
+        if (!(lost || odd) || col >= p.s.a.dim) return o;
+        const int k1 = s.end * KT, n0 = s.begin > s.p_tiles ? s.begin - s.p_tiles : 0, n1 = odd && s.end > s.p_tiles ? s.end - s.p_tiles : 0;
+        return attn_settle<typename std::conditional<BF16, __nv_bfloat16, __half>::type>(p.s.a, s.b, s.g, u, col, s.begin * KT,
+                                                                                           k1 < s.len ? k1 : s.len, n0 * KT, n1 * KT, o, lost);
       };
       if constexpr (C == 1) {
         if (warp_in) {
@@ -598,13 +595,12 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
             tc_ld32(o, my + Sh::COL_O + c * 32);
             tc_wait_ld();
             if (!in) continue;
-            if (odd && live) {
+            float zero[4] = {};  // NaN if one of them is not finite
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                float v = __uint_as_float(o[i]);
-                add_odd(v, c * 32 + i, u);
-                o[i] = __float_as_uint(v);
-              }
+            for (int i = 0; i < 32; ++i) zero[i & 3] = fmaf(__uint_as_float(o[i]), 0.0f, zero[i & 3]);
+            if (live && (odd || isnan(zero[0] + zero[1] + zero[2] + zero[3]))) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(settle(__uint_as_float(o[i]), c * 32 + i, u, isfinite(l)));
             }
             if (!s.whole) {
               float4* dst = reinterpret_cast<float4*>(p.s.part_o + at * DP + c * 32);
@@ -661,8 +657,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
 #pragma unroll
               for (int e = 0; e < 4; ++e) v[e] += exchange[(k * rows + r) * pitch + q * 4 + e];
             const float2 ml = sh.ml[r];  // 1 / l, and whether the row is there at all
-            if (odd && ml.y != 0.0f)
-              for (int e = 0; e < 4; ++e) add_odd(v[e], col + e, ru);
+            if (ml.y != 0.0f && (odd || !isfinite(v[0] + v[1] + v[2] + v[3])))
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = settle(v[e], col + e, ru, ml.x > 0.0f);
             if (!s.whole) {
               *reinterpret_cast<float4*>(p.s.part_o + part_row(s, r) * DP + col) = make_float4(v[0], v[1], v[2], v[3]);
             } else if (col < p.s.a.dim) {

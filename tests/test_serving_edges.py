@@ -110,3 +110,69 @@ def test_results_on_the_host_are_refused():
     mine = torch.full_like(q, 7)
     out, _ = plan(*args, out=mine)
     assert out is mine and not mine.any()
+
+
+# ---------------------------------------------------------------- cached values that are not finite
+def _plant(c, b, pos, head, element, value):
+    c["cv"][int(c["table"][b, pos // c["page"]]), head, pos % c["page"], element] = value
+
+
+def _check_planted(c, clean, hits, got):
+    """hits: (sequence, element, key head, value): what that element of all rows of these heads has to be."""
+    out, lse = got
+    group, hit = c["hq"] // c["hkv"], np.zeros_like(out, bool)
+    for b, d, g, value in hits:
+        rows = out[b, :, g * group:(g + 1) * group, d]
+        assert (np.isnan(rows) if np.isnan(value) else rows == value).all(), (b, d, g, value, rows)
+        hit[b, :, g * group:(g + 1) * group, d] = True
+    ts._check_attention(c, (np.where(hit, clean[0], out), lse), want=clean)
+
+
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("N,hq,hkv,dim", [(3, 2, 2, 64), (24, 4, 2, 64), (33, 4, 2, 64), (24, 3, 1, 40), (8, 8, 2, 128), (5, 2, 1, 256)])
+def test_cached_values_that_are_not_finite(dtype, N, hq, hkv, dim):
+    """One infinity, two of a sign, two of opposite signs, a NaN: in all forms of the kernels the element is what the sum is.
+    (Rows of heads up to 64 are held several times, for parts of the keys: an infinity in one part is no NaN in another.)"""
+    c = ts._attention_case(dim + N, dtype, [1, 70, 300], N, hq, hkv, dim, 16, parent=inputs.topology(N, 2, 6))
+    clean, g = ts._reference(c), hkv - 1
+    hits = [(0, 0, 0, -INF)]
+    _plant(c, 0, 0, 0, 0, -INF)
+    for pos in (3, 69):
+        _plant(c, 1, pos, g, 5, INF)
+    hits.append((1, 5, g, INF))
+    for pos, value in ((17, INF), (200, -INF)):
+        _plant(c, 2, pos, g, 6, value)
+    hits.append((2, 6, g, NAN))
+    _plant(c, 2, 250, 0, 7, NAN)
+    hits.append((2, 7, 0, NAN))
+    for pos in range(300):
+        _plant(c, 2, pos, 0, 9, -INF)
+    hits.append((2, 9, 0, -INF))
+    _check_planted(c, clean, hits, ts._run_attention(c))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("hq,hkv,dim", [(2, 2, 64), (4, 1, 128)])
+def test_infinities_whose_weight_is_below_the_type(dtype, hq, hkv, dim):
+    """Scores rise by 260 nats along a text that is cut into pieces: a 32-bit weight of its early tokens is zero, the definition's is not."""
+    n = 3000
+    c = ts._attention_case(7, dtype, [n, 100], 4, hq, hkv, dim, 16, parent=inputs.topology(4, 2, 2), nan=False)
+    c["qkv"][0, :, :hq] = 0
+    c["qkv"][0, :, :hq, 0] = 4.0
+    c["qkv"][0, :, hq:hq + hkv] = 0  # the nodes' scores are in the middle of it
+    for pos in range(n):
+        c["ck"][int(c["table"][0, pos // 16]), :, pos % 16, 0] = (pos / n - 0.5) * 260.0 / 4.0
+    clean = ts._reference(c, scale=1.0)
+    hits = []
+    for d, (pos, value) in enumerate([(0, INF), (40, -INF), (700, INF), (2990, -INF), (1500, NAN)]):
+        _plant(c, 0, pos, 0, 2 * d, value)
+        hits.append((0, 2 * d, 0, value))
+    _plant(c, 0, 5, 0, 21, INF)
+    _plant(c, 0, 2995, 0, 21, -INF)
+    hits.append((0, 21, 0, NAN))
+    _check_planted(c, clean, hits, ts._run_attention(c, scale=1.0))
