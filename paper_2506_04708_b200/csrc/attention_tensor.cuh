@@ -39,6 +39,12 @@ namespace stand {
 constexpr int TA_ROWS = 128;              // rows of a CTA: lanes of tensor memory
 constexpr int TA_THREADS = 224;
 constexpr float TA_SLACK = 8.0f;          // the maximum is raised only when scores pass it by 2^8 (below)
+// Weights of the second product are rounded to the input's type, since both operands of a 16-bit product have one type: each
+// is off by 2^-9 (bfloat16) or 2^-12 (half) of itself at most, independently, which is what rounding the result costs anyway;
+// their sum l is taken before the rounding, in fp32.  Half has few exponents: there weights are 2^TA_LIFT times larger (at most 2^15,
+// with the slack), as are l and o, so that those down to 2^-21 of the largest keep all bits and none above 2^-32 is lost
+// (unlifted, 40,000 keys of 2^-26 beside a dominant one were lost from o while they stayed in l).
+constexpr float TA_LIFT = 7.0f;
 constexpr int TA_XCOLS = 16;              // columns of O that the parts exchange at a time
 
 template <int DP, int C> struct TaShape {
@@ -475,7 +481,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
               }
             }
           }
-          const float base = m == -INFINITY ? 0.0f : m;
+          const float base = (m == -INFINITY ? 0.0f : m) - (BF16 ? 0.0f : TA_LIFT);
           const unsigned long long scale_2 = pack2(scale2, scale2), base_2 = pack2(-base, -base);
           unsigned long long sum_2 = pack2(0.0f, 0.0f);
 #pragma unroll 1
@@ -548,6 +554,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
       tc_fence_after();
       const bool odd = sh.odd[n_seg & 1] == n_seg + 1;
       ++n_seg;
+      if (!BF16) m -= TA_LIFT;  // what l and o are relative to
 
       // ---- the piece's result ---------------------------------------------------------------
       float factor = 1.0f;  // of this part's o

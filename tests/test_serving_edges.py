@@ -176,3 +176,41 @@ def test_infinities_whose_weight_is_below_the_type(dtype, hq, hkv, dim):
     _plant(c, 0, 2995, 0, 21, -INF)
     hits.append((0, 21, 0, NAN))
     _check_planted(c, clean, hits, ts._run_attention(c, scale=1.0))
+
+
+# ---------------------------------------------------------------- small weights of half precision
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,N,hq,hkv,dim,B", [(40000, 1, 2, 2, 64, 24), (40000, 4, 4, 1, 128, 40), (9000, 40, 1, 1, 64, 150), (20000, 1, 1, 1, 256, 60)])
+@pytest.mark.parametrize("last", [False, True])
+def test_many_small_weights_beside_a_dominant_one(dtype, n, N, hq, hkv, dim, B, last):
+    """One key takes nearly all weight and has the value 0; tens of thousands of others, near 2^-26 of it each, make the result.
+    So many sequences (over the same pages) that thousands of keys are summed relative to the dominant one.  Half: none of them may be lost.  Tolerance of test_serving.py with weights that keep all bits down to 2^-21 and 2^-32 of the
+    largest weight below that: 2^-32 sum |v| in place of 2^-25 sum |v|."""
+    c = ts._attention_case(n + dim, dtype, [n], N, hq, hkv, dim, 64, parent=inputs.topology(N, 3, 4), nan=False)
+    rng = np.random.default_rng(5)
+    import torch
+    c["qkv"][:] = 0
+    c["qkv"][:, :, :hq, 0] = 4.0
+    c["qkv"][:, :, hq:hq + hkv, 0] = -10.0  # the nodes themselves: next to nothing
+    flat = torch.from_numpy((-26 * np.log(2.0) / 4 + 0.05 * rng.standard_normal(n)).astype(np.float32))
+    at = n - 1 if last else 3
+    flat[at] = 0.0
+    ids = torch.from_numpy(c["table"][0].astype(np.int64))
+    keys = torch.zeros((len(ids) * 64,))
+    keys[:n] = flat
+    c["ck"][:] = 0
+    c["ck"][ids, :, :, 0] = keys.view(-1, 64)[:, None].expand(-1, hkv, -1).to(c["ck"].dtype)
+    c["cv"] = (1 + 0.25 * c["cv"].float()).to(c["cv"].dtype)
+    c["cv"][int(c["table"][0, at // 64]), :, at % 64] = 0
+    r_out, r_lse, weight, spread, reach = ts._reference(c, scale=1.0)
+    c.update(len=c["len"].repeat(B), table=c["table"].repeat(B, 0), qkv=c["qkv"].expand(B, -1, -1, -1).contiguous())
+    out, lse = ts._run_attention(c, scale=1.0)
+    u, e = ts.U[dtype], (dim + 8) * 2.0**-24 * reach
+    lost = 2.0**-32 * spread if dtype == "f16" else 0
+    tol = u * np.abs(r_out) + (u + 2 * e[..., None] + 2.0**-19) * weight + lost
+    if dtype == "f16":
+        tol = np.maximum(tol, 2.0**-25)  # the result's own type
+    assert np.median(np.abs(r_out)) > 1e-4
+    assert (np.abs(out - r_out) <= tol).all(), np.max(np.abs(out - r_out) / tol)
+    assert (np.abs(lse - r_lse) <= e + 2.0**-19 * (1 + np.abs(r_lse))).all()
