@@ -55,7 +55,6 @@ class Model:
             qkv = (self.norm(x) @ w["qkv"]).unflatten(-1, (-1, self.dim))
             q, k, v = qkv.split([self.hq, self.hkv, self.hkv], 2)
             q, k = self.rotate(q, pos), self.rotate(k, pos)
-            v = v.contiguous()
             ks.append(k)
             vs.append(v)
             x = x + attend(i, q, k, v).flatten(2) @ w["out"]

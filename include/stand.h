@@ -329,8 +329,11 @@ typedef struct {
   int32_t max_pages;  /* columns of the block table, >= 0; max_pages * page_size <= 2^30 */
   float scale;        /* scores are scale * q . k; > 0 */
   int64_t q_stride[3];      /* sequence, node, head */
-  int64_t kv_stride[3];     /* sequence, node, head (the nodes' keys and values alike) */
+  int64_t kv_stride[3];     /* sequence, node, head: the nodes' keys, and their values too unless own_v_stride is 1 */
   int64_t cache_stride[3];  /* page, head, token (both caches alike) */
+  int64_t v_stride[3];      /* sequence, node, head: the nodes' values, if own_v_stride is 1 */
+  int32_t own_v_stride;     /* 0 or 1 */
+  int32_t reserved;         /* must be 0 */
 } stand_attention;
 
 /* Attention of all nodes of B draft trees over the cached text and the nodes' ancestors (Sec. 4.2's tree, Sec. 5:

@@ -50,6 +50,7 @@ class StandAttention(C.Structure):
         ("B", C.c_int32), ("N", C.c_int32), ("heads_q", C.c_int32), ("heads_kv", C.c_int32), ("dim", C.c_int32),
         ("dtype", C.c_int32), ("page_size", C.c_int32), ("pages", C.c_int32), ("max_pages", C.c_int32),
         ("scale", C.c_float), ("q_stride", C.c_int64 * 3), ("kv_stride", C.c_int64 * 3), ("cache_stride", C.c_int64 * 3),
+        ("v_stride", C.c_int64 * 3), ("own_v_stride", C.c_int32), ("reserved", C.c_int32),
     ]
 
 

@@ -23,8 +23,9 @@ bool attention_valid(const stand_attention* c) {
   if (c->page_size < 16 || c->page_size > 4096 || c->page_size % 16 != 0 || c->pages < 0 || c->max_pages < 0) return false;
   if (!(c->scale > 0.0f && c->scale < INFINITY) || c->heads_q > 65535 || (long long)c->max_pages * c->page_size > (1ll << 30)) return false;
   if ((long long)c->N * (c->heads_q / c->heads_kv) >= (1ll << 20) || (long long)c->B * c->heads_kv > (1ll << 24)) return false;
+  if ((c->own_v_stride != 0 && c->own_v_stride != 1) || c->reserved != 0) return false;
   for (int i = 0; i < 3; ++i)
-    if (c->q_stride[i] < 0 || c->kv_stride[i] < 0 || c->cache_stride[i] < 0) return false;
+    if (c->q_stride[i] < 0 || c->kv_stride[i] < 0 || c->cache_stride[i] < 0 || (c->own_v_stride && c->v_stride[i] < 0)) return false;
   return true;
 }
 
@@ -56,7 +57,12 @@ int stand_tree_attention(const stand_attention* c, const void* dev_q, const void
   p.B = c->B; p.N = c->N; p.heads_q = c->heads_q; p.heads_kv = c->heads_kv; p.group = c->heads_q / c->heads_kv; p.dim = c->dim;
   p.page = c->page_size; p.pages = c->pages; p.cols = c->max_pages; p.mask_words = (c->N + 31) / 32;
   p.scale2 = (float)((double)c->scale * 1.4426950408889634);
-  for (int i = 0; i < 3; ++i) { p.q_stride[i] = c->q_stride[i]; p.kv_stride[i] = c->kv_stride[i]; p.cache_stride[i] = c->cache_stride[i]; }
+  for (int i = 0; i < 3; ++i) {
+    p.q_stride[i] = c->q_stride[i];
+    p.k_stride[i] = c->kv_stride[i];
+    p.v_stride[i] = c->own_v_stride ? c->v_stride[i] : c->kv_stride[i];
+    p.cache_stride[i] = c->cache_stride[i];
+  }
   cudaStream_t st = (cudaStream_t)cu_stream;
   int dev = -1, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return STAND_E_CUDA;

@@ -30,7 +30,7 @@ struct AttnParams {
   float* lse;
   int B, N, heads_q, heads_kv, group, dim, page, pages, cols, mask_words;
   float scale2;  // scale * log2(e)
-  long long q_stride[3], kv_stride[3], cache_stride[3];  // elements
+  long long q_stride[3], k_stride[3], v_stride[3], cache_stride[3];  // elements
 };
 
 template <typename T> __device__ __forceinline__ float to_float(T v);
@@ -96,9 +96,9 @@ __device__ __noinline__ float attn_settle(const AttnParams& p, int b, int g, int
       for (int i = 0; i < 8; ++i) add(f[i]);
     }
   }
-  const T* tree = reinterpret_cast<const T*>(p.v) + b * p.kv_stride[0] + g * p.kv_stride[2] + d;
+  const T* tree = reinterpret_cast<const T*>(p.v) + b * p.v_stride[0] + g * p.v_stride[2] + d;
   for (int v = n0; v < n1 && v <= u; ++v)
-    if (attn_sees(p, b, u, v)) add(to_float(tree[v * p.kv_stride[1]]));
+    if (attn_sees(p, b, u, v)) add(to_float(tree[v * p.v_stride[1]]));
   return !any ? o : (lost ? sum : o + sum);
 }
 

@@ -92,7 +92,8 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
         }
       } else {
         const int node = (tile - s.p_tiles) * KT + key;
-        if (node < p.a.N) src = kv[which] + s.b * p.a.kv_stride[0] + node * p.a.kv_stride[1] + s.g * p.a.kv_stride[2];
+        const long long* stride = which ? p.a.v_stride : p.a.k_stride;
+        if (node < p.a.N) src = kv[which] + s.b * stride[0] + node * stride[1] + s.g * stride[2];
       }
       s_src[tile % 3][which][key] = src;
     };
@@ -331,7 +332,7 @@ template <typename T, int DP> int launch_plain_rows(const AttnParams& a, void* s
   ta_split(p, a, PA_ROWS, DP, sms, plain_ctas(DP), 3, scratch);
   const size_t al = 4 * sizeof(T);
   uintptr_t bits = (uintptr_t)a.k | (uintptr_t)a.v | (a.cols > 0 ? (uintptr_t)a.cache_k | (uintptr_t)a.cache_v : 0);
-  for (int i = 0; i < 3; ++i) bits |= (uintptr_t)(a.kv_stride[i] * sizeof(T)) | (a.cols > 0 ? (uintptr_t)(a.cache_stride[i] * sizeof(T)) : 0);
+  for (int i = 0; i < 3; ++i) bits |= (uintptr_t)((a.k_stride[i] | a.v_stride[i]) * sizeof(T)) | (a.cols > 0 ? (uintptr_t)(a.cache_stride[i] * sizeof(T)) : 0);
   const bool wide = bits % al == 0 && a.dim % 4 == 0;
   static SmemLimit limit;
   const int smem = PaShape<DP>::SMEM;

@@ -744,11 +744,12 @@ template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams
   while (p.box_rows < TA_KT && a.page % (p.box_rows * 2) == 0) p.box_rows *= 2;
   p.wait_limit = wait_limit;
 
-  const long long tree_n[3] = {a.N, a.heads_kv, a.B}, tree_stride[3] = {a.kv_stride[1], a.kv_stride[2], a.kv_stride[0]};
+  const long long tree_n[3] = {a.N, a.heads_kv, a.B}, k_stride[3] = {a.k_stride[1], a.k_stride[2], a.k_stride[0]};
+  const long long v_stride[3] = {a.v_stride[1], a.v_stride[2], a.v_stride[0]};
   const long long q_n[3] = {a.heads_q, a.N, a.B}, q_stride[3] = {a.q_stride[2], a.q_stride[1], a.q_stride[0]};
   if (!encode_map(&p.q, a.q, BF16, a.dim, q_n, q_stride, a.group, p.s.tile_rows / a.group) ||
-      !encode_map(&p.tree_k, a.k, BF16, a.dim, tree_n, tree_stride, TA_KT, 1) ||
-      !encode_map(&p.tree_v, a.v, BF16, a.dim, tree_n, tree_stride, TA_KT, 1))
+      !encode_map(&p.tree_k, a.k, BF16, a.dim, tree_n, k_stride, TA_KT, 1) ||
+      !encode_map(&p.tree_v, a.v, BF16, a.dim, tree_n, v_stride, TA_KT, 1))
     return STAND_E_ARG;
   if (a.cols > 0) {
     const long long n[3] = {a.page, a.heads_kv, a.pages}, stride[3] = {a.cache_stride[2], a.cache_stride[1], a.cache_stride[0]};

@@ -28,6 +28,13 @@ def _need(cond, what):
         raise StandError(what)
 
 
+def _steps(x, what):
+    """The strides of all dimensions but the last, whose elements lie side by side.  A dimension of one element has none."""
+    shape, strides = x.shape, x.stride()
+    _need(shape[-1] == 1 or strides[-1] == 1, f"{what}: a contiguous last dimension")
+    return [s if n > 1 else 0 for n, s in zip(shape[:-1], strides)]
+
+
 class _Op:
     """Device, stream and workspace handling of the operators."""
 
@@ -114,8 +121,8 @@ class TreeAttention(_Op):
         return x.data_ptr()
 
     def __call__(self, q, k, v, cache_k, cache_v, table, length, tree_tokens=None, out=None, lse=None, stream=None):
-        """q [B, N, heads_q, dim], k / v [B, N, heads_kv, dim] (slices of one projection will do), caches
-        [pages, heads_kv, page_size, dim] (any strides), table [B, max_pages] int32, length [B] int64, tree_tokens
+        """q [B, N, heads_q, dim], k / v [B, N, heads_kv, dim] (any strides: slices of one projection will do, keys rotated
+        into a tensor of their own too), caches [pages, heads_kv, page_size, dim] (any strides, the same for both), table [B, max_pages] int32, length [B] int64, tree_tokens
         [B, N] int32 or None (nodes below 0 get empty rows).  Returns (out [B, N, heads_q, dim], lse [B, N, heads_q])."""
         t, c = self.torch, self.cfg
         pq, pk, pv = self._floats(q, self._q_shape, "q"), self._floats(k, self._kv_shape, "k"), self._floats(v, self._kv_shape, "v")
@@ -123,11 +130,10 @@ class TreeAttention(_Op):
         pcv = self._floats(cache_v, self._cache_shape, "cache_v")
         strides = q.stride(), k.stride(), v.stride(), cache_k.stride(), cache_v.stride()
         if strides != self._strides:
-            qs, ks, vs, cs, cvs = strides
-            if vs != ks or cvs != cs or qs[3] != 1 or ks[3] != 1 or cs[3] != 1:
-                raise StandError("TreeAttention: keys and values have the same strides, and a contiguous last dimension as q has")
-            c.q_stride[:], c.kv_stride[:], c.cache_stride[:] = qs[:3], ks[:3], cs[:3]
-            self._strides = strides
+            qs, ks, vs, cs = _steps(q, "q"), _steps(k, "k"), _steps(v, "v"), _steps(cache_k, "cache_k")
+            _need(_steps(cache_v, "cache_v") == cs, "TreeAttention: both caches have the same strides")
+            c.q_stride[:], c.kv_stride[:], c.v_stride[:], c.cache_stride[:] = qs, ks, vs, cs
+            c.own_v_stride, self._strides = 1, strides
         ptab = self._ints(table, t.int32, self._table_shape, "table")
         plen = self._ints(length, t.int64, self._len_shape, "length")
         ptree = self._opt(tree_tokens, t.int32, self._tree_shape, "tree_tokens")

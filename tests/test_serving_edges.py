@@ -214,3 +214,89 @@ def test_many_small_weights_beside_a_dominant_one(dtype, n, N, hq, hkv, dim, B, 
     assert np.median(np.abs(r_out)) > 1e-4
     assert (np.abs(out - r_out) <= tol).all(), np.max(np.abs(out - r_out) / tol)
     assert (np.abs(lse - r_lse) <= e + 2.0**-19 * (1 + np.abs(r_lse))).all()
+
+
+# ---------------------------------------------------------------- layouts of keys and values
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("how", ["rotated keys", "rotated keys, odd", "head-major values", "one value row for all heads"])
+def test_keys_and_values_of_different_layouts(dtype, how):
+    """Keys in a tensor of their own after a rotation, values still a slice of the projection, and the like."""
+    import torch
+    c = ts._attention_case(131, dtype, [0, 90, 300], 24, 4, 2, 64, 16, parent=inputs.topology(24, 6, 3), nan=False)
+    if how == "one value row for all heads":
+        c["qkv"][:, :, 5] = c["qkv"][:, :, 4]
+        c["qkv"][:, :, 6:] = c["qkv"][:, :, 6:7]
+    heads = 2 if how == "one value row for all heads" else 1  # value heads with an infinity: those are read again at the end
+    clean = dict(c, qkv=c["qkv"].clone())
+    clean["qkv"][1, 3, 6:6 + heads, 5] = 0.0
+    c["qkv"][1, 3, 6:6 + heads, 5] = INF
+
+    def move(q, k, v, ck, cv):
+        if how == "rotated keys":
+            return q, k.contiguous(), v, ck, cv
+        if how == "rotated keys, odd":
+            wide = torch.empty(k.shape[:-1] + (k.shape[-1] + 5,), dtype=k.dtype, device=k.device)[..., 2:-3]
+            return q, wide.copy_(k), v, ck, cv
+        if how == "head-major values":
+            return q, k, v.transpose(1, 2).contiguous().transpose(1, 2), ck, cv
+        return q, k, v[:, :, :1].contiguous().expand(-1, -1, 2, -1), ck, cv
+
+    out, lse = ts._run_attention(c, move=move)
+    want = ts._reference(clean)
+    hit = np.zeros_like(out, bool)
+    hit[1, ts.ref.ancestors(c["parent"])[:, 3], :2 * heads, 5] = True
+    assert (out[hit] == INF).all()
+    ts._check_attention(c, (np.where(hit, want[0], out), lse), want=want)
+
+
+@pytest.mark.gpu
+def test_strides_of_single_elements_do_not_matter():
+    """Dimensions of one element may have any stride: one sequence, one node, one key head, one page, a head size of one."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    for dim in (64, 1):
+        c = ts._attention_case(17 + dim, "bf16", [13], 1, 2, 1, dim, 16, parent=np.array([-1], np.int32), spare=0, nan=False)
+
+        def odd(x):
+            return torch.as_strided(x.contiguous(), x.shape, [s if n > 1 else 7 * s + 3 for n, s in zip(x.shape, x.contiguous().stride())])
+
+        def move(q, k, v, ck, cv):
+            return q, odd(k), v, odd(ck), cv
+        ts._check_attention(c, ts._run_attention(c, move=move))
+
+
+def test_strides_are_given_for_keys_and_values_apart():
+    import torch
+    bf = torch.bfloat16
+    p, args = _hostless_attention(B=2, N=3)
+    args[0], args[1] = _Tensor((2, 3, 2, 64), bf, stride=(2400, 800, 64, 1)), _Tensor((2, 3, 2, 64), bf, stride=(384, 128, 64, 1))
+    args[2] = _Tensor((2, 3, 2, 64), bf, stride=(2400, 800, 64, 1))
+    p(*args)
+    assert list(p.cfg.kv_stride) == [384, 128, 64] and list(p.cfg.v_stride) == [2400, 800, 64] and p.cfg.own_v_stride == 1
+    for i in (0, 1, 2, 3, 4):  # elements that do not lie side by side
+        bad = list(args)
+        bad[i] = _Tensor(args[i].shape, bf, stride=(9000, 3000, 1, 2))
+        with pytest.raises(binding.StandError):
+            p(*bad)
+    bad = list(args)
+    bad[4] = _Tensor(args[4].shape, bf, stride=(4096, 2048, 64, 1))
+    with pytest.raises(binding.StandError):
+        p(*bad)
+
+
+def test_value_strides_are_checked():
+    lib_build.build()
+    import ctypes as C
+    size = binding.lib().stand_tree_attention_scratch_bytes
+    good = ts._shape()
+    assert size(C.byref(good)) > 0
+    good.own_v_stride = 1
+    assert size(C.byref(good)) > 0
+    for field, value in (("own_v_stride", 2), ("own_v_stride", -1), ("reserved", 1)):
+        bad = ts._shape()
+        setattr(bad, field, value)
+        assert size(C.byref(bad)) == 0
+    bad = ts._shape()
+    bad.own_v_stride, bad.v_stride[2] = 1, -3
+    assert size(C.byref(bad)) == 0
