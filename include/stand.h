@@ -387,15 +387,18 @@ int stand_page_release(const int64_t* dev_len, const int32_t* dev_done, int32_t 
                        int32_t max_pages, const int32_t* dev_table, int32_t capacity, int32_t* dev_free,
                        const int32_t* dev_n_free, int64_t* dev_len_out, int32_t* dev_n_free_out, void* cu_stream);
 
-/* The shapes of stand_kv_commit.  Strides are in elements, dim is contiguous; keys and values have the same. */
+/* The shapes of stand_kv_commit.  Strides are in elements, dim is contiguous. */
 typedef struct {
   int32_t layers, B, N; /* N nodes per sequence in the source */
   int32_t heads, dim, dtype;
   int32_t page_size, pages;
   int32_t width;           /* columns of dev_slots and dev_path */
   int32_t reserved;        /* must be 0 */
-  int64_t src_stride[4];   /* layer, sequence, node, head */
-  int64_t cache_stride[4]; /* layer, page, head, token */
+  int64_t src_stride[4];   /* layer, sequence, node, head: the keys, and the values too unless own_v_stride is 1 */
+  int64_t cache_stride[4]; /* layer, page, head, token (both caches alike) */
+  int64_t v_stride[4];     /* layer, sequence, node, head: the values, if own_v_stride is 1 */
+  int32_t own_v_stride;    /* 0 or 1 */
+  int32_t reserved2;       /* must be 0 */
 } stand_kv_shape;
 
 /* Copies keys and values of chosen nodes into their slots, for all layers: row (l, b, dev_path[b, j], h) of dev_k and

@@ -59,6 +59,7 @@ class StandKvShape(C.Structure):
         ("layers", C.c_int32), ("B", C.c_int32), ("N", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32),
         ("dtype", C.c_int32), ("page_size", C.c_int32), ("pages", C.c_int32), ("width", C.c_int32),
         ("reserved", C.c_int32), ("src_stride", C.c_int64 * 4), ("cache_stride", C.c_int64 * 4),
+        ("v_stride", C.c_int64 * 4), ("own_v_stride", C.c_int32), ("reserved2", C.c_int32),
     ]
 
 

@@ -202,7 +202,7 @@ struct CommitParams {
   int layers, N, width, heads, page, units;  // units: 16-byte (or element) pieces of one row
   int layers_per_block;
   long long n_slots;
-  long long src[4], dst[4];  // strides in bytes
+  long long src_k[4], src_v[4], dst[4];  // strides in bytes
 };
 
 // A block copies one token's rows of some layers: a piece of W bytes per thread and step, four steps in flight (one layer
@@ -221,7 +221,8 @@ __global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(const CommitP
   const int l0 = blockIdx.y * p.layers_per_block;
   const int nl = p.layers - l0 < p.layers_per_block ? p.layers - l0 : p.layers_per_block;
   const long long page = slot / p.page;
-  const long long from = b * p.src[1] + node * p.src[2], to = page * p.dst[1] + (slot - page * p.page) * p.dst[3];
+  const long long from_k = b * p.src_k[1] + node * p.src_k[2], from_v = b * p.src_v[1] + node * p.src_v[2];
+  const long long to = page * p.dst[1] + (slot - page * p.page) * p.dst[3];
   const int per_layer = 2 * p.heads * p.units, total = nl * per_layer;
   for (int i0 = threadIdx.x; i0 < total; i0 += COMMIT_THREADS * COMMIT_UNROLL) {
     W got[COMMIT_UNROLL];
@@ -235,7 +236,8 @@ __global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(const CommitP
         const int row = in_layer / p.units, unit = in_layer - row * p.units;
         const bool is_v = row >= p.heads;
         const int h = is_v ? row - p.heads : row;
-        const char* src = (is_v ? p.v : p.k) + (l0 + l) * p.src[0] + from + h * p.src[3] + unit * (int)sizeof(W);
+        const char* src = is_v ? p.v + (l0 + l) * p.src_v[0] + from_v + h * p.src_v[3] : p.k + (l0 + l) * p.src_k[0] + from_k + h * p.src_k[3];
+        src += unit * (int)sizeof(W);
         dst[e] = (is_v ? p.cache_v : p.cache_k) + (l0 + l) * p.dst[0] + to + h * p.dst[2] + unit * (int)sizeof(W);
         got[e] = __ldg(reinterpret_cast<const W*>(src));
       }
@@ -296,15 +298,17 @@ int stand_kv_commit(const stand_kv_shape* c, const void* dev_k, const void* dev_
   if (c->layers < 1 || c->layers > 65535 || c->B < 1 || c->N < 1 || c->heads < 1 || c->dim < 1 || c->width < 1) return STAND_E_ARG;
   if (c->page_size < 1 || c->pages < 0 || c->reserved != 0 || c->dtype < STAND_DTYPE_F32 || c->dtype > STAND_DTYPE_F16) return STAND_E_ARG;
   if ((long long)c->heads * c->dim > (1 << 20) || (long long)c->B * c->width > 0x7FFFFFFFll) return STAND_E_ARG;
+  if ((c->own_v_stride != 0 && c->own_v_stride != 1) || c->reserved2 != 0) return STAND_E_ARG;
+  const int64_t* v_stride = c->own_v_stride ? c->v_stride : c->src_stride;
   for (int i = 0; i < 4; ++i)
-    if (c->src_stride[i] < 0 || c->cache_stride[i] < 0) return STAND_E_ARG;
+    if (c->src_stride[i] < 0 || c->cache_stride[i] < 0 || v_stride[i] < 0) return STAND_E_ARG;
   const int es = c->dtype == STAND_DTYPE_F32 ? 4 : 2;
   CommitParams p;
   p.k = (const char*)dev_k; p.v = (const char*)dev_v; p.cache_k = (char*)dev_cache_k; p.cache_v = (char*)dev_cache_v;
   p.path = dev_path; p.slots = (const long long*)dev_slots; p.layers = c->layers; p.N = c->N; p.width = c->width; p.heads = c->heads;
   p.page = c->page_size; p.n_slots = (long long)c->pages * c->page_size;
-  for (int i = 0; i < 4; ++i) { p.src[i] = c->src_stride[i] * es; p.dst[i] = c->cache_stride[i] * es; }
-  const bool wide = (c->dim * es) % 16 == 0 && aligned16(dev_k, p.src, 4) && aligned16(dev_v, p.src, 4) &&
+  for (int i = 0; i < 4; ++i) { p.src_k[i] = c->src_stride[i] * es; p.src_v[i] = v_stride[i] * es; p.dst[i] = c->cache_stride[i] * es; }
+  const bool wide = (c->dim * es) % 16 == 0 && aligned16(dev_k, p.src_k, 4) && aligned16(dev_v, p.src_v, 4) &&
                     aligned16(dev_cache_k, p.dst, 4) && aligned16(dev_cache_v, p.dst, 4);
   p.units = wide ? c->dim * es / 16 : c->dim;
   // enough layers per block for its threads to have COMMIT_UNROLL pieces each

@@ -215,18 +215,18 @@ class KvCommit(_Op):
         return x.data_ptr()
 
     def __call__(self, k, v, slots, cache_k, cache_v, path=None, stream=None):
-        """k / v [layers, B, N, heads, dim], slots [B, width] int64 (stand_page_map), path [B, width] int32
-        (stand_last_path; None: node j goes to slot j), caches [layers, pages, heads, page_size, dim]."""
+        """k / v [layers, B, N, heads, dim] (any strides), slots [B, width] int64 (stand_page_map), path [B, width] int32
+        (stand_last_path; None: node j goes to slot j), caches [layers, pages, heads, page_size, dim] (any
+        strides, the same for both)."""
         t, c = self.torch, self.cfg
         pk, pv = self._floats(k, self._src, "k"), self._floats(v, self._src, "v")
         pck, pcv = self._floats(cache_k, self._cache, "cache_k"), self._floats(cache_v, self._cache, "cache_v")
         strides = k.stride(), v.stride(), cache_k.stride(), cache_v.stride()
         if strides != self._strides:
-            ks, vs, cs, cvs = strides
-            if vs != ks or cvs != cs or ks[4] != 1 or cs[4] != 1:
-                raise StandError("KvCommit: keys and values have the same strides and a contiguous last dimension")
-            c.src_stride[:], c.cache_stride[:] = ks[:4], cs[:4]
-            self._strides = strides
+            ks, vs, cs = _steps(k, "k"), _steps(v, "v"), _steps(cache_k, "cache_k")
+            _need(_steps(cache_v, "cache_v") == cs, "KvCommit: both caches have the same strides")
+            c.src_stride[:], c.v_stride[:], c.cache_stride[:] = ks, vs, cs
+            c.own_v_stride, self._strides = 1, strides
         ps = self._ints(slots, t.int64, self._places, "slots")
         pp = self._opt(path, t.int32, self._places, "path")
         self._launch(stream, self._lib.stand_kv_commit, self._cfg_ptr, pk, pv, pp, ps, pck, pcv)

@@ -300,3 +300,39 @@ def test_value_strides_are_checked():
     bad = ts._shape()
     bad.own_v_stride, bad.v_stride[2] = 1, -3
     assert size(C.byref(bad)) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("how", ["slice of a projection", "head-major", "odd rows", "one row for all heads"])
+def test_commit_of_keys_and_values_of_different_layouts(dtype, how):
+    import torch
+    from paper_2506_04708_b200 import serving
+    L, B, N, H, D, page, pool, width = 3, 2, 9, 3, 24, 16, 5, 4
+    rng = np.random.default_rng(8)
+    dt = ts._dtype(dtype)
+    make = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(dt).to("cuda:0")  # noqa: E731
+    k, ck, cv = make(L, B, N, H, D), make(L, pool, H, page, D), make(L, pool, H, page, D)
+    v = {"slice of a projection": lambda: make(L, B, N, 3 * H, D)[:, :, :, 2 * H:], "head-major": lambda: make(L, B, H, N, D).transpose(2, 3),
+         "odd rows": lambda: make(L, B, N, H, D + 3)[..., 1:-2], "one row for all heads": lambda: make(L, B, N, 1, D).expand(-1, -1, -1, H, -1)}[how]()
+    slots = rng.permutation(pool * page)[: B * width].reshape(B, width).astype(np.int64)
+    path = np.sort(rng.integers(0, N, (B, width)), 1).astype(np.int32)
+    want = [ts.ref.kv_commit(s.float().cpu().numpy(), path, slots, c.float().cpu().numpy()) for s, c in ((k, ck), (v, cv))]
+    op = serving.KvCommit(L, B, N, H, D, dt, page, pool, width)
+    op(k, v, torch.from_numpy(slots).to("cuda:0"), ck, cv, path=torch.from_numpy(path).to("cuda:0"))
+    assert np.array_equal(ck.float().cpu().numpy(), want[0]) and np.array_equal(cv.float().cpu().numpy(), want[1])
+    for bad in ((k, v, ck, cv.transpose(2, 3).contiguous().transpose(2, 3)), (k.transpose(3, 4).contiguous().transpose(3, 4), v, ck, cv)):
+        with pytest.raises(binding.StandError):
+            op(bad[0], bad[1], torch.from_numpy(slots).to("cuda:0"), bad[2], bad[3])
+
+
+def test_commit_value_strides_are_checked():
+    lib_build.build()
+    import ctypes as C
+    at = C.c_void_p(0x100000)  # never touched: every call here is refused before a launch
+    for fields in (dict(own_v_stride=2), dict(own_v_stride=-1), dict(reserved2=1), dict(own_v_stride=1, v=(0, 0, -1, 0))):
+        s = binding.StandKvShape(1, 1, 4, 2, 64, 1, 16, 3, 2, 0)
+        s.v_stride[:] = fields.pop("v", (0, 0, 0, 0))
+        for name, value in fields.items():
+            setattr(s, name, value)
+        assert binding.lib().stand_kv_commit(C.byref(s), at, at, None, at, at, at, None) == -1
