@@ -372,8 +372,8 @@ int stand_tree_mask(const int32_t* host_parent, int32_t n, uint32_t* host_mask);
  * [0, width], its length is negative, it would need more than max_pages pages, or the pages needed by all sequences
  * up to and including it (those refused for the reasons before left out) are more than the list has while it needs
  * one itself.  dev_granted [B] int32: dev_new[b], or -1 where it was refused.
- * dev_len_out [B] int64, dev_n_free_out [1] int32: lengths and list size after the call.  They must not be the
- * input arrays (blocks read those while others write); dev_granted, dev_len_out may be NULL. */
+ * dev_len_out [B] int64, dev_n_free_out [1] int32: lengths and list size after the call.  Output arrays (dev_granted among
+ * them) must not overlap input arrays: blocks read those while others write; dev_granted, dev_len_out may be NULL. */
 int stand_page_map(const int64_t* dev_len, const int32_t* dev_new, int32_t B, int32_t width, int32_t page_size,
                    int32_t max_pages, const int32_t* dev_free, int32_t capacity, const int32_t* dev_n_free,
                    int32_t* dev_table, int64_t* dev_slots, int32_t* dev_granted, int64_t* dev_len_out, int32_t* dev_n_free_out,
@@ -382,7 +382,7 @@ int stand_page_map(const int64_t* dev_len, const int32_t* dev_new, int32_t B, in
 /* Gives the pages of finished sequences back: for every b with dev_done[b] != 0 the first ceil(len / page_size)
  * entries of its table row are pushed on the free list (dev_free has room for `capacity` page numbers), in the order
  * of the sequences, then of the text, and dev_len_out[b] is 0; other lengths are copied.  Pages that would not fit
- * the list are dropped (then the list was not this pool's).  Output arrays must not be input arrays. */
+ * the list are dropped (then the list was not this pool's).  Output arrays must not overlap input arrays. */
 int stand_page_release(const int64_t* dev_len, const int32_t* dev_done, int32_t B, int32_t page_size,
                        int32_t max_pages, const int32_t* dev_table, int32_t capacity, int32_t* dev_free,
                        const int32_t* dev_n_free, int64_t* dev_len_out, int32_t* dev_n_free_out, void* cu_stream);

@@ -248,6 +248,12 @@ __global__ void __launch_bounds__(COMMIT_THREADS) kv_commit_kernel(const CommitP
   }
 }
 
+// Blocks read these inputs while others write those outputs.
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && x < y + b_bytes && y < x + a_bytes;
+}
+
 bool aligned16(const void* p, const long long* strides, int n) {
   bool ok = ((uintptr_t)p & 15) == 0;
   for (int i = 0; i < n; ++i) ok = ok && (strides[i] & 15) == 0;
@@ -264,7 +270,10 @@ int stand_page_map(const int64_t* dev_len, const int32_t* dev_new, int32_t B, in
   if (B < 1 || width < 1 || width > (1 << 27) || page_size < 1 || page_size > (1 << 27) || max_pages < 0 || capacity < 0) return STAND_E_ARG;
   if (!dev_len || !dev_new || !dev_n_free || !dev_slots || !dev_n_free_out) return STAND_E_ARG;
   if ((max_pages > 0 && !dev_table) || (capacity > 0 && !dev_free)) return STAND_E_ARG;
-  if (dev_len_out == dev_len || dev_n_free_out == dev_n_free) return STAND_E_ARG;
+  const size_t longs = (size_t)B * 8, ints = (size_t)B * 4;
+  if (overlap(dev_len_out, longs, dev_len, longs) || overlap(dev_granted, ints, dev_new, ints) || overlap(dev_granted, ints, dev_n_free, 4) ||
+      overlap(dev_n_free_out, 4, dev_n_free, 4) || overlap(dev_n_free_out, 4, dev_new, ints))
+    return STAND_E_ARG;
   MapParams p;
   p.len = (const long long*)dev_len; p.n_new = dev_new; p.B = B; p.width = width; p.page = page_size; p.cols = max_pages;
   p.capacity = capacity; p.free_list = dev_free; p.n_free = dev_n_free; p.table = dev_table; p.slots = (long long*)dev_slots;
@@ -284,7 +293,9 @@ int stand_page_release(const int64_t* dev_len, const int32_t* dev_done, int32_t 
   if (B < 1 || page_size < 1 || max_pages < 0 || capacity < 0) return STAND_E_ARG;
   if (!dev_len || !dev_done || !dev_n_free || !dev_len_out || !dev_n_free_out) return STAND_E_ARG;
   if ((max_pages > 0 && !dev_table) || (capacity > 0 && !dev_free)) return STAND_E_ARG;
-  if (dev_len_out == dev_len || dev_n_free_out == dev_n_free) return STAND_E_ARG;
+  const size_t longs = (size_t)B * 8;
+  if (overlap(dev_len_out, longs, dev_len, longs) || overlap(dev_n_free_out, 4, dev_n_free, 4) || overlap(dev_n_free_out, 4, dev_done, (size_t)B * 4))
+    return STAND_E_ARG;
   ReleaseParams p;
   p.len = (const long long*)dev_len; p.done = dev_done; p.B = B; p.page = page_size; p.cols = max_pages; p.capacity = capacity;
   p.table = dev_table; p.free_list = dev_free; p.n_free = dev_n_free; p.len_out = (long long*)dev_len_out;

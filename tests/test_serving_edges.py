@@ -336,3 +336,48 @@ def test_commit_value_strides_are_checked():
         for name, value in fields.items():
             setattr(s, name, value)
         assert binding.lib().stand_kv_commit(C.byref(s), at, at, None, at, at, at, None) == -1
+
+
+# ---------------------------------------------------------------- page maps: arrays that overlap
+def test_page_maps_refuse_outputs_that_overlap_inputs():
+    """Each array at a place of its own, then one output laid over an input, whole or in part: refused before a launch."""
+    import ctypes as C
+    lib_build.build()
+    L = binding.lib()
+    at = {n: 0x100000 * (i + 1) for i, n in enumerate(("length", "new", "free", "n_free", "table", "slots", "granted", "len_out", "n_out", "done"))}
+    B = 5
+
+    def page_map(**kw):
+        p = {k: C.c_void_p(v) for k, v in dict(at, **kw).items()}
+        return L.stand_page_map(p["length"], p["new"], B, 3, 16, 4, p["free"], 9, p["n_free"], p["table"], p["slots"], p["granted"], p["len_out"],
+                                p["n_out"], None)
+
+    def release(**kw):
+        p = {k: C.c_void_p(v) for k, v in dict(at, **kw).items()}
+        return L.stand_page_release(p["length"], p["done"], B, 16, 4, p["table"], 9, p["free"], p["n_free"], p["len_out"], p["n_out"], None)
+
+    for bad in (dict(granted=at["new"]), dict(granted=at["new"] + 4), dict(granted=at["new"] - 16), dict(granted=at["n_free"]),
+                dict(granted=at["n_free"] - 16), dict(len_out=at["length"]), dict(len_out=at["length"] + 32), dict(n_out=at["n_free"]),
+                dict(n_out=at["new"] + 16)):
+        assert page_map(**bad) == -1, bad
+    for bad in (dict(len_out=at["length"]), dict(len_out=at["length"] - 32), dict(n_out=at["n_free"]), dict(n_out=at["done"] + 16)):
+        assert release(**bad) == -1, bad
+
+
+@pytest.mark.gpu
+def test_granted_counts_are_no_request():
+    """What a map granted may not be the next call's request in place; a copy of it may.  Neighbours in memory are no overlap."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    dev = "cuda:0"
+    plan = serving.PageMap(4, 3, 16, 4, 8)
+    i32, i64 = dict(dtype=torch.int32, device=dev), dict(dtype=torch.int64, device=dev)
+    table, free, n_free = torch.full((4, 4), -1, **i32), torch.arange(8, **i32), torch.full((1,), 8, **i32)
+    _, granted, length, n_free = plan(torch.zeros(4, **i64), torch.full((4,), 2, **i32), table, free, n_free)
+    with pytest.raises(binding.StandError):
+        plan(length, granted, table, free, n_free)
+    _, again, length, n_free = plan(length, granted.clone(), table, free, n_free)
+    assert again.tolist() == [2] * 4 and length.tolist() == [4] * 4 and int(n_free) == 4
+    both = torch.full((8,), 2, **i32)
+    plan.granted = both[4:]
+    assert plan(length, both[:4], table, free, n_free)[1].tolist() == [2] * 4
