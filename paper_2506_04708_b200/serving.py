@@ -162,11 +162,12 @@ class PageMap(_Op):
         _need(B >= 1 and width >= 1 and page_size >= 1 and max_pages >= 0 and capacity >= 0, "PageMap: invalid shapes")
         self.B, self.width, self.page_size, self.max_pages, self.capacity = B, width, page_size, max_pages, capacity
         self._b, self._table, self._list, self._one = (B,), (B, max_pages), (capacity,), (1,)
-        self.slots = t.full((B, width), -1, dtype=t.int64, device=self.dev)
-        self.granted = t.zeros(B, dtype=t.int32, device=self.dev)
+        # every call writes all of these; nothing is queued for them here, which could run after a call on another stream
+        self.slots = t.empty((B, width), dtype=t.int64, device=self.dev)
+        self.granted = t.empty(B, dtype=t.int32, device=self.dev)
         # two sets: what a call returned may be the next call's input
-        self._len = [t.zeros(B, dtype=t.int64, device=self.dev) for _ in range(2)]
-        self._n_free = [t.zeros(1, dtype=t.int32, device=self.dev) for _ in range(2)]
+        self._len = [t.empty(B, dtype=t.int64, device=self.dev) for _ in range(2)]
+        self._n_free = [t.empty(1, dtype=t.int32, device=self.dev) for _ in range(2)]
 
     def _outs(self, length, n_free):
         return (self._len[1] if length is self._len[0] else self._len[0],

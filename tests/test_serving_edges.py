@@ -381,3 +381,52 @@ def test_granted_counts_are_no_request():
     both = torch.full((8,), 2, **i32)
     plan.granted = both[4:]
     assert plan(length, both[:4], table, free, n_free)[1].tolist() == [2] * 4
+
+
+# ---------------------------------------------------------------- streams
+@pytest.mark.gpu
+def test_objects_made_on_a_busy_stream_and_used_on_another():
+    """Nothing that making an object queues on the current stream may run after, and over, a call on another stream."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    dev = "cuda:0"
+    i32, i64 = dict(dtype=torch.int32, device=dev), dict(dtype=torch.int64, device=dev)
+    table, free, n_free = torch.full((3, 4), 5, **i32), torch.arange(20, 32, **i32), torch.full((1,), 12, **i32)
+    length, new = torch.tensor([0, 15, 16], **i64), torch.tensor([2, 3, 0], **i32)
+    done = torch.tensor([0, 1, 0], **i32)
+    c = ts._attention_case(3, "bf16", [40, 0, 100], 8, 4, 2, 64, 16, nan=False)
+    qkv, ck, cv = c["qkv"].to(dev), c["ck"].to(dev), c["cv"].to(dev)
+    pages, lens = torch.from_numpy(c["table"]).to(dev), torch.from_numpy(c["len"]).to(dev)
+    x = torch.randn((2, 4, 1000), device=dev)
+    presence = torch.ones(2, device=dev)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def make():
+        return (serving.PageMap(3, 3, 16, 4, 12), serving.PageMap(3, 3, 16, 4, 12),
+                serving.TreeAttention(3, 8, 4, 2, 64, torch.bfloat16, 16, ck.shape[0], pages.shape[1]),
+                serving.LogitsProcessor(2, 4, 1000, torch.float32, parent=[-1, 0, 0, 1]))
+
+    y = torch.empty_like(x)
+
+    def call(plan, back, attend, op, table, free):
+        slots, granted, ln, nf = plan(length, new, table, free, n_free, stream=side)
+        ln2, nf2 = back.release(ln, done, table, free, nf, stream=side)
+        out, lse = attend(qkv[:, :, :4], qkv[:, :, 4:6], qkv[:, :, 6:], ck, cv, pages, lens, stream=side)
+        op(x, presence=presence, out=y, stream=side)
+        return slots, granted, ln, nf, ln2, nf2, out, lse
+
+    other = table.clone(), free.clone()
+    torch.cuda.synchronize()
+    call(*make(), *other)  # memory is at hand and kernels are loaded then
+    torch.cuda.synchronize()
+    torch.cuda._sleep(int(4e8))  # some 0.2 s
+    slots, granted, ln, nf, ln2, nf2, out, lse = call(*make(), table, free)
+    side.synchronize()
+    assert not torch.cuda.current_stream().query()  # still busy
+    torch.cuda.synchronize()
+    assert slots.tolist() == [[31 * 16, 31 * 16 + 1, -1], [5 * 16 + 15, 30 * 16, 30 * 16 + 1], [-1] * 3]
+    assert granted.tolist() == [2, 3, 0] and ln.tolist() == [2, 18, 16] and int(nf) == 10
+    assert ln2.tolist() == [2, 0, 16] and int(nf2) == 12
+    ts._check_attention(c, (out.double().cpu().numpy(), lse.double().cpu().numpy()))
+    assert torch.equal(y, x)
