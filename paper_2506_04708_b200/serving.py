@@ -170,8 +170,7 @@ class PageMap(_Op):
         self._n_free = [t.empty(1, dtype=t.int32, device=self.dev) for _ in range(2)]
 
     def _outs(self, length, n_free):
-        return (self._len[1] if length is self._len[0] else self._len[0],
-                self._n_free[1] if n_free is self._n_free[0] else self._n_free[0])
+        return [own[own[0].data_ptr() == given.data_ptr()] for own, given in ((self._len, length), (self._n_free, n_free))]
 
     def __call__(self, length, new, table, free, n_free, stream=None):
         """length [B] int64, new [B] int32, table [B, max_pages] int32 (gets the new pages), free [capacity] int32,

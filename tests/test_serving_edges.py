@@ -430,3 +430,32 @@ def test_objects_made_on_a_busy_stream_and_used_on_another():
     assert ln2.tolist() == [2, 0, 16] and int(nf2) == 12
     ts._check_attention(c, (out.double().cpu().numpy(), lse.double().cpu().numpy()))
     assert torch.equal(y, x)
+
+
+@pytest.mark.gpu
+def test_a_view_of_a_returned_length_is_the_next_input():
+    """What a call returned may come back as it is or as a view of it, and as a copy."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    i32, i64 = dict(dtype=torch.int32, device="cuda:0"), dict(dtype=torch.int64, device="cuda:0")
+    plan = serving.PageMap(3, 2, 16, 4, 12)
+    table, free, n_free = torch.full((3, 4), -1, **i32), torch.arange(12, **i32), torch.full((1,), 12, **i32)
+    length, new = torch.zeros(3, **i64), torch.full((3,), 2, **i32)
+    for i, again in enumerate((lambda t: t, lambda t: t[:], lambda t: t.view(-1), lambda t: t.detach(), lambda t: t.clone(), lambda t: t[:])):
+        _, _, length, n_free = plan(again(length), new, table, free, again(n_free))
+        assert length.tolist() == [2 * i + 2] * 3 and n_free.tolist() == [9]
+    length, n_free = plan.release(length[:], torch.tensor([0, 1, 0], **i32), table, free, n_free[:])
+    assert length.tolist() == [12, 0, 12] and n_free.tolist() == [10]
+
+
+def test_results_of_a_page_map_take_turns():
+    import torch
+    from paper_2506_04708_b200 import serving
+    p = object.__new__(serving.PageMap)
+    p._len, p._n_free = [torch.zeros(3), torch.zeros(3)], [torch.zeros(1), torch.zeros(1)]
+    for k in (0, 1):
+        for same in (lambda t: t, lambda t: t[:], lambda t: t.view(-1)):
+            length, n_free = p._outs(same(p._len[k]), same(p._n_free[1 - k]))
+            assert length is p._len[1 - k] and n_free is p._n_free[k]
+    length, n_free = p._outs(torch.zeros(3), torch.zeros(1))
+    assert length is p._len[0] and n_free is p._n_free[0]
