@@ -313,7 +313,8 @@ int stand_set_wait_limit(int64_t polls);
  *
  * The cache is a pool of `pages` pages of page_size tokens; block table row b lists the pages of sequence b in
  * text order (entries past its length may be anything).  Slot s of the pool is token s % page_size of page
- * s / page_size.  Problems found on the device never fault: see each entry. */
+ * s / page_size.  Problems found on the device never fault: see each entry.  Arrays are aligned to their elements
+ * (STAND_E_ARG otherwise). */
 
 /* The shapes of stand_tree_attention.  Strides are in elements; the innermost dimension (dim) is contiguous.
  * Queries, keys and values of the nodes may be slices of one projection's output. */

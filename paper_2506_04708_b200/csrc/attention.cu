@@ -48,6 +48,9 @@ int stand_tree_attention(const stand_attention* c, const void* dev_q, const void
                          float* dev_lse, void* cu_stream) {
   if (!attention_valid(c) || !dev_q || !dev_k || !dev_v || !dev_len || !dev_out) return STAND_E_ARG;
   if (c->max_pages > 0 && (!dev_table || !dev_cache_k || !dev_cache_v)) return STAND_E_ARG;
+  if (!aligned(c->dtype == STAND_DTYPE_F32 ? 4 : 2, dev_q, dev_k, dev_v, dev_cache_k, dev_cache_v, dev_out) || !aligned(8, dev_len) ||
+      !aligned(4, dev_table, dev_mask, dev_tree_tokens, dev_lse))
+    return STAND_E_ARG;
   if (dev_mask && (c->N > STAND_MAX_NODES || mask_stride < 0)) return STAND_E_ARG;
   if (!dev_scratch || ((uintptr_t)dev_scratch & 255) != 0 || scratch_bytes < stand_tree_attention_scratch_bytes(c)) return STAND_E_WORKSPACE;
   AttnParams p;

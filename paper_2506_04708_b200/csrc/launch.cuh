@@ -3,12 +3,16 @@
 #include "../../include/stand.h"
 
 #include <cuda_runtime.h>
+#include <stdint.h>
 #include <atomic>
 
 namespace stand {
 
 inline int cuda_ok(cudaError_t e) { return e == cudaSuccess ? STAND_OK : STAND_E_CUDA; }
 inline int launch_ok() { return cuda_ok(cudaGetLastError()); }
+
+// Are all of these (null among them) multiples of `bytes`?  An element that lies across that boundary would fault.
+template <typename... P> bool aligned(size_t bytes, const P*... p) { return ((... | (uintptr_t)p) & (bytes - 1)) == 0; }
 
 unsigned wait_limit();  // polls of a bounded wait (stand_set_wait_limit)
 

@@ -306,7 +306,9 @@ extern "C" int stand_process_logits(const stand_logits* c, const stand_logits_in
   if (x->bias_start && c->biases > 0 && (!x->bias_id || !x->bias_value)) return STAND_E_ARG;
   if ((x->mask != nullptr) != (x->mask_row != nullptr)) return STAND_E_ARG;
   const int es = c->dtype == STAND_DTYPE_F32 ? 4 : 2;
-  if (((uintptr_t)dev_in | (uintptr_t)dev_out) % es != 0) return STAND_E_ARG;
+  if (!aligned(es, dev_in, dev_out) || !aligned(8, x->n_text, x->n_prompt) ||
+      !aligned(4, x->text, x->tree_tokens, x->repetition, x->frequency, x->presence, x->bias_start, x->bias_id, x->bias_value, x->mask, x->mask_row))
+    return STAND_E_ARG;
   LogitsParams p;
   int depth[STAND_MAX_NODES];
   depth[0] = 0;

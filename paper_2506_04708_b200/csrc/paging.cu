@@ -270,6 +270,7 @@ int stand_page_map(const int64_t* dev_len, const int32_t* dev_new, int32_t B, in
   if (B < 1 || width < 1 || width > (1 << 27) || page_size < 1 || page_size > (1 << 27) || max_pages < 0 || capacity < 0) return STAND_E_ARG;
   if (!dev_len || !dev_new || !dev_n_free || !dev_slots || !dev_n_free_out) return STAND_E_ARG;
   if ((max_pages > 0 && !dev_table) || (capacity > 0 && !dev_free)) return STAND_E_ARG;
+  if (!aligned(8, dev_len, dev_slots, dev_len_out) || !aligned(4, dev_new, dev_free, dev_n_free, dev_table, dev_granted, dev_n_free_out)) return STAND_E_ARG;
   const size_t longs = (size_t)B * 8, ints = (size_t)B * 4;
   if (overlap(dev_len_out, longs, dev_len, longs) || overlap(dev_granted, ints, dev_new, ints) || overlap(dev_granted, ints, dev_n_free, 4) ||
       overlap(dev_n_free_out, 4, dev_n_free, 4) || overlap(dev_n_free_out, 4, dev_new, ints))
@@ -293,6 +294,7 @@ int stand_page_release(const int64_t* dev_len, const int32_t* dev_done, int32_t 
   if (B < 1 || page_size < 1 || max_pages < 0 || capacity < 0) return STAND_E_ARG;
   if (!dev_len || !dev_done || !dev_n_free || !dev_len_out || !dev_n_free_out) return STAND_E_ARG;
   if ((max_pages > 0 && !dev_table) || (capacity > 0 && !dev_free)) return STAND_E_ARG;
+  if (!aligned(8, dev_len, dev_len_out) || !aligned(4, dev_done, dev_table, dev_free, dev_n_free, dev_n_free_out)) return STAND_E_ARG;
   const size_t longs = (size_t)B * 8;
   if (overlap(dev_len_out, longs, dev_len, longs) || overlap(dev_n_free_out, 4, dev_n_free, 4) || overlap(dev_n_free_out, 4, dev_done, (size_t)B * 4))
     return STAND_E_ARG;
@@ -314,6 +316,7 @@ int stand_kv_commit(const stand_kv_shape* c, const void* dev_k, const void* dev_
   for (int i = 0; i < 4; ++i)
     if (c->src_stride[i] < 0 || c->cache_stride[i] < 0 || v_stride[i] < 0) return STAND_E_ARG;
   const int es = c->dtype == STAND_DTYPE_F32 ? 4 : 2;
+  if (!aligned(es, dev_k, dev_v, dev_cache_k, dev_cache_v) || !aligned(8, dev_slots) || !aligned(4, dev_path)) return STAND_E_ARG;
   CommitParams p;
   p.k = (const char*)dev_k; p.v = (const char*)dev_v; p.cache_k = (char*)dev_cache_k; p.cache_v = (char*)dev_cache_v;
   p.path = dev_path; p.slots = (const long long*)dev_slots; p.layers = c->layers; p.N = c->N; p.width = c->width; p.heads = c->heads;

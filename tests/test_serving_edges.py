@@ -459,3 +459,37 @@ def test_results_of_a_page_map_take_turns():
             assert length is p._len[1 - k] and n_free is p._n_free[k]
     length, n_free = p._outs(torch.zeros(3), torch.zeros(1))
     assert length is p._len[0] and n_free is p._n_free[0]
+
+
+# ---------------------------------------------------------------- alignment
+def test_arrays_off_their_elements_are_refused():
+    """Each array in turn a byte, and half an element, off its element's boundary: refused before a launch."""
+    import ctypes as C
+    lib_build.build()
+    L = binding.lib()
+
+    def places(sizes):  # (name, bytes of an element) -> a call's pointers with one of them off
+        for name, size in sizes.items():
+            for off in {1, size // 2}:
+                yield name, {n: C.c_void_p(0x100000 * (i + 1) + (off if n == name else 0)) for i, n in enumerate(sizes)}
+
+    for dtype, es in ((binding.DTYPE_BF16, 2), (binding.DTYPE_F32, 4)):
+        shape = ts._shape(dtype=dtype)
+        sizes = dict(q=es, k=es, v=es, ck=es, cv=es, table=4, length=8, mask=4, tree=4, out=es, lse=4)
+        for name, p in places(sizes):
+            assert L.stand_tree_attention(C.byref(shape), p["q"], p["k"], p["v"], p["ck"], p["cv"], p["table"], p["length"], p["mask"], 0, p["tree"],
+                                          C.c_void_p(0x2000000), 1 << 40, p["out"], p["lse"], None) == -1, name
+        kv = binding.StandKvShape(1, 1, 4, 2, 64, dtype, 16, 3, 2, 0)
+        for name, p in places(dict(k=es, v=es, path=4, slots=8, ck=es, cv=es)):
+            assert L.stand_kv_commit(C.byref(kv), p["k"], p["v"], p["path"], p["slots"], p["ck"], p["cv"], None) == -1, name
+        s = binding.StandLogits(2, 1, 100, dtype, None, 100, 100, 5, 1, 1, 0)
+        names = [n for n, _ in binding.StandLogitsInputs._fields_]
+        sizes = dict({n: 8 if n in ("n_text", "n_prompt") else 4 for n in names}, x_in=es, x_out=es)
+        for name, p in places(sizes):
+            x = binding.StandLogitsInputs(*[p[n] for n in names])
+            assert L.stand_process_logits(C.byref(s), C.byref(x), p["x_in"], p["x_out"], None) == -1, name
+    for name, p in places(dict(length=8, new=4, free=4, n_free=4, table=4, slots=8, granted=4, len_out=8, n_out=4)):
+        assert L.stand_page_map(p["length"], p["new"], 2, 3, 16, 4, p["free"], 9, p["n_free"], p["table"], p["slots"], p["granted"], p["len_out"],
+                                p["n_out"], None) == -1, name
+    for name, p in places(dict(length=8, done=4, free=4, n_free=4, table=4, len_out=8, n_out=4)):
+        assert L.stand_page_release(p["length"], p["done"], 2, 16, 4, p["table"], 9, p["free"], p["n_free"], p["len_out"], p["n_out"], None) == -1, name
