@@ -233,7 +233,6 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t q_smem = smem_addr(ta_smem), ring = q_smem + Sh::Q;
-  pdl_trigger();
   if (warp == 5) {
     tc_alloc(smem_addr(&sh.tmem), Sh::COLS);
   } else if (tid == 0) {
@@ -257,7 +256,12 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
   pdl_wait();
 
   TaWalk walk;
-  ta_begin<TA_THREADS>(p.s, walk, sh.range, [] { tc_fence_before(); }, [] { tc_fence_after(); });
+  // Dependents are released here, when the CTA has its tensor memory (behind ta_begin's barriers): a later launch of such a
+  // kernel may hold tensor memory while it waits for this one, so it must not come to the allocation first.
+  ta_begin<TA_THREADS>(p.s, walk, sh.range, [] { tc_fence_before(); }, [] {
+    tc_fence_after();
+    pdl_trigger();
+  });
   const uint32_t tmem = sh.tmem;
   volatile int* abort_flag = &sh.abort;
   const unsigned limit = p.wait_limit;

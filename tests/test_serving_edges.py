@@ -493,3 +493,35 @@ def test_arrays_off_their_elements_are_refused():
                                 p["n_out"], None) == -1, name
     for name, p in places(dict(length=8, done=4, free=4, n_free=4, table=4, len_out=8, n_out=4)):
         assert L.stand_page_release(p["length"], p["done"], 2, 16, 4, p["table"], 9, p["free"], p["n_free"], p["len_out"], p["n_out"], None) == -1, name
+
+
+# ---------------------------------------------------------------- launches in a row
+@pytest.mark.gpu
+def test_launches_of_all_head_sizes_in_a_row_and_on_two_streams():
+    """Launches that follow one another closely, with different shares of an SM's tensor memory, some on another stream at the same
+    time: the same bits as each by itself."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    dev, work = "cuda:0", []
+    for i, (dim, N, hq, hkv) in enumerate(((64, 8, 4, 2), (128, 24, 8, 2), (256, 9, 4, 2), (64, 40, 4, 2), (200, 3, 2, 1), (128, 1, 8, 8))):
+        c = ts._attention_case(i, "bf16", [700, 0, 129, 3000], N, hq, hkv, dim, 16, parent=inputs.topology(N, min(4, N - 1), 3), nan=False)
+        qkv = c["qkv"].to(dev)
+        args = (qkv[:, :, :hq], qkv[:, :, hq:hq + hkv], qkv[:, :, hq + hkv:], c["ck"].to(dev), c["cv"].to(dev), torch.from_numpy(c["table"]).to(dev),
+                torch.from_numpy(c["len"]).to(dev))
+        make = lambda: serving.TreeAttention(4, N, hq, hkv, dim, torch.bfloat16, 16, args[3].shape[0], args[5].shape[1], parent=c["parent"])  # noqa: E731
+        plans = make(), make()
+        alone = [t.clone() for t in plans[0](*args)]
+        torch.cuda.synchronize()
+        ts._check_attention(c, tuple(t.double().cpu().numpy() for t in alone))
+        work.append((args, plans, alone))
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(20):
+        for args, plans, _ in work:
+            for plan, stream in zip(plans, streams):
+                plan(*args, stream=stream)
+        torch.cuda.synchronize()
+        for _, plans, alone in work:
+            for plan in plans:
+                assert torch.equal(plan.out, alone[0]) and torch.equal(plan.lse, alone[1])
+                plan.out.fill_(7)
+        torch.cuda.synchronize()
