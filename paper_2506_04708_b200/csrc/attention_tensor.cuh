@@ -464,8 +464,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           top = fmaxf(top, top1) * scale2;
           // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores pass
           // it by TA_SLACK, so that o is seldom read, scaled and written (weights up to 2^8 lose nothing in either 16-bit
-          // type, sums are fp32).
-          if (__any_sync(FULL, top > m + TA_SLACK)) {
+          // type, sums are fp32).  The warp's rows move together, as rows that exist want it: what lies in the lanes of others is
+          // left from earlier kernels, and would make the weights' roundings differ from launch to launch.
+          if (__any_sync(FULL, in && top > m + TA_SLACK)) {
             const float raised = fmaxf(m, top);
             const float keep = raised == -INFINITY ? 1.0f : ta_ex2(m - raised);
             m = raised;

@@ -525,3 +525,31 @@ def test_launches_of_all_head_sizes_in_a_row_and_on_two_streams():
                 assert torch.equal(plan.out, alone[0]) and torch.equal(plan.lse, alone[1])
                 plan.out.fill_(7)
         torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("N,hq,hkv,dim", [(1, 4, 1, 128), (5, 4, 2, 64), (9, 6, 2, 64), (64, 7, 1, 128), (3, 2, 1, 256), (50, 1, 1, 64), (7, 3, 1, 96)])
+def test_results_do_not_depend_on_what_shared_memory_held(dtype, N, hq, hkv, dim):
+    """Rows that do not fill their tiles, after launches whose queries and keys leave large scores, infinities and NaN behind."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    c = ts._attention_case(dim * N, dtype, [700, 40, 2000], N, hq, hkv, dim, 16, parent=inputs.topology(N, min(4, N - 1), 3), nan=False)
+    c["qkv"][:, :, :hq] *= 3  # the maximum rises along the text
+    dev = "cuda:0"
+    qkv, ck, cv = c["qkv"].to(dev), c["ck"].to(dev), c["cv"].to(dev)
+    table, length = torch.from_numpy(c["table"]).to(dev), torch.from_numpy(c["len"]).to(dev)
+    plan = serving.TreeAttention(3, N, hq, hkv, dim, ts._dtype(dtype), 16, ck.shape[0], table.shape[1], parent=c["parent"])
+    # as many rows as a tile has, the same pages and lengths: all CTAs leave theirs behind
+    full = 128 // (hq // hkv)
+    spoil = serving.TreeAttention(3, full, hq, hkv, dim, ts._dtype(dtype), 16, ck.shape[0], table.shape[1])
+    first = None
+    for fill in (0.0, 1.0, -30.0, 1000.0, INF, NAN):
+        q = torch.full((3, full, hq, dim), fill, dtype=ts._dtype(dtype), device=dev)
+        kv = torch.full((3, full, hkv, dim), fill, dtype=ts._dtype(dtype), device=dev)
+        spoil(q, kv, kv, ck, cv, table, length)
+        out, lse = plan(qkv[:, :, :hq], qkv[:, :, hq:hq + hkv], qkv[:, :, hq + hkv:], ck, cv, table, length)
+        if first is None:
+            first = out.clone(), lse.clone()
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), fill
+    ts._check_attention(c, tuple(t.double().cpu().numpy() for t in first))
