@@ -50,7 +50,7 @@ constexpr int TA_XCOLS = 16;              // columns of O that the parts exchang
 template <int DP, int C> struct TaShape {
   static constexpr int CTAS = DP == 256 ? 1 : 2;              // per SM
   static constexpr int SLOT = TA_KT * DP * 2;                 // bytes of a tile of keys or values
-  static constexpr int K_SLOTS = DP == 64 ? (C > 1 ? 5 : 6) : 2, V_SLOTS = DP == 64 ? K_SLOTS : (C > 1 ? 2 : 3);
+  static constexpr int K_SLOTS = DP == 64 ? (C > 1 ? 5 : 6) : 2, V_SLOTS = DP == 64 ? K_SLOTS : 3;
   static constexpr int SLOTS = K_SLOTS + V_SLOTS;
   static constexpr int Q = TA_ROWS * DP * 2;
   static constexpr int COL_O = 0, COL_S = DP;                 // two places for S
@@ -58,6 +58,7 @@ template <int DP, int C> struct TaShape {
   static constexpr int X = C > 1 ? TA_ROWS * (TA_XCOLS + 1) * 4 : 0;  // exchange between the parts
   static constexpr int SHARED = C > 1 ? 1536 : 512;           // barriers and the like
   static constexpr int SMEM = Q + SLOTS * SLOT + X + SHARED;
+  static_assert(C == 1 || DP == 64, "parts of the lanes: small heads only");
   static_assert(COL_S + 2 * TA_KT <= COLS, "tensor memory");
   static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory");
 };

@@ -92,8 +92,9 @@ struct Penalty {
   float r, r_inv, f, p;
 };
 
-// The penalties' own arithmetic, each operation rounded by itself (no contraction).  x / r is x times 1 / r, an ulp of
-// single precision off at most; a division for each would cost as much as all the rest.
+// The penalties' own arithmetic, each operation rounded by itself (no contraction).  x / r is x times 1 / r, rounded
+// twice instead of once: an ulp of single precision off at most.  (With a division for each: 256 x 24 rows of 151,936 622 us
+// instead of 603, 64 rows of 50,257 17.5 instead of 16.8.)
 __device__ __forceinline__ float process(float x, bool met, uint32_t count, const Penalty& q, bool has_bias, float bias) {
   if (met) x = __fmul_rn(x, x > 0.0f ? q.r_inv : q.r);
   if (count) x = __fsub_rn(__fsub_rn(x, __fmul_rn(q.f, (float)count)), q.p);
