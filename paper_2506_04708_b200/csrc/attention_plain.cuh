@@ -5,10 +5,12 @@
 // values in shared memory (single precision: cp.async; 16-bit types are converted on the way).  A warp has four rows; for the
 // scores a lane has two keys, for the sums its share of the head size.  So every value from shared memory is used for four
 // rows, and no sum crosses a warp.
-// Measured, single precision, 8 x 16 nodes of 16 / 4 heads of 64, texts of 50 - 1,500: 39 us; one node each over texts of
-// 100 - 4,000: 45 us (8 rows a block there: the same; 64 rows a block need 230 registers, one block per SM: 65 instead of 42).
-// What bounds it: shared memory within a tile (3,200 cycles of passes with two blocks per SM), and with few tiles per
-// block the latency of beginning a piece.
+// Measured, single precision, 8 x 16 nodes of 16 / 4 heads of 64, texts of 50 - 1,500: 39 us; 32 x 16 nodes, texts of 500 - 4,000:
+// 259 us (8 rows a block: the same; 64 rows a block need 230 registers, one block per SM: 65 us where this took 42).
+// Where the time goes (8 x 16 nodes, texts of one length): blocks of one piece of two tiles 22 us with launch and joining, of two
+// pieces of one tile 27.5, each further tile 7.2 us with two blocks per SM.  So two tiles of an SM take 13,700 cycles; shared
+// memory is busy for 6,150 of them, the multiply-add pipe for 4,100.  Neither bounds it: sixteen warps that meet at two
+// barriers a tile do not hide the latencies of copy, products, softmax and sums, which follow one another.
 #pragma once
 #include "async.cuh"
 #include "attention_split.cuh"
@@ -329,7 +331,9 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
 
 template <typename T, int DP> int launch_plain_rows(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
   TaSplit p;
-  ta_split(p, a, PA_ROWS, DP, sms, plain_ctas(DP), 3, scratch);
+  // A piece's fixed cost in tiles: with 0, 1, 3, 6 16 x 8 nodes of heads of 128 over 10 - 1,000 take 66, 63, 66, 75 us, 32 x 16 nodes of heads
+  // of 64 over 500 - 4,000 261, 259, 268, 285.
+  ta_split(p, a, PA_ROWS, DP, sms, plain_ctas(DP), 1, scratch);
   const size_t al = 4 * sizeof(T);
   uintptr_t bits = (uintptr_t)a.k | (uintptr_t)a.v | (a.cols > 0 ? (uintptr_t)a.cache_k | (uintptr_t)a.cache_v : 0);
   for (int i = 0; i < 3; ++i) bits |= (uintptr_t)((a.k_stride[i] | a.v_stride[i]) * sizeof(T)) | (a.cols > 0 ? (uintptr_t)(a.cache_stride[i] * sizeof(T)) : 0);

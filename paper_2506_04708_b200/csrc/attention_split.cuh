@@ -14,7 +14,9 @@ namespace stand {
 constexpr int TA_SMS = 148;               // B200; scratch is laid out for that many
 constexpr int TA_GROUP = 4;               // row tiles that walk together, at most
 constexpr int TA_KT = 64;                 // keys per tile
-constexpr int TA_MIN_TILES = 2;           // fewest tiles worth a CTA of their own (one token over 700: 13.9, 12.9, 13.0, 13.3 us with 1 - 4)
+// Fewest tiles worth a CTA of their own.  With 1, 2, 3, 4: one token over 700 (32 / 8 heads of 128) 10.9, 11.0, 11.9, 14.0 us; one over
+// 3,000 (28 / 4 heads) 17.4, 13.4, 13.0, 13.9; 4 x 8 nodes over 300 (8 / 2 heads) 10.0, 12.5, 13.7, 14.2.
+constexpr int TA_MIN_TILES = 2;
 
 struct TaRecord {  // what the joining kernel has to do for the last pair that a group began
   int n_parts;     // 0: nothing (that pair ends within the group)

@@ -24,8 +24,10 @@
 //
 // Measured (keys and values read once, over the time): 256 sequences x 24 nodes, texts of 130 - 4,100, 32 / 8 heads of 128:
 // 390 - 404 us in short bursts = 5.8 - 6.0 TB/s (0.89 - 0.92 of the copy bandwidth), 460 - 480 us in loops of seconds, where the
-// board's power limit holds the clock at 1.24 - 1.4 GHz; 64 nodes over 32,001 tokens, 28 / 4 heads of 128: 51 us = 0.57 PFLOP/s;
-// one token over 700: 11 us.  No unit is near its limit then (tensor pipe 36 %, exponentials 27 %, issue 29 %, memory 81 % of
+// board's power limit holds the clock at 1.24 - 1.4 GHz; 64 nodes over 32,001 tokens, 28 / 4 heads of 128: 52 us = 0.57 PFLOP/s;
+// one token over 700: 11 us.  64 x 24 nodes, 130 - 4,100 tokens, 16 / 4 heads of 256: 117 us = 5.0 TB/s (one CTA per SM: nothing
+// overlaps the chain named below).  Prompts without a cache, 32 / 8 heads of 128: 4 x 4,096 rows 1,360 us, 1 x 16,384 4,950 us = 0.40 -
+// 0.44 PFLOP/s of the visible half.  No unit is near its limit then (tensor pipe 36 %, exponentials 27 %, issue 29 %, memory 81 % of
 // a copy): what bounds a tile is the chain scores - maximum - exponentials - product, about 2,200 cycles, which two CTAs overlap.
 #pragma once
 #include <cuda.h>
@@ -744,7 +746,8 @@ template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams
   using Sh = TaShape<DP, C>;
   TaParams p;
   // A piece's fixed cost in tiles, measured by trying 3 to 9: 16 sequences of 1 - 8,190 tokens with heads of 64 take 81, 71, 59,
-  // 58 us with 3, 5, 7, 9; 256 sequences of 130 - 4,100 with heads of 128 take 393, 389, 391, 398.
+  // 58 us with 3, 5, 7, 9; 256 sequences of 130 - 4,100 with heads of 128 take 393, 389, 391, 398; 64 of them with 16 / 4 heads of 256
+  // 149, 124, 117, 117 with 0, 2, 5, 8.
   ta_split(p.s, a, tensor_tile_rows(a.N, a.group), DP, sms, Sh::CTAS, DP == 64 ? 8 : 5, scratch);
   p.box_rows = 16;
   while (p.box_rows < TA_KT && a.page % (p.box_rows * 2) == 0) p.box_rows *= 2;

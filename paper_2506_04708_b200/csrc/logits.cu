@@ -11,6 +11,7 @@ using namespace stand;
 
 namespace {
 
+constexpr int LG_SMS = 148;        // multiprocessors of a B200
 constexpr int LG_THREADS = 256;
 constexpr int LG_CHUNK = 4096;     // tokens of the vocabulary per block in a large batch
 constexpr int LG_BLOCKS = 5;       // blocks per multiprocessor
@@ -330,9 +331,10 @@ extern "C" int stand_process_logits(const stand_logits* c, const stand_logits_in
   // A small batch is cut finer, so that it reaches all multiprocessors (two blocks each) down to 512 tokens (8 rows of 32,000:
   // 4.0 us instead of 9.2); a text is scanned once per chunk, so a large one is not.
   p.chunk = LG_CHUNK;
-  while (p.chunk > 512 && (long long)c->B * ((c->V + p.chunk - 1) / p.chunk) < 2 * 148) p.chunk /= 2;
-  // between one and two rounds of blocks: larger chunks, if that makes it one (64 rows of 50,257: part of 21 -> 17 us)
-  const long long round = 148 * LG_BLOCKS;
+  while (p.chunk > 512 && (long long)c->B * ((c->V + p.chunk - 1) / p.chunk) < 2 * LG_SMS) p.chunk /= 2;
+  // Between one and two rounds of blocks: larger chunks, if that makes it one.  With / without, texts of 6,000: 64 rows of 50,257 12.8 /
+  // 16.1 us, 76 of 40,000 12.6 / 14.9, 22 of 151,936 10.0 / 12.7, 93 of 32,000 13.1 / 15.2; just past one round (57 of 50,257) 12.9 / 12.3.
+  const long long round = LG_SMS * LG_BLOCKS;
   if (p.chunk == LG_CHUNK && (long long)c->B * ((c->V + LG_CHUNK - 1) / LG_CHUNK) > round)
     for (int ch = LG_CHUNK + 512; ch <= LG_CHUNK_MAX; ch += 512)
       if ((long long)c->B * ((c->V + ch - 1) / ch) <= round) {
