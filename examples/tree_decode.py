@@ -97,6 +97,7 @@ class Decoder:
         self.mask = mask
         self.mask_row = None if mask is None else torch.zeros((B, N), dtype=torch.int32, device=dev)
         self.path = torch.full((B, width), -1, dtype=torch.int32, device=dev)
+        self.short = torch.zeros(B, dtype=torch.bool, device=dev)  # sequences that outgrew their pages: their text is no longer to be trusted
         self.prefill(max(len(p) for p in prompts) - 1)
         tail = np.full((B, order), -1, np.int32)
         for b, p in enumerate(prompts):
@@ -123,6 +124,7 @@ class Decoder:
         self.seen = torch.where(pos < new[:, None], self.text[:, :n], -1).contiguous()
         _, k, v = m.forward(self.text[:, :n], pos, self.attend(chain))
         slots, granted, length, self.n_free = slots_of(self.len, new, self.table, self.free, self.n_free)
+        self.short |= granted < 0
         store(k, v, slots, self.cache_k, self.cache_v)
         self.len = length.clone()
 
@@ -136,6 +138,7 @@ class Decoder:
         emitted, n, tree = self.stand.step(logits)
         self.stand.path_device(self.path)
         slots, granted, self.len, self.n_free = self.map(self.len, n, self.table, self.free, self.n_free)
+        self.short |= granted < 0  # looked at when the host has a reason to wait anyway
         self.commit(k, v, slots, self.cache_k, self.cache_v, path=self.path)
         j = torch.arange(emitted.shape[1], device=self.text.device)[None]
         at = (self.n_text[:, None] + j).clamp(max=self.text.shape[1] - 1)
@@ -167,6 +170,8 @@ def main():
         dec.step()
     end.record()
     torch.cuda.synchronize()
+    if dec.short.any():
+        raise SystemExit("a sequence outgrew its pages")
     made = int((dec.n_text - dec.n_prompt).sum())
     print(f"{a.batch} sequences, {a.steps + 1} steps: {made} tokens ({made / (a.steps + 1) / a.batch:.2f} per step and sequence), "
           f"{start.elapsed_time(end) / a.steps:.3f} ms per step")

@@ -553,3 +553,20 @@ def test_results_do_not_depend_on_what_shared_memory_held(dtype, N, hq, hkv, dim
             first = out.clone(), lse.clone()
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), fill
     ts._check_attention(c, tuple(t.double().cpu().numpy() for t in first))
+
+
+# ---------------------------------------------------------------- the example
+@pytest.mark.gpu
+def test_the_loop_tells_when_a_sequence_outgrows_its_pages():
+    from examples import tree_decode as td
+    model = td.Model(V=300)
+    prompts = [np.arange(6, dtype=np.int32), np.arange(30, dtype=np.int32)]
+    dec = td.Decoder(model, prompts, most=48)  # three pages of 16 each
+    for _ in range(60):
+        before = int(dec.n_text[1])
+        dec.step()
+        if int(dec.n_text[1]) - 1 > 48:  # does not fit any more
+            break
+        assert not dec.short.any()
+    assert before <= 49 and dec.short.tolist()[1]
+    assert int(dec.len[1]) == before - 1
