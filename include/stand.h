@@ -347,7 +347,9 @@ typedef struct {
  * row's scaled scores.  An empty row (no visible key) gets zeros and -inf.  Keys and values that a row does not see
  * do not enter it, whatever they hold.  A value that it sees and that is not finite makes its element of the row +inf, -inf or
  * NaN as a sum of such values does, however small its weight.
- * Scores, softmax statistics and sums are 32-bit floats.  dev_len is int64; a length below 0 counts as 0, one beyond
+ * Scores, softmax statistics and sums are 32-bit floats.  In 16-bit calls the softmax weights are rounded to the inputs' type where
+ * they multiply the values (half: weights below 2^-32 of a row's largest may count as 0 there); STAND_DTYPE_F32 keeps 32 bits
+ * throughout.  dev_len is int64; a length below 0 counts as 0, one beyond
  * max_pages * page_size as that; a table entry outside [0, pages) reads as a page of zeros.  dev_scratch: 256-byte
  * aligned, stand_tree_attention_scratch_bytes (0: invalid shapes) of it; calls that may overlap need scratch of their
  * own.  If a bounded wait inside the kernel runs out (never seen; stand_set_wait_limit), every output that depended on

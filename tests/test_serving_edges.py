@@ -570,3 +570,31 @@ def test_the_loop_tells_when_a_sequence_outgrows_its_pages():
         assert not dec.short.any()
     assert before <= 49 and dec.short.tolist()[1]
     assert int(dec.len[1]) == before - 1
+
+
+# ---------------------------------------------------------------- page release by itself
+@pytest.mark.gpu
+@pytest.mark.parametrize("B", [1, 3, 300])
+@pytest.mark.parametrize("room", ["plenty", "short", "none"])
+def test_release_pushes_whole_pages_in_order(B, room):
+    """Lengths of zero and below, at and past a page's end, beyond the table (its columns count); a list that takes all, some or none."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    rng = np.random.default_rng(B)
+    page, cols = 16, 5
+    length = rng.choice([-4, 0, 1, 15, 16, 17, 33, 79, 80, 81, 10**12], B).astype(np.int64)
+    done = (rng.random(B) < 0.6).astype(np.int32) * rng.integers(-3, 4, B).astype(np.int32)
+    table = rng.permutation(B * cols).reshape(B, cols).astype(np.int32)
+    pages = [list(table[b, : min(-(-max(int(length[b]), 0) // page), cols)]) if done[b] else [] for b in range(B)]
+    given, held = sum(pages, []), 7
+    capacity = held + {"plenty": len(given) + 3, "short": len(given) // 2, "none": 0}[room]
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to("cuda:0")  # noqa: E731
+    free = np.full(capacity, -9, np.int32)
+    free[:held] = 1000 + np.arange(held)
+    t_free = dev(free)
+    plan = serving.PageMap(B, 1, page, cols, capacity)
+    ln, nf = plan.release(dev(length), dev(done), dev(table), t_free, dev(np.array([held], np.int32)))
+    n = min(held + len(given), capacity)
+    free[held:n] = given[: n - held]
+    assert int(nf) == n and np.array_equal(t_free.cpu().numpy(), free)
+    assert np.array_equal(ln.cpu().numpy(), np.where(done != 0, 0, length))
