@@ -27,7 +27,7 @@
 // board's power limit holds the clock at 1.24 - 1.4 GHz; 64 nodes over 32,001 tokens, 28 / 4 heads of 128: 52 us = 0.57 PFLOP/s;
 // one token over 700: 11 us.  64 x 24 nodes, 130 - 4,100 tokens, 16 / 4 heads of 256: 117 us = 5.0 TB/s (one CTA per SM: nothing
 // overlaps the chain named below).  Prompts without a cache, 32 / 8 heads of 128: 4 x 4,096 rows 1,360 us, 1 x 16,384 4,950 us = 0.40 -
-// 0.44 PFLOP/s of the visible half.  No unit is near its limit then (tensor pipe 36 %, exponentials 27 %, issue 29 %, memory 81 % of
+// 0.44 PFLOP/s of the visible half.  In the first case no unit is near its limit (tensor pipe 35 %, exponentials 27 %, issue 29 %, memory 82 % of
 // a copy): what bounds a tile is the chain scores - maximum - exponentials - product, about 2,200 cycles, which two CTAs overlap.
 #pragma once
 #include <cuda.h>
