@@ -43,10 +43,12 @@ constexpr int TA_THREADS = 224;
 constexpr float TA_SLACK = 8.0f;          // the maximum is raised only when scores pass it by 2^8 (below)
 // Weights of the second product are rounded to the input's type, since both operands of a 16-bit product have one type: each
 // is off by 2^-9 (bfloat16) or 2^-12 (half) of itself at most, independently, which is what rounding the result costs anyway;
-// their sum l is taken before the rounding, in fp32.  Half has few exponents: there weights are 2^TA_LIFT times larger (at most 2^15,
+// their sum l is taken before the rounding, in fp32.  Half has few exponents: there weights are 2^7 times larger (at most 2^15,
 // with the slack), as are l and o, so that those down to 2^-21 of the largest keep all bits and none above 2^-32 is lost
-// (unlifted, 40,000 keys of 2^-26 beside a dominant one were lost from o while they stayed in l).
-constexpr float TA_LIFT = 7.0f;
+// (unlifted, 40,000 keys of 2^-26 beside a dominant one were lost from o while they stayed in l).  Bfloat16 has the exponents of
+// fp32 and values as large: there the slack is taken off, so that no weight is above 1 and o passes fp32's range only
+// where the plain sum of the values does.
+template <bool BF16> constexpr float TA_LIFT = BF16 ? -TA_SLACK : 7.0f;
 constexpr int TA_XCOLS = 16;              // columns of O that the parts exchange at a time
 
 template <int DP, int C> struct TaShape {
@@ -466,8 +468,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           }
           top = fmaxf(top, top1) * scale2;
           // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores pass
-          // it by TA_SLACK, so that o is seldom read, scaled and written (weights up to 2^8 lose nothing in either 16-bit
-          // type, sums are fp32).  The warp's rows move together, as rows that exist want it: what lies in the lanes of others is
+          // it by TA_SLACK, so that o is seldom read, scaled and written (TA_LIFT keeps the weights within their type).  The warp's rows move together, as rows that exist want it: what lies in the lanes of others is
           // left from earlier kernels, and would make the weights' roundings differ from launch to launch.
           if (__any_sync(FULL, in && top > m + TA_SLACK)) {
             const float raised = fmaxf(m, top);
@@ -489,7 +490,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
               }
             }
           }
-          const float base = (m == -INFINITY ? 0.0f : m) - (BF16 ? 0.0f : TA_LIFT);
+          const float base = (m == -INFINITY ? 0.0f : m) - TA_LIFT<BF16>;
           const unsigned long long scale_2 = pack2(scale2, scale2), base_2 = pack2(-base, -base);
           unsigned long long sum_2 = pack2(0.0f, 0.0f);
 #pragma unroll 1
@@ -562,7 +563,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
       tc_fence_after();
       const bool odd = sh.odd[n_seg & 1] == n_seg + 1;
       ++n_seg;
-      if (!BF16) m -= TA_LIFT;  // what l and o are relative to
+      m -= TA_LIFT<BF16>;  // what l and o are relative to
 
       // ---- the piece's result ---------------------------------------------------------------
       float factor = 1.0f;  // of this part's o

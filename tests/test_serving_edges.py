@@ -598,3 +598,27 @@ def test_release_pushes_whole_pages_in_order(B, room):
     free[held:n] = given[: n - held]
     assert int(nf) == n and np.array_equal(t_free.cpu().numpy(), free)
     assert np.array_equal(ln.cpu().numpy(), np.where(done != 0, 0, length))
+
+
+# ---------------------------------------------------------------- large values
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,hq,hkv,dim", [(1, 2, 2, 64), (8, 8, 2, 128), (40, 4, 2, 64), (3, 2, 1, 256)])
+def test_values_near_the_end_of_the_range(dtype, N, hq, hkv, dim):
+    """Values of up to 2^117 under scores that rise by 5 nats after the first tile: 700 of them fit the range with room, and so does any
+    weighted mean of them."""
+    c = ts._attention_case(dim, dtype, [700] * 150, N, hq, hkv, dim, 16, parent=inputs.topology(N, min(N - 1, 3), 4), nan=False, spare=0)
+    c["qkv"][:, :, :hq] = 0
+    c["qkv"][:, :, :hq, 0] = 1.0
+    c["ck"][:, :, :, 0] = 5.0
+    for b in range(150):
+        for page in c["table"][b, :4]:
+            c["ck"][int(page), :, :, 0] = 0.0
+    big = 2.0**117
+    c["cv"] = (c["cv"].float().clamp(-1, 1) * 0.25 + 0.5).mul(big).to(c["cv"].dtype)
+    c["qkv"][:, :, hq + hkv:] = 0
+    few = dict(c, len=c["len"][:2], table=c["table"][:2], qkv=c["qkv"][:2])
+    want = ts._reference(few, scale=1.0)
+    out, lse = ts._run_attention(c, scale=1.0)
+    assert np.isfinite(out).all()
+    ts._check_attention(few, (out[:2] / big, lse[:2]), want=(want[0] / big, want[1], want[2] / big, want[3] / big, want[4]))
