@@ -441,7 +441,7 @@ typedef struct {
 } stand_logits_inputs;
 
 /* Processes the logits of every node of every tree before stand_step: dev_in [B * N rows of V] to dev_out (the same
- * pointer with the same stride: in place).  For token t in row (b, u), with the text of the sequence followed by the
+ * pointer with the same stride: in place; rows must not overlap otherwise).  For token t in row (b, u), with the text of the sequence followed by the
  * tokens on the path from below the root to u:
  *   met(t): t occurs in it;  c(t): how often it does, the prompt left out.
  *   x = met(t) ? (x > 0 ? x / repetition : x * repetition) : x

@@ -294,6 +294,16 @@ __global__ void __launch_bounds__(LG_THREADS, LG_BLOCKS) logits_kernel(const __g
   }
 }
 
+// Does a row of the output lie over another part of the input?  Rows of `row` bytes, `in_stride` and `out_stride` apart; the
+// same rows (in place) do not count, and rows of equal stride may lie between one another.
+bool rows_overlap(const void* in, const void* out, long long rows, long long row, long long in_stride, long long out_stride) {
+  const uintptr_t x = (uintptr_t)in, y = (uintptr_t)out;
+  if (x == y || x + (rows - 1) * in_stride + row <= y || y + (rows - 1) * out_stride + row <= x) return false;
+  if (in_stride != out_stride) return true;
+  const long long off = (long long)((y > x ? y - x : x - y) % (uintptr_t)in_stride);
+  return off < row || in_stride - off < row;
+}
+
 }  // namespace
 
 extern "C" int stand_process_logits(const stand_logits* c, const stand_logits_inputs* x, const void* dev_in, void* dev_out,
@@ -303,11 +313,12 @@ extern "C" int stand_process_logits(const stand_logits* c, const stand_logits_in
   if (c->dtype != STAND_DTYPE_F32 && c->dtype != STAND_DTYPE_BF16) return STAND_E_ARG;
   if (c->in_stride < c->V || c->out_stride < c->V || c->text_stride < 0 || c->masks < 0 || c->biases < 0 || c->reserved != 0) return STAND_E_ARG;
   if (dev_in == dev_out && c->in_stride != c->out_stride) return STAND_E_ARG;
+  const int es = c->dtype == STAND_DTYPE_F32 ? 4 : 2;
+  if (rows_overlap(dev_in, dev_out, (long long)c->B * c->N, (long long)c->V * es, c->in_stride * es, c->out_stride * es)) return STAND_E_ARG;
   if (!c->parent && c->N > 1) return STAND_E_ARG;
   if ((x->text != nullptr) != (x->n_text != nullptr) || (x->n_prompt && !x->text)) return STAND_E_ARG;
   if (x->bias_start && c->biases > 0 && (!x->bias_id || !x->bias_value)) return STAND_E_ARG;
   if ((x->mask != nullptr) != (x->mask_row != nullptr)) return STAND_E_ARG;
-  const int es = c->dtype == STAND_DTYPE_F32 ? 4 : 2;
   if (!aligned(es, dev_in, dev_out) || !aligned(8, x->n_text, x->n_prompt) ||
       !aligned(4, x->text, x->tree_tokens, x->repetition, x->frequency, x->presence, x->bias_start, x->bias_id, x->bias_value, x->mask, x->mask_row))
     return STAND_E_ARG;

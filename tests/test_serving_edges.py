@@ -622,3 +622,45 @@ def test_values_near_the_end_of_the_range(dtype, N, hq, hkv, dim):
     out, lse = ts._run_attention(c, scale=1.0)
     assert np.isfinite(out).all()
     ts._check_attention(few, (out[:2] / big, lse[:2]), want=(want[0] / big, want[1], want[2] / big, want[3] / big, want[4]))
+
+
+# ---------------------------------------------------------------- logits: rows over rows
+def test_logits_rows_laid_over_others_are_refused():
+    import ctypes as C
+    lib_build.build()
+    x = binding.StandLogitsInputs()
+    parent = np.array([-1, 0, 0], np.int32)
+
+    def call(out, in_stride=100, out_stride=100, at=0x1000000, dtype=binding.DTYPE_F32):
+        s = binding.StandLogits(2, 3, 100, dtype, parent.ctypes.data, in_stride, out_stride, 0, 0, 0, 0)
+        return binding.lib().stand_process_logits(C.byref(s), C.byref(x), C.c_void_p(at), C.c_void_p(out), None)
+
+    at = 0x1000000
+    for bad in (dict(out=at + 4), dict(out=at - 4), dict(out=at + 400), dict(out=at - 400 * 5), dict(out=at + 400 * 5 + 396),
+                dict(out=at + 396, in_stride=300, out_stride=300), dict(out=at + 804, in_stride=300, out_stride=300),
+                dict(out=at + 400, in_stride=200, out_stride=300), dict(out=at + 2, dtype=binding.DTYPE_BF16)):
+        assert call(**bad) == -1, bad
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("where", ["between", "behind", "before"])
+def test_logits_rows_between_others_are_taken(where):
+    """Output rows in the gaps between the input's, and right behind or before all of them, in one buffer."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    B, N, V = 3, 4, 1001
+    op = serving.LogitsProcessor(B, N, V, torch.float32, parent=[-1, 0, 0, 1])
+    pen = torch.ones(B, device="cuda:0")
+    text, n = torch.arange(7, dtype=torch.int32, device="cuda:0").expand(B, 7).contiguous(), torch.full((B,), 7, dtype=torch.int64, device="cuda:0")
+    if where == "between":
+        both = torch.randn((B, N, 2 * V), device="cuda:0")
+        x, y = both[..., :V], both[..., V:]
+    else:
+        both = torch.randn((2, B, N, V), device="cuda:0")
+        x, y = (both[0], both[1]) if where == "behind" else (both[1], both[0])
+    want = x.clone()
+    want[..., :7] -= 1
+    assert op(x, text, n, presence=pen, out=y) is y and torch.equal(y, want)
+    flat = torch.randn(B * N * V + 5, device="cuda:0")
+    with pytest.raises(binding.StandError):
+        op(flat[:-5].view(B, N, V), out=flat[5:].view(B, N, V))
