@@ -316,7 +316,7 @@ int stand_set_wait_limit(int64_t polls);
  * s / page_size.  Problems found on the device never fault: see each entry.  Arrays are aligned to their elements
  * (STAND_E_ARG otherwise). */
 
-/* The shapes of stand_tree_attention.  Strides are in elements; the innermost dimension (dim) is contiguous.
+/* The shapes of stand_tree_attention (zero the structure first: fields not used here must be 0).  Strides are in elements; the innermost dimension (dim) is contiguous.
  * Queries, keys and values of the nodes may be slices of one projection's output. */
 typedef struct {
   int32_t B;          /* sequences, >= 1 */
@@ -390,7 +390,7 @@ int stand_page_release(const int64_t* dev_len, const int32_t* dev_done, int32_t 
                        int32_t max_pages, const int32_t* dev_table, int32_t capacity, int32_t* dev_free,
                        const int32_t* dev_n_free, int64_t* dev_len_out, int32_t* dev_n_free_out, void* cu_stream);
 
-/* The shapes of stand_kv_commit.  Strides are in elements, dim is contiguous. */
+/* The shapes of stand_kv_commit (zero the structure first).  Strides are in elements, dim is contiguous. */
 typedef struct {
   int32_t layers, B, N; /* N nodes per sequence in the source */
   int32_t heads, dim, dtype;

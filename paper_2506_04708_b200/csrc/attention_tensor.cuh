@@ -468,9 +468,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           }
           top = fmaxf(top, top1) * scale2;
           // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores pass
-          // it by TA_SLACK, so that o is seldom read, scaled and written (TA_LIFT keeps the weights within their type).  The warp's rows move together, as rows that exist want it: what lies in the lanes of others is
-          // left from earlier kernels, and would make the weights' roundings differ from launch to launch.
-          if (__any_sync(FULL, in && top > m + TA_SLACK)) {
+          // it by TA_SLACK, so that o is seldom read, scaled and written (TA_LIFT keeps the weights within their type).  The warp's rows move together, as live rows want it: what lies in the lanes of others is
+          // left from earlier kernels or belongs to nodes that were not drafted, and would enter the roundings of the weights.
+          if (__any_sync(FULL, live && top > m + TA_SLACK)) {
             const float raised = fmaxf(m, top);
             const float keep = raised == -INFINITY ? 1.0f : ta_ex2(m - raised);
             m = raised;

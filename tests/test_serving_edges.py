@@ -664,3 +664,23 @@ def test_logits_rows_between_others_are_taken(where):
     flat = torch.randn(B * N * V + 5, device="cuda:0")
     with pytest.raises(binding.StandError):
         op(flat[:-5].view(B, N, V), out=flat[5:].view(B, N, V))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("hq,hkv,dim", [(4, 2, 64), (8, 2, 128), (4, 4, 64), (2, 1, 256)])
+def test_queries_of_undrafted_nodes_do_not_touch_other_rows(dtype, hq, hkv, dim):
+    """Bit for bit, whatever the projection left in the rows of nodes that were not drafted."""
+    N = 24
+    c = ts._attention_case(dim, dtype, [300, 40, 1000], N, hq, hkv, dim, 16, parent=inputs.topology(N, 6, 3), undrafted=0.4, nan=False)
+    dead = np.argwhere(c["tree"] < 0)
+    assert len(dead) > 3
+    c["qkv"][:, :, :hq] *= 3
+    first = None
+    for fill in (0.0, 5.0, -40.0, 3000.0, INF, NAN):
+        for b, u in dead:
+            c["qkv"][int(b), int(u), :hq] = fill
+        got = ts._run_attention(c)
+        first = first or got
+        assert np.array_equal(got[0], first[0]) and np.array_equal(got[1], first[1]), fill
+    ts._check_attention(c, first)
