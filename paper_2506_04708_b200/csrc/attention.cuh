@@ -67,39 +67,26 @@ __device__ __forceinline__ bool attn_sees(const AttnParams& p, int b, int u, int
 // Values that are not finite.  A row's element is the sum of those that it sees, whatever their weights: +inf, -inf or NaN.
 // The kernels' sums come out as NaN where such a value met a weight of zero - one that is below its type, or that of a
 // key which a lane only carries along - or a row that does not see it.  So an element that is NaN although the row's
-// weights are in order (`lost`), or one whose tree has values that were taken out of the product, is settled here: `o` with the
-// sum of the values that are not finite among the cached tokens k0 .. k1 - 1 (only if lost) and the visible nodes n0 .. n1 - 1.
-// Rare, so it only has to be right; eight reads at a time keep it within the other warps' waits.
-template <typename T>
-__device__ __noinline__ float attn_settle(const AttnParams& p, int b, int g, int u, int d, int k0, int k1, int n0, int n1, float o, bool lost) {
+// weights are in order is settled by a second look at the values, for all kernels with this: the sum of the values that are
+// not finite in element d among the cached tokens k0 .. k1 - 1 of sequence b.  Zero: there are none (such a sum is never zero).
+template <typename T> __device__ __forceinline__ float attn_odd_cached(const AttnParams& p, int b, int g, int d, int k0, int k1) {
+  const T* cache = reinterpret_cast<const T*>(p.cache_v) + g * p.cache_stride[1] + d;
   float sum = 0.0f;
-  bool any = false;
-  auto add = [&](float f) {
-    if (!isfinite(f)) {
-      sum += f;
-      any = true;
-    }
-  };
-  if (lost) {
-    const T* cache = reinterpret_cast<const T*>(p.cache_v) + g * p.cache_stride[1] + d;
-    for (int k = k0; k < k1 && !isnan(sum); k += 8) {
-      float f[8];
+  for (int k = k0; k < k1 && !isnan(sum); k += 8) {
+    float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int pos = k + i, col = pos / p.page;
-        f[i] = 0.0f;
-        if (pos >= k1) continue;
-        const int page = p.table[(long long)b * p.cols + col];
-        if (page >= 0 && page < p.pages) f[i] = to_float(cache[page * p.cache_stride[0] + (long long)(pos - col * p.page) * p.cache_stride[2]]);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) add(f[i]);
+    for (int i = 0; i < 8; ++i) {
+      const int pos = k + i, col = pos / p.page;
+      f[i] = 0.0f;
+      if (pos >= k1) continue;
+      const int page = p.table[(long long)b * p.cols + col];
+      if (page >= 0 && page < p.pages) f[i] = to_float(cache[page * p.cache_stride[0] + (long long)(pos - col * p.page) * p.cache_stride[2]]);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (!isfinite(f[i])) sum += f[i];
   }
-  const T* tree = reinterpret_cast<const T*>(p.v) + b * p.v_stride[0] + g * p.v_stride[2] + d;
-  for (int v = n0; v < n1 && v <= u; ++v)
-    if (attn_sees(p, b, u, v)) add(to_float(tree[v * p.v_stride[1]]));
-  return !any ? o : (lost ? sum : o + sum);
+  return sum;
 }
 
 }  // namespace stand

@@ -52,6 +52,19 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// An element that came out as NaN though its row's weights are in order: with the values that are not finite among what the
+// row sees, cached tokens k0 .. k1 - 1 and nodes n0 .. n1 - 1.  Rare, so it only has to be right.
+template <typename T>
+__device__ __noinline__ float plain_settle(const AttnParams& p, int b, int g, int u, int d, int k0, int k1, int n0, int n1, float o) {
+  float sum = attn_odd_cached<T>(p, b, g, d, k0, k1);
+  const T* tree = reinterpret_cast<const T*>(p.v) + b * p.v_stride[0] + g * p.v_stride[2] + d;
+  for (int v = n0; v < n1 && v <= u && !isnan(sum); ++v) {
+    const float f = to_float(tree[v * p.v_stride[1]]);
+    if (!isfinite(f) && attn_sees(p, b, u, v)) sum += f;
+  }
+  return sum == 0.0f ? o : sum;
+}
+
 // wide: bases and strides allow 4 elements at a time
 template <typename T, int DP>
 __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __grid_constant__ TaSplit p, const bool wide) {
@@ -311,7 +324,7 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
         for (int e = 0; e < E; ++e) {
           const int d = lane * EV + e / EV * 128 + e % EV;
           if (isnan(o[i][e]) && d < D)
-            o[i][e] = attn_settle<T>(p.a, s.b, s.g, node[i], d, s.begin * KT, k1 < s.len ? k1 : s.len, n0 * KT, n1 * KT, o[i][e], true);
+            o[i][e] = plain_settle<T>(p.a, s.b, s.g, node[i], d, s.begin * KT, k1 < s.len ? k1 : s.len, n0 * KT, n1 * KT, o[i][e]);
         }
       }
       if (lane == 0) {

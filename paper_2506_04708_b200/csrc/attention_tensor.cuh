@@ -216,6 +216,65 @@ __device__ __noinline__ bool ta_wait_on(uint32_t bar, uint32_t parity, volatile 
   return there;
 }
 
+// Values that are not finite, for the rows of a warp: a lane has E elements of the row of node u, at o, the first of them in
+// column c0 + at.  Elements with a bit in `lost` (NaN, though the row's weights are in order) become the sum of such cached values
+// k0 .. k1 - 1, if there are any; to those of live rows come such values of the visible nodes n0 .. n1 - 1, which were taken out of
+// the product.  A lane reads column c0 + lane, so that a value is read once for all rows: other warps wait meanwhile, and a sequence
+// of such values must not make them give up on others (one NaN in a prompt of 4,096 rows: 8 ms; 226 when each row read for itself).
+template <typename T, int E>
+__device__ __noinline__ void ta_settle(const AttnParams& p, int b, int g, int c0, int k0, int k1, int n0, int n1, float* o, int u, int at,
+                                       uint32_t lost, bool live) {
+  const int lane = threadIdx.x & 31, d = c0 + lane;
+  if (__any_sync(FULL, lost != 0)) {
+    const float mine = d < p.dim ? attn_odd_cached<T>(p, b, g, d, k0, k1) : 0.0f;
+    __syncwarp();
+    for (int j = 0; j < 32; ++j) {
+      const float sum = __shfl_sync(FULL, mine, j);
+      const int e = j - at;
+      if (e >= 0 && e < E && (lost >> e & 1u) && sum != 0.0f) o[e] = sum;
+    }
+  }
+  const T* tree = reinterpret_cast<const T*>(p.v) + b * p.v_stride[0] + g * p.v_stride[2] + d;
+  if (n1 > p.N) n1 = p.N;
+  constexpr int NONE = 0x7FFFFFFF;
+  int first = NONE, other = NONE;  // without a mask: the column's first such node, the first after it with another value
+  float value1 = 0.0f;
+  for (int v0 = n0; v0 < n1; v0 += 8) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = v0 + i < n1 && d < p.dim ? to_float(tree[(v0 + i) * p.v_stride[1]]) : 0.0f;
+    if (!p.mask) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (isfinite(f[i])) continue;
+        if (first == NONE) {
+          first = v0 + i;
+          value1 = f[i];
+        } else if (other == NONE && f[i] != value1) {
+          other = v0 + i;
+        }
+      }
+      continue;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      for (uint32_t bits = __ballot_sync(FULL, !isfinite(f[i])); bits; bits &= bits - 1) {
+        const int j = __ffs(bits) - 1, e = j - at;
+        const float value = __shfl_sync(FULL, f[i], j);
+        if (live && e >= 0 && e < E && attn_sees(p, b, u, v0 + i)) o[e] += value;
+        __syncwarp();
+      }
+  }
+  if (!p.mask && n1 > n0) {  // node u sees all up to itself: the sum changes at those two
+    __syncwarp();
+    for (int j = 0; j < 32; ++j) {
+      const int from = __shfl_sync(FULL, first, j), from2 = __shfl_sync(FULL, other, j), e = j - at;
+      const float value = __shfl_sync(FULL, value1, j);
+      if (live && e >= 0 && e < E && u >= from) o[e] += u >= from2 ? NAN : value;
+    }
+  }
+}
+
 // ---- the kernel -----------------------------------------------------------------------
 template <int DP, int C, bool BF16>
 __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
@@ -594,14 +653,9 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
         if (!s.whole) p.s.part_ml[at] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
         else if (p.s.a.lse) p.s.a.lse[out_row] = empty ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
       }
-      // o of a row whose sum of weights is in order (`sound`)
-      auto settle = [&](float o, int col, int u, bool sound) {
-        const bool lost = isnan(o) && sound;
-        if (!(lost || odd) || col >= p.s.a.dim) return o;
-        const int k1 = s.end * KT, n0 = s.begin > s.p_tiles ? s.begin - s.p_tiles : 0, n1 = odd && s.end > s.p_tiles ? s.end - s.p_tiles : 0;
-        return attn_settle<typename std::conditional<BF16, __nv_bfloat16, __half>::type>(p.s.a, s.b, s.g, u, col, s.begin * KT,
-                                                                                           k1 < s.len ? k1 : s.len, n0 * KT, n1 * KT, o, lost);
-      };
+      using T = typename std::conditional<BF16, __nv_bfloat16, __half>::type;
+      const int k0 = s.begin * KT, k1 = s.end * KT < s.len ? s.end * KT : s.len;  // cached tokens and nodes of the piece
+      const int n0 = (s.begin > s.p_tiles ? s.begin - s.p_tiles : 0) * KT, n1 = odd && s.end > s.p_tiles ? (s.end - s.p_tiles) * KT : 0;
       if constexpr (C == 1) {
         if (warp_in) {
 #pragma unroll 1
@@ -610,14 +664,22 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
             __syncwarp();  // rows that do not exist have gone another way
             tc_ld32(o, my + Sh::COL_O + c * 32);
             tc_wait_ld();
-            if (!in) continue;
             float zero[4] = {};  // NaN if one of them is not finite
 #pragma unroll
             for (int i = 0; i < 32; ++i) zero[i & 3] = fmaf(__uint_as_float(o[i]), 0.0f, zero[i & 3]);
-            if (live && (odd || isnan(zero[0] + zero[1] + zero[2] + zero[3]))) {
+            if (__any_sync(FULL, live && (odd || isnan(zero[0] + zero[1] + zero[2] + zero[3])))) {
+              float f[32];
+              uint32_t lost = 0;
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(settle(__uint_as_float(o[i]), c * 32 + i, u, isfinite(l)));
+              for (int i = 0; i < 32; ++i) {
+                f[i] = __uint_as_float(o[i]);
+                if (live && isfinite(l) && isnan(f[i])) lost |= 1u << i;
+              }
+              ta_settle<T, 32>(p.s.a, s.b, s.g, c * 32, k0, k1, n0, n1, f, u, 0, lost, live);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(f[i]);
             }
+            if (!in) continue;
             if (!s.whole) {
               float4* dst = reinterpret_cast<float4*>(p.s.part_o + at * DP + c * 32);
 #pragma unroll
@@ -663,19 +725,33 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           sync_rows();
           if (!ok) break;
           const int quads = cols / 4;
-          for (int i = tid; i < rows * quads; i += TA_ROWS) {
-            const int r = i / quads, q = i - r * quads, col = c0 + q * 4;
+          for (int i0 = 0; i0 < rows * quads; i0 += TA_ROWS) {  // whole warps
+            const int i = i0 + tid, r = i / quads, q = i - r * quads, col = c0 + q * 4;
             const int ru = s.row0 / p.s.a.group + r / p.s.a.group, rh = s.g * p.s.a.group + r % p.s.a.group;
-            if (ru >= p.s.a.N) continue;
+            const bool there = r < rows && ru < p.s.a.N;
             float v[4] = {};
+            float2 ml = make_float2(0.0f, 0.0f);
+            if (there) {
+              ml = sh.ml[r];  // 1 / l, and whether the row is there at all
 #pragma unroll
-            for (int k = 0; k < C; ++k)
+              for (int k = 0; k < C; ++k)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) v[e] += exchange[(k * rows + r) * pitch + q * 4 + e];
-            const float2 ml = sh.ml[r];  // 1 / l, and whether the row is there at all
-            if (ml.y != 0.0f && (odd || !isfinite(v[0] + v[1] + v[2] + v[3])))
+                for (int e = 0; e < 4; ++e) v[e] += exchange[(k * rows + r) * pitch + q * 4 + e];
+            }
+            if (__any_sync(FULL, ml.y != 0.0f && (odd || !isfinite(v[0] + v[1] + v[2] + v[3])))) {
+              float f[4];
+              uint32_t lost = 0;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) v[e] = settle(v[e], col + e, ru, ml.x > 0.0f);
+              for (int e = 0; e < 4; ++e) {
+                f[e] = v[e];
+                if (ml.y != 0.0f && ml.x > 0.0f && isnan(f[e])) lost |= 1u << e;
+              }
+              for (int at = 0; at < cols; at += 32)
+                ta_settle<T, 4>(p.s.a, s.b, s.g, c0 + at, k0, k1, n0, n1, f, ru, q * 4 - at, lost, ml.y != 0.0f);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = f[e];
+            }
+            if (!there) continue;
             if (!s.whole) {
               *reinterpret_cast<float4*>(p.s.part_o + part_row(s, r) * DP + col) = make_float4(v[0], v[1], v[2], v[3]);
             } else if (col < p.s.a.dim) {

@@ -684,3 +684,90 @@ def test_queries_of_undrafted_nodes_do_not_touch_other_rows(dtype, hq, hkv, dim)
         first = first or got
         assert np.array_equal(got[0], first[0]) and np.array_equal(got[1], first[1]), fill
     ts._check_attention(c, first)
+
+
+# ---------------------------------------------------------------- a sequence full of such values beside others
+@pytest.mark.gpu
+@pytest.mark.parametrize("how", ["prompt, one NaN", "prompt, all infinite", "cached infinities, heads of 64", "cached NaN, heads of 64"])
+def test_one_sequence_that_is_not_finite_does_not_hold_up_others(how):
+    """What is done for values that are not finite stays within waits of a few milliseconds (a sixty-fourth of what they
+    may last), so that no warp gives up and no other sequence is touched."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    dev, dt = "cuda:0", torch.bfloat16
+    g = torch.Generator(device=dev).manual_seed(4)
+    prompt = how.startswith("prompt")
+    B, N, hq, hkv, dim, L, page = (3, 4096, 8, 2, 128, 0, 16) if prompt else (6, 32, 16, 16, 64, 8192, 64)
+    pool, cols = B * L // page, L // page
+    ck, cv = (torch.randn((pool, hkv, page, dim), generator=g, device=dev, dtype=dt) for _ in range(2))
+    table = torch.arange(pool, dtype=torch.int32, device=dev).view(B, cols)
+    length = torch.full((B,), L, dtype=torch.int64, device=dev)
+    qkv = torch.randn((B, N, hq + 2 * hkv, dim), generator=g, device=dev, dtype=dt)
+    plan = serving.TreeAttention(B, N, hq, hkv, dim, dt, page, pool, cols, parent=None if prompt else inputs.topology(N, 4, 4))
+    args = qkv[:, :, :hq], qkv[:, :, hq:hq + hkv], qkv[:, :, hq + hkv:], ck, cv, table, length
+    clean = plan(*args)[0].clone()
+    touched = torch.zeros_like(clean, dtype=torch.bool)
+    if how == "prompt, one NaN":
+        qkv[1, 5, hq + hkv + 1, 9] = NAN
+        touched[1, 5:, hq // hkv:, 9] = True
+        value = NAN
+    elif how == "prompt, all infinite":
+        qkv[1, :, hq + hkv:] = -INF
+        touched[1] = True
+        value = -INF
+    else:
+        value = INF if "infinities" in how else NAN
+        for tile in range(cols):  # one token of every page
+            cv[int(table[1, tile]), :, tile % page] = value
+        touched[1] = True
+    torch.cuda.synchronize()
+    binding.set_wait_limit(2**16)
+    try:
+        out = plan(*args)[0]
+        torch.cuda.synchronize()
+    finally:
+        binding.set_wait_limit(-1)
+    assert torch.equal(out[~touched], clean[~touched])
+    assert (torch.isnan(out[touched]) if np.isnan(value) else out[touched] == value).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("N,hq,hkv,dim", [(150, 2, 1, 64), (20, 2, 2, 64), (700, 2, 1, 128), (90, 1, 1, 200)])
+def test_values_of_a_prompt_that_are_not_finite(dtype, N, hq, hkv, dim):
+    """Several in a column: of one sign, of both (NaN from the second on), NaN first; over a cached text that has some too."""
+    c = ts._attention_case(N, dtype, [0, 40], N, hq, hkv, dim, 16)
+    clean, v0 = ts._reference(c), hq + hkv
+    expect = {}
+
+    def put(b, node, d, value):
+        c["qkv"][b, node, v0, d] = value
+        with np.errstate(invalid="ignore"):
+            expect.setdefault((b, d), np.zeros(N))[node:] += value
+
+    for b in (0, 1):
+        put(b, 3, 0, INF)
+        put(b, 9, 0, INF)
+        put(b, N - 1, 0, -INF)
+        put(b, 5, 1, -INF)
+        put(b, 6, 1, NAN)
+        put(b, 2, 2, NAN)
+        put(b, 4, 2, INF)
+        put(b, 0, 5, -INF)
+    for node in range(7, N):
+        put(1, node, dim - 1, INF)
+    _plant(c, 1, 20, 0, 0, INF)
+    expect[1, 0] += INF
+    _plant(c, 1, 21, 0, 5, INF)
+    expect[1, 5] = np.full(N, NAN)
+    _plant(c, 1, 22, 0, 6, -INF)
+    expect[1, 6] = np.full(N, -INF)
+    out, lse = ts._run_attention(c)
+    hit = np.zeros_like(out, bool)
+    group = hq // hkv
+    for (b, d), want in expect.items():
+        odd = ~np.isfinite(want) | (want != 0)
+        got = out[b, :, :group, d]
+        assert np.array_equal(got[odd], np.repeat(want[odd, None], group, 1), equal_nan=True), (b, d)
+        hit[b, odd, :group, d] = True
+    ts._check_attention(c, (np.where(hit, clean[0], out), lse), want=clean)
