@@ -278,7 +278,7 @@ def prepare(case, seed):
         from paper_2506_04708_b200 import serving
 
         s["plan"] = serving.KvAppend(L, B, N, H, dim, dt, page, pool, width, packed=c["packed"], freq=s["freq"] if c["turn"] else None,
-                                     offset=s["offset"], interleaved=c["pairs"], norm=c["norm"], weight_k=s["weight_k"], eps=EPS)
+                                     offset=s["offset"] if c["turn"] else None, interleaved=c["pairs"], norm=c["norm"], weight_k=s["weight_k"], eps=EPS)
         s["back"] = serving.KvRead(L, B, H, dim, torch.bfloat16, page, pool, width, packed=True) if c["packed"] else None
     return s
 
