@@ -454,6 +454,87 @@ typedef struct {
 int stand_process_logits(const stand_logits* shape, const stand_logits_inputs* inputs, const void* dev_in, void* dev_out,
                          void* cu_stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * Positions, and a cache in 4 bits.
+ *
+ * The 4-bit form.  A row's elements in groups of 16: a scale s of 8 bits (a float of 5 exponent bits with bias 15 and 3
+ * fraction bits, without a sign, subnormals included) and 16 whole numbers k of -8 .. 7; an element is k s, exact in
+ * bfloat16 (and in half while it is within its range).  Storing a row takes the smallest s with 7 s >= the group's largest magnitude
+ * (61440 if there is none) and the nearest k in -7 .. 7, the even one in a tie; the quotient is rounded to 32 bits first.  A group that holds a
+ * value that is not finite gets the scale 0xFF; scales from 0xF8 on make the whole group read as NaN.  So 4.5 bits an element.
+ * k + 8 is held in 4 bits: 4 bytes hold 8 elements e, bits 4 (e / 2) .. of the low (e even) or high (e odd) two bytes.
+ * A packed cache is a pool of pages like the other; for each page and head one block: the codes of its page_size tokens (dim / 2
+ * bytes each), then their scales (dim / 16 bytes each): STAND_PACKED_BLOCK_BYTES.  Blocks begin at multiples of 16
+ * bytes; dim and page_size are multiples of 16. */
+#define STAND_PACKED_BLOCK_BYTES(page_size, dim) ((size_t)(page_size) * (size_t)(dim) / 16 * 9)
+
+/* The shapes of stand_rotate_heads (zero the structure first).  Strides are in elements; dim is contiguous. */
+typedef struct {
+  int32_t B, N;           /* sequences, tokens (or nodes) of each */
+  int32_t heads_q, heads_kv;
+  int32_t dim;            /* 1..256 */
+  int32_t dtype;
+  int32_t rotary_dim;     /* elements of a row that are turned: the first ones; even, 0..dim (0: dev_freq is NULL) */
+  int32_t interleaved;    /* pair i is elements 2i, 2i + 1 (1) or i, i + rotary_dim / 2 (0) */
+  int32_t norm;           /* 1: rows are normalised first */
+  float eps;              /* > 0 with norm */
+  int32_t reserved, reserved2;  /* must be 0 */
+  int64_t q_stride[3], k_stride[3];          /* sequence, node, head */
+  int64_t q_out_stride[3], k_out_stride[3];
+  int64_t offset_stride;  /* elements between the offsets of two sequences; 0: all share one row */
+} stand_rotation;
+
+/* Norms of queries and keys per head and the position rotation, in one pass (Sec. 5's target model needs them before
+ * stand_tree_attention).  Per row x of a head, in 32-bit floats, rounded once at the end:
+ *   y = norm ? x / sqrt(mean(x^2) + eps) * weight : x
+ *   (a, b) of pair i becomes (a cos t - b sin t, a sin t + b cos t),  t = (dev_base[b] + dev_offset[b, n]) * dev_freq[i]
+ * with the angle worked out in 64 bits (positions up to 2^31 in magnitude).  dev_weight_q, dev_weight_k [dim] of the rows' type (NULL: ones).
+ * dev_freq [rotary_dim / 2] float.  dev_base [B] int64 (NULL: 0) is what a sequence's positions begin with, dev_offset int32 what a node adds:
+ * [N] or [B, N] (NULL: its number n).  Outputs may be the inputs themselves (same pointer and strides); they must not
+ * overlap them otherwise. */
+int stand_rotate_heads(const stand_rotation* shape, const void* dev_q, const void* dev_k, const void* dev_weight_q,
+                       const void* dev_weight_k, const float* dev_freq, const int64_t* dev_base, const int32_t* dev_offset,
+                       void* dev_q_out, void* dev_k_out, void* cu_stream);
+
+/* The shapes of stand_kv_append and stand_kv_read (zero the structure first). */
+typedef struct {
+  int32_t layers, B, N;    /* N nodes per sequence in the source; layers up to 4096 */
+  int32_t heads, dim;      /* up to 4096; 1..256 */
+  int32_t dtype;           /* of the rows, and of a cache that is not packed */
+  int32_t page_size, pages; /* page_size up to 4096 */
+  int32_t width;           /* columns of dev_slots and dev_path */
+  int32_t packed;          /* 1: the caches are in the 4-bit form */
+  int32_t rotary_dim, interleaved, norm;  /* of the keys, as in stand_rotation */
+  float eps;
+  int32_t reserved, reserved2; /* must be 0 */
+  int64_t k_stride[4], v_stride[4];  /* elements: layer, sequence, node, head */
+  int64_t cache_stride[4]; /* layer, page, head, token, in elements; packed: layer, page, head in bytes (multiples of 16), then 0 */
+  int64_t offset_stride;
+} stand_kv_rows;
+
+/* stand_kv_commit with norm and rotation of the keys, and the 4-bit form, on the way: row (l, b, dev_path[b, j], h) of dev_k -
+ * normalised and turned as by stand_rotate_heads, dev_weight_k [layers, dim] - and of dev_v goes to slot dev_slots[b, j].  A packed
+ * cache gets what a cache of the rows' type would hold, in 4 bits.  dev_path NULL: node j.  Places with a slot
+ * outside [0, pages * page_size) or a node outside [0, N) are skipped.  Slots of one call must be distinct; the
+ * source must not overlap the caches.  Nothing but the slots' own bytes is written. */
+int stand_kv_append(const stand_kv_rows* shape, const void* dev_k, const void* dev_v, const void* dev_weight_k,
+                    const float* dev_freq, const int64_t* dev_base, const int32_t* dev_offset, const int32_t* dev_path,
+                    const int64_t* dev_slots, void* dev_cache_k, void* dev_cache_v, void* cu_stream);
+
+/* Rows of the cache as values of type dtype (any for a packed cache): dev_k, dev_v [layers, B, width, heads, dim], contiguous.
+ * Places with a slot outside the pool give zeros.  The fields of the source rows and of norm and rotation are not used: 0. */
+int stand_kv_read(const stand_kv_rows* shape, const void* dev_cache_k, const void* dev_cache_v, const int64_t* dev_slots,
+                  void* dev_k, void* dev_v, void* cu_stream);
+
+/* stand_tree_attention over packed caches: the same shapes, arguments, scratch and results, with cached keys and values what
+ * their codes stand for.  dim is a multiple of 16; cache_stride: page and head in bytes (multiples of 16), then 0; caches
+ * begin at multiples of 16 bytes.  The nodes' own keys and values are of type dtype. */
+int stand_packed_tree_attention(const stand_attention* shape, const void* dev_q, const void* dev_k, const void* dev_v,
+                                const void* dev_cache_k, const void* dev_cache_v, const int32_t* dev_table,
+                                const int64_t* dev_len, const uint32_t* dev_mask, int64_t mask_stride,
+                                const int32_t* dev_tree_tokens, void* dev_scratch, size_t scratch_bytes, void* dev_out,
+                                float* dev_lse, void* cu_stream);
+
 /* How many kernels the library has launched through this context so far. */
 uint64_t stand_launch_count(const stand_ctx* ctx);
 

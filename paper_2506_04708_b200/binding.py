@@ -24,7 +24,8 @@ EXPORTS = [
     "stand_state_load", "stand_profile_row_pass", "stand_profile_stages", "stand_node_accepts", "stand_prune_tree",
     "stand_initial_tree", "stand_launch_count", "stand_set_wait_limit", "stand_strerror",
     "stand_tree_attention_scratch_bytes", "stand_tree_attention", "stand_tree_mask", "stand_page_map",
-    "stand_page_release", "stand_kv_commit", "stand_process_logits",
+    "stand_page_release", "stand_kv_commit", "stand_process_logits", "stand_rotate_heads", "stand_kv_append", "stand_kv_read",
+    "stand_packed_tree_attention",
 ]
 
 
@@ -60,6 +61,25 @@ class StandKvShape(C.Structure):
         ("dtype", C.c_int32), ("page_size", C.c_int32), ("pages", C.c_int32), ("width", C.c_int32),
         ("reserved", C.c_int32), ("src_stride", C.c_int64 * 4), ("cache_stride", C.c_int64 * 4),
         ("v_stride", C.c_int64 * 4), ("own_v_stride", C.c_int32), ("reserved2", C.c_int32),
+    ]
+
+
+class StandRotation(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("N", C.c_int32), ("heads_q", C.c_int32), ("heads_kv", C.c_int32), ("dim", C.c_int32),
+        ("dtype", C.c_int32), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float),
+        ("reserved", C.c_int32), ("reserved2", C.c_int32), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
+        ("q_out_stride", C.c_int64 * 3), ("k_out_stride", C.c_int64 * 3), ("offset_stride", C.c_int64),
+    ]
+
+
+class StandKvRows(C.Structure):
+    _fields_ = [
+        ("layers", C.c_int32), ("B", C.c_int32), ("N", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32),
+        ("dtype", C.c_int32), ("page_size", C.c_int32), ("pages", C.c_int32), ("width", C.c_int32), ("packed", C.c_int32),
+        ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float),
+        ("reserved", C.c_int32), ("reserved2", C.c_int32), ("k_stride", C.c_int64 * 4), ("v_stride", C.c_int64 * 4),
+        ("cache_stride", C.c_int64 * 4), ("offset_stride", C.c_int64),
     ]
 
 
@@ -154,6 +174,14 @@ def lib():
     L.stand_page_release.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]
     L.stand_kv_commit.restype = C.c_int
     L.stand_kv_commit.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+    L.stand_rotate_heads.restype = C.c_int
+    L.stand_rotate_heads.argtypes = [vp] * 11
+    L.stand_kv_append.restype = C.c_int
+    L.stand_kv_append.argtypes = [vp] * 12
+    L.stand_kv_read.restype = C.c_int
+    L.stand_kv_read.argtypes = [vp] * 7
+    L.stand_packed_tree_attention.restype = C.c_int
+    L.stand_packed_tree_attention.argtypes = L.stand_tree_attention.argtypes
     L.stand_process_logits.restype = C.c_int
     L.stand_process_logits.argtypes = [vp, vp, vp, vp, vp]
     for name in ["stand_init", "stand_destroy", "stand_reset_sequences", "stand_verify_tree", "stand_ngram_update",

@@ -10,6 +10,7 @@
 #include "attention_plain.cuh"
 #include "attention_tensor.cuh"
 #include "launch.cuh"
+#include "packed.cuh"
 
 using namespace stand;
 
@@ -42,12 +43,18 @@ size_t stand_tree_attention_scratch_bytes(const stand_attention* c) {
   return tensor > plain ? tensor : plain;  // alignment decides, and that is not known here
 }
 
-int stand_tree_attention(const stand_attention* c, const void* dev_q, const void* dev_k, const void* dev_v, const void* dev_cache_k,
-                         const void* dev_cache_v, const int32_t* dev_table, const int64_t* dev_len, const uint32_t* dev_mask,
+}  // extern "C"
+
+namespace {
+
+int attention_call(const stand_attention* c, bool packed, const void* dev_q, const void* dev_k, const void* dev_v, const void* dev_cache_k,
+                   const void* dev_cache_v, const int32_t* dev_table, const int64_t* dev_len, const uint32_t* dev_mask,
                          int64_t mask_stride, const int32_t* dev_tree_tokens, void* dev_scratch, size_t scratch_bytes, void* dev_out,
                          float* dev_lse, void* cu_stream) {
   if (!attention_valid(c) || !dev_q || !dev_k || !dev_v || !dev_len || !dev_out) return STAND_E_ARG;
   if (c->max_pages > 0 && (!dev_table || !dev_cache_k || !dev_cache_v)) return STAND_E_ARG;
+  if (packed && (c->dim % PK_GROUP != 0 || c->cache_stride[2] != 0 || ((c->cache_stride[0] | c->cache_stride[1]) & 15) != 0 || !aligned(16, dev_cache_k, dev_cache_v)))
+    return STAND_E_ARG;
   if (!aligned(c->dtype == STAND_DTYPE_F32 ? 4 : 2, dev_q, dev_k, dev_v, dev_cache_k, dev_cache_v, dev_out) || !aligned(8, dev_len) ||
       !aligned(4, dev_table, dev_mask, dev_tree_tokens, dev_lse))
     return STAND_E_ARG;
@@ -69,6 +76,11 @@ int stand_tree_attention(const stand_attention* c, const void* dev_q, const void
   cudaStream_t st = (cudaStream_t)cu_stream;
   int dev = -1, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return STAND_E_CUDA;
+  if (packed) {
+    if (c->dtype == STAND_DTYPE_F32) return launch_plain_attention<float, true>(p, dev_scratch, sms, st);
+    if (c->dtype == STAND_DTYPE_BF16) return launch_plain_attention<__nv_bfloat16, true>(p, dev_scratch, sms, st);
+    return launch_plain_attention<__half, true>(p, dev_scratch, sms, st);
+  }
   if (tensor_takes(p, c->dtype)) {
     const int dp = tensor_dim(p.dim);
     const bool bf = c->dtype == STAND_DTYPE_BF16;
@@ -82,6 +94,26 @@ int stand_tree_attention(const stand_attention* c, const void* dev_q, const void
   if (c->dtype == STAND_DTYPE_F32) return launch_plain_attention<float>(p, dev_scratch, sms, st);
   if (c->dtype == STAND_DTYPE_BF16) return launch_plain_attention<__nv_bfloat16>(p, dev_scratch, sms, st);
   return launch_plain_attention<__half>(p, dev_scratch, sms, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int stand_tree_attention(const stand_attention* c, const void* dev_q, const void* dev_k, const void* dev_v, const void* dev_cache_k,
+                         const void* dev_cache_v, const int32_t* dev_table, const int64_t* dev_len, const uint32_t* dev_mask,
+                         int64_t mask_stride, const int32_t* dev_tree_tokens, void* dev_scratch, size_t scratch_bytes, void* dev_out,
+                         float* dev_lse, void* cu_stream) {
+  return attention_call(c, false, dev_q, dev_k, dev_v, dev_cache_k, dev_cache_v, dev_table, dev_len, dev_mask, mask_stride, dev_tree_tokens,
+                        dev_scratch, scratch_bytes, dev_out, dev_lse, cu_stream);
+}
+
+int stand_packed_tree_attention(const stand_attention* c, const void* dev_q, const void* dev_k, const void* dev_v, const void* dev_cache_k,
+                                const void* dev_cache_v, const int32_t* dev_table, const int64_t* dev_len, const uint32_t* dev_mask,
+                                int64_t mask_stride, const int32_t* dev_tree_tokens, void* dev_scratch, size_t scratch_bytes, void* dev_out,
+                                float* dev_lse, void* cu_stream) {
+  return attention_call(c, true, dev_q, dev_k, dev_v, dev_cache_k, dev_cache_v, dev_table, dev_len, dev_mask, mask_stride, dev_tree_tokens,
+                        dev_scratch, scratch_bytes, dev_out, dev_lse, cu_stream);
 }
 
 int stand_tree_mask(const int32_t* host_parent, int32_t n, uint32_t* host_mask) {

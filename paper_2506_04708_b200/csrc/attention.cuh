@@ -30,7 +30,7 @@ struct AttnParams {
   float* lse;
   int B, N, heads_q, heads_kv, group, dim, page, pages, cols, mask_words;
   float scale2;  // scale * log2(e)
-  long long q_stride[3], k_stride[3], v_stride[3], cache_stride[3];  // elements
+  long long q_stride[3], k_stride[3], v_stride[3], cache_stride[3];  // elements (packed cache: bytes)
 };
 
 template <typename T> __device__ __forceinline__ float to_float(T v);
@@ -69,7 +69,22 @@ __device__ __forceinline__ bool attn_sees(const AttnParams& p, int b, int u, int
 // key which a lane only carries along - or a row that does not see it.  So an element that is NaN although the row's
 // weights are in order is settled by a second look at the values, for all kernels with this: the sum of the values that are
 // not finite in element d among the cached tokens k0 .. k1 - 1 of sequence b.  Zero: there are none (such a sum is never zero).
-template <typename T> __device__ __forceinline__ float attn_odd_cached(const AttnParams& p, int b, int g, int d, int k0, int k1) {
+// (A packed group is finite or NaN throughout.)
+template <typename T, bool PACKED = false> __device__ __forceinline__ float attn_odd_cached(const AttnParams& p, int b, int g, int d, int k0, int k1) {
+  if constexpr (PACKED) {
+    bool bad = false;
+    const unsigned char* scales = reinterpret_cast<const unsigned char*>(p.cache_v) + g * p.cache_stride[1] + (long long)p.page * (p.dim / 2) + d / 16;
+    for (int k = k0; k < k1 && !bad; k += 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int pos = k + i, col = pos / p.page;
+        if (pos >= k1) continue;
+        const int page = p.table[(long long)b * p.cols + col];
+        if (page >= 0 && page < p.pages) bad = bad || scales[page * p.cache_stride[0] + (pos - col * p.page) * (p.dim / 16)] >= 0xF8;
+      }
+    }
+    return bad ? NAN : 0.0f;
+  }
   const T* cache = reinterpret_cast<const T*>(p.cache_v) + g * p.cache_stride[1] + d;
   float sum = 0.0f;
   for (int k = k0; k < k1 && !isnan(sum); k += 8) {

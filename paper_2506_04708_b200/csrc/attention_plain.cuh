@@ -15,6 +15,7 @@
 #include "async.cuh"
 #include "attention_split.cuh"
 #include "launch.cuh"
+#include "packed.cuh"
 
 namespace stand {
 
@@ -54,9 +55,9 @@ template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.as
 
 // An element that came out as NaN though its row's weights are in order: with the values that are not finite among what the
 // row sees, cached tokens k0 .. k1 - 1 and nodes n0 .. n1 - 1.  Rare, so it only has to be right.
-template <typename T>
+template <typename T, bool PACKED>
 __device__ __noinline__ float plain_settle(const AttnParams& p, int b, int g, int u, int d, int k0, int k1, int n0, int n1, float o) {
-  float sum = attn_odd_cached<T>(p, b, g, d, k0, k1);
+  float sum = attn_odd_cached<T, PACKED>(p, b, g, d, k0, k1);
   const T* tree = reinterpret_cast<const T*>(p.v) + b * p.v_stride[0] + g * p.v_stride[2] + d;
   for (int v = n0; v < n1 && v <= u && !isnan(sum); ++v) {
     const float f = to_float(tree[v * p.v_stride[1]]);
@@ -66,13 +67,14 @@ __device__ __noinline__ float plain_settle(const AttnParams& p, int b, int g, in
 }
 
 // wide: bases and strides allow 4 elements at a time
-template <typename T, int DP>
+template <typename T, int DP, bool PACKED>
 __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __grid_constant__ TaSplit p, const bool wide) {
   using Sh = PaShape<DP>;
   constexpr int KT = TA_KT, KP = Sh::KP, STAGES = Sh::STAGES, R = PA_ROWS / PA_WARPS, E = DP / 32;
   constexpr int EV = E < 4 ? E : 4;  // elements of the head size that lie together: lane * EV + 128 * i
   extern __shared__ float pa_smem[];
   __shared__ const T* s_src[3][2][KT];  // where keys and values of a tile lie; null: zeros
+  __shared__ const unsigned char* s_scale[PACKED ? 3 : 1][2][KT];  // a packed row's scales (its codes lie at s_src); null: a tree's row
   __shared__ TaRange<PA_THREADS> s_range;
   float* const sq = pa_smem + STAGES * Sh::STAGE;                      // [PA_ROWS][KP]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, D = p.a.dim, D4 = (D + 3) & ~3;
@@ -98,11 +100,19 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
       if (tile >= s.end) return;
       const int key = i % KT, which = i / KT;
       const T* src = nullptr;
+      const unsigned char* scale = nullptr;
       if (tile < s.p_tiles) {
         const int pos = tile * KT + key, c = pos / p.a.page;
         if (pos < s.len) {
           const int page = p.a.table[(long long)s.b * p.a.cols + c];
-          if (page >= 0 && page < p.a.pages)
+          if (PACKED) {
+            if (page >= 0 && page < p.a.pages) {
+              const unsigned char* block = reinterpret_cast<const unsigned char*>(cache[which]) + page * p.a.cache_stride[0] + s.g * p.a.cache_stride[1];
+              const int token = pos - c * p.a.page;
+              src = reinterpret_cast<const T*>(block + token * (D / 2));
+              scale = block + (long long)p.a.page * (D / 2) + token * (D / 16);
+            }
+          } else if (page >= 0 && page < p.a.pages)
             src = cache[which] + page * p.a.cache_stride[0] + s.g * p.a.cache_stride[1] + (long long)(pos - c * p.a.page) * p.a.cache_stride[2];
         }
       } else {
@@ -111,11 +121,28 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
         if (node < p.a.N) src = kv[which] + s.b * stride[0] + node * stride[1] + s.g * stride[2];
       }
       s_src[tile % 3][which][key] = src;
+      if (PACKED) s_scale[tile % 3][which][key] = scale;
     };
     auto fetch = [&](int tile) {
       if (tile < s.end) {
         float* const base = pa_smem + (tile % STAGES) * Sh::STAGE;
-        if (wide) {
+        if (PACKED && tile < s.p_tiles) {
+          const int groups = D / PK_GROUP;
+          for (int i = tid; i < 2 * KT * groups; i += PA_THREADS) {
+            const int row = i / groups, c = i - row * groups, key = row % KT;
+            const unsigned char* scales = s_scale[tile % 3][row / KT][key];
+            float* dst = (row < KT ? base + key * KP : base + KT * KP + key * DP) + c * PK_GROUP;
+            float v[PK_GROUP] = {};
+            if (scales) {
+              const uint2 w = reinterpret_cast<const uint2*>(s_src[tile % 3][row / KT][key])[c];
+              const float scale = pk_scale(scales[c]);
+              pk_values(w.x, scale, v);
+              pk_values(w.y, scale, v + 8);
+            }
+#pragma unroll
+            for (int e = 0; e < PK_GROUP; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+          }
+        } else if (wide) {
           const int quads = D / 4;
           for (int i = tid; i < 2 * KT * quads; i += PA_THREADS) {
             const int row = i / quads, q = i - row * quads, key = row % KT;
@@ -324,7 +351,7 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
         for (int e = 0; e < E; ++e) {
           const int d = lane * EV + e / EV * 128 + e % EV;
           if (isnan(o[i][e]) && d < D)
-            o[i][e] = plain_settle<T>(p.a, s.b, s.g, node[i], d, s.begin * KT, k1 < s.len ? k1 : s.len, n0 * KT, n1 * KT, o[i][e]);
+            o[i][e] = plain_settle<T, PACKED>(p.a, s.b, s.g, node[i], d, s.begin * KT, k1 < s.len ? k1 : s.len, n0 * KT, n1 * KT, o[i][e]);
         }
       }
       if (lane == 0) {
@@ -342,29 +369,30 @@ __global__ void __launch_bounds__(PA_THREADS) plain_attention_kernel(const __gri
   if (tid == 0 && blockIdx.x % p.group_ctas == 0) p.records[blockIdx.x / p.group_ctas] = note.r;
 }
 
-template <typename T, int DP> int launch_plain_rows(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
+template <typename T, int DP, bool PACKED> int launch_plain_rows(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
   TaSplit p;
   // A piece's fixed cost in tiles: with 0, 1, 3, 6 16 x 8 nodes of heads of 128 over 10 - 1,000 take 66, 63, 66, 75 us, 32 x 16 nodes of heads
   // of 64 over 500 - 4,000 261, 259, 268, 285.
   ta_split(p, a, PA_ROWS, DP, sms, plain_ctas(DP), 1, scratch);
   const size_t al = 4 * sizeof(T);
-  uintptr_t bits = (uintptr_t)a.k | (uintptr_t)a.v | (a.cols > 0 ? (uintptr_t)a.cache_k | (uintptr_t)a.cache_v : 0);
-  for (int i = 0; i < 3; ++i) bits |= (uintptr_t)((a.k_stride[i] | a.v_stride[i]) * sizeof(T)) | (a.cols > 0 ? (uintptr_t)(a.cache_stride[i] * sizeof(T)) : 0);
+  const bool cached = !PACKED && a.cols > 0;
+  uintptr_t bits = (uintptr_t)a.k | (uintptr_t)a.v | (cached ? (uintptr_t)a.cache_k | (uintptr_t)a.cache_v : 0);
+  for (int i = 0; i < 3; ++i) bits |= (uintptr_t)((a.k_stride[i] | a.v_stride[i]) * sizeof(T)) | (cached ? (uintptr_t)(a.cache_stride[i] * sizeof(T)) : 0);
   const bool wide = bits % al == 0 && a.dim % 4 == 0;
   static SmemLimit limit;
   const int smem = PaShape<DP>::SMEM;
-  int rc = limit.raise(plain_attention_kernel<T, DP>, smem);
+  int rc = limit.raise(plain_attention_kernel<T, DP, PACKED>, smem);
   if (rc) return rc;
-  rc = launch_dependent2(plain_attention_kernel<T, DP>, dim3((unsigned)(p.groups * p.group_ctas)), PA_THREADS, st, (size_t)smem, p, wide);
+  rc = launch_dependent2(plain_attention_kernel<T, DP, PACKED>, dim3((unsigned)(p.groups * p.group_ctas)), PA_THREADS, st, (size_t)smem, p, wide);
   if (rc) return rc;
   return launch_join<DP, T>(p, st);
 }
 
-template <typename T> int launch_plain_attention(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
+template <typename T, bool PACKED = false> int launch_plain_attention(const AttnParams& a, void* scratch, int sms, cudaStream_t st) {
   const int dp = tensor_dim(a.dim);
-  if (dp == 64) return launch_plain_rows<T, 64>(a, scratch, sms, st);
-  if (dp == 128) return launch_plain_rows<T, 128>(a, scratch, sms, st);
-  return launch_plain_rows<T, 256>(a, scratch, sms, st);
+  if (dp == 64) return launch_plain_rows<T, 64, PACKED>(a, scratch, sms, st);
+  if (dp == 128) return launch_plain_rows<T, 128, PACKED>(a, scratch, sms, st);
+  return launch_plain_rows<T, 256, PACKED>(a, scratch, sms, st);
 }
 
 }  // namespace stand

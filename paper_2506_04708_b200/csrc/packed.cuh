@@ -1,0 +1,83 @@
+// The 4-bit form of cached rows.
+//
+// A row's elements in groups of 16: a scale s of 8 bits - 5 exponent bits (bias 15), 3 fraction bits, no sign, subnormals, the
+// bits of a half between its sign and its last seven - and 16 whole numbers k of -8 .. 7 as k + 8 in 4 bits; an element is k s.
+// That has at most 7 significant bits: exact in bfloat16 and in half, so products of values are those of the definition.
+// s is the smallest with 7 s >= the group's largest magnitude, k the nearest whole number (even in a tie).  Exponent 31: not finite,
+// the whole group reads as NaN.
+// Four bytes hold 8 elements: the even ones in the low half, the odd ones in the high half, each from the low bits on, so that one
+// mask brings two neighbours into the two halves of a word.
+// A block is one head's tokens of one page: the codes of all tokens (dim / 2 bytes each), then their scales (dim / 16 each).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace stand {
+
+constexpr int PK_GROUP = 16;
+constexpr uint32_t PK_BAD = 0xF8;         // scales from here on are not finite
+constexpr uint32_t PK_LAST = 0xF7;        // the largest scale: 61440
+constexpr float PK_MOST = 7.0f * 61440.0f;
+
+__host__ __device__ __forceinline__ long long pk_block_bytes(int page, int dim) { return (long long)page * dim / 2 + (long long)page * dim / 16; }
+
+__device__ __forceinline__ float pk_scale(uint32_t byte) {
+  return byte >= PK_BAD ? __uint_as_float(0x7FC00000u) : __half2float(__ushort_as_half((unsigned short)(byte << 7)));
+}
+
+// The scale of a group whose largest magnitude has these bits (of a 32-bit float without its sign; NaN and infinity are the
+// largest).  A first guess by rounding amax / 7 up, then put right by the definition, since 7 s is exact.
+__device__ __forceinline__ uint32_t pk_scale_byte(uint32_t amax_bits) {
+  if (amax_bits >= 0x7F800000u) return 0xFF;
+  const float amax = __uint_as_float(amax_bits), t = amax * (1.0f / 7.0f);
+  uint32_t b;
+  if (t >= 0x1p-14f) {
+    b = (__float_as_uint(t) + 0xFFFFFu) >> 20;
+    b -= 112u << 3;
+    b = b > PK_LAST ? PK_LAST : b;
+  } else {
+    b = (uint32_t)ceilf(t * 0x1p17f);
+  }
+  if (b < PK_LAST && 7.0f * pk_scale(b) < amax) ++b;
+  else if (b > 0 && 7.0f * pk_scale(b - 1) >= amax) --b;
+  return b;
+}
+
+// The codes of 16 elements.  Elements of 16 bits: an element has at most 11 significant bits and s has 4, so a quotient that is
+// no tie is at least 2^-12 from one; the product with the reciprocal is off by 7 * 2^-23 at most, and rounding it to multiples
+// of 2^-13 first makes a tie one again.  32 bits: the quotient rounded to 32 bits, then to a whole number.
+template <bool EXACT_TIES>
+__device__ __forceinline__ uint2 pk_codes(const float (&y)[PK_GROUP], uint32_t byte) {
+  if (byte == 0 || byte >= PK_BAD) return make_uint2(0x88888888u, 0x88888888u);
+  const float s = pk_scale(byte), inv = 1.0f / s;
+  uint32_t k[PK_GROUP];
+#pragma unroll
+  for (int i = 0; i < PK_GROUP; ++i) {
+    float r;
+    if (EXACT_TIES) r = fmaf(y[i], inv, 1536.0f) - 1536.0f;
+    else r = __fdiv_rn(y[i], s);
+    r = fminf(fmaxf(r, -7.0f), 7.0f);  // only beyond the largest scale
+    k[i] = __float_as_uint(r + (12582912.0f + 8.0f)) & 15u;  // the whole number + 8 in the last bits
+  }
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t* e = k + 8 * h;
+    w[h] = e[0] | e[2] << 4 | e[4] << 8 | e[6] << 12 | e[1] << 16 | e[3] << 20 | e[5] << 24 | e[7] << 28;
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+// 8 elements of a word as floats.
+__device__ __forceinline__ void pk_values(uint32_t w, float s, float* v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = (float)((int)(w >> (4 * i) & 15u) - 8) * s;
+    v[2 * i + 1] = (float)((int)(w >> (4 * i + 16) & 15u) - 8) * s;
+  }
+}
+
+}  // namespace stand

@@ -1,0 +1,428 @@
+// Norms of queries and keys per head with the position rotation in the same pass; rows into the paged cache with both on the way,
+// in their own type or in 4 bits; rows of the cache back as values.
+#include "../../include/stand.h"
+
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "launch.cuh"
+#include "packed.cuh"
+#include "rotation.cuh"
+
+using namespace stand;
+
+namespace {
+
+constexpr int ROT_THREADS = 256;
+constexpr int ROW_COUNT = 4096;  // layers, heads: their product counts rows in 32 bits
+constexpr int ROT_TOKENS = 16;  // tokens of a block, at most: their cosines and sines lie in shared memory
+
+// A digit of a row number that counts in steps: no divisions in the loop.
+struct Step {
+  int h, l, t;  // heads, layers, tokens
+  __device__ __forceinline__ Step(int i, int heads, int layers) : h(i % heads), l(i / heads % layers), t(i / heads / layers) {}
+  __device__ __forceinline__ void add(const Step& o, int heads, int layers) {
+    h += o.h;
+    l += o.l;
+    t += o.t;
+    if (h >= heads) h -= heads, ++l;
+    if (l >= layers) l -= layers, ++t;
+  }
+};
+
+// The block's table of cosines and sines; the caller's barrier follows.
+template <typename F> __device__ __forceinline__ void turn_tables(const Turn& t, float* cs, int tokens, F position) {
+  const int floats = turn_floats(t.columns, t.pairs);
+  for (int i = threadIdx.x; i < tokens * t.half; i += ROT_THREADS) {
+    const int tok = i / t.half, k = i - tok * t.half;
+    float c, s;
+    turn_angle(position(tok), t.freq[k], c, s);
+    float* at = cs + tok * 2 * floats + turn_at(t, k);
+    at[0] = c;
+    at[floats] = s;
+  }
+}
+
+struct RotateParams {
+  Turn t;
+  const void* q;
+  const void* k;
+  void* q_out;
+  void* k_out;
+  const void* weight_q;
+  const void* weight_k;
+  int B, N, heads_q, heads;  // heads: of queries and keys together
+  int tokens;                // of a block
+  int heads_block;           // heads of a block (grid.y blocks share a token's heads)
+  long long q_in[3], k_in[3], q_to[3], k_to[3];
+};
+
+template <typename T, bool WIDE> __global__ void __launch_bounds__(ROT_THREADS) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
+  extern __shared__ __align__(16) float rot_cs[];
+  pdl_trigger();
+  pdl_wait();
+  const int tid = threadIdx.x, lanes = p.t.lanes, c = tid & (lanes - 1), group = tid / lanes, groups = ROT_THREADS / lanes;
+  const long long first = (long long)blockIdx.x * p.tokens, all = (long long)p.B * p.N;
+  const int tokens = all - first < p.tokens ? (int)(all - first) : p.tokens;
+  const int h0 = blockIdx.y * p.heads_block, heads = p.heads - h0 < p.heads_block ? p.heads - h0 : p.heads_block;
+  const int floats = 2 * turn_floats(p.t.columns, p.t.pairs);
+  if (p.t.freq) {
+    turn_tables(p.t, rot_cs, tokens, [&](int tok) {
+      const long long at = first + tok;
+      const int b = (int)(at / p.N);
+      return turn_position(p.t, b, (int)(at - (long long)b * p.N));
+    });
+    __syncthreads();
+  }
+  const int rows = tokens * heads;
+  const Step step(groups, heads, 1);
+  Step at(group, heads, 1);
+  int tok_b = (int)(first / p.N), tok_n = (int)(first - (long long)tok_b * p.N);  // of the block's first token
+  for (int r = group; r - group < rows; r += groups, at.add(step, heads, 1)) {
+    const bool in = r < rows, there = in && c * ROT_E < p.t.dim;
+    const int tok = at.t + at.l, head = h0 + at.h;  // one layer: its carry goes to the token
+    int b = tok_b, n = tok_n + tok;
+    while (n >= p.N) n -= p.N, ++b;
+    const bool is_q = head < p.heads_q;
+    const int h = is_q ? head : head - p.heads_q;
+    const long long* in_s = is_q ? p.q_in : p.k_in;
+    const T* row = reinterpret_cast<const T*>(is_q ? p.q : p.k) + b * in_s[0] + n * in_s[1] + h * in_s[2];
+    const T* weight = reinterpret_cast<const T*>(is_q ? p.weight_q : p.weight_k);
+    float y[ROT_E];
+    row_group<T, WIDE>(p.t, row, weight, rot_cs + tok * floats, c, there, true, p.t.freq != nullptr, y);
+    __syncwarp();  // in place: all lanes of a row have read
+    if (!there) continue;
+    const long long* out_s = is_q ? p.q_to : p.k_to;
+    T* to = reinterpret_cast<T*>(is_q ? p.q_out : p.k_out) + b * out_s[0] + n * out_s[1] + h * out_s[2] + c * ROT_E;
+    if (WIDE) {
+      store_row16(to, y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < ROT_E; ++i)
+        if (c * ROT_E + i < p.t.dim) to[i] = from_float<T>(y[i]);
+    }
+  }
+}
+
+struct AppendParams {
+  Turn t;
+  const void* k;
+  const void* v;
+  const void* weight;
+  const int* path;
+  const long long* slots;
+  char* cache_k;
+  char* cache_v;
+  int layers, N, width, heads, page;
+  long long places;  // B * width
+  int tokens, layers_block;
+  long long n_slots;
+  long long k_in[4], v_in[4];  // elements
+  long long to[4];             // bytes: layer, page, head, token
+};
+
+template <typename T, bool WIDE, bool PACKED>
+__global__ void __launch_bounds__(ROT_THREADS) kv_append_kernel(const __grid_constant__ AppendParams p) {
+  extern __shared__ __align__(16) float rot_cs[];
+  __shared__ long long s_page[ROT_TOKENS];  // -1: nothing is stored
+  __shared__ int s_b[ROT_TOKENS], s_node[ROT_TOKENS], s_token[ROT_TOKENS];
+  pdl_trigger();
+  pdl_wait();
+  const int tid = threadIdx.x, lanes = p.t.lanes, c = tid & (lanes - 1), group = tid / lanes, groups = ROT_THREADS / lanes;
+  const long long first = (long long)blockIdx.x * p.tokens;
+  const int tokens = p.places - first < p.tokens ? (int)(p.places - first) : p.tokens;
+  const int l0 = blockIdx.y * p.layers_block, layers = p.layers - l0 < p.layers_block ? p.layers - l0 : p.layers_block;
+  const int floats = 2 * turn_floats(p.t.columns, p.t.pairs);
+  if (tid < tokens) {
+    const long long place = first + tid, slot = p.slots[place];
+    const int b = (int)(place / p.width), j = (int)(place - (long long)b * p.width), node = p.path ? p.path[place] : j;
+    const long long page = slot >= 0 && slot < p.n_slots && node >= 0 && node < p.N ? slot / p.page : -1;
+    s_page[tid] = page;
+    s_token[tid] = (int)(slot - page * p.page);
+    s_b[tid] = b;
+    s_node[tid] = node;
+  }
+  __syncthreads();
+  if (p.t.freq) {
+    turn_tables(p.t, rot_cs, tokens, [&](int tok) { return s_page[tok] < 0 ? 0ll : turn_position(p.t, s_b[tok], s_node[tok]); });
+    __syncthreads();
+  }
+  const int heads = 2 * p.heads, rows = tokens * layers * heads;
+  const Step step(groups, heads, layers);
+  Step at(group, heads, layers);
+  for (int r = group; r - group < rows; r += groups, at.add(step, heads, layers)) {
+    const bool in = r < rows;
+    const int tok = in ? at.t : 0, l = l0 + at.l;
+    const long long page = s_page[tok];
+    const bool there = in && page >= 0 && c * ROT_E < p.t.dim, is_v = at.h >= p.heads;
+    const int h = is_v ? at.h - p.heads : at.h;
+    const long long* in_s = is_v ? p.v_in : p.k_in;
+    const T* row = reinterpret_cast<const T*>(is_v ? p.v : p.k) + l * in_s[0] + s_b[tok] * in_s[1] + s_node[tok] * in_s[2] + h * in_s[3];
+    const T* weight = p.weight ? reinterpret_cast<const T*>(p.weight) + (long long)l * p.t.dim : nullptr;
+    float y[ROT_E];
+    row_group<T, WIDE>(p.t, row, weight, rot_cs + tok * floats, c, there, !is_v, !is_v && p.t.freq, y);
+    if (!there) continue;
+    const int token = s_token[tok];
+    char* to = (is_v ? p.cache_v : p.cache_k) + l * p.to[0] + page * p.to[1] + h * p.to[2];
+    if constexpr (PACKED) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < ROT_E; ++i) {
+        y[i] = to_float(from_float<T>(y[i]));  // what a cache of this type would hold
+        const uint32_t bits = __float_as_uint(y[i]) & 0x7FFFFFFFu;
+        most = bits > most ? bits : most;
+      }
+      const uint32_t byte = pk_scale_byte(most);
+      *reinterpret_cast<uint2*>(to + token * (p.t.dim / 2) + c * 8) = pk_codes<sizeof(T) == 2>(y, byte);
+      to[(long long)p.page * (p.t.dim / 2) + token * (p.t.dim / 16) + c] = (char)byte;
+    } else {
+      T* out = reinterpret_cast<T*>(to + token * p.to[3]) + c * ROT_E;
+      if (WIDE) {
+        store_row16(out, y);
+      } else {
+#pragma unroll
+        for (int i = 0; i < ROT_E; ++i)
+          if (c * ROT_E + i < p.t.dim) out[i] = from_float<T>(y[i]);
+      }
+    }
+  }
+}
+
+struct ReadParams {
+  const char* cache_k;
+  const char* cache_v;
+  const long long* slots;
+  void* k_out;
+  void* v_out;
+  int layers, heads, dim, page, lanes;
+  long long places, n_slots;
+  int tokens, layers_block;
+  long long from[4];  // bytes: layer, page, head, token
+};
+
+// A lane: 16 elements of a row.  Places without a slot give zeros.
+template <typename T, bool WIDE, bool PACKED>
+__global__ void __launch_bounds__(ROT_THREADS) kv_read_kernel(const __grid_constant__ ReadParams p) {
+  pdl_trigger();
+  pdl_wait();
+  __shared__ long long s_page[ROT_TOKENS];  // -1: no slot
+  __shared__ int s_token[ROT_TOKENS];
+  const int tid = threadIdx.x, c = tid & (p.lanes - 1), group = tid / p.lanes, groups = ROT_THREADS / p.lanes;
+  const long long first = (long long)blockIdx.x * p.tokens;
+  const int tokens = p.places - first < p.tokens ? (int)(p.places - first) : p.tokens;
+  const int l0 = blockIdx.y * p.layers_block, layers = p.layers - l0 < p.layers_block ? p.layers - l0 : p.layers_block;
+  if (tid < tokens) {
+    const long long slot = p.slots[first + tid], page = slot >= 0 && slot < p.n_slots ? slot / p.page : -1;
+    s_page[tid] = page;
+    s_token[tid] = (int)(slot - page * p.page);
+  }
+  __syncthreads();
+  if (c * ROT_E >= p.dim) return;
+  const int heads = 2 * p.heads, rows = tokens * layers * heads;
+  const Step step(groups, heads, layers);
+  Step at(group, heads, layers);
+  for (int r = group; r < rows; r += groups, at.add(step, heads, layers)) {
+    const long long place = first + at.t, page = s_page[at.t];
+    const int l = l0 + at.l;
+    const bool is_v = at.h >= p.heads;
+    const int h = is_v ? at.h - p.heads : at.h;
+    T* out = reinterpret_cast<T*>(is_v ? p.v_out : p.k_out) + ((l * p.places + place) * p.heads + h) * p.dim + c * ROT_E;
+    float y[ROT_E] = {};
+    if (page >= 0) {
+      const int token = s_token[at.t];
+      const char* from = (is_v ? p.cache_v : p.cache_k) + l * p.from[0] + page * p.from[1] + h * p.from[2];
+      if constexpr (PACKED) {
+        const uint2 w = *reinterpret_cast<const uint2*>(from + token * (p.dim / 2) + c * 8);
+        const float s = pk_scale((unsigned char)from[(long long)p.page * (p.dim / 2) + token * (p.dim / 16) + c]);
+        pk_values(w.x, s, y);
+        pk_values(w.y, s, y + 8);
+      } else {
+        const T* row = reinterpret_cast<const T*>(from + token * p.from[3]) + c * ROT_E;
+        if (WIDE) {
+          load_row16(row, y);
+        } else {
+#pragma unroll
+          for (int i = 0; i < ROT_E; ++i)
+            if (c * ROT_E + i < p.dim) y[i] = to_float(row[i]);
+        }
+      }
+    }
+    if (WIDE) {
+      store_row16(out, y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < ROT_E; ++i)
+        if (c * ROT_E + i < p.dim) out[i] = from_float<T>(y[i]);
+    }
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------
+bool fits16(const void* p, const long long* strides, int n, int es) {
+  uintptr_t bits = (uintptr_t)p;
+  for (int i = 0; i < n; ++i) bits |= (uintptr_t)(strides[i] * es);
+  return (bits & 15) == 0;
+}
+
+int element_size(int dtype) { return dtype == STAND_DTYPE_F32 ? 4 : 2; }
+bool type_valid(int dtype) { return dtype >= STAND_DTYPE_F32 && dtype <= STAND_DTYPE_F16; }
+
+// Tokens of a block: as many as make work for its threads (each group of lanes some rows), but no fewer blocks than fill the GPU.
+int tokens_per_block(long long places, int rows_of_token, int lanes) {
+  const int groups = ROT_THREADS / lanes;
+  int tokens = 1;
+  while (tokens < ROT_TOKENS && tokens * rows_of_token < 4 * groups && places / (2 * tokens) >= 2 * 148) tokens *= 2;
+  return tokens;
+}
+
+template <typename T> int launch_rotate(const RotateParams& p, bool wide, dim3 grid, size_t smem, cudaStream_t st) {
+  if (wide) return launch_dependent(rotate_heads_kernel<T, true>, grid, ROT_THREADS, st, p, smem);
+  return launch_dependent(rotate_heads_kernel<T, false>, grid, ROT_THREADS, st, p, smem);
+}
+template <typename T> int launch_append(const AppendParams& p, bool wide, bool packed, dim3 grid, size_t smem, cudaStream_t st) {
+  if (packed) {
+    if (wide) return launch_dependent(kv_append_kernel<T, true, true>, grid, ROT_THREADS, st, p, smem);
+    return launch_dependent(kv_append_kernel<T, false, true>, grid, ROT_THREADS, st, p, smem);
+  }
+  if (wide) return launch_dependent(kv_append_kernel<T, true, false>, grid, ROT_THREADS, st, p, smem);
+  return launch_dependent(kv_append_kernel<T, false, false>, grid, ROT_THREADS, st, p, smem);
+}
+template <typename T> int launch_read(const ReadParams& p, bool wide, bool packed, dim3 grid, cudaStream_t st) {
+  if (packed) {
+    if (wide) return launch_dependent(kv_read_kernel<T, true, true>, grid, ROT_THREADS, st, p);
+    return launch_dependent(kv_read_kernel<T, false, true>, grid, ROT_THREADS, st, p);
+  }
+  if (wide) return launch_dependent(kv_read_kernel<T, true, false>, grid, ROT_THREADS, st, p);
+  return launch_dependent(kv_read_kernel<T, false, false>, grid, ROT_THREADS, st, p);
+}
+
+// What both entry points that turn rows check and derive alike.
+bool make_turn(Turn& t, int dim, int rotary, int interleaved, int norm, float eps, const float* freq, const int64_t* base, const int32_t* offset,
+               int64_t offset_stride) {
+  if (dim < 1 || dim > ROT_DIM_MAX || rotary < 0 || rotary > dim || rotary % 2 != 0 || (rotary > 0) != (freq != nullptr)) return false;
+  if ((interleaved != 0 && interleaved != 1) || (norm != 0 && norm != 1) || offset_stride < 0) return false;
+  if (norm && !(eps > 0.0f && eps < INFINITY)) return false;
+  if (!aligned(4, freq, offset) || !aligned(8, base)) return false;
+  t.freq = freq; t.base = (const long long*)base; t.offset = offset; t.offset_stride = offset_stride;
+  t.half = rotary / 2; t.pairs = interleaved; t.columns = turn_columns(t.half, t.pairs); t.norm = norm; t.eps = eps; t.inv_dim = 1.0f / (float)dim;
+  t.dim = dim; t.lanes = row_lanes(dim);
+  return true;
+}
+
+bool packed_strides(const void* a, const void* b, const int64_t (&stride)[4]) {
+  if (stride[3] != 0) return false;
+  return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)stride[0] | (uintptr_t)stride[1] | (uintptr_t)stride[2]) & 15) == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int stand_rotate_heads(const stand_rotation* c, const void* dev_q, const void* dev_k, const void* dev_weight_q, const void* dev_weight_k,
+                       const float* dev_freq, const int64_t* dev_base, const int32_t* dev_offset, void* dev_q_out, void* dev_k_out,
+                       void* cu_stream) {
+  if (!c || !dev_q || !dev_k || !dev_q_out || !dev_k_out || c->B < 1 || c->N < 1 || c->heads_q < 1 || c->heads_kv < 1) return STAND_E_ARG;
+  if (!type_valid(c->dtype) || (c->reserved | c->reserved2) != 0 || c->heads_q > (1 << 16) || c->heads_kv > (1 << 16)) return STAND_E_ARG;
+  RotateParams p;
+  if (!make_turn(p.t, c->dim, c->rotary_dim, c->interleaved, c->norm, c->eps, dev_freq, dev_base, dev_offset, c->offset_stride)) return STAND_E_ARG;
+  if (!c->norm && (dev_weight_q || dev_weight_k)) return STAND_E_ARG;
+  const int es = element_size(c->dtype);
+  if (!aligned(es, dev_q, dev_k, dev_q_out, dev_k_out, dev_weight_q, dev_weight_k)) return STAND_E_ARG;
+  for (int i = 0; i < 3; ++i) {
+    p.q_in[i] = c->q_stride[i], p.k_in[i] = c->k_stride[i], p.q_to[i] = c->q_out_stride[i], p.k_to[i] = c->k_out_stride[i];
+    if (p.q_in[i] < 0 || p.k_in[i] < 0 || p.q_to[i] < 0 || p.k_to[i] < 0) return STAND_E_ARG;
+  }
+  p.q = dev_q; p.k = dev_k; p.q_out = dev_q_out; p.k_out = dev_k_out; p.weight_q = dev_weight_q; p.weight_k = dev_weight_k;
+  p.B = c->B; p.N = c->N; p.heads_q = c->heads_q; p.heads = c->heads_q + c->heads_kv;
+  const bool wide = turn_wide(p.t) && fits16(dev_q, p.q_in, 3, es) && fits16(dev_k, p.k_in, 3, es) && fits16(dev_q_out, p.q_to, 3, es) &&
+                    fits16(dev_k_out, p.k_to, 3, es) && (((uintptr_t)dev_weight_q | (uintptr_t)dev_weight_k) & 15) == 0;
+  const long long places = (long long)p.B * p.N;
+  p.tokens = tokens_per_block(places, p.heads, p.t.lanes);
+  // few tokens: their heads are shared out over blocks of a row per group of lanes
+  p.heads_block = p.heads;
+  const int groups = ROT_THREADS / p.t.lanes;
+  if (places * ((p.heads + groups - 1) / groups) <= 4 * 148) p.heads_block = groups < p.heads ? groups : p.heads;
+  const long long blocks = (places + p.tokens - 1) / p.tokens;
+  if (blocks > 0x7FFFFFFFll) return STAND_E_ARG;
+  const dim3 grid((unsigned)blocks, (unsigned)((p.heads + p.heads_block - 1) / p.heads_block));
+  const size_t smem = (size_t)p.tokens * 2 * turn_floats(p.t.columns, p.t.pairs) * sizeof(float);
+  cudaStream_t st = (cudaStream_t)cu_stream;
+  if (c->dtype == STAND_DTYPE_F32) return launch_rotate<float>(p, wide, grid, smem, st);
+  if (c->dtype == STAND_DTYPE_BF16) return launch_rotate<__nv_bfloat16>(p, wide, grid, smem, st);
+  return launch_rotate<__half>(p, wide, grid, smem, st);
+}
+
+int stand_kv_append(const stand_kv_rows* c, const void* dev_k, const void* dev_v, const void* dev_weight_k, const float* dev_freq,
+                    const int64_t* dev_base, const int32_t* dev_offset, const int32_t* dev_path, const int64_t* dev_slots, void* dev_cache_k,
+                    void* dev_cache_v, void* cu_stream) {
+  if (!c || !dev_k || !dev_v || !dev_slots || !dev_cache_k || !dev_cache_v) return STAND_E_ARG;
+  if (c->layers < 1 || c->layers > ROW_COUNT || c->B < 1 || c->N < 1 || c->heads < 1 || c->heads > ROW_COUNT || c->width < 1) return STAND_E_ARG;
+  if (c->page_size < 1 || c->page_size > 4096 || c->pages < 0 || !type_valid(c->dtype) || (c->packed != 0 && c->packed != 1) || (c->reserved | c->reserved2) != 0) return STAND_E_ARG;
+  if ((long long)c->B * c->width > 0x7FFFFFFFll) return STAND_E_ARG;
+  AppendParams p;
+  if (!make_turn(p.t, c->dim, c->rotary_dim, c->interleaved, c->norm, c->eps, dev_freq, dev_base, dev_offset, c->offset_stride)) return STAND_E_ARG;
+  if (!c->norm && dev_weight_k) return STAND_E_ARG;
+  const int es = element_size(c->dtype);
+  if (!aligned(es, dev_k, dev_v, dev_weight_k) || !aligned(8, dev_slots) || !aligned(4, dev_path)) return STAND_E_ARG;
+  if (c->packed ? c->dim % PK_GROUP != 0 || c->page_size % 16 != 0 || !packed_strides(dev_cache_k, dev_cache_v, c->cache_stride)
+                : !aligned(es, dev_cache_k, dev_cache_v))
+    return STAND_E_ARG;
+  for (int i = 0; i < 4; ++i) {
+    p.k_in[i] = c->k_stride[i], p.v_in[i] = c->v_stride[i], p.to[i] = c->cache_stride[i] * (c->packed ? 1 : es);
+    if (p.k_in[i] < 0 || p.v_in[i] < 0 || p.to[i] < 0) return STAND_E_ARG;
+  }
+  p.k = dev_k; p.v = dev_v; p.weight = dev_weight_k; p.path = dev_path; p.slots = (const long long*)dev_slots;
+  p.cache_k = (char*)dev_cache_k; p.cache_v = (char*)dev_cache_v;
+  p.layers = c->layers; p.N = c->N; p.width = c->width; p.heads = c->heads; p.page = c->page_size; p.places = (long long)c->B * c->width;
+  p.n_slots = (long long)c->pages * c->page_size;
+  const bool wide = turn_wide(p.t) && fits16(dev_k, p.k_in, 4, es) && fits16(dev_v, p.v_in, 4, es) && ((uintptr_t)dev_weight_k & 15) == 0 &&
+                    (c->packed || (fits16(dev_cache_k, p.to, 4, 1) && fits16(dev_cache_v, p.to, 4, 1)));
+  // A token's angles are worked out once for all layers of a block: few blocks per token, but enough to fill the GPU.
+  const int groups = ROT_THREADS / p.t.lanes, rows = 2 * p.heads;
+  int lpb = p.layers;
+  while (lpb > 1 && lpb * rows > 2 * groups && p.places * ((p.layers + lpb - 1) / lpb) < 4 * 148) lpb = (lpb + 1) / 2;
+  p.layers_block = lpb;
+  p.tokens = tokens_per_block(p.places, rows * lpb, p.t.lanes);
+  const dim3 grid((unsigned)((p.places + p.tokens - 1) / p.tokens), (unsigned)((p.layers + lpb - 1) / lpb));
+  const size_t smem = (size_t)p.tokens * 2 * turn_floats(p.t.columns, p.t.pairs) * sizeof(float);
+  cudaStream_t st = (cudaStream_t)cu_stream;
+  if (c->dtype == STAND_DTYPE_F32) return launch_append<float>(p, wide, c->packed, grid, smem, st);
+  if (c->dtype == STAND_DTYPE_BF16) return launch_append<__nv_bfloat16>(p, wide, c->packed, grid, smem, st);
+  return launch_append<__half>(p, wide, c->packed, grid, smem, st);
+}
+
+int stand_kv_read(const stand_kv_rows* c, const void* dev_cache_k, const void* dev_cache_v, const int64_t* dev_slots, void* dev_k, void* dev_v,
+                  void* cu_stream) {
+  if (!c || !dev_k || !dev_v || !dev_slots || !dev_cache_k || !dev_cache_v) return STAND_E_ARG;
+  if (c->layers < 1 || c->layers > ROW_COUNT || c->B < 1 || c->heads < 1 || c->heads > ROW_COUNT || c->width < 1 || c->dim < 1 || c->dim > ROT_DIM_MAX) return STAND_E_ARG;
+  if (c->page_size < 1 || c->page_size > 4096 || c->pages < 0 || !type_valid(c->dtype) || (c->packed != 0 && c->packed != 1) || (c->reserved | c->reserved2) != 0) return STAND_E_ARG;
+  if (c->rotary_dim != 0 || c->norm != 0 || (long long)c->B * c->width > 0x7FFFFFFFll) return STAND_E_ARG;
+  const int es = element_size(c->dtype);
+  if (!aligned(es, dev_k, dev_v) || !aligned(8, dev_slots)) return STAND_E_ARG;
+  if (c->packed ? c->dim % PK_GROUP != 0 || c->page_size % 16 != 0 || !packed_strides(dev_cache_k, dev_cache_v, c->cache_stride)
+                : !aligned(es, dev_cache_k, dev_cache_v))
+    return STAND_E_ARG;
+  ReadParams p;
+  for (int i = 0; i < 4; ++i) {
+    p.from[i] = c->cache_stride[i] * (c->packed ? 1 : es);
+    if (p.from[i] < 0) return STAND_E_ARG;
+  }
+  p.cache_k = (const char*)dev_cache_k; p.cache_v = (const char*)dev_cache_v; p.slots = (const long long*)dev_slots; p.k_out = dev_k; p.v_out = dev_v;
+  p.layers = c->layers; p.heads = c->heads; p.dim = c->dim; p.page = c->page_size; p.lanes = row_lanes(c->dim);
+  p.places = (long long)c->B * c->width; p.n_slots = (long long)c->pages * c->page_size;
+  const bool wide = p.dim % ROT_E == 0 && (((uintptr_t)dev_k | (uintptr_t)dev_v) & 15) == 0 &&
+                    (c->packed || (fits16(dev_cache_k, p.from, 4, 1) && fits16(dev_cache_v, p.from, 4, 1)));
+  const int groups = ROT_THREADS / p.lanes, rows = 2 * p.heads;
+  int lpb = p.layers;
+  while (lpb > 1 && lpb * rows > 4 * groups) lpb = (lpb + 1) / 2;
+  p.layers_block = lpb;
+  p.tokens = tokens_per_block(p.places, rows * lpb, p.lanes);
+  const dim3 grid((unsigned)((p.places + p.tokens - 1) / p.tokens), (unsigned)((p.layers + lpb - 1) / lpb));
+  cudaStream_t st = (cudaStream_t)cu_stream;
+  if (c->dtype == STAND_DTYPE_F32) return launch_read<float>(p, wide, c->packed, grid, st);
+  if (c->dtype == STAND_DTYPE_BF16) return launch_read<__nv_bfloat16>(p, wide, c->packed, grid, st);
+  return launch_read<__half>(p, wide, c->packed, grid, st);
+}
+
+}  // extern "C"

@@ -1,6 +1,7 @@
 """Thin binding of the operators around the decoding step (include/stand.h, second half).
 
-`TreeAttention`, `PageMap`, `KvCommit` and `LogitsProcessor` hold what stays the same from step to step - shapes, the
+`TreeAttention`, `PageMap`, `KvCommit` and `LogitsProcessor`, and for positions and a cache in 4 bits `HeadRotation`, `KvAppend`,
+`KvRead` and `PackedTreeAttention`, hold what stays the same from step to step - shapes, the
 tree, workspaces, result tensors - and are called with the step's device tensors.  Argument marshalling only: the work
 runs in the CUDA kernels of libstand.so.  Calls only enqueue work on the current stream (or `stream`) and return; the
 result tensors of an object are overwritten by its next call unless the caller passes its own.  An object, and tensors given
@@ -11,8 +12,8 @@ import math
 
 import numpy as np
 
-from .binding import (DTYPE_BF16, DTYPE_F16, DTYPE_F32, StandAttention, StandError, StandKvShape, StandLogits,
-                      StandLogitsInputs, _check, lib)
+from .binding import (DTYPE_BF16, DTYPE_F16, DTYPE_F32, StandAttention, StandError, StandKvRows, StandKvShape, StandLogits,
+                      StandLogitsInputs, StandRotation, _check, lib)
 
 
 def _dtype_code(dtype):
@@ -29,8 +30,11 @@ def _need(cond, what):
 
 
 def _steps(x, what):
-    """The strides of all dimensions but the last, whose elements lie side by side.  A dimension of one element has none."""
+    """The strides of all dimensions but the last, whose elements lie side by side.  A dimension of one element has none, an empty
+    tensor neither."""
     shape, strides = x.shape, x.stride()
+    if 0 in shape:
+        return [0] * (len(shape) - 1)
     _need(shape[-1] == 1 or strides[-1] == 1, f"{what}: a contiguous last dimension")
     return [s if n > 1 else 0 for n, s in zip(shape[:-1], strides)]
 
@@ -67,6 +71,12 @@ class _Op:
 
     def _opt(self, t, dtype, shape, what):
         return None if t is None else self._ints(t, dtype, shape, what)
+
+    def _floats(self, x, shape, what):
+        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index:
+            raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev}, "
+                             f"got {x.dtype} {tuple(x.shape)} on {x.device}")
+        return x.data_ptr()
 
 
 def tree_mask(parent):
@@ -105,7 +115,7 @@ class TreeAttention(_Op):
             self.mask, self.mask_stride = mask, N * words if mask.dim() == 3 else 0
         self._mask_ptr = None if self.mask is None else self.mask.data_ptr()
         self._q_shape, self._kv_shape = (B, N, heads_q, dim), (B, N, heads_kv, dim)
-        self._cache_shape = (pages, heads_kv, page_size, dim)
+        self._cache_shape = self._block(pages, heads_kv, page_size, dim)
         self._table_shape, self._len_shape, self._tree_shape = (B, max_pages), (B,), (B, N)
         self.scratch = t.empty(need + 256, dtype=t.uint8, device=self.dev)
         self._scratch = self.scratch.data_ptr() + (-self.scratch.data_ptr()) % 256
@@ -114,11 +124,14 @@ class TreeAttention(_Op):
         self.lse = t.empty((B, N, heads_q), dtype=t.float32, device=self.dev)
         self._cfg_ptr, self._strides = C.addressof(self.cfg), None
 
-    def _floats(self, x, shape, what):
-        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index:
-            raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev}, "
-                             f"got {x.dtype} {tuple(x.shape)} on {x.device}")
-        return x.data_ptr()
+    _entry = "stand_tree_attention"
+
+    @staticmethod
+    def _block(pages, heads, page_size, dim):
+        return (pages, heads, page_size, dim)
+
+    def _cached(self, x, what):
+        return self._floats(x, self._cache_shape, what)
 
     def __call__(self, q, k, v, cache_k, cache_v, table, length, tree_tokens=None, out=None, lse=None, stream=None):
         """q [B, N, heads_q, dim], k / v [B, N, heads_kv, dim] (any strides: slices of one projection will do, keys rotated
@@ -126,13 +139,12 @@ class TreeAttention(_Op):
         [B, N] int32 or None (nodes below 0 get empty rows).  Returns (out [B, N, heads_q, dim], lse [B, N, heads_q])."""
         t, c = self.torch, self.cfg
         pq, pk, pv = self._floats(q, self._q_shape, "q"), self._floats(k, self._kv_shape, "k"), self._floats(v, self._kv_shape, "v")
-        pck = self._floats(cache_k, self._cache_shape, "cache_k")
-        pcv = self._floats(cache_v, self._cache_shape, "cache_v")
+        pck, pcv = self._cached(cache_k, "cache_k"), self._cached(cache_v, "cache_v")
         strides = q.stride(), k.stride(), v.stride(), cache_k.stride(), cache_v.stride()
         if strides != self._strides:
             qs, ks, vs, cs = _steps(q, "q"), _steps(k, "k"), _steps(v, "v"), _steps(cache_k, "cache_k")
             _need(_steps(cache_v, "cache_v") == cs, "TreeAttention: both caches have the same strides")
-            c.q_stride[:], c.kv_stride[:], c.v_stride[:], c.cache_stride[:] = qs, ks, vs, cs
+            c.q_stride[:], c.kv_stride[:], c.v_stride[:], c.cache_stride[:] = qs, ks, vs, cs + [0] * (3 - len(cs))
             c.own_v_stride, self._strides = 1, strides
         ptab = self._ints(table, t.int32, self._table_shape, "table")
         plen = self._ints(length, t.int64, self._len_shape, "length")
@@ -145,9 +157,186 @@ class TreeAttention(_Op):
         if lse is None:
             lse = self.lse
         plse = self._ints(lse, t.float32, self.lse.shape, "lse")
-        self._launch(stream, self._lib.stand_tree_attention, self._cfg_ptr, pq, pk, pv, pck, pcv, ptab, plen, self._mask_ptr,
+        self._launch(stream, getattr(self._lib, self._entry), self._cfg_ptr, pq, pk, pv, pck, pcv, ptab, plen, self._mask_ptr,
                      self.mask_stride, ptree, self._scratch, self._scratch_bytes, out.data_ptr(), plse)
         return out, lse
+
+
+def packed_block_bytes(page_size, dim):
+    """Bytes of a page of one head in the 4-bit form: codes of all its tokens, then their scales (include/stand.h)."""
+    return page_size * dim // 16 * 9
+
+
+def _packed_shapes(page_size, dim, what):
+    _need(dim >= 16 and dim % 16 == 0 and page_size >= 16 and page_size % 16 == 0, f"{what}: the 4-bit form wants dim and page_size to be multiples of 16")
+
+
+class PackedTreeAttention(TreeAttention):
+    """TreeAttention over caches in the 4-bit form (stand_packed_tree_attention): cache_k / cache_v are uint8
+    [pages, heads_kv, packed_block_bytes(page_size, dim)], page and head at multiples of 16 bytes.  All else is the same."""
+
+    _entry = "stand_packed_tree_attention"
+
+    def __init__(self, B, N, heads_q, heads_kv, dim, dtype, page_size, *args, **kw):
+        _packed_shapes(page_size, dim, "PackedTreeAttention")
+        super().__init__(B, N, heads_q, heads_kv, dim, dtype, page_size, *args, **kw)
+
+    @staticmethod
+    def _block(pages, heads, page_size, dim):
+        return (pages, heads, packed_block_bytes(page_size, dim))
+
+    def _cached(self, x, what):
+        return _packed_cache(self, x, self._cache_shape, what)
+
+
+def _packed_cache(op, x, shape, what):
+    if x.dtype is not op.torch.uint8 or x.shape != shape or x.get_device() != op._index:
+        raise StandError(f"{what}: wants a uint8 tensor {shape} on {op.dev}, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+class HeadRotation(_Op):
+    """Norms of queries and keys per head and the position rotation, in one pass (stand_rotate_heads).
+
+    freq: float32 [rotary_dim / 2], the angle per position of each pair (None: no rotation); interleaved: pairs are neighbours
+    (else half of rotary_dim apart); offset: int32 [N] or [B, N], what a node's position adds to its sequence's (None: its
+    number); norm with weight_q, weight_k [dim] (None: ones)."""
+
+    def __init__(self, B, N, heads_q, heads_kv, dim, dtype, freq=None, offset=None, interleaved=False, norm=False, weight_q=None,
+                 weight_k=None, eps=1e-6, device="cuda:0"):
+        self._init_device(device)
+        t = self.torch
+        self.dtype = dtype
+        _need(B >= 1 and N >= 1 and heads_q >= 1 and heads_kv >= 1 and 1 <= dim <= 256, "HeadRotation: invalid shapes")
+        self._turn = _Turn(self, B, N, dim, freq, offset, norm, (weight_q, weight_k), (dim,), eps, "HeadRotation")
+        self.cfg = StandRotation(B, N, heads_q, heads_kv, dim, _dtype_code(dtype), self._turn.rotary, int(bool(interleaved)), int(bool(norm)),
+                                 float(eps) if norm else 0.0)
+        self.cfg.offset_stride = self._turn.offset_stride
+        self._q, self._k, self._b = (B, N, heads_q, dim), (B, N, heads_kv, dim), (B,)
+        self.q_out = t.empty(self._q, dtype=dtype, device=self.dev)
+        self.k_out = t.empty(self._k, dtype=dtype, device=self.dev)
+        self._cfg_ptr, self._strides = C.addressof(self.cfg), None
+
+    def __call__(self, q, k, base=None, q_out=None, k_out=None, stream=None):
+        """q [B, N, heads_q, dim], k [B, N, heads_kv, dim] (any strides), base [B] int64: the position that each sequence's nodes
+        begin at (None: 0).  q_out / k_out: tensors to write (q and k themselves: in place); None: tensors kept by this object.
+        Returns (q_out, k_out)."""
+        c = self.cfg
+        q_out, k_out = self.q_out if q_out is None else q_out, self.k_out if k_out is None else k_out
+        pq, pk = self._floats(q, self._q, "q"), self._floats(k, self._k, "k")
+        pqo, pko = self._floats(q_out, self._q, "q_out"), self._floats(k_out, self._k, "k_out")
+        strides = q.stride(), k.stride(), q_out.stride(), k_out.stride()
+        if strides != self._strides:
+            c.q_stride[:], c.k_stride[:] = _steps(q, "q"), _steps(k, "k")
+            c.q_out_stride[:], c.k_out_stride[:] = _steps(q_out, "q_out"), _steps(k_out, "k_out")
+            self._strides = strides
+        r = self._turn
+        pb = self._opt(base, self.torch.int64, self._b, "base")
+        self._launch(stream, self._lib.stand_rotate_heads, self._cfg_ptr, pq, pk, r.weights[0], r.weights[1], r.freq, pb, r.offset, pqo, pko)
+        return q_out, k_out
+
+
+class _Turn:
+    """What rotations are made with: device pointers of freq, offset and weights, whose tensors are kept."""
+
+    def __init__(self, op, B, N, dim, freq, offset, norm, weights, weight_shape, eps, what):
+        t = op.torch
+        self.rotary = 0
+        self.freq = self.offset = None
+        self.offset_stride = 0
+        self.kept = freq, offset, weights
+        if freq is not None:
+            _need(freq.dim() == 1 and 1 <= freq.shape[0] <= dim // 2, f"{what}: freq has 1 .. dim / 2 entries")
+            self.freq, self.rotary = op._ints(freq, t.float32, freq.shape, "freq"), 2 * freq.shape[0]
+        if offset is not None:
+            _need(freq is not None, f"{what}: offset goes with freq")
+            self.offset = op._ints(offset, t.int32, (N,) if offset.dim() == 1 else (B, N), "offset")
+            self.offset_stride = 0 if offset.dim() == 1 else N
+        _need(not norm or (eps > 0.0 and math.isfinite(eps)), f"{what}: eps > 0")
+        _need(norm or all(w is None for w in weights), f"{what}: weights go with norm")
+        self.weights = [op._opt(w, op.dtype, weight_shape, "weight") for w in weights]
+
+
+class KvAppend(_Op):
+    """Keys and values of chosen nodes into the cache, all layers at once, with the keys' norm and position rotation and the
+    4-bit form on the way (stand_kv_append).
+
+    packed: the caches are uint8 [layers, pages, heads, packed_block_bytes(page_size, dim)], else [layers, pages, heads, page_size, dim]
+    of `dtype`.  freq, offset, interleaved, norm, eps as in HeadRotation; weight_k [layers, dim]."""
+
+    def __init__(self, layers, B, N, heads, dim, dtype, page_size, pages, width, packed=False, freq=None, offset=None, interleaved=False,
+                 norm=False, weight_k=None, eps=1e-6, device="cuda:0"):
+        self._init_device(device)
+        self.dtype, self.packed = dtype, bool(packed)
+        _need(1 <= layers <= 4096 and B >= 1 and N >= 1 and 1 <= heads <= 4096 and 1 <= dim <= 256 and width >= 1 and 1 <= page_size <= 4096
+              and pages >= 0, "KvAppend: invalid shapes")
+        if packed:
+            _packed_shapes(page_size, dim, "KvAppend")
+        self._turn = _Turn(self, B, N, dim, freq, offset, norm, (weight_k,), (layers, dim), eps, "KvAppend")
+        self.cfg = StandKvRows(layers, B, N, heads, dim, _dtype_code(dtype), page_size, pages, width, int(self.packed), self._turn.rotary,
+                               int(bool(interleaved)), int(bool(norm)), float(eps) if norm else 0.0)
+        self.cfg.offset_stride = self._turn.offset_stride
+        self._src, self._places, self._b = (layers, B, N, heads, dim), (B, width), (B,)
+        self._cache = (layers, pages, heads, packed_block_bytes(page_size, dim)) if packed else (layers, pages, heads, page_size, dim)
+        self._cfg_ptr, self._strides = C.addressof(self.cfg), None
+
+    def __call__(self, k, v, slots, cache_k, cache_v, base=None, path=None, stream=None):
+        """k / v [layers, B, N, heads, dim] (any strides), slots [B, width] int64 (PageMap), base [B] int64: the position that
+        each sequence's nodes begin at (None: 0), path [B, width] int32 (None: node j goes to slot j), caches of any strides, the
+        same for both."""
+        t, c, r = self.torch, self.cfg, self._turn
+        pk, pv = self._floats(k, self._src, "k"), self._floats(v, self._src, "v")
+        if self.packed:
+            pck, pcv = _packed_cache(self, cache_k, self._cache, "cache_k"), _packed_cache(self, cache_v, self._cache, "cache_v")
+        else:
+            pck, pcv = self._floats(cache_k, self._cache, "cache_k"), self._floats(cache_v, self._cache, "cache_v")
+        strides = k.stride(), v.stride(), cache_k.stride(), cache_v.stride()
+        if strides != self._strides:
+            ks, vs, cs = _steps(k, "k"), _steps(v, "v"), _steps(cache_k, "cache_k")
+            _need(_steps(cache_v, "cache_v") == cs, "KvAppend: both caches have the same strides")
+            c.k_stride[:], c.v_stride[:], c.cache_stride[:] = ks, vs, cs + [0] * (4 - len(cs))
+            self._strides = strides
+        ps, pp = self._ints(slots, t.int64, self._places, "slots"), self._opt(path, t.int32, self._places, "path")
+        pb = self._opt(base, t.int64, self._b, "base")
+        self._launch(stream, self._lib.stand_kv_append, self._cfg_ptr, pk, pv, r.weights[0], r.freq, pb, r.offset, pp, ps, pck, pcv)
+
+
+class KvRead(_Op):
+    """Rows of the cache back as values (stand_kv_read), from the 4-bit form (packed) in any `dtype`, else in the cache's own."""
+
+    def __init__(self, layers, B, heads, dim, dtype, page_size, pages, width, packed=False, device="cuda:0"):
+        self._init_device(device)
+        t = self.torch
+        self.dtype, self.packed = dtype, bool(packed)
+        _need(1 <= layers <= 4096 and B >= 1 and 1 <= heads <= 4096 and 1 <= dim <= 256 and width >= 1 and 1 <= page_size <= 4096 and pages >= 0,
+              "KvRead: invalid shapes")
+        if packed:
+            _packed_shapes(page_size, dim, "KvRead")
+        self.cfg = StandKvRows(layers, B, 0, heads, dim, _dtype_code(dtype), page_size, pages, width, int(self.packed))
+        self._places, self._out = (B, width), (layers, B, width, heads, dim)
+        self._cache = (layers, pages, heads, packed_block_bytes(page_size, dim)) if packed else (layers, pages, heads, page_size, dim)
+        self.k, self.v = (t.empty(self._out, dtype=dtype, device=self.dev) for _ in range(2))
+        self._cfg_ptr, self._strides = C.addressof(self.cfg), None
+
+    def __call__(self, slots, cache_k, cache_v, k=None, v=None, stream=None):
+        """slots [B, width] int64 (a place without one: zeros), caches as KvAppend takes them.  k / v: contiguous tensors
+        [layers, B, width, heads, dim] to write; None: tensors kept by this object.  Returns (k, v)."""
+        c = self.cfg
+        k, v = self.k if k is None else k, self.v if v is None else v
+        pk, pv = self._floats(k, self._out, "k"), self._floats(v, self._out, "v")
+        _need(k.is_contiguous() and v.is_contiguous(), "KvRead: contiguous results")
+        if self.packed:
+            pck, pcv = _packed_cache(self, cache_k, self._cache, "cache_k"), _packed_cache(self, cache_v, self._cache, "cache_v")
+        else:
+            pck, pcv = self._floats(cache_k, self._cache, "cache_k"), self._floats(cache_v, self._cache, "cache_v")
+        strides = cache_k.stride(), cache_v.stride()
+        if strides != self._strides:
+            cs = _steps(cache_k, "cache_k")
+            _need(_steps(cache_v, "cache_v") == cs, "KvRead: both caches have the same strides")
+            c.cache_stride[:], self._strides = cs + [0] * (4 - len(cs)), strides
+        ps = self._ints(slots, self.torch.int64, self._places, "slots")
+        self._launch(stream, self._lib.stand_kv_read, self._cfg_ptr, pck, pcv, ps, pk, pv)
+        return k, v
 
 
 class PageMap(_Op):
@@ -207,12 +396,6 @@ class KvCommit(_Op):
         self._src, self._cache = (layers, B, N, heads, dim), (layers, pages, heads, page_size, dim)
         self._places = (B, width)
         self._cfg_ptr, self._strides = C.addressof(self.cfg), None
-
-    def _floats(self, x, shape, what):
-        if x.dtype is not self.dtype or x.shape != shape or x.get_device() != self._index:
-            raise StandError(f"{what}: wants a {self.dtype} tensor {shape} on {self.dev}, "
-                             f"got {x.dtype} {tuple(x.shape)} on {x.device}")
-        return x.data_ptr()
 
     def __call__(self, k, v, slots, cache_k, cache_v, path=None, stream=None):
         """k / v [layers, B, N, heads, dim] (any strides), slots [B, width] int64 (stand_page_map), path [B, width] int32
