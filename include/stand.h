@@ -528,7 +528,8 @@ int stand_kv_read(const stand_kv_rows* shape, const void* dev_cache_k, const voi
 
 /* stand_tree_attention over packed caches: the same shapes, arguments, scratch and results, with cached keys and values what
  * their codes stand for.  dim is a multiple of 16; cache_stride: page and head in bytes (multiples of 16), then 0; caches
- * begin at multiples of 16 bytes.  The nodes' own keys and values are of type dtype. */
+ * begin at multiples of 16 bytes.  The nodes' own keys and values are of type dtype.  In 16-bit calls the softmax weights of cached
+ * tokens are halves where they multiply the values: those below 2^-32 of a row's largest may count as 0. */
 int stand_packed_tree_attention(const stand_attention* shape, const void* dev_q, const void* dev_k, const void* dev_v,
                                 const void* dev_cache_k, const void* dev_cache_v, const int32_t* dev_table,
                                 const int64_t* dev_len, const uint32_t* dev_mask, int64_t mask_stride,

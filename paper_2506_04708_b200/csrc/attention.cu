@@ -8,6 +8,7 @@
 
 #include "attention.cuh"
 #include "attention_plain.cuh"
+#include "attention_rows.cuh"
 #include "attention_tensor.cuh"
 #include "launch.cuh"
 #include "packed.cuh"
@@ -37,7 +38,11 @@ extern "C" {
 size_t stand_tree_attention_scratch_bytes(const stand_attention* c) {
   if (!attention_valid(c)) return 0;
   const int group = c->heads_q / c->heads_kv;
-  const size_t plain = ta_scratch_bytes(PA_ROWS, c->dim, plain_ctas(c->dim));
+  size_t plain = ta_scratch_bytes(PA_ROWS, c->dim, plain_ctas(c->dim));
+  if (c->N * group <= PR_ROWS_MOST) {
+    const size_t rows = ta_scratch_bytes(c->N * group, c->dim, rows_ctas(c->N * group, c->dim));
+    plain = rows > plain ? rows : plain;
+  }
   if (c->dtype == STAND_DTYPE_F32 || group > TA_ROWS) return plain;
   const size_t tensor = ta_scratch_bytes(tensor_tile_rows(c->N, group), c->dim, tensor_ctas(c->dim));
   return tensor > plain ? tensor : plain;  // alignment decides, and that is not known here
@@ -77,6 +82,12 @@ int attention_call(const stand_attention* c, bool packed, const void* dev_q, con
   int dev = -1, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return STAND_E_CUDA;
   if (packed) {
+    const bool bf = c->dtype == STAND_DTYPE_BF16;
+    if (rows_takes(p, c->dtype)) {
+      const unsigned limit = wait_limit();
+      if (p.dim == 64) return bf ? launch_packed_rows<64, true>(p, dev_scratch, sms, limit, st) : launch_packed_rows<64, false>(p, dev_scratch, sms, limit, st);
+      return bf ? launch_packed_rows<128, true>(p, dev_scratch, sms, limit, st) : launch_packed_rows<128, false>(p, dev_scratch, sms, limit, st);
+    }
     if (c->dtype == STAND_DTYPE_F32) return launch_plain_attention<float, true>(p, dev_scratch, sms, st);
     if (c->dtype == STAND_DTYPE_BF16) return launch_plain_attention<__nv_bfloat16, true>(p, dev_scratch, sms, st);
     return launch_plain_attention<__half, true>(p, dev_scratch, sms, st);
