@@ -83,10 +83,18 @@ int attention_call(const stand_attention* c, bool packed, const void* dev_q, con
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return STAND_E_CUDA;
   if (packed) {
     const bool bf = c->dtype == STAND_DTYPE_BF16;
+    const unsigned limit = wait_limit();
     if (rows_takes(p, c->dtype)) {
-      const unsigned limit = wait_limit();
       if (p.dim == 64) return bf ? launch_packed_rows<64, true>(p, dev_scratch, sms, limit, st) : launch_packed_rows<64, false>(p, dev_scratch, sms, limit, st);
       return bf ? launch_packed_rows<128, true>(p, dev_scratch, sms, limit, st) : launch_packed_rows<128, false>(p, dev_scratch, sms, limit, st);
+    }
+    if (tensor_takes(p, c->dtype)) {
+      const int dp = tensor_dim(p.dim);
+      int rc;
+      if (dp == 64) rc = bf ? launch_tensor_parts<64, true, true>(p, dev_scratch, sms, limit, st) : launch_tensor_parts<64, false, true>(p, dev_scratch, sms, limit, st);
+      else if (dp == 128) rc = bf ? launch_tensor_parts<128, true, true>(p, dev_scratch, sms, limit, st) : launch_tensor_parts<128, false, true>(p, dev_scratch, sms, limit, st);
+      else rc = bf ? launch_tensor_parts<256, true, true>(p, dev_scratch, sms, limit, st) : launch_tensor_parts<256, false, true>(p, dev_scratch, sms, limit, st);
+      if (rc != STAND_E_ARG) return rc;
     }
     if (c->dtype == STAND_DTYPE_F32) return launch_plain_attention<float, true>(p, dev_scratch, sms, st);
     if (c->dtype == STAND_DTYPE_BF16) return launch_plain_attention<__nv_bfloat16, true>(p, dev_scratch, sms, st);

@@ -73,11 +73,6 @@ struct PkPair {
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(z) : "r"(s), "r"(0x54805480u), "r"(c));
   }
 };
-__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {  // one instruction
-  uint32_t r;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
-  return r;
-}
 // The codes of a word as pairs of values: 8 neighbours, or (woven) 4 elements of two keys.
 __device__ __forceinline__ void pk_pairs(uint32_t w, const PkPair& p, uint32_t (&v)[4]) {
 #pragma unroll

@@ -35,11 +35,12 @@
 #include "async.cuh"
 #include "attention_split.cuh"
 #include "launch.cuh"
+#include "packed.cuh"
 
 namespace stand {
 
 constexpr int TA_ROWS = 128;              // rows of a CTA: lanes of tensor memory
-constexpr int TA_THREADS = 224;
+template <bool PACKED> constexpr int TA_THREADS_OF = PACKED ? 288 : 224;
 constexpr float TA_SLACK = 8.0f;          // the maximum is raised only when scores pass it by 2^8 (below)
 // Weights of the second product are rounded to the input's type, since both operands of a 16-bit product have one type: each
 // is off by 2^-9 (bfloat16) or 2^-12 (half) of itself at most, independently, which is what rounding the result costs anyway;
@@ -221,12 +222,12 @@ __device__ __noinline__ bool ta_wait_on(uint32_t bar, uint32_t parity, volatile 
 // k0 .. k1 - 1, if there are any; to those of live rows come such values of the visible nodes n0 .. n1 - 1, which were taken out of
 // the product.  A lane reads column c0 + lane, so that a value is read once for all rows: other warps wait meanwhile, and a sequence
 // of such values must not make them give up on others (one NaN in a prompt of 4,096 rows: 8 ms; 226 when each row read for itself).
-template <typename T, int E>
+template <typename T, int E, bool PACKED>
 __device__ __noinline__ void ta_settle(const AttnParams& p, int b, int g, int c0, int k0, int k1, int n0, int n1, float* o, int u, int at,
                                        uint32_t lost, bool live) {
   const int lane = threadIdx.x & 31, d = c0 + lane;
   if (__any_sync(FULL, lost != 0)) {
-    const float mine = d < p.dim ? attn_odd_cached<T>(p, b, g, d, k0, k1) : 0.0f;
+    const float mine = d < p.dim ? attn_odd_cached<T, PACKED>(p, b, g, d, k0, k1) : 0.0f;
     __syncwarp();
     for (int j = 0; j < 32; ++j) {
       const float sum = __shfl_sync(FULL, mine, j);
@@ -275,10 +276,56 @@ __device__ __noinline__ void ta_settle(const AttnParams& p, int b, int g, int c0
   }
 }
 
+// ---- packed caches ------------------------------------------------------------------------
+// A word of 8 codes as 8 values of the call's type (16 bytes), with the scale of its group.  bfloat16: a code n in bits 1 - 4 of a bfloat16
+// that begins at 64 is 64 + n, and (64 + n) s - 72 s is exact, 72 s having 7 significant bits; an infinite scale gives infinity less infinity.
+// Half: 1024 + n, less 1032, times s.
+template <bool BF16> struct PkScale {
+  uint32_t s, c;
+  __device__ __forceinline__ explicit PkScale(uint32_t byte) {
+    if constexpr (BF16) {
+      const float f = __half2float(__ushort_as_half((unsigned short)(byte << 7)));
+      s = ta_pack<true>(f, f);
+      c = ta_pack<true>(-72.0f * f, -72.0f * f);
+    } else {
+      s = (byte >= PK_BAD ? 0x7E00u : byte << 7) * 0x10001u;
+      c = 0;
+    }
+  }
+};
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {  // one instruction
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+  return r;
+}
+template <bool BF16> __device__ __forceinline__ uint4 pk_word(uint32_t w, const PkScale<BF16>& p) {
+  uint32_t v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) {
+      const uint32_t x = and_or(i == 0 ? w << 1 : w >> (4 * i - 1), 0x001E001Eu, 0x42804280u);
+      asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(x), "r"(p.s), "r"(p.c));
+    } else {
+      const uint32_t x = and_or(w >> (4 * i), 0x000F000Fu, 0x64006400u);
+      uint32_t k;
+      asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(k) : "r"(x), "r"(0x64086408u));
+      asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(v[i]) : "r"(k), "r"(p.s));
+    }
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// A warp's share of a tile's packed rows, 32 keys, on its way through registers: lane (key, group of 16 elements), UNITS of them.
+template <int DP> struct PkUnits {
+  static constexpr int GROUPS = DP / 16, KEYS = 32 / GROUPS, UNITS = GROUPS;  // keys of a step; steps
+  uint2 codes[UNITS];
+  unsigned char scale[UNITS];
+};
+
 // ---- the kernel -----------------------------------------------------------------------
-template <int DP, int C, bool BF16>
-__global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
+template <int DP, int C, bool BF16, bool PACKED>
+__global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
   using Sh = TaShape<DP, C>;
+  constexpr int TA_THREADS = TA_THREADS_OF<PACKED>;
   constexpr int KT = TA_KT, HALVES = DP / 64, SLOTS = Sh::SLOTS, K_SLOTS = Sh::K_SLOTS, V_SLOTS = Sh::V_SLOTS;
   constexpr int PART_ROWS = TA_ROWS / C, W = KT / C, CH = W < 32 ? W : 32;  // rows of a part; keys of a tile that it takes
   extern __shared__ __align__(1024) char ta_smem[];
@@ -301,7 +348,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
     tc_alloc(smem_addr(&sh.tmem), Sh::COLS);
   } else if (tid == 0) {
     for (int i = 0; i < SLOTS; ++i) {
-      mbar_init(smem_addr(&sh.full[i]), 1);
+      mbar_init(smem_addr(&sh.full[i]), PACKED ? 2 : 1);  // packed: two warps fill a slot
       mbar_init(smem_addr(&sh.empty[i]), 1);
     }
     mbar_init(smem_addr(&sh.q), 1);
@@ -337,7 +384,106 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
                  bar_p = smem_addr(sh.p), bar_o = smem_addr(sh.o), bar_x = smem_addr(&sh.x);
   auto part_row = [&](const TaSeg& s, int row) { return ta_part_row(p.s, s, row); };
 
-  if (warp == 4 || warp == 6) {
+  if (PACKED && (warp == 4 || warp >= 6)) {
+    // ---- packed keys (warps 4 and 7), packed values (6 and 8): half a tile each ------------------
+    // A lane has the 16 elements of a group of some keys; the codes of the next tile are on their way to registers while those of this one become
+    // values in the slot.  Past the text's end, and in pages outside the pool, a scale of zero makes zeros.
+    using U = PkUnits<DP>;
+    const bool value = warp == 6 || warp == 8, second = warp >= 7;
+    const char* cache = value ? p.s.a.cache_v : p.s.a.cache_k;
+    const CUtensorMap* tree_map = value ? &p.tree_v : &p.tree_k;
+    const uint32_t slot0 = value ? K_SLOTS : 0, slots = value ? V_SLOTS : K_SLOTS;
+    const uint32_t elected = elect_one();
+    const int D = p.s.a.dim, key0 = (second ? 32 : 0) + lane / U::GROUPS, group = lane % U::GROUPS;
+    const bool has = group * 16 < D;
+    // where the unit's two pieces lie in a slot; half of the lanes write them the other way round, for the banks
+    const int swap = DP > 64 ? group >> 2 & 1 : 0;
+    const uint32_t column = (group >> 2) * (KT * 128);
+    TaSeg s;
+    uint32_t slot = 0, phase = 1, used = 0, tree_from = 0, tree_to = 0;  // uses with a copy of tree rows
+    bool ok = *abort_flag == 0;
+    TaNote note(walk);
+    while (walk.next(p.s, s)) {
+      if (warp == 4) note.piece(walk, s, sh.range.total, sh.range.groups, blockIdx.x / p.s.group_ctas);
+      if (!ok) continue;  // gave up: only the record is still to be found
+      if (s.begin >= s.end) {
+        if (s.rows && !s.whole && warp == 4)  // a piece of others that this CTA's rows do not see
+          for (int i = lane; i < p.s.tile_rows; i += 32) p.s.part_ml[part_row(s, i)] = make_float2(-INFINITY, 0.0f);
+        continue;
+      }
+      const int b = uniform(s.b), g = uniform(s.g), len = uniform(s.len), p_tiles = uniform(s.p_tiles), begin = uniform(s.begin), end = uniform(s.end);
+      const int* table = p.s.a.table + (long long)b * p.s.a.cols;
+      const char* head = cache + g * p.s.a.cache_stride[1];
+      // lanes 0 and 1 keep the places of the warp's two parts of pages, and their pages' numbers a tile further ahead
+      int pos = begin * KT + (second ? 32 : 0) + lane * 16, col = pos / p.s.a.page, in_page = pos - col * p.s.a.page;
+      int next = lane < 2 && pos < len ? __ldg(table + col) : -1;
+      auto fetch = [&](int tile, U& u) {
+        const bool there = lane < 2 && pos < len && next >= 0 && next < p.s.a.pages;
+        const long long block = there ? next * p.s.a.cache_stride[0] : -1;
+        const int at = in_page;
+        pos += KT;
+        for (in_page += KT; in_page >= p.s.a.page; in_page -= p.s.a.page) ++col;
+        if (lane < 2 && pos < len) next = __ldg(table + col);
+        const long long block0 = __shfl_sync(FULL, block, 0), block1 = __shfl_sync(FULL, block, 1);
+        const int at0 = __shfl_sync(FULL, at, 0), at1 = __shfl_sync(FULL, at, 1);
+#pragma unroll
+        for (int i = 0; i < U::UNITS; ++i) {
+          constexpr int HALF_UNITS = U::UNITS / 2;
+          const int key = key0 + i * U::KEYS;  // of the tile; the first half of them in the first part
+          const long long from = i < HALF_UNITS ? block0 : block1;
+          const int token = (i < HALF_UNITS ? at0 : at1) + (key & 15);
+          const bool in = has && from >= 0 && tile * KT + key < len;
+          u.codes[i] = make_uint2(0, 0);
+          u.scale[i] = 0;
+          if (in) {
+            u.codes[i] = __ldg(reinterpret_cast<const uint2*>(head + from + token * (D / 2)) + group);
+            u.scale[i] = __ldg(reinterpret_cast<const unsigned char*>(head + from + (long long)p.s.a.page * (D / 2)) + token * (D / 16) + group);
+          }
+        }
+      };
+      U now;
+      if (begin < p_tiles) fetch(begin, now);
+      for (int tile = begin; tile < end; ++tile) {
+        U after;
+        if (tile + 1 < p_tiles && tile + 1 < end) fetch(tile + 1, after);
+        if (!(ok = wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
+        const uint32_t bar = bar_full + 8 * (slot0 + slot), dst = ring + (slot0 + slot) * Sh::SLOT;
+        if (tile < p_tiles) {
+          char* to = ta_smem + Sh::Q + (slot0 + slot) * Sh::SLOT + column;
+#pragma unroll
+          for (int i = 0; i < U::UNITS; ++i) {
+            const int key = key0 + i * U::KEYS;
+            const PkScale<BF16> scale(now.scale[i]);
+            const uint4 v0 = pk_word<BF16>(swap ? now.codes[i].y : now.codes[i].x, scale), v1 = pk_word<BF16>(swap ? now.codes[i].x : now.codes[i].y, scale);
+            const int piece = (group & 3) * 2 + swap;
+            *reinterpret_cast<uint4*>(to + key * 128 + ((piece ^ (key & 7)) << 4)) = v0;
+            *reinterpret_cast<uint4*>(to + key * 128 + ((piece ^ 1 ^ (key & 7)) << 4)) = v1;
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar);
+          now = after;
+        } else if (second) {
+          if (lane == 0) mbar_arrive(bar);
+        } else {
+          if (elected) mbar_expect_tx(bar, Sh::SLOT);
+#pragma unroll
+          for (int half = 0; half < HALVES; ++half)
+            tma_load_4d(dst + half * (KT * 128), tree_map, bar, half * 64, (tile - p_tiles) * KT, g, b, elected);
+          if (tree_to != used) tree_from = used;
+          tree_to = used + 1;
+        }
+        ++used;
+        if (++slot == slots) slot = 0, phase ^= 1u;
+      }
+    }
+    if (warp == 4 && lane == 0 && blockIdx.x % p.s.group_ctas == 0) p.s.records[blockIdx.x / p.s.group_ctas] = note.r;
+    if (!ok && lane == 0 && !second) {  // copies in flight land before the block ends
+      for (unsigned i = tree_to > tree_from + slots ? tree_to - slots : tree_from; i < tree_to; ++i)
+        mbar_wait_timed(bar_full + 8 * (slot0 + i % slots), (i / slots) & 1u, nullptr, SPIN_LIMIT);
+    }
+    __syncwarp();
+  } else if (!PACKED && (warp == 4 || warp == 6)) {
     // ---- keys (warp 4), values (warp 6) --------------------------------------------------
     // A tile is copied in boxes of box_rows rows of one page; lane i keeps the place of the tile's i-th box and reads its
     // page's number a tile ahead.
@@ -578,7 +724,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           l += sum0 + sum1;
           tc_wait_st();
         }
-        if (tree || partial) {
+        if (tree || (partial && !PACKED)) {
           // Values that no row sees must not enter the product, 0 times them included: those past the text's end become
           // zero.  In the tree some rows may see what others do not: there, elements that are not finite become zero and
           // are added at the end to the rows that do see them.
@@ -587,7 +733,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
           ok = wait_warp(bar_full + 8 * slot, (n / V_SLOTS) & 1u);
           if (!ok) break;
           char* v0 = ta_smem + Sh::Q + slot * Sh::SLOT;
-          if (partial) {
+          if (partial) {  // (not packed: there they are zeros already)
             for (int i = left * 8 + tid; i < KT * 8; i += TA_ROWS)
 #pragma unroll
               for (int hh = 0; hh < HALVES; ++hh) *reinterpret_cast<uint4*>(v0 + hh * (KT * 128) + i * 16) = make_uint4(0, 0, 0, 0);
@@ -675,7 +821,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
                 f[i] = __uint_as_float(o[i]);
                 if (live && isfinite(l) && isnan(f[i])) lost |= 1u << i;
               }
-              ta_settle<T, 32>(p.s.a, s.b, s.g, c * 32, k0, k1, n0, n1, f, u, 0, lost, live);
+              ta_settle<T, 32, PACKED>(p.s.a, s.b, s.g, c * 32, k0, k1, n0, n1, f, u, 0, lost, live);
 #pragma unroll
               for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(f[i]);
             }
@@ -747,7 +893,7 @@ __global__ void __launch_bounds__(TA_THREADS, TaShape<DP, C>::CTAS) tensor_atten
                 if (ml.y != 0.0f && ml.x > 0.0f && isnan(f[e])) lost |= 1u << e;
               }
               for (int at = 0; at < cols; at += 32)
-                ta_settle<T, 4>(p.s.a, s.b, s.g, c0 + at, k0, k1, n0, n1, f, ru, q * 4 - at, lost, ml.y != 0.0f);
+                ta_settle<T, 4, PACKED>(p.s.a, s.b, s.g, c0 + at, k0, k1, n0, n1, f, ru, q * 4 - at, lost, ml.y != 0.0f);
 #pragma unroll
               for (int e = 0; e < 4; ++e) v[e] = f[e];
             }
@@ -819,7 +965,7 @@ inline int tensor_tile_rows(int n, int group) { return (long long)n * group <= T
 inline int tensor_ctas(int dim) { return tensor_dim(dim) == 256 ? 1 : 2; }
 
 // STAND_E_ARG: not a call for these kernels (what the copy unit cannot address); nothing was launched.
-template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
+template <int DP, int C, bool BF16, bool PACKED> int launch_tensor_attention(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
   using Sh = TaShape<DP, C>;
   TaParams p;
   // A piece's fixed cost in tiles, measured by trying 3 to 9: 16 sequences of 1 - 8,190 tokens with heads of 64 take 81, 71, 59,
@@ -837,33 +983,33 @@ template <int DP, int C, bool BF16> int launch_tensor_attention(const AttnParams
       !encode_map(&p.tree_k, a.k, BF16, a.dim, tree_n, k_stride, TA_KT, 1) ||
       !encode_map(&p.tree_v, a.v, BF16, a.dim, tree_n, v_stride, TA_KT, 1))
     return STAND_E_ARG;
-  if (a.cols > 0) {
+  if (!PACKED && a.cols > 0) {
     const long long n[3] = {a.page, a.heads_kv, a.pages}, stride[3] = {a.cache_stride[2], a.cache_stride[1], a.cache_stride[0]};
     if (a.pages < 1 || !encode_map(&p.cache_k, a.cache_k, BF16, a.dim, n, stride, p.box_rows, 1) ||
         !encode_map(&p.cache_v, a.cache_v, BF16, a.dim, n, stride, p.box_rows, 1))
       return STAND_E_ARG;
-  } else {  // no cache: never read
+  } else {  // no cache, or not by these: never read
     p.cache_k = p.tree_k;
     p.cache_v = p.tree_v;
   }
   static SmemLimit limit;
-  int rc = limit.raise(tensor_attention_kernel<DP, C, BF16>, Sh::SMEM);
+  int rc = limit.raise(tensor_attention_kernel<DP, C, BF16, PACKED>, Sh::SMEM);
   if (rc) return STAND_E_CUDA;
-  rc = launch_dependent(tensor_attention_kernel<DP, C, BF16>, dim3((unsigned)(p.s.groups * p.s.group_ctas)), TA_THREADS, st, p, Sh::SMEM);
+  rc = launch_dependent(tensor_attention_kernel<DP, C, BF16, PACKED>, dim3((unsigned)(p.s.groups * p.s.group_ctas)), TA_THREADS_OF<PACKED>, st, p, Sh::SMEM);
   if (rc) return rc;
   return launch_join<DP, typename std::conditional<BF16, __nv_bfloat16, __half>::type>(p.s, st);
 }
 
-template <int DP, bool BF16> int launch_tensor_parts(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
+template <int DP, bool BF16, bool PACKED = false> int launch_tensor_parts(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
   // Few rows of small heads in four (two) parts.  Measured, parts / none: 16 sequences of 1 - 8,190 tokens, 16 / 16 heads of
   // 64, with 1 node 52 / 63 us, 32 nodes 59 / 66, 48 nodes 68 / 80.  Not for larger heads, whose tiles wait for memory and not
   // for the softmax, and where the exchange takes room from the rings: head size 128, 48 rows, 129 / 108; 16 rows, 193 / 184.
   if constexpr (DP == 64) {
     const int rows = tensor_tile_rows(a.N, a.group);
-    if (rows <= TA_ROWS / 4) return launch_tensor_attention<DP, 4, BF16>(a, scratch, sms, wait_limit, st);
-    if (rows <= TA_ROWS / 2) return launch_tensor_attention<DP, 2, BF16>(a, scratch, sms, wait_limit, st);
+    if (rows <= TA_ROWS / 4) return launch_tensor_attention<DP, 4, BF16, PACKED>(a, scratch, sms, wait_limit, st);
+    if (rows <= TA_ROWS / 2) return launch_tensor_attention<DP, 2, BF16, PACKED>(a, scratch, sms, wait_limit, st);
   }
-  return launch_tensor_attention<DP, 1, BF16>(a, scratch, sms, wait_limit, st);
+  return launch_tensor_attention<DP, 1, BF16, PACKED>(a, scratch, sms, wait_limit, st);
 }
 
 // Rows of 16-byte pieces (strides are looked at when they are encoded).

@@ -766,7 +766,7 @@ def test_a_run_of_all_operators_in_a_graph():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("N,dim", [(1, 128), (2, 64), (4, 128)])
+@pytest.mark.parametrize("N,dim", [(1, 128), (2, 64), (4, 128), (24, 128), (24, 64), (9, 256)])
 def test_packed_a_wait_that_runs_out_gives_nan_and_leaves_the_gpu_usable(lib, dtype, N, dim):
     c = _packed_case(71, dtype, [300, 20, 0], N, 4, 2, dim, 16, parent=inputs.topology(N, min(4, N - 1), 3))
     assert lib.stand_set_wait_limit(0) == 0
