@@ -54,14 +54,6 @@ struct PrParams {
   unsigned wait_limit;
 };
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t elected) {
-  asm volatile(
-      "{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %4, 0;\n\t"
-      "@e cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}" ::"r"(dst),
-      "l"(src), "r"(bytes), "r"(bar), "r"(elected)
-      : "memory");
-}
-
 // ---- unpacking to pairs of halves ------------------------------------------------------------
 constexpr float PK_SHARE = 128.0f;  // values come out as this part of themselves
 // Scales (/ 128) of two elements, of one key or of two, from two bytes in the halves of a word.

@@ -52,17 +52,20 @@ constexpr float TA_SLACK = 8.0f;          // the maximum is raised only when sco
 template <bool BF16> constexpr float TA_LIFT = BF16 ? -TA_SLACK : 7.0f;
 constexpr int TA_XCOLS = 16;              // columns of O that the parts exchange at a time
 
-template <int DP, int C> struct TaShape {
+template <int DP, int C, bool PACKED> struct TaShape {
   static constexpr int CTAS = DP == 256 ? 1 : 2;              // per SM
   static constexpr int SLOT = TA_KT * DP * 2;                 // bytes of a tile of keys or values
-  static constexpr int K_SLOTS = DP == 64 ? (C > 1 ? 5 : 6) : 2, V_SLOTS = DP == 64 ? K_SLOTS : 3;
+  static constexpr int K_SLOTS = PACKED ? (DP == 64 ? 3 : 1) : (DP == 64 ? (C > 1 ? 5 : 6) : 2);
+  static constexpr int V_SLOTS = PACKED ? (DP == 64 ? 3 : 2) : (DP == 64 ? K_SLOTS : 3);
   static constexpr int SLOTS = K_SLOTS + V_SLOTS;
   static constexpr int Q = TA_ROWS * DP * 2;
   static constexpr int COL_O = 0, COL_S = DP;                 // two places for S
   static constexpr int COLS = DP == 256 ? 512 : 256;          // tensor memory columns allocated
   static constexpr int X = C > 1 ? TA_ROWS * (TA_XCOLS + 1) * 4 : 0;  // exchange between the parts
-  static constexpr int SHARED = C > 1 ? 1536 : 512;           // barriers and the like
-  static constexpr int SMEM = Q + SLOTS * SLOT + X + SHARED;
+  static constexpr int STAGES = PACKED ? (DP == 64 ? 4 : 3) : 0;      // of packed rows, for each of the four warps that unpack
+  static constexpr int STAGE = 32 * (DP / 2 + DP / 16);               // 32 keys: codes, then scales
+  static constexpr int SHARED = C > 1 || PACKED ? 1536 : 512; // barriers and the like
+  static constexpr int SMEM = Q + SLOTS * SLOT + X + 4 * STAGES * STAGE + SHARED;
   static_assert(C == 1 || DP == 64, "parts of the lanes: small heads only");
   static_assert(COL_S + 2 * TA_KT <= COLS, "tensor memory");
   static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory");
@@ -314,17 +317,18 @@ template <bool BF16> __device__ __forceinline__ uint4 pk_word(uint32_t w, const 
   }
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
-// A warp's share of a tile's packed rows, 32 keys, on its way through registers: lane (key, group of 16 elements), UNITS of them.
-template <int DP> struct PkUnits {
-  static constexpr int GROUPS = DP / 16, KEYS = 32 / GROUPS, UNITS = GROUPS;  // keys of a step; steps
-  uint2 codes[UNITS];
-  unsigned char scale[UNITS];
-};
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t elected) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %4, 0;\n\t"
+      "@e cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}" ::"r"(dst),
+      "l"(src), "r"(bytes), "r"(bar), "r"(elected)
+      : "memory");
+}
 
 // ---- the kernel -----------------------------------------------------------------------
 template <int DP, int C, bool BF16, bool PACKED>
-__global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
-  using Sh = TaShape<DP, C>;
+__global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
+  using Sh = TaShape<DP, C, PACKED>;
   constexpr int TA_THREADS = TA_THREADS_OF<PACKED>;
   constexpr int KT = TA_KT, HALVES = DP / 64, SLOTS = Sh::SLOTS, K_SLOTS = Sh::K_SLOTS, V_SLOTS = Sh::V_SLOTS;
   constexpr int PART_ROWS = TA_ROWS / C, W = KT / C, CH = W < 32 ? W : 32;  // rows of a part; keys of a tile that it takes
@@ -334,13 +338,14 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C>::CTAS) t
     TaRange<TA_THREADS> range;
     float2 ml[C > 1 ? TA_ROWS : 1];
     TaSeg seg;         // the piece that the rows in shared memory belong to; b < 0: no more
+    uint64_t staged[PACKED ? 4 : 1][PACKED ? Sh::STAGES : 1];
     unsigned odd[2];   // 1 + the last piece (even ones, odd ones) whose tree has values that are not finite
     uint32_t tmem;
     int abort;
   };
   static_assert(sizeof(Shared) <= Sh::SHARED, "barriers");
   float* const exchange = reinterpret_cast<float*>(ta_smem + Sh::Q + SLOTS * Sh::SLOT);
-  Shared& sh = *reinterpret_cast<Shared*>(ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X);
+  Shared& sh = *reinterpret_cast<Shared*>(ta_smem + Sh::SMEM - Sh::SHARED);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t q_smem = smem_addr(ta_smem), ring = q_smem + Sh::Q;
@@ -359,6 +364,8 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C>::CTAS) t
     mbar_init(smem_addr(&sh.o[0]), 1);
     mbar_init(smem_addr(&sh.o[1]), 1);
     mbar_init(smem_addr(&sh.x), 4);
+    if constexpr (PACKED)
+      for (int i = 0; i < 4 * Sh::STAGES; ++i) mbar_init(smem_addr(&sh.staged[0][0] + i), 1);
     mbar_init(smem_addr(&sh.drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.abort = (q_smem & 1023) != 0 || p.wait_limit == 0;  // the swizzle goes by address bits; no waiting allowed
@@ -386,21 +393,71 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C>::CTAS) t
 
   if (PACKED && (warp == 4 || warp >= 6)) {
     // ---- packed keys (warps 4 and 7), packed values (6 and 8): half a tile each ------------------
-    // A lane has the 16 elements of a group of some keys; the codes of the next tile are on their way to registers while those of this one become
-    // values in the slot.  Past the text's end, and in pages outside the pool, a scale of zero makes zeros.
-    using U = PkUnits<DP>;
+    // Each warp copies the codes and scales of its 32 keys into stages of its own, some tiles ahead and across the ends of pieces, and turns
+    // them into values in the slot: a lane the 16 elements of a group of some keys.  Past the text's end, and in pages outside the pool, a scale of
+    // zero makes zeros.
+    constexpr int GROUPS = DP / 16, KEYS = 32 / GROUPS, UNITS = GROUPS;  // keys of a step, steps
+    constexpr int STAGES = Sh::STAGES;
     const bool value = warp == 6 || warp == 8, second = warp >= 7;
     const char* cache = value ? p.s.a.cache_v : p.s.a.cache_k;
     const CUtensorMap* tree_map = value ? &p.tree_v : &p.tree_k;
     const uint32_t slot0 = value ? K_SLOTS : 0, slots = value ? V_SLOTS : K_SLOTS;
     const uint32_t elected = elect_one();
-    const int D = p.s.a.dim, key0 = (second ? 32 : 0) + lane / U::GROUPS, group = lane % U::GROUPS;
+    const int D = p.s.a.dim, row0 = lane / GROUPS, group = lane % GROUPS;
     const bool has = group * 16 < D;
     // where the unit's two pieces lie in a slot; half of the lanes write them the other way round, for the banks
-    const int swap = DP > 64 ? group >> 2 & 1 : 0;
-    const uint32_t column = (group >> 2) * (KT * 128);
+    const int swap = DP > 64 ? group >> 2 & 1 : 0, piece = (group & 3) * 2 + swap;
+    const uint32_t column = (group >> 2) * (KT * 128) + ((second ? 32 : 0) + row0) * 128;
+    const int me = (value ? 2 : 0) + (second ? 1 : 0);
+    char* const stages = ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X + me * STAGES * Sh::STAGE;
+    const uint32_t stages_smem = smem_addr(stages), bar_staged = smem_addr(sh.staged[me]);
+    const int rows = p.box_rows < 32 ? p.box_rows : 32, parts = 32 / rows;  // of a page by one copy; copies of codes (or scales) for 32 keys
+    const uint32_t codes = rows * D / 2, scales = rows * D / 16, scales_at = 16 * D;
+
+    // what is copied: a walk of its own, `issued` tiles so far; lane i has the place of the i-th part of the tile to come
+    TaWalk ahead = walk;
+    TaSeg as;
+    int a_tile = -1, a_end = 0, a_page = -1, a_at = 0;
+    uint32_t issued = 0, taken = 0, known = 0;  // known: two bits per stage, parts that are in the pool
+    bool more = *abort_flag == 0;
+    auto advance = [&]() {
+      ++a_tile;
+      while (a_tile >= a_end) {
+        if (!(more = ahead.next(p.s, as))) return;
+        a_tile = as.begin;
+        a_end = as.end < as.p_tiles ? as.end : as.p_tiles;
+      }
+      const int pos = a_tile * KT + (second ? 32 : 0) + lane * rows, col = pos / p.s.a.page;
+      a_at = pos - col * p.s.a.page;
+      a_page = lane < parts && pos < as.len ? __ldg(p.s.a.table + (long long)as.b * p.s.a.cols + col) : -1;
+    };
+    auto issue = [&]() {
+      if (!more) return;
+      const uint32_t stage = issued % STAGES, bar = bar_staged + 8 * stage, to = stages_smem + stage * Sh::STAGE;
+      const uint32_t here = __ballot_sync(FULL, a_page >= 0 && a_page < p.s.a.pages);
+      const long long block = a_page * p.s.a.cache_stride[0] + as.g * p.s.a.cache_stride[1];
+      known = (known & ~(3u << (2 * stage))) | here << (2 * stage);
+      if (elected) {
+        if (here) mbar_expect_tx(bar, __popc(here) * (codes + scales));
+        else mbar_arrive(bar);
+      }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (!(here >> i & 1u)) continue;
+        const char* from = cache + __shfl_sync(FULL, block, i);
+        const int token = __shfl_sync(FULL, a_at, i);
+        bulk_load(to + i * codes, from + token * (D / 2), codes, bar, elected);
+        bulk_load(to + scales_at + i * scales, from + p.s.a.page * (D / 2) + token * (D / 16), scales, bar, elected);
+      }
+      ++issued;
+      advance();
+    };
+    if (more) advance();
+    for (int i = 0; i < STAGES; ++i) issue();
+
     TaSeg s;
-    uint32_t slot = 0, phase = 1, used = 0, tree_from = 0, tree_to = 0;  // uses with a copy of tree rows
+    uint32_t slot = 0, phase = 1, used = 0, tree_from = 0, tree_to = 0;  // uses of slots with a copy of tree rows
     bool ok = *abort_flag == 0;
     TaNote note(walk);
     while (walk.next(p.s, s)) {
@@ -411,74 +468,56 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C>::CTAS) t
           for (int i = lane; i < p.s.tile_rows; i += 32) p.s.part_ml[part_row(s, i)] = make_float2(-INFINITY, 0.0f);
         continue;
       }
-      const int b = uniform(s.b), g = uniform(s.g), len = uniform(s.len), p_tiles = uniform(s.p_tiles), begin = uniform(s.begin), end = uniform(s.end);
-      const int* table = p.s.a.table + (long long)b * p.s.a.cols;
-      const char* head = cache + g * p.s.a.cache_stride[1];
-      // lanes 0 and 1 keep the places of the warp's two parts of pages, and their pages' numbers a tile further ahead
-      int pos = begin * KT + (second ? 32 : 0) + lane * 16, col = pos / p.s.a.page, in_page = pos - col * p.s.a.page;
-      int next = lane < 2 && pos < len ? __ldg(table + col) : -1;
-      auto fetch = [&](int tile, U& u) {
-        const bool there = lane < 2 && pos < len && next >= 0 && next < p.s.a.pages;
-        const long long block = there ? next * p.s.a.cache_stride[0] : -1;
-        const int at = in_page;
-        pos += KT;
-        for (in_page += KT; in_page >= p.s.a.page; in_page -= p.s.a.page) ++col;
-        if (lane < 2 && pos < len) next = __ldg(table + col);
-        const long long block0 = __shfl_sync(FULL, block, 0), block1 = __shfl_sync(FULL, block, 1);
-        const int at0 = __shfl_sync(FULL, at, 0), at1 = __shfl_sync(FULL, at, 1);
-#pragma unroll
-        for (int i = 0; i < U::UNITS; ++i) {
-          constexpr int HALF_UNITS = U::UNITS / 2;
-          const int key = key0 + i * U::KEYS;  // of the tile; the first half of them in the first part
-          const long long from = i < HALF_UNITS ? block0 : block1;
-          const int token = (i < HALF_UNITS ? at0 : at1) + (key & 15);
-          const bool in = has && from >= 0 && tile * KT + key < len;
-          u.codes[i] = make_uint2(0, 0);
-          u.scale[i] = 0;
-          if (in) {
-            u.codes[i] = __ldg(reinterpret_cast<const uint2*>(head + from + token * (D / 2)) + group);
-            u.scale[i] = __ldg(reinterpret_cast<const unsigned char*>(head + from + (long long)p.s.a.page * (D / 2)) + token * (D / 16) + group);
-          }
-        }
-      };
-      U now;
-      if (begin < p_tiles) fetch(begin, now);
+      const int b = uniform(s.b), g = uniform(s.g), p_tiles = uniform(s.p_tiles), begin = uniform(s.begin), end = uniform(s.end);
       for (int tile = begin; tile < end; ++tile) {
-        U after;
-        if (tile + 1 < p_tiles && tile + 1 < end) fetch(tile + 1, after);
-        if (!(ok = wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
         const uint32_t bar = bar_full + 8 * (slot0 + slot), dst = ring + (slot0 + slot) * Sh::SLOT;
         if (tile < p_tiles) {
+          const uint32_t stage = taken % STAGES;
+          if (!(ok = wait_warp(bar_staged + 8 * stage, (taken / STAGES) & 1u) && wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
+          const char* from = stages + stage * Sh::STAGE;
           char* to = ta_smem + Sh::Q + (slot0 + slot) * Sh::SLOT + column;
+          const uint32_t in = known >> (2 * stage);
+          const int left = s.len - tile * KT - (second ? 32 : 0);  // of the text from this warp's keys on
 #pragma unroll
-          for (int i = 0; i < U::UNITS; ++i) {
-            const int key = key0 + i * U::KEYS;
-            const PkScale<BF16> scale(now.scale[i]);
-            const uint4 v0 = pk_word<BF16>(swap ? now.codes[i].y : now.codes[i].x, scale), v1 = pk_word<BF16>(swap ? now.codes[i].x : now.codes[i].y, scale);
-            const int piece = (group & 3) * 2 + swap;
-            *reinterpret_cast<uint4*>(to + key * 128 + ((piece ^ (key & 7)) << 4)) = v0;
-            *reinterpret_cast<uint4*>(to + key * 128 + ((piece ^ 1 ^ (key & 7)) << 4)) = v1;
+          for (int i = 0; i < UNITS; ++i) {
+            const int row = row0 + i * KEYS;  // of the warp's
+            uint2 w = make_uint2(0, 0);
+            uint32_t byte = 0;
+            if (has) {
+              w = *reinterpret_cast<const uint2*>(from + row * (D / 2) + group * 8);
+              byte = *reinterpret_cast<const unsigned char*>(from + scales_at + row * (D / 16) + group);
+            }
+            if (row >= left || !(in >> (parts == 1 ? 0 : i / (UNITS / 2)) & 1u)) byte = 0;
+            const PkScale<BF16> scale(byte);
+            const uint4 v0 = pk_word<BF16>(swap ? w.y : w.x, scale), v1 = pk_word<BF16>(swap ? w.x : w.y, scale);
+            *reinterpret_cast<uint4*>(to + i * KEYS * 128 + ((piece ^ (row & 7)) << 4)) = v0;
+            *reinterpret_cast<uint4*>(to + i * KEYS * 128 + ((piece ^ 1 ^ (row & 7)) << 4)) = v1;
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(bar);
-          now = after;
-        } else if (second) {
-          if (lane == 0) mbar_arrive(bar);
+          ++taken;
+          issue();
         } else {
-          if (elected) mbar_expect_tx(bar, Sh::SLOT);
+          if (!(ok = wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
+          if (second) {
+            if (lane == 0) mbar_arrive(bar);
+          } else {
+            if (elected) mbar_expect_tx(bar, Sh::SLOT);
 #pragma unroll
-          for (int half = 0; half < HALVES; ++half)
-            tma_load_4d(dst + half * (KT * 128), tree_map, bar, half * 64, (tile - p_tiles) * KT, g, b, elected);
-          if (tree_to != used) tree_from = used;
-          tree_to = used + 1;
+            for (int half = 0; half < HALVES; ++half)
+              tma_load_4d(dst + half * (KT * 128), tree_map, bar, half * 64, (tile - p_tiles) * KT, g, b, elected);
+            if (tree_to != used) tree_from = used;
+            tree_to = used + 1;
+          }
         }
         ++used;
         if (++slot == slots) slot = 0, phase ^= 1u;
       }
     }
     if (warp == 4 && lane == 0 && blockIdx.x % p.s.group_ctas == 0) p.s.records[blockIdx.x / p.s.group_ctas] = note.r;
-    if (!ok && lane == 0 && !second) {  // copies in flight land before the block ends
+    if (!ok && lane == 0) {  // copies in flight land before the block ends
+      for (; taken < issued; ++taken) mbar_wait_timed(bar_staged + 8 * (taken % STAGES), (taken / STAGES) & 1u, nullptr, SPIN_LIMIT);
       for (unsigned i = tree_to > tree_from + slots ? tree_to - slots : tree_from; i < tree_to; ++i)
         mbar_wait_timed(bar_full + 8 * (slot0 + i % slots), (i / slots) & 1u, nullptr, SPIN_LIMIT);
     }
@@ -966,7 +1005,7 @@ inline int tensor_ctas(int dim) { return tensor_dim(dim) == 256 ? 1 : 2; }
 
 // STAND_E_ARG: not a call for these kernels (what the copy unit cannot address); nothing was launched.
 template <int DP, int C, bool BF16, bool PACKED> int launch_tensor_attention(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
-  using Sh = TaShape<DP, C>;
+  using Sh = TaShape<DP, C, PACKED>;
   TaParams p;
   // A piece's fixed cost in tiles, measured by trying 3 to 9: 16 sequences of 1 - 8,190 tokens with heads of 64 take 81, 71, 59,
   // 58 us with 3, 5, 7, 9; 256 sequences of 130 - 4,100 with heads of 128 take 393, 389, 391, 398; 64 of them with 16 / 4 heads of 256
