@@ -40,7 +40,7 @@
 namespace stand {
 
 constexpr int TA_ROWS = 128;              // rows of a CTA: lanes of tensor memory
-template <bool PACKED> constexpr int TA_THREADS_OF = PACKED ? 288 : 224;
+template <bool PACKED> constexpr int TA_THREADS_OF = PACKED ? 320 : 224;
 constexpr float TA_SLACK = 8.0f;          // the maximum is raised only when scores pass it by 2^8 (below)
 // Weights of the second product are rounded to the input's type, since both operands of a 16-bit product have one type: each
 // is off by 2^-9 (bfloat16) or 2^-12 (half) of itself at most, independently, which is what rounding the result costs anyway;
@@ -62,10 +62,11 @@ template <int DP, int C, bool PACKED> struct TaShape {
   static constexpr int COL_O = 0, COL_S = DP;                 // two places for S
   static constexpr int COLS = DP == 256 ? 512 : 256;          // tensor memory columns allocated
   static constexpr int X = C > 1 ? TA_ROWS * (TA_XCOLS + 1) * 4 : 0;  // exchange between the parts
-  static constexpr int STAGES = PACKED ? (DP == 64 ? 4 : 3) : 0;      // of packed rows, for each of the four warps that unpack
-  static constexpr int STAGE = 32 * (DP / 2 + DP / 16);               // 32 keys: codes, then scales
+  static constexpr int STAGES = PACKED ? (DP == 64 ? 4 : 3) : 0;      // of packed tiles
+  static constexpr int STAGE_HALF = TA_KT * (DP / 2 + DP / 16);       // keys (then values): codes, then scales
+  static constexpr int STAGE = 2 * STAGE_HALF;
   static constexpr int SHARED = C > 1 || PACKED ? 1536 : 512; // barriers and the like
-  static constexpr int SMEM = Q + SLOTS * SLOT + X + 4 * STAGES * STAGE + SHARED;
+  static constexpr int SMEM = Q + SLOTS * SLOT + X + STAGES * STAGE + SHARED;
   static_assert(C == 1 || DP == 64, "parts of the lanes: small heads only");
   static_assert(COL_S + 2 * TA_KT <= COLS, "tensor memory");
   static_assert(CTAS * (SMEM + 1024) <= 228 * 1024, "shared memory");
@@ -338,7 +339,8 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
     TaRange<TA_THREADS> range;
     float2 ml[C > 1 ? TA_ROWS : 1];
     TaSeg seg;         // the piece that the rows in shared memory belong to; b < 0: no more
-    uint64_t staged[PACKED ? 4 : 1][PACKED ? Sh::STAGES : 1];
+    uint64_t staged[PACKED ? Sh::STAGES : 1], taken[PACKED ? Sh::STAGES : 1];
+    uint32_t known[PACKED ? Sh::STAGES : 1];  // parts of a staged tile that are in the pool, a bit for each 16 keys
     unsigned odd[2];   // 1 + the last piece (even ones, odd ones) whose tree has values that are not finite
     uint32_t tmem;
     int abort;
@@ -365,7 +367,10 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
     mbar_init(smem_addr(&sh.o[1]), 1);
     mbar_init(smem_addr(&sh.x), 4);
     if constexpr (PACKED)
-      for (int i = 0; i < 4 * Sh::STAGES; ++i) mbar_init(smem_addr(&sh.staged[0][0] + i), 1);
+      for (int i = 0; i < Sh::STAGES; ++i) {
+        mbar_init(smem_addr(&sh.staged[i]), 1);
+        mbar_init(smem_addr(&sh.taken[i]), 4);
+      }
     mbar_init(smem_addr(&sh.drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sh.abort = (q_smem & 1023) != 0 || p.wait_limit == 0;  // the swizzle goes by address bits; no waiting allowed
@@ -391,73 +396,79 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
                  bar_p = smem_addr(sh.p), bar_o = smem_addr(sh.o), bar_x = smem_addr(&sh.x);
   auto part_row = [&](const TaSeg& s, int row) { return ta_part_row(p.s, s, row); };
 
-  if (PACKED && (warp == 4 || warp >= 6)) {
-    // ---- packed keys (warps 4 and 7), packed values (6 and 8): half a tile each ------------------
-    // Each warp copies the codes and scales of its 32 keys into stages of its own, some tiles ahead and across the ends of pieces, and turns
-    // them into values in the slot: a lane the 16 elements of a group of some keys.  Past the text's end, and in pages outside the pool, a scale of
-    // zero makes zeros.
-    constexpr int GROUPS = DP / 16, KEYS = 32 / GROUPS, UNITS = GROUPS;  // keys of a step, steps
+  if (PACKED && warp == 9) {
+    // ---- packed tiles: codes and scales of keys and values as they lie in the pages ----------------
     constexpr int STAGES = Sh::STAGES;
+    const uint32_t stages = q_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X, bar_staged = smem_addr(sh.staged), bar_taken = smem_addr(sh.taken);
+    const uint32_t elected = elect_one();
+    const int D = p.s.a.dim, page_size = p.s.a.page, rows = p.box_rows, n_boxes = KT / rows;
+    const uint32_t codes = rows * D / 2, scales = rows * D / 16, bits = rows == 16 ? 1 : (rows == 32 ? 3 : 15);
+    TaSeg s;
+    uint32_t stage = 0, phase = 1, used = 0;
+    bool ok = *abort_flag == 0;
+    while (ok && walk.next(p.s, s)) {
+      const int end = s.end < s.p_tiles ? s.end : s.p_tiles;
+      if (s.begin >= end) continue;
+      int pos = s.begin * KT + lane * rows, col = pos / page_size, in_page = pos - col * page_size;
+      const int* table = p.s.a.table + (long long)s.b * p.s.a.cols;
+      int next = lane < n_boxes && pos < s.len ? __ldg(table + col) : -1;
+      for (int tile = s.begin; tile < end; ++tile) {
+        const uint32_t here = __ballot_sync(FULL, next >= 0 && next < p.s.a.pages);
+        const long long block = next * p.s.a.cache_stride[0] + s.g * p.s.a.cache_stride[1];
+        const int at = in_page;
+        pos += KT;
+        for (in_page += KT; in_page >= page_size; in_page -= page_size) ++col;
+        next = lane < n_boxes && pos < s.len ? __ldg(table + col) : -1;
+        if (!(ok = wait_warp(bar_taken + 8 * stage, phase))) break;
+        const uint32_t bar = bar_staged + 8 * stage, to = stages + stage * Sh::STAGE;
+        if (elected) {
+          uint32_t known = 0;
+          for (int i = 0; i < n_boxes; ++i)
+            if (here >> i & 1u) known |= bits << (i * (rows >> 4));
+          sh.known[stage] = known;
+          if (here) mbar_expect_tx(bar, __popc(here) * 2 * (codes + scales));
+          else mbar_arrive(bar);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < KT / 16; ++i) {
+          if (!(here >> i & 1u)) continue;
+          const long long from = __shfl_sync(FULL, block, i);
+          const int token = __shfl_sync(FULL, at, i);
+          const char *k = p.s.a.cache_k + from, *v = p.s.a.cache_v + from;
+          const uint32_t dst = to + i * codes, dst2 = to + KT * D / 2 + i * scales, code = token * (D / 2), scale = page_size * (D / 2) + token * (D / 16);
+          bulk_load(dst, k + code, codes, bar, elected);
+          bulk_load(dst2, k + scale, scales, bar, elected);
+          bulk_load(dst + Sh::STAGE_HALF, v + code, codes, bar, elected);
+          bulk_load(dst2 + Sh::STAGE_HALF, v + scale, scales, bar, elected);
+        }
+        ++used;
+        if (++stage == STAGES) stage = 0, phase ^= 1u;
+      }
+    }
+    if (!ok && lane == 0) {  // copies in flight land before the block ends
+      for (unsigned i = used > STAGES ? used - STAGES : 0; i < used; ++i)
+        mbar_wait_timed(bar_staged + 8 * (i % STAGES), (i / STAGES) & 1u, nullptr, SPIN_LIMIT);
+    }
+    __syncwarp();
+  } else if (PACKED && (warp == 4 || warp >= 6)) {
+    // ---- packed keys (warps 4 and 7), packed values (6 and 8): half a tile each into its slot ---------
+    // A lane has the 16 elements of a group of some keys.  Past the text's end, and in pages outside the pool, a scale of zero makes zeros.
+    constexpr int GROUPS = DP / 16, KEYS = 32 / GROUPS, UNITS = GROUPS;  // keys of a step, steps
+    constexpr int STAGES = Sh::STAGES, BATCH = UNITS < 8 ? UNITS : 8;
     const bool value = warp == 6 || warp == 8, second = warp >= 7;
-    const char* cache = value ? p.s.a.cache_v : p.s.a.cache_k;
     const CUtensorMap* tree_map = value ? &p.tree_v : &p.tree_k;
     const uint32_t slot0 = value ? K_SLOTS : 0, slots = value ? V_SLOTS : K_SLOTS;
-    const uint32_t elected = elect_one();
-    const int D = p.s.a.dim, row0 = lane / GROUPS, group = lane % GROUPS;
+    const uint32_t elected = elect_one(), bar_staged = smem_addr(sh.staged), bar_taken = smem_addr(sh.taken);
+    const int D = p.s.a.dim, row0 = (second ? 32 : 0) + lane / GROUPS, group = lane % GROUPS;
     const bool has = group * 16 < D;
     // where the unit's two pieces lie in a slot; half of the lanes write them the other way round, for the banks
     const int swap = DP > 64 ? group >> 2 & 1 : 0, piece = (group & 3) * 2 + swap;
-    const uint32_t column = (group >> 2) * (KT * 128) + ((second ? 32 : 0) + row0) * 128;
-    const int me = (value ? 2 : 0) + (second ? 1 : 0);
-    char* const stages = ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X + me * STAGES * Sh::STAGE;
-    const uint32_t stages_smem = smem_addr(stages), bar_staged = smem_addr(sh.staged[me]);
-    const int rows = p.box_rows < 32 ? p.box_rows : 32, parts = 32 / rows;  // of a page by one copy; copies of codes (or scales) for 32 keys
-    const uint32_t codes = rows * D / 2, scales = rows * D / 16, scales_at = 16 * D;
-
-    // what is copied: a walk of its own, `issued` tiles so far; lane i has the place of the i-th part of the tile to come
-    TaWalk ahead = walk;
-    TaSeg as;
-    int a_tile = -1, a_end = 0, a_page = -1, a_at = 0;
-    uint32_t issued = 0, taken = 0, known = 0;  // known: two bits per stage, parts that are in the pool
-    bool more = *abort_flag == 0;
-    auto advance = [&]() {
-      ++a_tile;
-      while (a_tile >= a_end) {
-        if (!(more = ahead.next(p.s, as))) return;
-        a_tile = as.begin;
-        a_end = as.end < as.p_tiles ? as.end : as.p_tiles;
-      }
-      const int pos = a_tile * KT + (second ? 32 : 0) + lane * rows, col = pos / p.s.a.page;
-      a_at = pos - col * p.s.a.page;
-      a_page = lane < parts && pos < as.len ? __ldg(p.s.a.table + (long long)as.b * p.s.a.cols + col) : -1;
-    };
-    auto issue = [&]() {
-      if (!more) return;
-      const uint32_t stage = issued % STAGES, bar = bar_staged + 8 * stage, to = stages_smem + stage * Sh::STAGE;
-      const uint32_t here = __ballot_sync(FULL, a_page >= 0 && a_page < p.s.a.pages);
-      const long long block = a_page * p.s.a.cache_stride[0] + as.g * p.s.a.cache_stride[1];
-      known = (known & ~(3u << (2 * stage))) | here << (2 * stage);
-      if (elected) {
-        if (here) mbar_expect_tx(bar, __popc(here) * (codes + scales));
-        else mbar_arrive(bar);
-      }
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (!(here >> i & 1u)) continue;
-        const char* from = cache + __shfl_sync(FULL, block, i);
-        const int token = __shfl_sync(FULL, a_at, i);
-        bulk_load(to + i * codes, from + token * (D / 2), codes, bar, elected);
-        bulk_load(to + scales_at + i * scales, from + p.s.a.page * (D / 2) + token * (D / 16), scales, bar, elected);
-      }
-      ++issued;
-      advance();
-    };
-    if (more) advance();
-    for (int i = 0; i < STAGES; ++i) issue();
-
+    const uint32_t column = (group >> 2) * (KT * 128) + row0 * 128;
+    const char* const codes0 = ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X + (value ? Sh::STAGE_HALF : 0) + row0 * (D / 2) + (has ? group * 8 : 0);
+    const char* const scales0 = ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X + (value ? Sh::STAGE_HALF : 0) + KT * D / 2 + row0 * (D / 16) + (has ? group : 0);
     TaSeg s;
-    uint32_t slot = 0, phase = 1, used = 0, tree_from = 0, tree_to = 0;  // uses of slots with a copy of tree rows
+    uint32_t slot = 0, phase = 1, used = 0, stage = 0, stage_phase = 0, tree_from = 0, tree_to = 0;  // tree: uses of slots with a copy of its rows
     bool ok = *abort_flag == 0;
     TaNote note(walk);
     while (walk.next(p.s, s)) {
@@ -472,32 +483,47 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
       for (int tile = begin; tile < end; ++tile) {
         const uint32_t bar = bar_full + 8 * (slot0 + slot), dst = ring + (slot0 + slot) * Sh::SLOT;
         if (tile < p_tiles) {
-          const uint32_t stage = taken % STAGES;
-          if (!(ok = wait_warp(bar_staged + 8 * stage, (taken / STAGES) & 1u) && wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
-          const char* from = stages + stage * Sh::STAGE;
+          if (!(ok = wait_warp(bar_staged + 8 * stage, stage_phase))) break;
+          const char *codes = codes0 + stage * Sh::STAGE, *scales = scales0 + stage * Sh::STAGE;
           char* to = ta_smem + Sh::Q + (slot0 + slot) * Sh::SLOT + column;
-          const uint32_t in = known >> (2 * stage);
-          const int left = s.len - tile * KT - (second ? 32 : 0);  // of the text from this warp's keys on
+          const uint32_t known = sh.known[stage];
+          const int left = s.len - tile * KT;  // of the text from this tile on
 #pragma unroll
-          for (int i = 0; i < UNITS; ++i) {
-            const int row = row0 + i * KEYS;  // of the warp's
-            uint2 w = make_uint2(0, 0);
-            uint32_t byte = 0;
-            if (has) {
-              w = *reinterpret_cast<const uint2*>(from + row * (D / 2) + group * 8);
-              byte = *reinterpret_cast<const unsigned char*>(from + scales_at + row * (D / 16) + group);
+          for (int i0 = 0; i0 < UNITS; i0 += BATCH) {
+            // all are read before the first is written: the compiler cannot know that they lie apart
+            uint2 w[BATCH];
+            uint32_t byte[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+              const int row = (i0 + i) * KEYS;
+              w[i] = *reinterpret_cast<const uint2*>(codes + row * (D / 2));
+              byte[i] = *reinterpret_cast<const unsigned char*>(scales + row * (D / 16));
             }
-            if (row >= left || !(in >> (parts == 1 ? 0 : i / (UNITS / 2)) & 1u)) byte = 0;
-            const PkScale<BF16> scale(byte);
-            const uint4 v0 = pk_word<BF16>(swap ? w.y : w.x, scale), v1 = pk_word<BF16>(swap ? w.x : w.y, scale);
-            *reinterpret_cast<uint4*>(to + i * KEYS * 128 + ((piece ^ (row & 7)) << 4)) = v0;
-            *reinterpret_cast<uint4*>(to + i * KEYS * 128 + ((piece ^ 1 ^ (row & 7)) << 4)) = v1;
+            if (!has || left < KT || known != 15u) {
+#pragma unroll
+              for (int i = 0; i < BATCH; ++i) {
+                const int row = row0 + (i0 + i) * KEYS;
+                if (!has || row >= left || !(known >> (row >> 4) & 1u)) byte[i] = 0;
+              }
+            }
+            if (i0 == 0 && !(ok = wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+              const int row = row0 + (i0 + i) * KEYS;
+              const PkScale<BF16> scale(byte[i]);
+              const uint4 v0 = pk_word<BF16>(swap ? w[i].y : w[i].x, scale), v1 = pk_word<BF16>(swap ? w[i].x : w[i].y, scale);
+              *reinterpret_cast<uint4*>(to + (i0 + i) * KEYS * 128 + ((piece ^ (row & 7)) << 4)) = v0;
+              *reinterpret_cast<uint4*>(to + (i0 + i) * KEYS * 128 + ((piece ^ 1 ^ (row & 7)) << 4)) = v1;
+            }
           }
+          if (!ok) break;
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar);
-          ++taken;
-          issue();
+          if (lane == 0) {
+            mbar_arrive(bar);
+            mbar_arrive(bar_taken + 8 * stage);
+          }
+          if (++stage == STAGES) stage = 0, stage_phase ^= 1u;
         } else {
           if (!(ok = wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
           if (second) {
@@ -516,8 +542,7 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
       }
     }
     if (warp == 4 && lane == 0 && blockIdx.x % p.s.group_ctas == 0) p.s.records[blockIdx.x / p.s.group_ctas] = note.r;
-    if (!ok && lane == 0) {  // copies in flight land before the block ends
-      for (; taken < issued; ++taken) mbar_wait_timed(bar_staged + 8 * (taken % STAGES), (taken / STAGES) & 1u, nullptr, SPIN_LIMIT);
+    if (!ok && lane == 0 && !second) {  // copies in flight land before the block ends
       for (unsigned i = tree_to > tree_from + slots ? tree_to - slots : tree_from; i < tree_to; ++i)
         mbar_wait_timed(bar_full + 8 * (slot0 + i % slots), (i / slots) & 1u, nullptr, SPIN_LIMIT);
     }
