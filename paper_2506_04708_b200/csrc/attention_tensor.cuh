@@ -331,6 +331,7 @@ template <int DP, int C, bool BF16, bool PACKED>
 __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
   using Sh = TaShape<DP, C, PACKED>;
   constexpr int TA_THREADS = TA_THREADS_OF<PACKED>;
+  constexpr int MMA_WARP = PACKED ? 8 : 5;  // packed: warps 4 - 7 unpack, one for each scheduler as the softmax warps are (two of them beside one: 420 us became 400)
   constexpr int KT = TA_KT, HALVES = DP / 64, SLOTS = Sh::SLOTS, K_SLOTS = Sh::K_SLOTS, V_SLOTS = Sh::V_SLOTS;
   constexpr int PART_ROWS = TA_ROWS / C, W = KT / C, CH = W < 32 ? W : 32;  // rows of a part; keys of a tile that it takes
   extern __shared__ __align__(1024) char ta_smem[];
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t q_smem = smem_addr(ta_smem), ring = q_smem + Sh::Q;
-  if (warp == 5) {
+  if (warp == MMA_WARP) {
     tc_alloc(smem_addr(&sh.tmem), Sh::COLS);
   } else if (tid == 0) {
     for (int i = 0; i < SLOTS; ++i) {
@@ -451,12 +452,12 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
         mbar_wait_timed(bar_staged + 8 * (i % STAGES), (i / STAGES) & 1u, nullptr, SPIN_LIMIT);
     }
     __syncwarp();
-  } else if (PACKED && (warp == 4 || warp >= 6)) {
-    // ---- packed keys (warps 4 and 7), packed values (6 and 8): half a tile each into its slot ---------
+  } else if (PACKED && warp >= 4 && warp < 8) {
+    // ---- packed keys (warps 4 and 5), packed values (6 and 7): half a tile each into its slot ---------
     // A lane has the 16 elements of a group of some keys.  Past the text's end, and in pages outside the pool, a scale of zero makes zeros.
     constexpr int GROUPS = DP / 16, KEYS = 32 / GROUPS, UNITS = GROUPS;  // keys of a step, steps
     constexpr int STAGES = Sh::STAGES, BATCH = UNITS < 8 ? UNITS : 8;
-    const bool value = warp == 6 || warp == 8, second = warp >= 7;
+    const bool value = warp >= 6, second = warp & 1;
     const CUtensorMap* tree_map = value ? &p.tree_v : &p.tree_k;
     const uint32_t slot0 = value ? K_SLOTS : 0, slots = value ? V_SLOTS : K_SLOTS;
     const uint32_t elected = elect_one(), bar_staged = smem_addr(sh.staged), bar_taken = smem_addr(sh.taken);
@@ -609,7 +610,7 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
         mbar_wait_timed(bar_full + 8 * (slot0 + i % slots), (i / slots) & 1u, nullptr, SPIN_LIMIT);
     }
     __syncwarp();
-  } else if (warp == 5) {
+  } else if (warp == MMA_WARP) {
     // ---- products -----------------------------------------------------------------------
     constexpr uint32_t IDESC_S = mma_desc(BF16, false, KT), IDESC_O = mma_desc(BF16, true, DP);
     TaSeg s;
@@ -991,7 +992,7 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
     }
   }
   __syncthreads();
-  if (warp == 5) tc_dealloc(tmem, Sh::COLS);
+  if (warp == MMA_WARP) tc_dealloc(tmem, Sh::COLS);
 }
 
 // ---- launch ------------------------------------------------------------------------------
