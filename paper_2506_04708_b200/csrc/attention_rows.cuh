@@ -8,7 +8,7 @@
 // Which element is which index of the summed dimension does not matter as long as both operands agree, so both read their words as
 // they lie.  P goes from the first product's result to the second's operand by a transposition in registers.  So a warp needs no
 // other: it takes 16 keys (one part of a page) of each tile of 64, has its own maximum, sum and O, and the four are joined at the end of a
-// piece.  A fifth warp copies codes and scales of the tiles ahead into a ring (bulk copies, across the ends of pieces).
+// piece.  A fifth warp copies codes and scales of the tiles ahead into a ring, across the ends of pieces.
 // The matrix instructions are the warp-wide ones: 16 x 8 is all that these rows fill, and tcgen05 would need the values in shared memory.
 //
 // Unpacking is most of the work, and its logic instructions, which issue every other cycle, are what counts: in half a word of 8 codes is
@@ -36,7 +36,7 @@ template <int DP, int NB> struct PrShape {
   // heads of 64, 64 tokens over 500 - 8,000: 95 / 84.
   static constexpr int CTAS = NB == 1 ? (DP == 64 ? 4 : 3) : (DP == 64 ? 3 : 2);
   static constexpr int CODES = DP / 2, SCALES = DP / 16;     // bytes of a row
-  static constexpr int HALF = TA_KT * (CODES + SCALES);      // bytes of a tile's keys (or values): codes, then scales
+  static constexpr int HALF = TA_KT * (CODES + SCALES);      // bytes of a tile's keys, then of its values
   static constexpr int SLOT = 2 * HALF;
   static constexpr int STAGES = DP == 128 ? 6 : 8;
   static constexpr int ROWS = 8 * NB;
@@ -50,7 +50,6 @@ template <int DP, int NB> struct PrShape {
 
 struct PrParams {
   TaSplit s;
-  int box_rows;         // rows of a page that one copy takes
   unsigned wait_limit;
 };
 
@@ -121,7 +120,7 @@ __global__ void __launch_bounds__(PR_THREADS, PrShape<DP, NB>::CTAS) packed_rows
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) {
-      mbar_init(smem_addr(&sh.full[i]), 1);
+      mbar_init(smem_addr(&sh.full[i]), 32);
       mbar_init(smem_addr(&sh.empty[i]), PR_WARPS);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -141,67 +140,26 @@ __global__ void __launch_bounds__(PR_THREADS, PrShape<DP, NB>::CTAS) packed_rows
   bool ok = *abort_flag == 0;
 
   if (warp == PR_WARPS) {
-    // ---- copies: lane i keeps the place of a tile's i-th part of a page ------------------------
-    // The whole warp goes through the copies and an elected lane makes them, so that their operands are uniform (copies by a lane each
-    // took 27 instructions a piece).
-    const int rows = p.box_rows, n_boxes = TA_KT / rows;
-    const uint32_t ring = smem_addr(pr_smem), elected = elect_one();
-    const long long stride0 = a.cache_stride[0], stride1 = a.cache_stride[1];
-    const uint32_t codes = rows * Sh::CODES, scales = rows * Sh::SCALES;
-    uint32_t stage = 0, phase = 1, used = 0;
+    // ---- copies ------------------------------------------------------------------------------
+    const uint32_t ring = smem_addr(pr_smem);
+    uint32_t stage = 0, phase = 1;
     TaSeg s;
     TaNote note(walk);
+    PkCopies copies;
     while (walk.next(p.s, s)) {
       note.piece(walk, s, sh.range.total, sh.range.groups, blockIdx.x);
       if (!ok) continue;  // gave up: only the record is still to be found
       const int end = s.end < s.p_tiles ? s.end : s.p_tiles;
       if (s.begin >= end) continue;
-      int pos = s.begin * TA_KT + lane * rows, col = pos / a.page, in_page = pos - col * a.page;
-      const int* table = a.table + (long long)s.b * a.cols;
-      int next = lane < n_boxes && pos < s.len ? __ldg(table + col) : -1;
+      copies.begin(a, s, lane);
       for (int tile = s.begin; tile < end; ++tile) {
-        const bool in = lane < n_boxes && pos < s.len, there = in && next >= 0 && next < a.pages;
-        const long long block = next * stride0 + s.g * stride1;
-        const int at = in_page;
-        pos += TA_KT;
-        for (in_page += TA_KT; in_page >= a.page; in_page -= a.page) ++col;
-        if (lane < n_boxes && pos < s.len) next = __ldg(table + col);
         if (!(ok = wait_warp(smem_addr(&sh.empty[stage]), phase))) break;
-        const uint32_t bar = smem_addr(&sh.full[stage]), to = ring + stage * Sh::SLOT;
-        const uint32_t here = __ballot_sync(FULL, there);
-        if (in && !there) {  // outside the pool: scales of zero make zeros of any codes
-          char* zero = pr_smem + stage * Sh::SLOT + TA_KT * Sh::CODES + lane * scales;
-          for (int i = 0; i < (int)scales; i += 16) *reinterpret_cast<uint4*>(zero + i) = *reinterpret_cast<uint4*>(zero + Sh::HALF + i) = make_uint4(0, 0, 0, 0);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        }
-        __syncwarp();
-        if (elected) {
-          if (here) mbar_expect_tx(bar, __popc(here) * 2 * (codes + scales));
-          else mbar_arrive(bar);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < PR_WARPS; ++i) {
-          if (!(here >> i & 1u)) continue;
-          const long long from = __shfl_sync(FULL, block, i);
-          const int token = __shfl_sync(FULL, at, i);
-          const char *k = a.cache_k + from, *v = a.cache_v + from;
-          const uint32_t dst = to + i * codes, dst2 = to + TA_KT * Sh::CODES + i * scales, code = token * Sh::CODES, scale = a.page * Sh::CODES + token * Sh::SCALES;
-          bulk_load(dst, k + code, codes, bar, elected);
-          bulk_load(dst2, k + scale, scales, bar, elected);
-          bulk_load(dst + Sh::HALF, v + code, codes, bar, elected);
-          bulk_load(dst2 + Sh::HALF, v + scale, scales, bar, elected);
-        }
-        ++used;
+        copies.tile<DP>(a, DP, lane, ring + stage * Sh::SLOT, Sh::HALF, smem_addr(&sh.full[stage]));
         if (++stage == STAGES) stage = 0, phase ^= 1u;
       }
     }
     if (lane == 0) p.s.records[blockIdx.x] = note.r;
-    if (!ok && lane == 0) {  // copies in flight land before the block ends
-      for (unsigned i = used > STAGES ? used - STAGES : 0; i < used; ++i)
-        mbar_wait_timed(smem_addr(&sh.full[i % STAGES]), (i / STAGES) & 1u, nullptr, SPIN_LIMIT);
-    }
-    __syncwarp();
+    cp_wait<0>();
     return;
   }
 
@@ -333,7 +291,7 @@ __global__ void __launch_bounds__(PR_THREADS, PrShape<DP, NB>::CTAS) packed_rows
 
     // Products of the rows with this warp's 16 keys of a tile.
     auto products = [&](const char* tile, float (&x)[NB][4]) {
-      const char *codes = tile + warp * PR_BOX * Sh::CODES + t * (KD / 2), *scales = tile + TA_KT * Sh::CODES + warp * PR_BOX * Sh::SCALES + t * (KD / 16);
+      const char *codes = tile + warp * 9 * DP + t * (KD / 2), *scales = tile + warp * 9 * DP + 8 * DP + t * (KD / 16);
       // keys key0 and key0 + 8: words of 8 elements, two products each
       uint32_t k[2][KD / 8], scale[2];
 #pragma unroll
@@ -368,8 +326,7 @@ __global__ void __launch_bounds__(PR_THREADS, PrShape<DP, NB>::CTAS) packed_rows
     // O += V^T P^T of this warp's keys, `left` of them there.  Keys (2 t, 2 t + 1) and the same + 8 of the product, in the order of key0.
     auto sums = [&](const char* tile, const uint32_t (&w)[NB][2], int left, auto whole) {
       constexpr bool WHOLE = decltype(whole)::value;
-      const char* codes = tile + Sh::HALF + warp * PR_BOX * Sh::CODES + g * (VD / 2);
-      const char* scales = tile + Sh::HALF + TA_KT * Sh::CODES + warp * PR_BOX * Sh::SCALES + g * VD / 16;
+      const char *codes = tile + Sh::HALF + warp * 9 * DP + g * (VD / 2), *scales = tile + Sh::HALF + warp * 9 * DP + 8 * DP + g * VD / 16;
       uint32_t v[2][2][VD / 8], sv[2][2];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -604,8 +561,6 @@ template <int DP, int NB, bool BF16> int launch_packed_rows(const AttnParams& a,
   using Sh = PrShape<DP, NB>;
   PrParams p;
   ta_split(p.s, a, a.N * a.group, DP, sms, Sh::CTAS, 4, scratch);
-  p.box_rows = 16;
-  while (p.box_rows < TA_KT && a.page % (p.box_rows * 2) == 0) p.box_rows *= 2;
   p.wait_limit = wait_limit;
   static SmemLimit limit;
   int rc = limit.raise(packed_rows_kernel<DP, NB, BF16>, Sh::SMEM);

@@ -191,6 +191,56 @@ __device__ __forceinline__ void ta_begin(const TaSplit& p, TaWalk& walk, TaRange
   }
 }
 
+// ---- packed tiles ---------------------------------------------------------------------
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool there) {  // zeros are written where it is not
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+// The copies of packed tiles by one warp, for both kernels that unpack them.  A stage holds the keys' four lots of 16 tokens (the least part of a page), then
+// the values': a lot is 16 rows of codes, then 16 of scales.  Eight lanes copy a lot in 16-byte pieces, so no lane needs another's address; lots
+// past the text's end and of pages outside the pool become zeros, which are values of zero.  (By bulk copies, whose operands one
+// lane has to gather, this warp took 1,100 - 1,500 cycles a tile and held the others up.)
+struct PkCopies {
+  const char *k, *v;  // of the pair's head
+  const int* table;
+  int len, pos, col, in_page, next;
+
+  __device__ __forceinline__ void begin(const AttnParams& a, const TaSeg& s, int lane) {
+    k = a.cache_k + s.g * a.cache_stride[1];
+    v = a.cache_v + s.g * a.cache_stride[1];
+    table = a.table + (long long)s.b * a.cols;
+    len = s.len;
+    pos = s.begin * TA_KT + (lane >> 3) * 16;
+    col = pos / a.page;
+    in_page = pos - col * a.page;
+    next = pos < len ? __ldg(table + col) : -1;
+  }
+  // One tile to `to`; DIM: the head size, at most DP.  The barrier, of 32 arrivals, completes when the pieces are there.
+  template <int DP> __device__ __forceinline__ void tile(const AttnParams& a, int dim, int lane, uint32_t to, int half, uint32_t bar) {
+    const bool there = next >= 0 && next < a.pages;
+    const int c = lane & 7;
+    const long long block = there ? next * a.cache_stride[0] : 0;
+    const int code = (there ? in_page * (dim / 2) : 0) + c * 16, scale = (there ? a.page * (dim / 2) + in_page * (dim / 16) : 0) + c * 16;
+    const char *pk = k + block, *pv = v + block;
+    pos += TA_KT;
+    for (in_page += TA_KT; in_page >= a.page; in_page -= a.page) ++col;
+    next = pos < len ? __ldg(table + col) : -1;
+    to += (lane >> 3) * 9 * dim + c * 16;
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i)
+      if (i * 16 < dim) {
+        cp_async16_or_zero(to + i * 128, pk + code + i * 128, there);
+        cp_async16_or_zero(to + half + i * 128, pv + code + i * 128, there);
+      }
+#pragma unroll
+    for (int i = 0; i < (DP + 127) / 128; ++i)
+      if ((c + 8 * i) * 16 < dim) {
+        cp_async16_or_zero(to + 8 * dim + i * 128, pk + scale + i * 128, there);
+        cp_async16_or_zero(to + half + 8 * dim + i * 128, pv + scale + i * 128, there);
+      }
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+  }
+};
+
 // ---- joining the pieces ---------------------------------------------------------------
 constexpr int TJ_WARPS = 8;
 

@@ -63,7 +63,7 @@ template <int DP, int C, bool PACKED> struct TaShape {
   static constexpr int COLS = DP == 256 ? 512 : 256;          // tensor memory columns allocated
   static constexpr int X = C > 1 ? TA_ROWS * (TA_XCOLS + 1) * 4 : 0;  // exchange between the parts
   static constexpr int STAGES = PACKED ? (DP == 64 ? 4 : 3) : 0;      // of packed tiles
-  static constexpr int STAGE_HALF = TA_KT * (DP / 2 + DP / 16);       // keys (then values): codes, then scales
+  static constexpr int STAGE_HALF = TA_KT * (DP / 2 + DP / 16);       // keys, then values
   static constexpr int STAGE = 2 * STAGE_HALF;
   static constexpr int SHARED = C > 1 || PACKED ? 1536 : 512; // barriers and the like
   static constexpr int SMEM = Q + SLOTS * SLOT + X + STAGES * STAGE + SHARED;
@@ -318,14 +318,6 @@ template <bool BF16> __device__ __forceinline__ uint4 pk_word(uint32_t w, const 
   }
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t elected) {
-  asm volatile(
-      "{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %4, 0;\n\t"
-      "@e cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}" ::"r"(dst),
-      "l"(src), "r"(bytes), "r"(bar), "r"(elected)
-      : "memory");
-}
-
 // ---- the kernel -----------------------------------------------------------------------
 template <int DP, int C, bool BF16, bool PACKED>
 __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
@@ -341,7 +333,6 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
     float2 ml[C > 1 ? TA_ROWS : 1];
     TaSeg seg;         // the piece that the rows in shared memory belong to; b < 0: no more
     uint64_t staged[PACKED ? Sh::STAGES : 1], taken[PACKED ? Sh::STAGES : 1];
-    uint32_t known[PACKED ? Sh::STAGES : 1];  // parts of a staged tile that are in the pool, a bit for each 16 keys
     unsigned odd[2];   // 1 + the last piece (even ones, odd ones) whose tree has values that are not finite
     uint32_t tmem;
     int abort;
@@ -369,7 +360,7 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
     mbar_init(smem_addr(&sh.x), 4);
     if constexpr (PACKED)
       for (int i = 0; i < Sh::STAGES; ++i) {
-        mbar_init(smem_addr(&sh.staged[i]), 1);
+        mbar_init(smem_addr(&sh.staged[i]), 32);
         mbar_init(smem_addr(&sh.taken[i]), 4);
       }
     mbar_init(smem_addr(&sh.drain), 1);
@@ -398,63 +389,28 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
   auto part_row = [&](const TaSeg& s, int row) { return ta_part_row(p.s, s, row); };
 
   if (PACKED && warp == 9) {
-    // ---- packed tiles: codes and scales of keys and values as they lie in the pages ----------------
+    // ---- packed tiles into stages --------------------------------------------------------
     constexpr int STAGES = Sh::STAGES;
     const uint32_t stages = q_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X, bar_staged = smem_addr(sh.staged), bar_taken = smem_addr(sh.taken);
-    const uint32_t elected = elect_one();
-    const int D = p.s.a.dim, page_size = p.s.a.page, rows = p.box_rows, n_boxes = KT / rows;
-    const uint32_t codes = rows * D / 2, scales = rows * D / 16, bits = rows == 16 ? 1 : (rows == 32 ? 3 : 15);
     TaSeg s;
-    uint32_t stage = 0, phase = 1, used = 0;
+    PkCopies copies;
+    uint32_t stage = 0, phase = 1;
     bool ok = *abort_flag == 0;
     while (ok && walk.next(p.s, s)) {
       const int end = s.end < s.p_tiles ? s.end : s.p_tiles;
       if (s.begin >= end) continue;
-      int pos = s.begin * KT + lane * rows, col = pos / page_size, in_page = pos - col * page_size;
-      const int* table = p.s.a.table + (long long)s.b * p.s.a.cols;
-      int next = lane < n_boxes && pos < s.len ? __ldg(table + col) : -1;
+      copies.begin(p.s.a, s, lane);
       for (int tile = s.begin; tile < end; ++tile) {
-        const uint32_t here = __ballot_sync(FULL, next >= 0 && next < p.s.a.pages);
-        const long long block = next * p.s.a.cache_stride[0] + s.g * p.s.a.cache_stride[1];
-        const int at = in_page;
-        pos += KT;
-        for (in_page += KT; in_page >= page_size; in_page -= page_size) ++col;
-        next = lane < n_boxes && pos < s.len ? __ldg(table + col) : -1;
         if (!(ok = wait_warp(bar_taken + 8 * stage, phase))) break;
-        const uint32_t bar = bar_staged + 8 * stage, to = stages + stage * Sh::STAGE;
-        if (elected) {
-          uint32_t known = 0;
-          for (int i = 0; i < n_boxes; ++i)
-            if (here >> i & 1u) known |= bits << (i * (rows >> 4));
-          sh.known[stage] = known;
-          if (here) mbar_expect_tx(bar, __popc(here) * 2 * (codes + scales));
-          else mbar_arrive(bar);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < KT / 16; ++i) {
-          if (!(here >> i & 1u)) continue;
-          const long long from = __shfl_sync(FULL, block, i);
-          const int token = __shfl_sync(FULL, at, i);
-          const char *k = p.s.a.cache_k + from, *v = p.s.a.cache_v + from;
-          const uint32_t dst = to + i * codes, dst2 = to + KT * D / 2 + i * scales, code = token * (D / 2), scale = page_size * (D / 2) + token * (D / 16);
-          bulk_load(dst, k + code, codes, bar, elected);
-          bulk_load(dst2, k + scale, scales, bar, elected);
-          bulk_load(dst + Sh::STAGE_HALF, v + code, codes, bar, elected);
-          bulk_load(dst2 + Sh::STAGE_HALF, v + scale, scales, bar, elected);
-        }
-        ++used;
+        copies.tile<DP>(p.s.a, p.s.a.dim, lane, stages + stage * Sh::STAGE, Sh::STAGE_HALF, bar_staged + 8 * stage);
         if (++stage == STAGES) stage = 0, phase ^= 1u;
       }
     }
-    if (!ok && lane == 0) {  // copies in flight land before the block ends
-      for (unsigned i = used > STAGES ? used - STAGES : 0; i < used; ++i)
-        mbar_wait_timed(bar_staged + 8 * (i % STAGES), (i / STAGES) & 1u, nullptr, SPIN_LIMIT);
-    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncwarp();
   } else if (PACKED && warp >= 4 && warp < 8) {
     // ---- packed keys (warps 4 and 5), packed values (6 and 7): half a tile each into its slot ---------
-    // A lane has the 16 elements of a group of some keys.  Past the text's end, and in pages outside the pool, a scale of zero makes zeros.
+    // A lane has the 16 elements of a group of some keys.  Past the text's end a scale of zero makes zeros.
     constexpr int GROUPS = DP / 16, KEYS = 32 / GROUPS, UNITS = GROUPS;  // keys of a step, steps
     constexpr int STAGES = Sh::STAGES, BATCH = UNITS < 8 ? UNITS : 8;
     const bool value = warp >= 6, second = warp & 1;
@@ -466,8 +422,10 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
     // where the unit's two pieces lie in a slot; half of the lanes write them the other way round, for the banks
     const int swap = DP > 64 ? group >> 2 & 1 : 0, piece = (group & 3) * 2 + swap;
     const uint32_t column = (group >> 2) * (KT * 128) + row0 * 128;
-    const char* const codes0 = ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X + (value ? Sh::STAGE_HALF : 0) + row0 * (D / 2) + (has ? group * 8 : 0);
-    const char* const scales0 = ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X + (value ? Sh::STAGE_HALF : 0) + KT * D / 2 + row0 * (D / 16) + (has ? group : 0);
+    // this lane's codes and scales in the first of the warp's two lots of 16 keys; the second lies 9 D further on
+    const char* const lot = ta_smem + Sh::Q + SLOTS * Sh::SLOT + Sh::X + (value ? Sh::STAGE_HALF : 0) + (second ? 18 * D : 0);
+    const char* const codes0 = lot + lane / GROUPS * (D / 2) + (has ? group * 8 : 0);
+    const char* const scales0 = lot + 8 * D + lane / GROUPS * (D / 16) + (has ? group : 0);
     TaSeg s;
     uint32_t slot = 0, phase = 1, used = 0, stage = 0, stage_phase = 0, tree_from = 0, tree_to = 0;  // tree: uses of slots with a copy of its rows
     bool ok = *abort_flag == 0;
@@ -487,7 +445,6 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
           if (!(ok = wait_warp(bar_staged + 8 * stage, stage_phase))) break;
           const char *codes = codes0 + stage * Sh::STAGE, *scales = scales0 + stage * Sh::STAGE;
           char* to = ta_smem + Sh::Q + (slot0 + slot) * Sh::SLOT + column;
-          const uint32_t known = sh.known[stage];
           const int left = s.len - tile * KT;  // of the text from this tile on
 #pragma unroll
           for (int i0 = 0; i0 < UNITS; i0 += BATCH) {
@@ -496,15 +453,15 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
             uint32_t byte[BATCH];
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
-              const int row = (i0 + i) * KEYS;
-              w[i] = *reinterpret_cast<const uint2*>(codes + row * (D / 2));
-              byte[i] = *reinterpret_cast<const unsigned char*>(scales + row * (D / 16));
+              const int row = (i0 + i) % (UNITS / 2) * KEYS, at = (i0 + i) / (UNITS / 2) * 9 * D;
+              w[i] = *reinterpret_cast<const uint2*>(codes + at + row * (D / 2));
+              byte[i] = *reinterpret_cast<const unsigned char*>(scales + at + row * (D / 16));
             }
-            if (!has || left < KT || known != 15u) {
+            if (!has || left < KT) {
 #pragma unroll
               for (int i = 0; i < BATCH; ++i) {
                 const int row = row0 + (i0 + i) * KEYS;
-                if (!has || row >= left || !(known >> (row >> 4) & 1u)) byte[i] = 0;
+                if (!has || row >= left) byte[i] = 0;
               }
             }
             if (i0 == 0 && !(ok = wait_warp(bar_empty + 8 * (slot0 + slot), phase))) break;
