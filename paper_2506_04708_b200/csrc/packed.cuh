@@ -48,25 +48,29 @@ __device__ __forceinline__ uint32_t pk_scale_byte(uint32_t amax_bits) {
 
 // The codes of 16 elements.  Elements of 16 bits: an element has at most 11 significant bits and s has 4, so a quotient that is
 // no tie is at least 2^-12 from one; the product with the reciprocal is off by 7 * 2^-23 at most, and rounding it to multiples
-// of 2^-13 first makes a tie one again.  32 bits: the quotient rounded to 32 bits, then to a whole number.
-template <bool EXACT_TIES>
-__device__ __forceinline__ uint2 pk_codes(const float (&y)[PK_GROUP], uint32_t byte) {
+// of 2^-13 (the sum with 1536) makes a tie one again; the second sum rounds to whole numbers.  32 bits: the quotient rounded to 32
+// bits, then to a whole number.  Four whole numbers + 8 are put together as digits of a float, which costs less than shifts and masks.
+template <bool SHORT>
+__device__ __forceinline__ uint2 pk_codes(float (&y)[PK_GROUP], uint32_t amax_bits, uint32_t byte) {
   if (byte == 0 || byte >= PK_BAD) return make_uint2(0x88888888u, 0x88888888u);
+  if (amax_bits > __float_as_uint(PK_MOST)) {
+#pragma unroll
+    for (int i = 0; i < PK_GROUP; ++i) y[i] = fminf(fmaxf(y[i], -PK_MOST), PK_MOST);
+  }
   const float s = pk_scale(byte), inv = 1.0f / s;
-  uint32_t k[PK_GROUP];
+  float k[PK_GROUP];
 #pragma unroll
   for (int i = 0; i < PK_GROUP; ++i) {
-    float r;
-    if (EXACT_TIES) r = fmaf(y[i], inv, 1536.0f) - 1536.0f;
-    else r = __fdiv_rn(y[i], s);
-    r = fminf(fmaxf(r, -7.0f), 7.0f);  // only beyond the largest scale
-    k[i] = __float_as_uint(r + (12582912.0f + 8.0f)) & 15u;  // the whole number + 8 in the last bits
+    if (SHORT) k[i] = fmaf(y[i], inv, 1536.0f) + (12582912.0f + 8.0f - 1536.0f);
+    else k[i] = __fdiv_rn(y[i], s) + (12582912.0f + 8.0f);
+    k[i] -= 12582912.0f;
   }
   uint32_t w[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const uint32_t* e = k + 8 * h;
-    w[h] = e[0] | e[2] << 4 | e[4] << 8 | e[6] << 12 | e[1] << 16 | e[3] << 20 | e[5] << 24 | e[7] << 28;
+    const float* e = k + 8 * h;
+    const float even = fmaf(fmaf(fmaf(e[6], 16.0f, e[4]), 16.0f, e[2]), 16.0f, e[0]), odd = fmaf(fmaf(fmaf(e[7], 16.0f, e[5]), 16.0f, e[3]), 16.0f, e[1]);
+    w[h] = __byte_perm(__float_as_uint(even + 8388608.0f), __float_as_uint(odd + 8388608.0f), 0x5410);
   }
   return make_uint2(w[0], w[1]);
 }

@@ -15,6 +15,7 @@ using namespace stand;
 namespace {
 
 constexpr int ROT_THREADS = 256;
+constexpr int ROT_E = 16;  // elements of a lane that reads
 constexpr int ROW_COUNT = 4096;  // layers, heads: their product counts rows in 32 bits
 constexpr int ROT_TOKENS = 16;  // tokens of a block, at most: their cosines and sines lie in shared memory
 
@@ -32,13 +33,13 @@ struct Step {
 };
 
 // The block's table of cosines and sines; the caller's barrier follows.
-template <typename F> __device__ __forceinline__ void turn_tables(const Turn& t, float* cs, int tokens, F position) {
-  const int floats = turn_floats(t.columns, t.pairs);
-  for (int i = threadIdx.x; i < tokens * t.half; i += ROT_THREADS) {
-    const int tok = i / t.half, k = i - tok * t.half;
-    float c, s;
-    turn_angle(position(tok), t.freq[k], c, s);
-    float* at = cs + tok * 2 * floats + turn_at(t, k);
+template <int VE, typename F> __device__ __forceinline__ void turn_tables(const Turn& t, float* cs, int tokens, F position) {
+  const int floats = turn_floats<VE>(t.columns), angles = t.columns * VE;
+  for (int i = threadIdx.x; i < tokens * angles; i += ROT_THREADS) {
+    const int tok = i / angles, k = i - tok * angles;
+    float c = 1.0f, s = 0.0f;
+    if (k < t.half) turn_angle(position(tok), t.freq[k], c, s);
+    float* at = cs + tok * 2 * floats + turn_at<VE>(t.columns, k);
     at[0] = c;
     at[floats] = s;
   }
@@ -58,50 +59,46 @@ struct RotateParams {
   long long q_in[3], k_in[3], q_to[3], k_to[3];
 };
 
-template <typename T, bool WIDE> __global__ void __launch_bounds__(ROT_THREADS) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
+template <typename T, int VE> __global__ void __launch_bounds__(ROT_THREADS) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
   extern __shared__ __align__(16) float rot_cs[];
+  __shared__ __align__(16) float s_weight[2][ROT_DIM_MAX];
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, lanes = p.t.lanes, c = tid & (lanes - 1), group = tid / lanes, groups = ROT_THREADS / lanes;
   const long long first = (long long)blockIdx.x * p.tokens, all = (long long)p.B * p.N;
   const int tokens = all - first < p.tokens ? (int)(all - first) : p.tokens;
   const int h0 = blockIdx.y * p.heads_block, heads = p.heads - h0 < p.heads_block ? p.heads - h0 : p.heads_block;
-  const int floats = 2 * turn_floats(p.t.columns, p.t.pairs);
-  if (p.t.freq) {
-    turn_tables(p.t, rot_cs, tokens, [&](int tok) {
+  const int floats = 2 * turn_floats<VE>(p.t.columns);
+  if (p.t.freq)
+    turn_tables<VE>(p.t, rot_cs, tokens, [&](int tok) {
       const long long at = first + tok;
       const int b = (int)(at / p.N);
       return turn_position(p.t, b, (int)(at - (long long)b * p.N));
     });
-    __syncthreads();
-  }
+  if (p.t.norm)
+    for (int i = tid; i < p.t.dim; i += ROT_THREADS) {
+      s_weight[0][i] = p.weight_q ? to_float(reinterpret_cast<const T*>(p.weight_q)[i]) : 1.0f;
+      s_weight[1][i] = p.weight_k ? to_float(reinterpret_cast<const T*>(p.weight_k)[i]) : 1.0f;
+    }
+  __syncthreads();
   const int rows = tokens * heads;
   const Step step(groups, heads, 1);
   Step at(group, heads, 1);
-  int tok_b = (int)(first / p.N), tok_n = (int)(first - (long long)tok_b * p.N);  // of the block's first token
+  const int tok_b = (int)(first / p.N), tok_n = (int)(first - (long long)tok_b * p.N);  // of the block's first token
   for (int r = group; r - group < rows; r += groups, at.add(step, heads, 1)) {
-    const bool in = r < rows, there = in && c * ROT_E < p.t.dim;
     const int tok = at.t + at.l, head = h0 + at.h;  // one layer: its carry goes to the token
     int b = tok_b, n = tok_n + tok;
     while (n >= p.N) n -= p.N, ++b;
     const bool is_q = head < p.heads_q;
     const int h = is_q ? head : head - p.heads_q;
     const long long* in_s = is_q ? p.q_in : p.k_in;
-    const T* row = reinterpret_cast<const T*>(is_q ? p.q : p.k) + b * in_s[0] + n * in_s[1] + h * in_s[2];
-    const T* weight = reinterpret_cast<const T*>(is_q ? p.weight_q : p.weight_k);
-    float y[ROT_E];
-    row_group<T, WIDE>(p.t, row, weight, rot_cs + tok * floats, c, there, true, p.t.freq != nullptr, y);
-    __syncwarp();  // in place: all lanes of a row have read
-    if (!there) continue;
     const long long* out_s = is_q ? p.q_to : p.k_to;
-    T* to = reinterpret_cast<T*>(is_q ? p.q_out : p.k_out) + b * out_s[0] + n * out_s[1] + h * out_s[2] + c * ROT_E;
-    if (WIDE) {
-      store_row16(to, y);
-    } else {
-#pragma unroll
-      for (int i = 0; i < ROT_E; ++i)
-        if (c * ROT_E + i < p.t.dim) to[i] = from_float<T>(y[i]);
-    }
+    const T* row = reinterpret_cast<const T*>(is_q ? p.q : p.k) + b * in_s[0] + n * in_s[1] + h * in_s[2];
+    T* to = reinterpret_cast<T*>(is_q ? p.q_out : p.k_out) + b * out_s[0] + n * out_s[1] + h * out_s[2];
+    row_units<T, VE>(p.t, row, s_weight[is_q ? 0 : 1], rot_cs + tok * floats, c, r < rows, true, p.t.freq != nullptr, [&](float (&y)[2 * VE], int a, int b2) {
+      store_vec<T, VE>(to + a, y);
+      if (b2 < p.t.dim) store_vec<T, VE>(to + b2, y + VE);
+    });
   }
 }
 
@@ -117,12 +114,15 @@ struct AppendParams {
   int layers, N, width, heads, page;
   long long places;  // B * width
   int tokens, layers_block;
+  int table_floats;  // of all tokens; a block's rows on their way to groups of 16 lie behind them
   long long n_slots;
   long long k_in[4], v_in[4];  // elements
   long long to[4];             // bytes: layer, page, head, token
 };
 
-template <typename T, bool WIDE, bool PACKED>
+// Packed: a lane takes a group of 16 elements.  Where units are such groups they stay in registers; else (halves that are turned, short units) the
+// row goes through shared memory, as what a cache of its type would hold.
+template <typename T, int VE, bool PACKED>
 __global__ void __launch_bounds__(ROT_THREADS) kv_append_kernel(const __grid_constant__ AppendParams p) {
   extern __shared__ __align__(16) float rot_cs[];
   __shared__ long long s_page[ROT_TOKENS];  // -1: nothing is stored
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(ROT_THREADS) kv_append_kernel(const __grid_con
   const long long first = (long long)blockIdx.x * p.tokens;
   const int tokens = p.places - first < p.tokens ? (int)(p.places - first) : p.tokens;
   const int l0 = blockIdx.y * p.layers_block, layers = p.layers - l0 < p.layers_block ? p.layers - l0 : p.layers_block;
-  const int floats = 2 * turn_floats(p.t.columns, p.t.pairs);
+  const int floats = 2 * turn_floats<VE>(p.t.columns), dim = p.t.dim;
   if (tid < tokens) {
     const long long place = first + tid, slot = p.slots[place];
     const int b = (int)(place / p.width), j = (int)(place - (long long)b * p.width), node = p.path ? p.path[place] : j;
@@ -145,46 +145,56 @@ __global__ void __launch_bounds__(ROT_THREADS) kv_append_kernel(const __grid_con
   }
   __syncthreads();
   if (p.t.freq) {
-    turn_tables(p.t, rot_cs, tokens, [&](int tok) { return s_page[tok] < 0 ? 0ll : turn_position(p.t, s_b[tok], s_node[tok]); });
+    turn_tables<VE>(p.t, rot_cs, tokens, [&](int tok) { return s_page[tok] < 0 ? 0ll : turn_position(p.t, s_b[tok], s_node[tok]); });
     __syncthreads();
   }
+  T* const mine = reinterpret_cast<T*>(rot_cs + p.table_floats) + group * dim;
   const int heads = 2 * p.heads, rows = tokens * layers * heads;
   const Step step(groups, heads, layers);
   Step at(group, heads, layers);
   for (int r = group; r - group < rows; r += groups, at.add(step, heads, layers)) {
-    const bool in = r < rows;
-    const int tok = in ? at.t : 0, l = l0 + at.l;
+    const int tok = r < rows ? at.t : 0, l = l0 + at.l;
     const long long page = s_page[tok];
-    const bool there = in && page >= 0 && c * ROT_E < p.t.dim, is_v = at.h >= p.heads;
-    const int h = is_v ? at.h - p.heads : at.h;
+    const bool in = r < rows && page >= 0, is_v = at.h >= p.heads, turn = !is_v && p.t.freq;
+    const int h = is_v ? at.h - p.heads : at.h, token = s_token[tok];
     const long long* in_s = is_v ? p.v_in : p.k_in;
     const T* row = reinterpret_cast<const T*>(is_v ? p.v : p.k) + l * in_s[0] + s_b[tok] * in_s[1] + s_node[tok] * in_s[2] + h * in_s[3];
-    const T* weight = p.weight ? reinterpret_cast<const T*>(p.weight) + (long long)l * p.t.dim : nullptr;
-    float y[ROT_E];
-    row_group<T, WIDE>(p.t, row, weight, rot_cs + tok * floats, c, there, !is_v, !is_v && p.t.freq, y);
-    if (!there) continue;
-    const int token = s_token[tok];
+    const T* weight = p.weight ? reinterpret_cast<const T*>(p.weight) + (long long)l * dim : nullptr;
     char* to = (is_v ? p.cache_v : p.cache_k) + l * p.to[0] + page * p.to[1] + h * p.to[2];
-    if constexpr (PACKED) {
-      uint32_t most = 0;
-#pragma unroll
-      for (int i = 0; i < ROT_E; ++i) {
-        y[i] = to_float(from_float<T>(y[i]));  // what a cache of this type would hold
-        const uint32_t bits = __float_as_uint(y[i]) & 0x7FFFFFFFu;
-        most = bits > most ? bits : most;
-      }
-      const uint32_t byte = pk_scale_byte(most);
-      *reinterpret_cast<uint2*>(to + token * (p.t.dim / 2) + c * 8) = pk_codes<sizeof(T) == 2>(y, byte);
-      to[(long long)p.page * (p.t.dim / 2) + token * (p.t.dim / 16) + c] = (char)byte;
+    if constexpr (!PACKED) {
+      T* out = reinterpret_cast<T*>(to + token * p.to[3]);
+      row_units<T, VE>(p.t, row, weight, rot_cs + tok * floats, c, in, !is_v, turn, [&](float (&y)[2 * VE], int a, int b) {
+        store_vec<T, VE>(out + a, y);
+        if (b < dim) store_vec<T, VE>(out + b, y + VE);
+      });
     } else {
-      T* out = reinterpret_cast<T*>(to + token * p.to[3]) + c * ROT_E;
-      if (WIDE) {
-        store_row16(out, y);
-      } else {
+      const bool direct = VE == 8 && !(turn && !p.t.pairs);
+      float z[PK_GROUP];
+      row_units<T, VE>(p.t, row, weight, rot_cs + tok * floats, c, in, !is_v, turn, [&](float (&y)[2 * VE], int a, int b) {
+        if (direct) {
+          if constexpr (VE == 8) {
 #pragma unroll
-        for (int i = 0; i < ROT_E; ++i)
-          if (c * ROT_E + i < p.t.dim) out[i] = from_float<T>(y[i]);
+            for (int i = 0; i < PK_GROUP; ++i) z[i] = to_float(from_float<T>(y[i]));
+          }
+        } else {
+          store_vec<T, VE>(mine + a, y);
+          if (b < dim) store_vec<T, VE>(mine + b, y + VE);
+        }
+      });
+      __syncwarp();
+      if (in && c * PK_GROUP < dim) {
+        if (!direct) {
+          load_vec<T, 8>(mine + c * PK_GROUP, z);
+          load_vec<T, 8>(mine + c * PK_GROUP + 8, z + 8);
+        }
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < PK_GROUP; ++i) most = max(most, __float_as_uint(z[i]) & 0x7FFFFFFFu);
+        const uint32_t byte = pk_scale_byte(most);
+        *reinterpret_cast<uint2*>(to + token * (dim / 2) + c * 8) = pk_codes<sizeof(T) == 2>(z, most, byte);
+        to[(long long)p.page * (dim / 2) + token * (dim / 16) + c] = (char)byte;
       }
+      __syncwarp();  // the row in shared memory has been read
     }
   }
 }
@@ -240,7 +250,7 @@ __global__ void __launch_bounds__(ROT_THREADS) kv_read_kernel(const __grid_const
       } else {
         const T* row = reinterpret_cast<const T*>(from + token * p.from[3]) + c * ROT_E;
         if (WIDE) {
-          load_row16(row, y);
+          load_vec<T, 16>(row, y);
         } else {
 #pragma unroll
           for (int i = 0; i < ROT_E; ++i)
@@ -249,7 +259,7 @@ __global__ void __launch_bounds__(ROT_THREADS) kv_read_kernel(const __grid_const
       }
     }
     if (WIDE) {
-      store_row16(out, y);
+      store_vec<T, 16>(out, y);
     } else {
 #pragma unroll
       for (int i = 0; i < ROT_E; ++i)
@@ -259,10 +269,21 @@ __global__ void __launch_bounds__(ROT_THREADS) kv_read_kernel(const __grid_const
 }
 
 // ---- host ------------------------------------------------------------------------------------
-bool fits16(const void* p, const long long* strides, int n, int es) {
+// The bits of an address and its strides: what accesses have to be aligned to goes by the lowest.
+uintptr_t bits_of(const void* p, const long long* strides, int n, int es) {
   uintptr_t bits = (uintptr_t)p;
   for (int i = 0; i < n; ++i) bits |= (uintptr_t)(strides[i] * es);
-  return (bits & 15) == 0;
+  return bits;
+}
+// Elements of a unit's vectors: 8 or 4 where rows allow (accesses of 16 bytes; 8 bytes for 4 short elements), else 1.
+int unit_width(const Turn& t, uintptr_t bits, int es) {
+  if (turn_fits(t, 8) && (bits & 15) == 0) return 8;
+  return turn_fits(t, 4) && (bits & (4 * es - 1)) == 0 ? 4 : 1;
+}
+int row_lanes(int dim) {  // of 16 elements
+  int n = 1;
+  while (n * ROT_E < dim) n *= 2;
+  return n;
 }
 
 int element_size(int dtype) { return dtype == STAND_DTYPE_F32 ? 4 : 2; }
@@ -276,17 +297,40 @@ int tokens_per_block(long long places, int rows_of_token, int lanes) {
   return tokens;
 }
 
-template <typename T> int launch_rotate(const RotateParams& p, bool wide, dim3 grid, size_t smem, cudaStream_t st) {
-  if (wide) return launch_dependent(rotate_heads_kernel<T, true>, grid, ROT_THREADS, st, p, smem);
-  return launch_dependent(rotate_heads_kernel<T, false>, grid, ROT_THREADS, st, p, smem);
+template <typename T, int VE> int launch_rotate(RotateParams& p, cudaStream_t st) {
+  turn_units(p.t, VE);
+  const long long places = (long long)p.B * p.N;
+  p.tokens = tokens_per_block(places, p.heads, p.t.lanes);
+  // few tokens: their heads are shared out over blocks of a row per group of lanes
+  p.heads_block = p.heads;
+  const int groups = ROT_THREADS / p.t.lanes;
+  if (places * ((p.heads + groups - 1) / groups) <= 4 * 148) p.heads_block = groups < p.heads ? groups : p.heads;
+  const long long blocks = (places + p.tokens - 1) / p.tokens;
+  if (blocks > 0x7FFFFFFFll) return STAND_E_ARG;
+  const dim3 grid((unsigned)blocks, (unsigned)((p.heads + p.heads_block - 1) / p.heads_block));
+  const size_t smem = (size_t)p.tokens * 2 * turn_floats<VE>(p.t.columns) * sizeof(float);
+  return launch_dependent(rotate_heads_kernel<T, VE>, grid, ROT_THREADS, st, p, smem);
 }
-template <typename T> int launch_append(const AppendParams& p, bool wide, bool packed, dim3 grid, size_t smem, cudaStream_t st) {
-  if (packed) {
-    if (wide) return launch_dependent(kv_append_kernel<T, true, true>, grid, ROT_THREADS, st, p, smem);
-    return launch_dependent(kv_append_kernel<T, false, true>, grid, ROT_THREADS, st, p, smem);
-  }
-  if (wide) return launch_dependent(kv_append_kernel<T, true, false>, grid, ROT_THREADS, st, p, smem);
-  return launch_dependent(kv_append_kernel<T, false, false>, grid, ROT_THREADS, st, p, smem);
+template <typename T> int launch_rotate(RotateParams& p, int ve, cudaStream_t st) {
+  return ve == 8 ? launch_rotate<T, 8>(p, st) : (ve == 4 ? launch_rotate<T, 4>(p, st) : launch_rotate<T, 1>(p, st));
+}
+
+template <typename T, int VE> int launch_append(AppendParams& p, bool packed, cudaStream_t st) {
+  turn_units(p.t, VE);
+  // A token's angles are worked out once for all layers of a block: few blocks per token, but enough to fill the GPU.
+  const int groups = ROT_THREADS / p.t.lanes, rows = 2 * p.heads;
+  int lpb = p.layers;
+  while (lpb > 1 && lpb * rows > 2 * groups && p.places * ((p.layers + lpb - 1) / lpb) < 4 * 148) lpb = (lpb + 1) / 2;
+  p.layers_block = lpb;
+  p.tokens = tokens_per_block(p.places, rows * lpb, p.t.lanes);
+  const dim3 grid((unsigned)((p.places + p.tokens - 1) / p.tokens), (unsigned)((p.layers + lpb - 1) / lpb));
+  p.table_floats = p.tokens * 2 * turn_floats<VE>(p.t.columns);
+  const size_t smem = p.table_floats * sizeof(float) + (packed ? (size_t)groups * p.t.dim * sizeof(T) : 0);
+  if (packed) return launch_dependent(kv_append_kernel<T, VE, true>, grid, ROT_THREADS, st, p, smem);
+  return launch_dependent(kv_append_kernel<T, VE, false>, grid, ROT_THREADS, st, p, smem);
+}
+template <typename T> int launch_append(AppendParams& p, int ve, bool packed, cudaStream_t st) {
+  return ve == 8 ? launch_append<T, 8>(p, packed, st) : (ve == 4 ? launch_append<T, 4>(p, packed, st) : launch_append<T, 1>(p, packed, st));
 }
 template <typename T> int launch_read(const ReadParams& p, bool wide, bool packed, dim3 grid, cudaStream_t st) {
   if (packed) {
@@ -305,8 +349,8 @@ bool make_turn(Turn& t, int dim, int rotary, int interleaved, int norm, float ep
   if (norm && !(eps > 0.0f && eps < INFINITY)) return false;
   if (!aligned(4, freq, offset) || !aligned(8, base)) return false;
   t.freq = freq; t.base = (const long long*)base; t.offset = offset; t.offset_stride = offset_stride;
-  t.half = rotary / 2; t.pairs = interleaved; t.columns = turn_columns(t.half, t.pairs); t.norm = norm; t.eps = eps; t.inv_dim = 1.0f / (float)dim;
-  t.dim = dim; t.lanes = row_lanes(dim);
+  t.half = rotary / 2; t.pairs = interleaved; t.norm = norm; t.eps = eps; t.inv_dim = 1.0f / (float)dim;
+  t.dim = dim;
   return true;
 }
 
@@ -335,22 +379,11 @@ int stand_rotate_heads(const stand_rotation* c, const void* dev_q, const void* d
   }
   p.q = dev_q; p.k = dev_k; p.q_out = dev_q_out; p.k_out = dev_k_out; p.weight_q = dev_weight_q; p.weight_k = dev_weight_k;
   p.B = c->B; p.N = c->N; p.heads_q = c->heads_q; p.heads = c->heads_q + c->heads_kv;
-  const bool wide = turn_wide(p.t) && fits16(dev_q, p.q_in, 3, es) && fits16(dev_k, p.k_in, 3, es) && fits16(dev_q_out, p.q_to, 3, es) &&
-                    fits16(dev_k_out, p.k_to, 3, es) && (((uintptr_t)dev_weight_q | (uintptr_t)dev_weight_k) & 15) == 0;
-  const long long places = (long long)p.B * p.N;
-  p.tokens = tokens_per_block(places, p.heads, p.t.lanes);
-  // few tokens: their heads are shared out over blocks of a row per group of lanes
-  p.heads_block = p.heads;
-  const int groups = ROT_THREADS / p.t.lanes;
-  if (places * ((p.heads + groups - 1) / groups) <= 4 * 148) p.heads_block = groups < p.heads ? groups : p.heads;
-  const long long blocks = (places + p.tokens - 1) / p.tokens;
-  if (blocks > 0x7FFFFFFFll) return STAND_E_ARG;
-  const dim3 grid((unsigned)blocks, (unsigned)((p.heads + p.heads_block - 1) / p.heads_block));
-  const size_t smem = (size_t)p.tokens * 2 * turn_floats(p.t.columns, p.t.pairs) * sizeof(float);
+  const int ve = unit_width(p.t, bits_of(dev_q, p.q_in, 3, es) | bits_of(dev_k, p.k_in, 3, es) | bits_of(dev_q_out, p.q_to, 3, es) | bits_of(dev_k_out, p.k_to, 3, es), es);
   cudaStream_t st = (cudaStream_t)cu_stream;
-  if (c->dtype == STAND_DTYPE_F32) return launch_rotate<float>(p, wide, grid, smem, st);
-  if (c->dtype == STAND_DTYPE_BF16) return launch_rotate<__nv_bfloat16>(p, wide, grid, smem, st);
-  return launch_rotate<__half>(p, wide, grid, smem, st);
+  if (c->dtype == STAND_DTYPE_F32) return launch_rotate<float>(p, ve, st);
+  if (c->dtype == STAND_DTYPE_BF16) return launch_rotate<__nv_bfloat16>(p, ve, st);
+  return launch_rotate<__half>(p, ve, st);
 }
 
 int stand_kv_append(const stand_kv_rows* c, const void* dev_k, const void* dev_v, const void* dev_weight_k, const float* dev_freq,
@@ -376,20 +409,13 @@ int stand_kv_append(const stand_kv_rows* c, const void* dev_k, const void* dev_v
   p.cache_k = (char*)dev_cache_k; p.cache_v = (char*)dev_cache_v;
   p.layers = c->layers; p.N = c->N; p.width = c->width; p.heads = c->heads; p.page = c->page_size; p.places = (long long)c->B * c->width;
   p.n_slots = (long long)c->pages * c->page_size;
-  const bool wide = turn_wide(p.t) && fits16(dev_k, p.k_in, 4, es) && fits16(dev_v, p.v_in, 4, es) && ((uintptr_t)dev_weight_k & 15) == 0 &&
-                    (c->packed || (fits16(dev_cache_k, p.to, 4, 1) && fits16(dev_cache_v, p.to, 4, 1)));
-  // A token's angles are worked out once for all layers of a block: few blocks per token, but enough to fill the GPU.
-  const int groups = ROT_THREADS / p.t.lanes, rows = 2 * p.heads;
-  int lpb = p.layers;
-  while (lpb > 1 && lpb * rows > 2 * groups && p.places * ((p.layers + lpb - 1) / lpb) < 4 * 148) lpb = (lpb + 1) / 2;
-  p.layers_block = lpb;
-  p.tokens = tokens_per_block(p.places, rows * lpb, p.t.lanes);
-  const dim3 grid((unsigned)((p.places + p.tokens - 1) / p.tokens), (unsigned)((p.layers + lpb - 1) / lpb));
-  const size_t smem = (size_t)p.tokens * 2 * turn_floats(p.t.columns, p.t.pairs) * sizeof(float);
+  uintptr_t bits = bits_of(dev_k, p.k_in, 4, es) | bits_of(dev_v, p.v_in, 4, es) | (uintptr_t)dev_weight_k;
+  if (!c->packed) bits |= bits_of(dev_cache_k, p.to, 4, 1) | bits_of(dev_cache_v, p.to, 4, 1);
+  const int ve = unit_width(p.t, bits, es);
   cudaStream_t st = (cudaStream_t)cu_stream;
-  if (c->dtype == STAND_DTYPE_F32) return launch_append<float>(p, wide, c->packed, grid, smem, st);
-  if (c->dtype == STAND_DTYPE_BF16) return launch_append<__nv_bfloat16>(p, wide, c->packed, grid, smem, st);
-  return launch_append<__half>(p, wide, c->packed, grid, smem, st);
+  if (c->dtype == STAND_DTYPE_F32) return launch_append<float>(p, ve, c->packed, st);
+  if (c->dtype == STAND_DTYPE_BF16) return launch_append<__nv_bfloat16>(p, ve, c->packed, st);
+  return launch_append<__half>(p, ve, c->packed, st);
 }
 
 int stand_kv_read(const stand_kv_rows* c, const void* dev_cache_k, const void* dev_cache_v, const int64_t* dev_slots, void* dev_k, void* dev_v,
@@ -412,7 +438,7 @@ int stand_kv_read(const stand_kv_rows* c, const void* dev_cache_k, const void* d
   p.layers = c->layers; p.heads = c->heads; p.dim = c->dim; p.page = c->page_size; p.lanes = row_lanes(c->dim);
   p.places = (long long)c->B * c->width; p.n_slots = (long long)c->pages * c->page_size;
   const bool wide = p.dim % ROT_E == 0 && (((uintptr_t)dev_k | (uintptr_t)dev_v) & 15) == 0 &&
-                    (c->packed || (fits16(dev_cache_k, p.from, 4, 1) && fits16(dev_cache_v, p.from, 4, 1)));
+                    (c->packed || ((bits_of(dev_cache_k, p.from, 4, 1) | bits_of(dev_cache_v, p.from, 4, 1)) & 15) == 0);
   const int groups = ROT_THREADS / p.lanes, rows = 2 * p.heads;
   int lpb = p.layers;
   while (lpb > 1 && lpb * rows > 4 * groups) lpb = (lpb + 1) / 2;
