@@ -13,6 +13,7 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include "attention.cuh"
 #include "common.cuh"
 
 namespace stand {
@@ -29,10 +30,11 @@ __device__ __forceinline__ float pk_scale(uint32_t byte) {
 }
 
 // The scale of a group whose largest magnitude has these bits (of a 32-bit float without its sign; NaN and infinity are the
-// largest).  A first guess by rounding amax / 7 up, then put right by the definition, since 7 s is exact.
-__device__ __forceinline__ uint32_t pk_scale_byte(uint32_t amax_bits) {
+// largest): amax / 7 rounded up to 4 significant bits.  SHORT: amax has at most 11 of them, so it is either 7 s exactly or 2^-11 away
+// from it, and the product with a constant just below 1 / 7 rounds up to the right one.  32 bits: a first guess, put right by the definition.
+template <bool SHORT> __device__ __forceinline__ uint32_t pk_scale_byte(uint32_t amax_bits) {
   if (amax_bits >= 0x7F800000u) return 0xFF;
-  const float amax = __uint_as_float(amax_bits), t = amax * (1.0f / 7.0f);
+  const float amax = __uint_as_float(amax_bits), t = amax * __uint_as_float(0x3E124924u);  // 1 / 7 (1 - 2^-24)
   uint32_t b;
   if (t >= 0x1p-14f) {
     b = (__float_as_uint(t) + 0xFFFFFu) >> 20;
@@ -41,12 +43,13 @@ __device__ __forceinline__ uint32_t pk_scale_byte(uint32_t amax_bits) {
   } else {
     b = (uint32_t)ceilf(t * 0x1p17f);
   }
+  if (SHORT) return b;
   if (b < PK_LAST && 7.0f * pk_scale(b) < amax) ++b;
   else if (b > 0 && 7.0f * pk_scale(b - 1) >= amax) --b;
   return b;
 }
 
-// The codes of 16 elements.  Elements of 16 bits: an element has at most 11 significant bits and s has 4, so a quotient that is
+// The codes of 16 elements.  SHORT: an element has at most 11 significant bits and s has 4, so a quotient that is
 // no tie is at least 2^-12 from one; the product with the reciprocal is off by 7 * 2^-23 at most, and rounding it to multiples
 // of 2^-13 (the sum with 1536) makes a tie one again; the second sum rounds to whole numbers.  32 bits: the quotient rounded to 32
 // bits, then to a whole number.  Four whole numbers + 8 are put together as digits of a float, which costs less than shifts and masks.
@@ -57,23 +60,47 @@ __device__ __forceinline__ uint2 pk_codes(float (&y)[PK_GROUP], uint32_t amax_bi
 #pragma unroll
     for (int i = 0; i < PK_GROUP; ++i) y[i] = fminf(fmaxf(y[i], -PK_MOST), PK_MOST);
   }
-  const float s = pk_scale(byte), inv = 1.0f / s;
-  float k[PK_GROUP];
-#pragma unroll
-  for (int i = 0; i < PK_GROUP; ++i) {
-    if (SHORT) k[i] = fmaf(y[i], inv, 1536.0f) + (12582912.0f + 8.0f - 1536.0f);
-    else k[i] = __fdiv_rn(y[i], s) + (12582912.0f + 8.0f);
-    k[i] -= 12582912.0f;
-  }
+  const float s = pk_scale(byte), inv = __frcp_rn(s);
   uint32_t w[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const float* e = k + 8 * h;
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (SHORT) e[i] = fmaf(y[8 * h + i], inv, 1536.0f) + (12582912.0f + 8.0f - 1536.0f);
+      else e[i] = __fdiv_rn(y[8 * h + i], s) + (12582912.0f + 8.0f);
+      e[i] -= 12582912.0f;
+    }
     const float even = fmaf(fmaf(fmaf(e[6], 16.0f, e[4]), 16.0f, e[2]), 16.0f, e[0]), odd = fmaf(fmaf(fmaf(e[7], 16.0f, e[5]), 16.0f, e[3]), 16.0f, e[1]);
     w[h] = __byte_perm(__float_as_uint(even + 8388608.0f), __float_as_uint(odd + 8388608.0f), 0x5410);
   }
   return make_uint2(w[0], w[1]);
 }
+
+// A group as it lies: 16 elements of type T in words.  Its codes and its scale's byte.
+template <typename T> struct PkGroup {
+  static constexpr int WORDS = PK_GROUP * sizeof(T) / 4;
+  uint32_t w[WORDS];
+
+  __device__ __forceinline__ uint2 codes(uint32_t& byte) const {
+    uint32_t most = 0;
+    float y[PK_GROUP];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) most = __vmaxu2(most, w[i] & 0x7FFF7FFFu);
+      most = max(most & 0xFFFFu, most >> 16);
+      const unsigned short bits = (unsigned short)most;
+      most = __float_as_uint(to_float(*reinterpret_cast<const T*>(&bits)));
+#pragma unroll
+      for (int i = 0; i < PK_GROUP; ++i) y[i] = to_float(reinterpret_cast<const T*>(w)[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PK_GROUP; ++i) most = max(most, w[i] & 0x7FFFFFFFu), y[i] = __uint_as_float(w[i]);
+    }
+    byte = pk_scale_byte<sizeof(T) == 2>(most);
+    return pk_codes<sizeof(T) == 2>(y, most, byte);
+  }
+};
 
 // 8 elements of a word as floats.
 __device__ __forceinline__ void pk_values(uint32_t w, float s, float* v) {

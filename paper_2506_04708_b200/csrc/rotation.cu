@@ -123,10 +123,11 @@ struct AppendParams {
 // Packed: a lane takes a group of 16 elements.  Where units are such groups they stay in registers; else (halves that are turned, short units) the
 // row goes through shared memory, as what a cache of its type would hold.
 template <typename T, int VE, bool PACKED>
-__global__ void __launch_bounds__(ROT_THREADS) kv_append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(ROT_THREADS, sizeof(T) == 2 ? 4 : 3) kv_append_kernel(const __grid_constant__ AppendParams p) {
   extern __shared__ __align__(16) float rot_cs[];
-  __shared__ long long s_page[ROT_TOKENS];  // -1: nothing is stored
-  __shared__ int s_b[ROT_TOKENS], s_node[ROT_TOKENS], s_token[ROT_TOKENS];
+  // of a token: where its rows come from (elements) and go to (bytes; -1: nothing is stored) in the first layer and head; its scales
+  __shared__ long long s_from[2][ROT_TOKENS], s_to[ROT_TOKENS], s_at[ROT_TOKENS];
+  __shared__ int s_scale[ROT_TOKENS];
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, lanes = p.t.lanes, c = tid & (lanes - 1), group = tid / lanes, groups = ROT_THREADS / lanes;
@@ -138,14 +139,16 @@ __global__ void __launch_bounds__(ROT_THREADS) kv_append_kernel(const __grid_con
     const long long place = first + tid, slot = p.slots[place];
     const int b = (int)(place / p.width), j = (int)(place - (long long)b * p.width), node = p.path ? p.path[place] : j;
     const long long page = slot >= 0 && slot < p.n_slots && node >= 0 && node < p.N ? slot / p.page : -1;
-    s_page[tid] = page;
-    s_token[tid] = (int)(slot - page * p.page);
-    s_b[tid] = b;
-    s_node[tid] = node;
+    const int token = (int)(slot - page * p.page);
+    s_from[0][tid] = b * p.k_in[1] + node * p.k_in[2];
+    s_from[1][tid] = b * p.v_in[1] + node * p.v_in[2];
+    s_to[tid] = page < 0 ? -1 : page * p.to[1] + (PACKED ? token * (dim / 2) : token * p.to[3]);
+    s_scale[tid] = p.page * (dim / 2) + token * (dim / 16) - token * (dim / 2);
+    s_at[tid] = page < 0 ? 0 : turn_position(p.t, b, node);
   }
   __syncthreads();
   if (p.t.freq) {
-    turn_tables<VE>(p.t, rot_cs, tokens, [&](int tok) { return s_page[tok] < 0 ? 0ll : turn_position(p.t, s_b[tok], s_node[tok]); });
+    turn_tables<VE>(p.t, rot_cs, tokens, [&](int tok) { return s_at[tok]; });
     __syncthreads();
   }
   T* const mine = reinterpret_cast<T*>(rot_cs + p.table_floats) + group * dim;
@@ -154,45 +157,44 @@ __global__ void __launch_bounds__(ROT_THREADS) kv_append_kernel(const __grid_con
   Step at(group, heads, layers);
   for (int r = group; r - group < rows; r += groups, at.add(step, heads, layers)) {
     const int tok = r < rows ? at.t : 0, l = l0 + at.l;
-    const long long page = s_page[tok];
-    const bool in = r < rows && page >= 0, is_v = at.h >= p.heads, turn = !is_v && p.t.freq;
-    const int h = is_v ? at.h - p.heads : at.h, token = s_token[tok];
-    const long long* in_s = is_v ? p.v_in : p.k_in;
-    const T* row = reinterpret_cast<const T*>(is_v ? p.v : p.k) + l * in_s[0] + s_b[tok] * in_s[1] + s_node[tok] * in_s[2] + h * in_s[3];
+    const long long base = s_to[tok];
+    const bool in = r < rows && base >= 0, is_v = at.h >= p.heads, turn = !is_v && p.t.freq;
+    const int h = is_v ? at.h - p.heads : at.h;
+    const T* row = is_v ? reinterpret_cast<const T*>(p.v) + s_from[1][tok] + l * p.v_in[0] + h * p.v_in[3]
+                        : reinterpret_cast<const T*>(p.k) + s_from[0][tok] + l * p.k_in[0] + h * p.k_in[3];
     const T* weight = p.weight ? reinterpret_cast<const T*>(p.weight) + (long long)l * dim : nullptr;
-    char* to = (is_v ? p.cache_v : p.cache_k) + l * p.to[0] + page * p.to[1] + h * p.to[2];
+    char* to = (is_v ? p.cache_v : p.cache_k) + base + l * p.to[0] + h * p.to[2];
     if constexpr (!PACKED) {
-      T* out = reinterpret_cast<T*>(to + token * p.to[3]);
+      T* out = reinterpret_cast<T*>(to);
       row_units<T, VE>(p.t, row, weight, rot_cs + tok * floats, c, in, !is_v, turn, [&](float (&y)[2 * VE], int a, int b) {
         store_vec<T, VE>(out + a, y);
         if (b < dim) store_vec<T, VE>(out + b, y + VE);
       });
     } else {
-      const bool direct = VE == 8 && !(turn && !p.t.pairs);
-      float z[PK_GROUP];
-      row_units<T, VE>(p.t, row, weight, rot_cs + tok * floats, c, in, !is_v, turn, [&](float (&y)[2 * VE], int a, int b) {
-        if (direct) {
-          if constexpr (VE == 8) {
+      // rows that stay as they are go straight to their groups, and so do units that are groups
+      const bool same = VE == 8 && !turn && (is_v || !p.t.norm), direct = VE == 8 && !(turn && !p.t.pairs), has = in && c * PK_GROUP < dim;
+      PkGroup<T> z;
+      if (same && has) {
 #pragma unroll
-            for (int i = 0; i < PK_GROUP; ++i) z[i] = to_float(from_float<T>(y[i]));
-          }
+        for (int i = 0; i < PkGroup<T>::WORDS / 4; ++i) reinterpret_cast<uint4*>(z.w)[i] = reinterpret_cast<const uint4*>(row + c * PK_GROUP)[i];
+      }
+      row_units<T, VE>(p.t, row, weight, rot_cs + tok * floats, c, in && !same, !is_v, turn, [&](float (&y)[2 * VE], int a, int b) {
+        if (direct) {
+          if constexpr (VE == 8) store_vec<T, 16>(reinterpret_cast<T*>(z.w), y);
         } else {
           store_vec<T, VE>(mine + a, y);
           if (b < dim) store_vec<T, VE>(mine + b, y + VE);
         }
       });
       __syncwarp();
-      if (in && c * PK_GROUP < dim) {
+      if (has) {
         if (!direct) {
-          load_vec<T, 8>(mine + c * PK_GROUP, z);
-          load_vec<T, 8>(mine + c * PK_GROUP + 8, z + 8);
-        }
-        uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < PK_GROUP; ++i) most = max(most, __float_as_uint(z[i]) & 0x7FFFFFFFu);
-        const uint32_t byte = pk_scale_byte(most);
-        *reinterpret_cast<uint2*>(to + token * (dim / 2) + c * 8) = pk_codes<sizeof(T) == 2>(z, most, byte);
-        to[(long long)p.page * (dim / 2) + token * (dim / 16) + c] = (char)byte;
+          for (int i = 0; i < PkGroup<T>::WORDS / 4; ++i) reinterpret_cast<uint4*>(z.w)[i] = reinterpret_cast<const uint4*>(mine + c * PK_GROUP)[i];
+        }
+        uint32_t byte;
+        *reinterpret_cast<uint2*>(to + c * 8) = z.codes(byte);
+        to[s_scale[tok] + c] = (char)byte;
       }
       __syncwarp();  // the row in shared memory has been read
     }
