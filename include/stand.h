@@ -470,7 +470,7 @@ int stand_process_logits(const stand_logits* shape, const stand_logits_inputs* i
 
 /* The shapes of stand_rotate_heads (zero the structure first).  Strides are in elements; dim is contiguous. */
 typedef struct {
-  int32_t B, N;           /* sequences, tokens (or nodes) of each */
+  int32_t B, N;           /* sequences, tokens (or nodes) of each; B * N below 2^31 */
   int32_t heads_q, heads_kv;
   int32_t dim;            /* 1..256 */
   int32_t dtype;

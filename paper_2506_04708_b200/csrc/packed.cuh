@@ -80,7 +80,7 @@ __device__ __forceinline__ uint2 pk_codes(float (&y)[PK_GROUP], uint32_t amax_bi
 // A group as it lies: 16 elements of type T in words.  Its codes and its scale's byte.
 template <typename T> struct PkGroup {
   static constexpr int WORDS = PK_GROUP * sizeof(T) / 4;
-  uint32_t w[WORDS];
+  alignas(16) uint32_t w[WORDS];
 
   __device__ __forceinline__ uint2 codes(uint32_t& byte) const {
     uint32_t most = 0;

@@ -6,6 +6,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "launch.cuh"
 #include "packed.cuh"
 #include "rotation.cuh"
@@ -19,10 +21,11 @@ constexpr int ROT_E = 16;  // elements of a lane that reads
 constexpr int ROW_COUNT = 4096;  // layers, heads: their product counts rows in 32 bits
 constexpr int ROT_TOKENS = 16;  // tokens of a block, at most: their cosines and sines lie in shared memory
 
-// A digit of a row number that counts in steps: no divisions in the loop.
+// The digits of a row number that counts in steps: no divisions in the loop, and the step's own are worked out on the host.
 struct Step {
   int h, l, t;  // heads, layers, tokens
-  __device__ __forceinline__ Step(int i, int heads, int layers) : h(i % heads), l(i / heads % layers), t(i / heads / layers) {}
+  Step() = default;
+  __host__ __device__ __forceinline__ Step(int i, int heads, int layers) : h(i % heads), l(i / heads % layers), t(i / heads / layers) {}
   __device__ __forceinline__ void add(const Step& o, int heads, int layers) {
     h += o.h;
     l += o.l;
@@ -56,50 +59,80 @@ struct RotateParams {
   int B, N, heads_q, heads;  // heads: of queries and keys together
   int tokens;                // of a block
   int heads_block;           // heads of a block (grid.y blocks share a token's heads)
+  bool narrow;               // offsets fit 31 bits, those of a block's steps past the end too
   long long q_in[3], k_in[3], q_to[3], k_to[3];
 };
 
-template <typename T, int VE> __global__ void __launch_bounds__(ROT_THREADS) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
+// I: the type of offsets; 32 bits where they fit, for they are most of the arithmetic.
+template <typename T, int VE, typename I> __global__ void __launch_bounds__(ROT_THREADS, 4) rotate_heads_kernel(const __grid_constant__ RotateParams p) {
   extern __shared__ __align__(16) float rot_cs[];
-  __shared__ __align__(16) float s_weight[2][ROT_DIM_MAX];
+  __shared__ __align__(16) float s_weight[2][ROT_DIM_MAX];  // lanes * units * elements: a power of two, at most 256
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, lanes = p.t.lanes, c = tid & (lanes - 1), group = tid / lanes, groups = ROT_THREADS / lanes;
-  const long long first = (long long)blockIdx.x * p.tokens, all = (long long)p.B * p.N;
-  const int tokens = all - first < p.tokens ? (int)(all - first) : p.tokens;
-  const int h0 = blockIdx.y * p.heads_block, heads = p.heads - h0 < p.heads_block ? p.heads - h0 : p.heads_block;
+  const int first = blockIdx.x * p.tokens, tokens = p.B * p.N - first < p.tokens ? p.B * p.N - first : p.tokens;
   const int floats = 2 * turn_floats<VE>(p.t.columns);
-  if (p.t.freq)
+  const int tok_b = first / p.N, tok_n = first - tok_b * p.N;  // of the block's first token
+  if (p.t.freq) {
     turn_tables<VE>(p.t, rot_cs, tokens, [&](int tok) {
-      const long long at = first + tok;
-      const int b = (int)(at / p.N);
-      return turn_position(p.t, b, (int)(at - (long long)b * p.N));
-    });
-  if (p.t.norm)
-    for (int i = tid; i < p.t.dim; i += ROT_THREADS) {
-      s_weight[0][i] = p.weight_q ? to_float(reinterpret_cast<const T*>(p.weight_q)[i]) : 1.0f;
-      s_weight[1][i] = p.weight_k ? to_float(reinterpret_cast<const T*>(p.weight_k)[i]) : 1.0f;
-    }
-  __syncthreads();
-  const int rows = tokens * heads;
-  const Step step(groups, heads, 1);
-  Step at(group, heads, 1);
-  const int tok_b = (int)(first / p.N), tok_n = (int)(first - (long long)tok_b * p.N);  // of the block's first token
-  for (int r = group; r - group < rows; r += groups, at.add(step, heads, 1)) {
-    const int tok = at.t + at.l, head = h0 + at.h;  // one layer: its carry goes to the token
-    int b = tok_b, n = tok_n + tok;
-    while (n >= p.N) n -= p.N, ++b;
-    const bool is_q = head < p.heads_q;
-    const int h = is_q ? head : head - p.heads_q;
-    const long long* in_s = is_q ? p.q_in : p.k_in;
-    const long long* out_s = is_q ? p.q_to : p.k_to;
-    const T* row = reinterpret_cast<const T*>(is_q ? p.q : p.k) + b * in_s[0] + n * in_s[1] + h * in_s[2];
-    T* to = reinterpret_cast<T*>(is_q ? p.q_out : p.k_out) + b * out_s[0] + n * out_s[1] + h * out_s[2];
-    row_units<T, VE>(p.t, row, s_weight[is_q ? 0 : 1], rot_cs + tok * floats, c, r < rows, true, p.t.freq != nullptr, [&](float (&y)[2 * VE], int a, int b2) {
-      store_vec<T, VE>(to + a, y);
-      if (b2 < p.t.dim) store_vec<T, VE>(to + b2, y + VE);
+      int b = tok_b, n = tok_n + tok;
+      while (n >= p.N) n -= p.N, ++b;
+      return turn_position(p.t, b, n);
     });
   }
+  // Weights in the order of the lanes: element e of lane l's unit k at (k * 2 VE + e) * lanes + l, four elements of a lane together (VE = 1: two apart),
+  // so that a row's lanes read without conflict.
+  constexpr int K = RowLane<T, VE>::K, Q = VE < 4 ? 1 : 4;
+  if (p.weight_q || p.weight_k)
+    for (int i = tid; i < lanes * 2 * VE * K; i += ROT_THREADS) {
+      const int l = i / Q % lanes, e = i / (Q * lanes) * Q + i % Q, k = e / (2 * VE), in_unit = e % (2 * VE);
+      const RowLane<T, VE> at(p.t, l, p.t.freq != nullptr);
+      int from = 0;
+#pragma unroll
+      for (int kk = 0; kk < K; ++kk)
+        if (kk == k) from = in_unit < VE ? at.a[kk] + in_unit : at.b[kk] + in_unit - VE;
+      if (p.weight_q) s_weight[0][i] = to_float(reinterpret_cast<const T*>(p.weight_q)[from]);
+      if (p.weight_k) s_weight[1][i] = to_float(reinterpret_cast<const T*>(p.weight_k)[from]);
+    }
+  __syncthreads();
+  const bool norm = p.t.norm;
+  // some heads of all of the block's tokens; queries and keys one after the other, so that strides and weights are the same for all lanes
+  auto kind = [&](const void* src, void* dst, const long long (&in_s)[3], const long long (&out_s)[3], const float* weight, int head0, int heads) {
+    if (heads <= 0) return;
+    RowLane<T, VE> lane(p.t, c, p.t.freq != nullptr);
+    const int rows = tokens * heads, step_h = groups % heads, step_t = groups / heads;
+    int h = group % heads, tok = group / heads, n = tok_n + tok;
+    const I in0 = (I)in_s[0], in1 = (I)in_s[1], in2 = (I)in_s[2], out0 = (I)out_s[0], out1 = (I)out_s[1], out2 = (I)out_s[2];
+    const T* const from = reinterpret_cast<const T*>(src) + tok_b * in0 + tok_n * in1 + head0 * in2;
+    T* const to = reinterpret_cast<T*>(dst) + tok_b * out0 + tok_n * out1 + head0 * out2;
+    I in_at = h * in2 + tok * in1, out_at = h * out2 + tok * out1;
+    // a step further, and what is put right where the heads of a token or the tokens of a sequence end
+    const I in_step = step_h * in2 + step_t * in1, in_head = in1 - heads * in2, in_seq = in0 - p.N * in1;
+    const I out_step = step_h * out2 + step_t * out1, out_head = out1 - heads * out2, out_seq = out0 - p.N * out1;
+    auto weights = [&](float (&w)[2 * VE], int k) {
+#pragma unroll
+      for (int e = 0; e < 2 * VE; e += Q) {
+        const float* at = weight + ((k * 2 * VE + e) * lanes + c * Q);
+        if constexpr (Q == 4) *reinterpret_cast<float4*>(w + e) = *reinterpret_cast<const float4*>(at);
+        else w[e] = *at;
+      }
+    };
+    for (int r = group; r - group < rows; r += groups) {
+      while (n >= p.N) n -= p.N, in_at += in_seq, out_at += out_seq;
+      const bool in = r < rows;
+      T* const out = to + out_at;
+      lane.row(p.t, from + (in ? in_at : 0), weight != nullptr, weights, rot_cs + (in ? tok * floats : 0), in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
+        store_vec<T, VE>(out + a, y);
+        if (two) store_vec<T, VE>(out + b, y + VE);
+      });
+      h += step_h, tok += step_t, n += step_t, in_at += in_step, out_at += out_step;
+      if (h >= heads) h -= heads, ++tok, ++n, in_at += in_head, out_at += out_head;
+    }
+  };
+  const int h0 = blockIdx.y * p.heads_block, h1 = h0 + p.heads_block < p.heads ? h0 + p.heads_block : p.heads;
+  kind(p.q, p.q_out, p.q_in, p.q_to, p.weight_q ? s_weight[0] : nullptr, h0, (h1 < p.heads_q ? h1 : p.heads_q) - h0);
+  const int k0 = h0 > p.heads_q ? h0 : p.heads_q;
+  kind(p.k, p.k_out, p.k_in, p.k_to, p.weight_k ? s_weight[1] : nullptr, k0 - p.heads_q, h1 - k0);
 }
 
 struct AppendParams {
@@ -114,6 +147,7 @@ struct AppendParams {
   int layers, N, width, heads, page;
   long long places;  // B * width
   int tokens, layers_block;
+  Step step;         // rows that a block takes at a time
   int table_floats;  // of all tokens; a block's rows on their way to groups of 16 lie behind them
   long long n_slots;
   long long k_in[4], v_in[4];  // elements
@@ -136,8 +170,9 @@ __global__ void __launch_bounds__(ROT_THREADS, sizeof(T) == 2 ? 4 : 3) kv_append
   const int l0 = blockIdx.y * p.layers_block, layers = p.layers - l0 < p.layers_block ? p.layers - l0 : p.layers_block;
   const int floats = 2 * turn_floats<VE>(p.t.columns), dim = p.t.dim;
   if (tid < tokens) {
-    const long long place = first + tid, slot = p.slots[place];
-    const int b = (int)(place / p.width), j = (int)(place - (long long)b * p.width), node = p.path ? p.path[place] : j;
+    const int place = (int)first + tid;  // below 2^31
+    const long long slot = p.slots[place];
+    const int b = place / p.width, j = place - b * p.width, node = p.path ? p.path[place] : j;
     const long long page = slot >= 0 && slot < p.n_slots && node >= 0 && node < p.N ? slot / p.page : -1;
     const int token = (int)(slot - page * p.page);
     s_from[0][tid] = b * p.k_in[1] + node * p.k_in[2];
@@ -152,53 +187,61 @@ __global__ void __launch_bounds__(ROT_THREADS, sizeof(T) == 2 ? 4 : 3) kv_append
     __syncthreads();
   }
   T* const mine = reinterpret_cast<T*>(rot_cs + p.table_floats) + group * dim;
-  const int heads = 2 * p.heads, rows = tokens * layers * heads;
-  const Step step(groups, heads, layers);
-  Step at(group, heads, layers);
-  for (int r = group; r - group < rows; r += groups, at.add(step, heads, layers)) {
-    const int tok = r < rows ? at.t : 0, l = l0 + at.l;
-    const long long base = s_to[tok];
-    const bool in = r < rows && base >= 0, is_v = at.h >= p.heads, turn = !is_v && p.t.freq;
-    const int h = is_v ? at.h - p.heads : at.h;
-    const T* row = is_v ? reinterpret_cast<const T*>(p.v) + s_from[1][tok] + l * p.v_in[0] + h * p.v_in[3]
-                        : reinterpret_cast<const T*>(p.k) + s_from[0][tok] + l * p.k_in[0] + h * p.k_in[3];
-    const T* weight = p.weight ? reinterpret_cast<const T*>(p.weight) + (long long)l * dim : nullptr;
-    char* to = (is_v ? p.cache_v : p.cache_k) + base + l * p.to[0] + h * p.to[2];
-    if constexpr (!PACKED) {
-      T* out = reinterpret_cast<T*>(to);
-      row_units<T, VE>(p.t, row, weight, rot_cs + tok * floats, c, in, !is_v, turn, [&](float (&y)[2 * VE], int a, int b) {
-        store_vec<T, VE>(out + a, y);
-        if (b < dim) store_vec<T, VE>(out + b, y + VE);
-      });
-    } else {
-      // rows that stay as they are go straight to their groups, and so do units that are groups
-      const bool same = VE == 8 && !turn && (is_v || !p.t.norm), direct = VE == 8 && !(turn && !p.t.pairs), has = in && c * PK_GROUP < dim;
-      PkGroup<T> z;
-      if (same && has) {
-#pragma unroll
-        for (int i = 0; i < PkGroup<T>::WORDS / 4; ++i) reinterpret_cast<uint4*>(z.w)[i] = reinterpret_cast<const uint4*>(row + c * PK_GROUP)[i];
-      }
-      row_units<T, VE>(p.t, row, weight, rot_cs + tok * floats, c, in && !same, !is_v, turn, [&](float (&y)[2 * VE], int a, int b) {
-        if (direct) {
-          if constexpr (VE == 8) store_vec<T, 16>(reinterpret_cast<T*>(z.w), y);
+  const int rows = tokens * layers * p.heads;
+  const Step step = layers == p.layers_block ? p.step : Step(groups, p.heads, layers);  // the last layers' blocks may have fewer
+  // keys, then values: strides and what is done are the same for all lanes
+  auto kind = [&](const void* src, const long long (&in_s)[4], const long long* from, char* cache, auto are_keys) {
+    constexpr bool KEYS = decltype(are_keys)::value;
+    const bool turn = KEYS && p.t.freq, norm = KEYS && p.t.norm;
+    RowLane<T, VE> lane(p.t, c, turn);
+    // rows that stay as they are go straight to their groups, and so do units that are groups
+    const bool same = PACKED && VE == 8 && !turn && !norm, direct = VE == 8 && !(turn && !p.t.pairs);
+    Step at(group, p.heads, layers);
+    for (int r = group; r - group < rows; r += groups, at.add(step, p.heads, layers)) {
+      const int tok = r < rows ? at.t : 0, l = l0 + at.l;
+      const long long base = s_to[tok];
+      const bool in = r < rows && base >= 0;
+      const T* row = reinterpret_cast<const T*>(src) + (in ? from[tok] + l * in_s[0] + at.h * in_s[3] : 0);
+      const T* weight = reinterpret_cast<const T*>(p.weight) + (long long)(in ? l : 0) * dim;
+      auto weights = [&](float (&w)[2 * VE], int k) {
+        load_vec<T, VE>(weight + lane.a[k], w);
+        load_vec<T, VE>(weight + lane.b[k], w + VE);
+      };
+      char* to = cache + base + l * p.to[0] + at.h * p.to[2];
+      if constexpr (!PACKED) {
+        T* out = reinterpret_cast<T*>(to);
+        lane.row(p.t, row, p.weight != nullptr, weights, rot_cs + tok * floats, in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
+          store_vec<T, VE>(out + a, y);
+          if (two) store_vec<T, VE>(out + b, y + VE);
+        });
+      } else {
+        const bool has = in && c * PK_GROUP < dim;
+        PkGroup<T> z;
+        if (same) {
+          if (has) copy_vec<T, 16>(reinterpret_cast<T*>(z.w), row + c * PK_GROUP);
         } else {
-          store_vec<T, VE>(mine + a, y);
-          if (b < dim) store_vec<T, VE>(mine + b, y + VE);
+          lane.row(p.t, row, p.weight != nullptr, weights, rot_cs + tok * floats, in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
+            if (direct) {
+              if constexpr (VE == 8) store_vec<T, 16>(reinterpret_cast<T*>(z.w), y);
+            } else {
+              store_vec<T, VE>(mine + a, y);
+              if (two) store_vec<T, VE>(mine + b, y + VE);
+            }
+          });
+          __syncwarp();
+          if (!direct && has) copy_vec<T, 16>(reinterpret_cast<T*>(z.w), mine + c * PK_GROUP);
+          __syncwarp();  // the row in shared memory has been read
         }
-      });
-      __syncwarp();
-      if (has) {
-        if (!direct) {
-#pragma unroll
-          for (int i = 0; i < PkGroup<T>::WORDS / 4; ++i) reinterpret_cast<uint4*>(z.w)[i] = reinterpret_cast<const uint4*>(mine + c * PK_GROUP)[i];
+        if (has) {
+          uint32_t byte;
+          *reinterpret_cast<uint2*>(to + c * 8) = z.codes(byte);
+          to[s_scale[tok] + c] = (char)byte;
         }
-        uint32_t byte;
-        *reinterpret_cast<uint2*>(to + c * 8) = z.codes(byte);
-        to[s_scale[tok] + c] = (char)byte;
       }
-      __syncwarp();  // the row in shared memory has been read
     }
-  }
+  };
+  kind(p.k, p.k_in, s_from[0], p.cache_k, std::true_type{});
+  kind(p.v, p.v_in, s_from[1], p.cache_v, std::false_type{});
 }
 
 struct ReadParams {
@@ -295,7 +338,7 @@ bool type_valid(int dtype) { return dtype >= STAND_DTYPE_F32 && dtype <= STAND_D
 int tokens_per_block(long long places, int rows_of_token, int lanes) {
   const int groups = ROT_THREADS / lanes;
   int tokens = 1;
-  while (tokens < ROT_TOKENS && tokens * rows_of_token < 4 * groups && places / (2 * tokens) >= 2 * 148) tokens *= 2;
+  while (tokens < ROT_TOKENS && tokens * rows_of_token < 8 * groups && places / (2 * tokens) >= 2 * 148) tokens *= 2;
   return tokens;
 }
 
@@ -308,10 +351,10 @@ template <typename T, int VE> int launch_rotate(RotateParams& p, cudaStream_t st
   const int groups = ROT_THREADS / p.t.lanes;
   if (places * ((p.heads + groups - 1) / groups) <= 4 * 148) p.heads_block = groups < p.heads ? groups : p.heads;
   const long long blocks = (places + p.tokens - 1) / p.tokens;
-  if (blocks > 0x7FFFFFFFll) return STAND_E_ARG;
   const dim3 grid((unsigned)blocks, (unsigned)((p.heads + p.heads_block - 1) / p.heads_block));
   const size_t smem = (size_t)p.tokens * 2 * turn_floats<VE>(p.t.columns) * sizeof(float);
-  return launch_dependent(rotate_heads_kernel<T, VE>, grid, ROT_THREADS, st, p, smem);
+  if (p.narrow) return launch_dependent(rotate_heads_kernel<T, VE, int>, grid, ROT_THREADS, st, p, smem);
+  return launch_dependent(rotate_heads_kernel<T, VE, long long>, grid, ROT_THREADS, st, p, smem);
 }
 template <typename T> int launch_rotate(RotateParams& p, int ve, cudaStream_t st) {
   return ve == 8 ? launch_rotate<T, 8>(p, st) : (ve == 4 ? launch_rotate<T, 4>(p, st) : launch_rotate<T, 1>(p, st));
@@ -325,6 +368,7 @@ template <typename T, int VE> int launch_append(AppendParams& p, bool packed, cu
   while (lpb > 1 && lpb * rows > 2 * groups && p.places * ((p.layers + lpb - 1) / lpb) < 4 * 148) lpb = (lpb + 1) / 2;
   p.layers_block = lpb;
   p.tokens = tokens_per_block(p.places, rows * lpb, p.t.lanes);
+  p.step = Step(groups, p.heads, lpb);
   const dim3 grid((unsigned)((p.places + p.tokens - 1) / p.tokens), (unsigned)((p.layers + lpb - 1) / lpb));
   p.table_floats = p.tokens * 2 * turn_floats<VE>(p.t.columns);
   const size_t smem = p.table_floats * sizeof(float) + (packed ? (size_t)groups * p.t.dim * sizeof(T) : 0);
@@ -370,6 +414,7 @@ int stand_rotate_heads(const stand_rotation* c, const void* dev_q, const void* d
                        void* cu_stream) {
   if (!c || !dev_q || !dev_k || !dev_q_out || !dev_k_out || c->B < 1 || c->N < 1 || c->heads_q < 1 || c->heads_kv < 1) return STAND_E_ARG;
   if (!type_valid(c->dtype) || (c->reserved | c->reserved2) != 0 || c->heads_q > (1 << 16) || c->heads_kv > (1 << 16)) return STAND_E_ARG;
+  if ((long long)c->B * c->N > 0x7FFFFFFFll) return STAND_E_ARG;
   RotateParams p;
   if (!make_turn(p.t, c->dim, c->rotary_dim, c->interleaved, c->norm, c->eps, dev_freq, dev_base, dev_offset, c->offset_stride)) return STAND_E_ARG;
   if (!c->norm && (dev_weight_q || dev_weight_k)) return STAND_E_ARG;
@@ -381,6 +426,10 @@ int stand_rotate_heads(const stand_rotation* c, const void* dev_q, const void* d
   }
   p.q = dev_q; p.k = dev_k; p.q_out = dev_q_out; p.k_out = dev_k_out; p.weight_q = dev_weight_q; p.weight_k = dev_weight_k;
   p.B = c->B; p.N = c->N; p.heads_q = c->heads_q; p.heads = c->heads_q + c->heads_kv;
+  // (a step past the last row is at most 256 rows, of heads or tokens, further)
+  auto reach = [&](const long long (&s3)[3], int heads) { return (long double)(p.B + 1) * s3[0] + (long double)(p.N + 256) * s3[1] + (long double)(heads + 256) * s3[2] + c->dim; };
+  p.narrow = reach(p.q_in, c->heads_q) < 2147483647.0L && reach(p.k_in, c->heads_kv) < 2147483647.0L && reach(p.q_to, c->heads_q) < 2147483647.0L &&
+             reach(p.k_to, c->heads_kv) < 2147483647.0L;
   const int ve = unit_width(p.t, bits_of(dev_q, p.q_in, 3, es) | bits_of(dev_k, p.k_in, 3, es) | bits_of(dev_q_out, p.q_to, 3, es) | bits_of(dev_k_out, p.k_to, 3, es), es);
   cudaStream_t st = (cudaStream_t)cu_stream;
   if (c->dtype == STAND_DTYPE_F32) return launch_rotate<float>(p, ve, st);

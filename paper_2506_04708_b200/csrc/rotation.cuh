@@ -53,21 +53,22 @@ __device__ __forceinline__ void turn_angle(long long position, float freq, float
   s = fmaf(c0, left, s0);
 }
 
-// VE elements as they lie: 16, 8 or 4 (2) bytes at a time.
-template <typename T, int VE> __device__ __forceinline__ void load_vec(const T* p, float* v) {
+// VE elements, 16, 8 or 4 (2) bytes at a time: as they lie, and as floats.
+template <typename T, int VE> __device__ __forceinline__ void copy_vec(T* to, const T* from) {
   if constexpr (sizeof(T) * VE >= 8) {
     using W = typename std::conditional<(sizeof(T) * VE >= 16), uint4, uint2>::type;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) * VE / sizeof(W)); ++i) {
-      const W w = reinterpret_cast<const W*>(p)[i];
-      const T* e = reinterpret_cast<const T*>(&w);
-#pragma unroll
-      for (int k = 0; k < (int)(sizeof(W) / sizeof(T)); ++k) v[i * (sizeof(W) / sizeof(T)) + k] = to_float(e[k]);
-    }
+    for (int i = 0; i < (int)(sizeof(T) * VE / sizeof(W)); ++i) reinterpret_cast<W*>(to)[i] = reinterpret_cast<const W*>(from)[i];
   } else {
 #pragma unroll
-    for (int k = 0; k < VE; ++k) v[k] = to_float(p[k]);
+    for (int k = 0; k < VE; ++k) to[k] = from[k];
   }
+}
+template <typename T, int VE> __device__ __forceinline__ void load_vec(const T* p, float* v) {
+  alignas(16) T e[VE];
+  copy_vec<T, VE>(e, p);
+#pragma unroll
+  for (int k = 0; k < VE; ++k) v[k] = to_float(e[k]);
 }
 template <typename T, int VE> __device__ __forceinline__ void store_vec(T* p, const float* y) {
   if constexpr (sizeof(T) * VE >= 8) {
@@ -86,22 +87,10 @@ template <typename T, int VE> __device__ __forceinline__ void store_vec(T* p, co
   }
 }
 
-// Where unit u of a row lies: elements a .. and b .. (each VE of them, if below dim).  turn: of this row.
-template <int VE> __device__ __forceinline__ bool unit_place(const Turn& t, bool turn, int u, int& a, int& b) {
-  const bool turned = turn && u < t.columns;
-  a = u * 2 * VE;
-  b = a + VE;
-  if (turn && !t.pairs) {
-    if (turned) a = u * VE, b = t.half + a;
-    else a = 2 * t.half + (u - t.columns) * 2 * VE, b = a + VE;
-  }
-  return turned;
-}
-
-// 1 / the root of the mean square of a row, of whose squares this lane has `sum`.  All lanes of the warp.
-__device__ __forceinline__ float row_scale(const Turn& t, float sum) {
-  for (int o = 1; o < t.lanes; o <<= 1) sum += __shfl_xor_sync(FULL, sum, o);
-  return rsqrtf(fmaf(sum, t.inv_dim, t.eps));
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 
 template <int VE> __device__ __forceinline__ void turn_unit(const Turn& t, const float* cs, int u, float (&y)[2 * VE]) {
@@ -126,60 +115,97 @@ template <int VE> __device__ __forceinline__ void turn_unit(const Turn& t, const
       y[2 * i + 1] = fmaf(a, s[i], b * c[i]);
     }
   } else {
+    if constexpr (VE >= 4) {
 #pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      const float a = y[i], b = y[VE + i];
-      y[i] = fmaf(a, c[i], -b * s[i]);
-      y[VE + i] = fmaf(a, s[i], b * c[i]);
+      for (int i = 0; i < VE; i += 2) {
+        const unsigned long long a = pack2(y[i], y[i + 1]), b = pack2(y[VE + i], y[VE + i + 1]), c2 = pack2(c[i], c[i + 1]), s2 = pack2(s[i], s[i + 1]);
+        unpack2(fma2(mul2(b, s2), pack2(-1.0f, -1.0f), mul2(a, c2)), y[i], y[i + 1]);
+        unpack2(fma2(a, s2, mul2(b, c2)), y[VE + i], y[VE + i + 1]);
+      }
+    } else {
+      const float a = y[0], b = y[1];
+      y[0] = fmaf(a, c[0], -b * s[0]);
+      y[1] = fmaf(a, s[0], b * c[0]);
     }
   }
 }
 
-// Every unit of a row that this lane has, read, normalised by `weight` (null: ones) and turned by the table `cs`, given to put(y, a, b) with
-// the places of its two vectors.  All lanes of the warp call it; in: the row is there.  norm, turn: of this row.
-template <typename T, int VE, typename WT, typename F>
-__device__ __forceinline__ void row_units(const Turn& t, const T* row, const WT* weight, const float* cs, int lane, bool in, bool norm, bool turn, F put) {
-  constexpr int K = VE == 1 ? 4 : 1;  // units of a lane
-  float y[K][2 * VE];
-  int a[K], b[K];
-  bool turned[K];
-  float sum = 0.0f;
+// What a lane does in every row of one kind (queries, keys, values): the places of its units.
+template <typename T, int VE> struct RowLane {
+  static constexpr int K = VE == 1 ? 4 : 1;  // units
+  int unit, a[K], b[K];                      // elements a .. and b .. (each VE of them)
+  bool turned[K], has_a[K], has_b[K];        // where there is nothing the row's first elements are read and not used: loads have no conditions
+
+  __device__ __forceinline__ RowLane(const Turn& t, int lane, bool turn) : unit(lane) {
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int u = lane + k * t.lanes;
-    turned[k] = unit_place<VE>(t, turn, u, a[k], b[k]);
-    if (!in) a[k] = b[k] = t.dim;
-#pragma unroll
-    for (int i = 0; i < 2 * VE; ++i) y[k][i] = 0.0f;
-    if (a[k] < t.dim) load_vec<T, VE>(row + a[k], y[k]);
-    if (b[k] < t.dim) load_vec<T, VE>(row + b[k], y[k] + VE);
-  }
-  if (t.norm) {  // of the call; rows of a warp may differ in `norm`, the exchange is everybody's
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-      for (int i = 0; i < 2 * VE; ++i) sum = fmaf(y[k][i], y[k][i], sum);
-    const float r = row_scale(t, sum);
-    if (norm) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        float w[2 * VE];
-#pragma unroll
-        for (int i = 0; i < 2 * VE; ++i) w[i] = 1.0f;
-        if (weight && a[k] < t.dim) load_vec<WT, VE>(weight + a[k], w);
-        if (weight && b[k] < t.dim) load_vec<WT, VE>(weight + b[k], w + VE);
-#pragma unroll
-        for (int i = 0; i < 2 * VE; ++i) y[k][i] = y[k][i] * r * w[i];
+    for (int k = 0; k < K; ++k) {
+      const int u = lane + k * t.lanes;
+      turned[k] = turn && u < t.columns;
+      a[k] = u * 2 * VE;
+      b[k] = a[k] + VE;
+      if (turn && !t.pairs) {
+        if (turned[k]) a[k] = u * VE, b[k] = t.half + a[k];
+        else a[k] = 2 * t.half + (u - t.columns) * 2 * VE, b[k] = a[k] + VE;
       }
+      has_a[k] = a[k] < t.dim;
+      has_b[k] = b[k] < t.dim;
+      if (!has_a[k]) a[k] = 0;
+      if (!has_b[k]) b[k] = 0;
     }
   }
+  // A row, read, normalised (weighted: by what weights(w, k) gives for unit k), turned by the table cs and, if it is there (in; else any row that
+  // may be read), given to put(y, a, b, whether there is a second vector) unit by unit.  All lanes of the warp.
+  template <typename W, typename F>
+  __device__ __forceinline__ void row(const Turn& t, const T* from, bool weighted, W weights, const float* cs, bool in, bool norm, F put) const {
+    float y[K][2 * VE];
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    if (a[k] >= t.dim) continue;
-    if (turned[k]) turn_unit<VE>(t, cs, lane + k * t.lanes, y[k]);
-    put(y[k], a[k], b[k]);
+    for (int k = 0; k < K; ++k) {
+      load_vec<T, VE>(from + a[k], y[k]);
+      load_vec<T, VE>(from + b[k], y[k] + VE);
+    }
+    if (norm) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float part;
+          const float* v = y[k] + h * VE;
+          if constexpr (VE >= 4) {
+            unsigned long long sum2 = mul2(pack2(v[0], v[1]), pack2(v[0], v[1]));
+#pragma unroll
+            for (int i = 2; i < VE; i += 2) sum2 = fma2(pack2(v[i], v[i + 1]), pack2(v[i], v[i + 1]), sum2);
+            float lo, hi;
+            unpack2(sum2, lo, hi);
+            part = lo + hi;
+          } else {
+            part = v[0] * v[0];
+          }
+          sum += (h ? has_b[k] : has_a[k]) ? part : 0.0f;
+        }
+      for (int o = 1; o < t.lanes; o <<= 1) sum += __shfl_xor_sync(FULL, sum, o);
+      const float r = rsqrtf(fmaf(sum, t.inv_dim, t.eps));
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < 2 * VE; i += 2) unpack2(mul2(pack2(y[k][i], y[k][i + 1]), pack2(r, r)), y[k][i], y[k][i + 1]);
+      if (weighted) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          alignas(16) float w[2 * VE];
+          weights(w, k);
+#pragma unroll
+          for (int i = 0; i < 2 * VE; i += 2) unpack2(mul2(pack2(y[k][i], y[k][i + 1]), pack2(w[i], w[i + 1])), y[k][i], y[k][i + 1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (turned[k]) turn_unit<VE>(t, cs, unit + k * t.lanes, y[k]);
+      if (in && has_a[k]) put(y[k], a[k], b[k], has_b[k]);
+    }
   }
-}
+};
 
 // Units of VE elements: every vector lies within one kind of element.
 inline bool turn_fits(const Turn& t, int ve) { return t.dim % ve == 0 && (!t.freq || t.pairs || t.half % ve == 0); }
