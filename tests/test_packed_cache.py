@@ -776,3 +776,57 @@ def test_packed_a_wait_that_runs_out_gives_nan_and_leaves_the_gpu_usable(lib, dt
         lib.stand_set_wait_limit(-1)
     assert np.isnan(out).all() and np.isnan(lse).all()
     _check(c, _run_packed(c))
+
+
+# ---------------------------------------------------------------- all of them together: examples/tree_decode.py
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch,head_norm", [(1, False), (4, True)])
+def test_a_decoding_loop_over_a_cache_in_4_bits(dtype, batch, head_norm):
+    """Per step and layer, attention over the packed cache against attention over its values in a cache of the model's type (bfloat16
+    and single precision hold them exactly): two kernels, each within u (|o| + sum p|v|) and single-precision sums of
+    the definition, so within 4 u max |v| + 2^-12 max |v| of one another (scores here are below 2^5 and e below 2^-13)."""
+    import torch
+    from examples import tree_decode as td
+    from paper_2506_04708_b200 import serving
+    model = td.Model(dtype=ts._dtype(dtype), V=300, head_norm=head_norm)
+    dec = td.Decoder(model, td.prompts_for(batch, model.V, seed=batch), most=256, packed=True)
+    pool, page, L = dec.cache_k.shape[1], dec.page, model.layers
+    every = serving.KvRead(L, 1, model.hkv, model.dim, model.dtype, page, pool, pool * page, packed=True)
+    slots = torch.arange(pool * page, device=DEV)[None]
+    plain = serving.TreeAttention(batch, dec.N, model.hq, model.hkv, model.dim, model.dtype, page, pool, dec.table.shape[1], parent=dec.parent)
+    worst, deepest = 0.0, 0
+
+    def attend(attention):
+        caches = [c.view(L, pool, page, model.hkv, model.dim).transpose(2, 3) for c in every(slots, dec.cache_k, dec.cache_v)]
+
+        def f(layer, q, k, v):
+            nonlocal worst
+            out = attention(q, k, v, dec.cache_k[layer], dec.cache_v[layer], dec.table, dec.len, tree_tokens=dec.seen)[0]
+            want = plain(q, k, v, caches[0][layer], caches[1][layer], dec.table, dec.len, tree_tokens=dec.seen)[0]
+            top = max(float(v.abs().max()), float(caches[1][layer].abs().max()))
+            worst = max(worst, float((out.float() - want.float()).abs().max()) / top)
+            return out
+        return f
+    dec.attend = attend
+    for _ in range(16):
+        _, _, n = dec.step()
+        deepest = max(deepest, int(n.max()))
+    assert worst <= 4 * ts.U[dtype] + 2.0**-12, worst
+    assert deepest >= 2 or batch == 1
+    assert torch.equal(dec.len + 1, dec.n_text) and not dec.short.any()
+    # the cache holds what the model's keys are, in 4 bits: the text run through the first layer's projections
+    n = int(dec.len[0])
+    tokens, pos = dec.text[:1, :n], torch.arange(n, device=DEV)[None]
+    qkv = (model.norm(model.embed[tokens.long()]) @ model.blocks[0]["qkv"]).unflatten(-1, (-1, model.dim))
+    q, k, v = qkv.split([model.hq, model.hkv, model.hkv], 2)
+    w = None if not head_norm else model.weight_k[0]
+    turned = serving.HeadRotation(1, n, model.hq, model.hkv, model.dim, model.dtype, freq=model.freq, interleaved=True, norm=head_norm, weight_q=w, weight_k=w)(q, k)[1]
+    at = dec.table[0, pos[0] // page].long() * page + pos[0] % page
+    read = serving.KvRead(L, 1, model.hkv, model.dim, torch.float32, page, pool, n, packed=True)
+    got = read(at[None], dec.cache_k, dec.cache_v)
+    for rows, x in ((got[0][0, 0], turned[0]), (got[1][0, 0], v[0])):
+        want = torch.from_numpy(pref.values(*pref.pack(x.float().cpu().numpy()))).to(DEV)
+        # products of other shapes may round otherwise: a code may differ by one there, and few do
+        step = want.abs().unflatten(-1, (-1, 16)).amax(-1, keepdim=True).expand(*want.shape[:-1], -1, 16).flatten(-2) / 7 * 1.26
+        assert ((rows - want).abs() <= step + 1e-12).all() and float(((rows - want).abs() > 1e-6).double().mean()) < 0.05
