@@ -102,6 +102,49 @@ template <typename T> struct PkGroup {
   }
 };
 
+__device__ __forceinline__ uint32_t pk_two(float f) {  // twice, as bfloat16
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %1;" : "=r"(r) : "f"(f));
+  return r;
+}
+// A word of 8 codes as 8 values of the call's type (16 bytes), with the scale of its group.  bfloat16: a code n in bits 1 - 4 of a bfloat16
+// that begins at 64 is 64 + n, and (64 + n) s - 72 s is exact, 72 s having 7 significant bits; an infinite scale gives infinity less infinity.
+// Half: 1024 + n, less 1032, times s.
+template <bool BF16> struct PkScale {
+  uint32_t s, c;
+  __device__ __forceinline__ explicit PkScale(uint32_t byte) {
+    if constexpr (BF16) {
+      const float f = __half2float(__ushort_as_half((unsigned short)(byte << 7)));
+      s = pk_two(f);
+      c = pk_two(-72.0f * f);
+    } else {
+      s = (byte >= PK_BAD ? 0x7E00u : byte << 7) * 0x10001u;
+      c = 0;
+    }
+  }
+};
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {  // one instruction
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
+  return r;
+}
+template <bool BF16> __device__ __forceinline__ uint4 pk_word(uint32_t w, const PkScale<BF16>& p) {
+  uint32_t v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (BF16) {
+      const uint32_t x = and_or(i == 0 ? w << 1 : w >> (4 * i - 1), 0x001E001Eu, 0x42804280u);
+      asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(x), "r"(p.s), "r"(p.c));
+    } else {
+      const uint32_t x = and_or(w >> (4 * i), 0x000F000Fu, 0x64006400u);
+      uint32_t k;
+      asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(k) : "r"(x), "r"(0x64086408u));
+      asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(v[i]) : "r"(k), "r"(p.s));
+    }
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 // 8 elements of a word as floats.
 __device__ __forceinline__ void pk_values(uint32_t w, float s, float* v) {
 #pragma unroll

@@ -21,20 +21,6 @@ constexpr int ROT_E = 16;  // elements of a lane that reads
 constexpr int ROW_COUNT = 4096;  // layers, heads: their product counts rows in 32 bits
 constexpr int ROT_TOKENS = 16;  // tokens of a block, at most: their cosines and sines lie in shared memory
 
-// The digits of a row number that counts in steps: no divisions in the loop, and the step's own are worked out on the host.
-struct Step {
-  int h, l, t;  // heads, layers, tokens
-  Step() = default;
-  __host__ __device__ __forceinline__ Step(int i, int heads, int layers) : h(i % heads), l(i / heads % layers), t(i / heads / layers) {}
-  __device__ __forceinline__ void add(const Step& o, int heads, int layers) {
-    h += o.h;
-    l += o.l;
-    t += o.t;
-    if (h >= heads) h -= heads, ++l;
-    if (l >= layers) l -= layers, ++t;
-  }
-};
-
 // The block's table of cosines and sines; the caller's barrier follows.
 template <int VE, typename F> __device__ __forceinline__ void turn_tables(const Turn& t, float* cs, int tokens, F position) {
   const int floats = turn_floats<VE>(t.columns), angles = t.columns * VE;
@@ -121,7 +107,9 @@ template <typename T, int VE, typename I> __global__ void __launch_bounds__(ROT_
       while (n >= p.N) n -= p.N, in_at += in_seq, out_at += out_seq;
       const bool in = r < rows;
       T* const out = to + out_at;
-      lane.row(p.t, from + (in ? in_at : 0), weight != nullptr, weights, rot_cs + (in ? tok * floats : 0), in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
+      typename RowLane<T, VE>::Raw raw;
+      lane.read(from + (in ? in_at : 0), raw);
+      lane.row(p.t, raw, weight != nullptr, weights, rot_cs + (in ? tok * floats : 0), in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
         store_vec<T, VE>(out + a, y);
         if (two) store_vec<T, VE>(out + b, y + VE);
       });
@@ -147,7 +135,6 @@ struct AppendParams {
   int layers, N, width, heads, page;
   long long places;  // B * width
   int tokens, layers_block;
-  Step step;         // rows that a block takes at a time
   int table_floats;  // of all tokens; a block's rows on their way to groups of 16 lie behind them
   long long n_slots;
   long long k_in[4], v_in[4];  // elements
@@ -187,56 +174,69 @@ __global__ void __launch_bounds__(ROT_THREADS, sizeof(T) == 2 ? 4 : 3) kv_append
     __syncthreads();
   }
   T* const mine = reinterpret_cast<T*>(rot_cs + p.table_floats) + group * dim;
-  const int rows = tokens * layers * p.heads;
-  const Step step = layers == p.layers_block ? p.step : Step(groups, p.heads, layers);  // the last layers' blocks may have fewer
-  // keys, then values: strides and what is done are the same for all lanes
+  // Keys, then values: strides and what is done are the same for all lanes.  A group of lanes has one token's head in all of the block's layers, the
+  // next layer's row on its way while one is worked on.
   auto kind = [&](const void* src, const long long (&in_s)[4], const long long* from, char* cache, auto are_keys) {
     constexpr bool KEYS = decltype(are_keys)::value;
     const bool turn = KEYS && p.t.freq, norm = KEYS && p.t.norm;
     RowLane<T, VE> lane(p.t, c, turn);
-    // rows that stay as they are go straight to their groups, and so do units that are groups
+    // packed rows that stay as they are go straight to their groups, and so do units that are groups
     const bool same = PACKED && VE == 8 && !turn && !norm, direct = VE == 8 && !(turn && !p.t.pairs);
-    Step at(group, p.heads, layers);
-    for (int r = group; r - group < rows; r += groups, at.add(step, p.heads, layers)) {
-      const int tok = r < rows ? at.t : 0, l = l0 + at.l;
+    const int rows = tokens * p.heads;
+    for (int r = group; r - group < rows; r += groups) {
+      const int tok = r < rows ? r / p.heads : 0, h = r < rows ? r - tok * p.heads : 0;
       const long long base = s_to[tok];
       const bool in = r < rows && base >= 0;
-      const T* row = reinterpret_cast<const T*>(src) + (in ? from[tok] + l * in_s[0] + at.h * in_s[3] : 0);
-      const T* weight = reinterpret_cast<const T*>(p.weight) + (long long)(in ? l : 0) * dim;
-      auto weights = [&](float (&w)[2 * VE], int k) {
-        load_vec<T, VE>(weight + lane.a[k], w);
-        load_vec<T, VE>(weight + lane.b[k], w + VE);
-      };
-      char* to = cache + base + l * p.to[0] + at.h * p.to[2];
-      if constexpr (!PACKED) {
-        T* out = reinterpret_cast<T*>(to);
-        lane.row(p.t, row, p.weight != nullptr, weights, rot_cs + tok * floats, in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
-          store_vec<T, VE>(out + a, y);
-          if (two) store_vec<T, VE>(out + b, y + VE);
-        });
-      } else {
-        const bool has = in && c * PK_GROUP < dim;
-        PkGroup<T> z;
-        if (same) {
-          if (has) copy_vec<T, 16>(reinterpret_cast<T*>(z.w), row + c * PK_GROUP);
-        } else {
-          lane.row(p.t, row, p.weight != nullptr, weights, rot_cs + tok * floats, in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
-            if (direct) {
-              if constexpr (VE == 8) store_vec<T, 16>(reinterpret_cast<T*>(z.w), y);
-            } else {
-              store_vec<T, VE>(mine + a, y);
-              if (two) store_vec<T, VE>(mine + b, y + VE);
-            }
+      if (!__any_sync(FULL, in)) continue;
+      const T* row = reinterpret_cast<const T*>(src) + (in ? from[tok] + l0 * in_s[0] + h * in_s[3] : 0);
+      const long long to_next_row = in ? in_s[0] : 0;
+      char* to = cache + base + l0 * p.to[0] + h * p.to[2];
+      const T* weight = reinterpret_cast<const T*>(p.weight) + (long long)l0 * dim;
+      const float* cs = rot_cs + tok * floats;
+      const int scale_at = s_scale[tok] + c;
+      typename RowLane<T, VE>::Raw now, next;
+      lane.read(row, now);
+      for (int l = 0; l < layers; ++l) {
+        row += to_next_row;
+        if (l + 1 < layers) lane.read(row, next);
+        auto weights = [&](float (&w)[2 * VE], int k) {
+          load_vec<T, VE>(weight + lane.a[k], w);
+          load_vec<T, VE>(weight + lane.b[k], w + VE);
+        };
+        if constexpr (!PACKED) {
+          T* out = reinterpret_cast<T*>(to);
+          lane.row(p.t, now, p.weight != nullptr, weights, cs, in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
+            store_vec<T, VE>(out + a, y);
+            if (two) store_vec<T, VE>(out + b, y + VE);
           });
-          __syncwarp();
-          if (!direct && has) copy_vec<T, 16>(reinterpret_cast<T*>(z.w), mine + c * PK_GROUP);
-          __syncwarp();  // the row in shared memory has been read
+        } else {
+          const bool has = in && c * PK_GROUP < dim;
+          PkGroup<T> z;
+          if (same) {
+#pragma unroll
+            for (int i = 0; i < PkGroup<T>::WORDS; ++i) z.w[i] = reinterpret_cast<const uint32_t*>(now.e[0])[VE == 8 ? i : 0];
+          } else {
+            lane.row(p.t, now, p.weight != nullptr, weights, cs, in, norm, [&](float (&y)[2 * VE], int a, int b, bool two) {
+              if (direct) {
+                if constexpr (VE == 8) store_vec<T, 16>(reinterpret_cast<T*>(z.w), y);
+              } else {
+                store_vec<T, VE>(mine + a, y);
+                if (two) store_vec<T, VE>(mine + b, y + VE);
+              }
+            });
+            __syncwarp();
+            if (!direct && has) copy_vec<T, 16>(reinterpret_cast<T*>(z.w), mine + c * PK_GROUP);
+            __syncwarp();  // the row in shared memory has been read
+          }
+          if (has) {
+            uint32_t byte;
+            *reinterpret_cast<uint2*>(to + c * 8) = z.codes(byte);
+            to[scale_at] = (char)byte;
+          }
         }
-        if (has) {
-          uint32_t byte;
-          *reinterpret_cast<uint2*>(to + c * 8) = z.codes(byte);
-          to[s_scale[tok] + c] = (char)byte;
-        }
+        to += p.to[0];
+        weight += dim;
+        now = next;
       }
     }
   };
@@ -252,48 +252,52 @@ struct ReadParams {
   void* v_out;
   int layers, heads, dim, page, lanes;
   long long places, n_slots;
-  int tokens, layers_block;
+  int layers_block;
   long long from[4];  // bytes: layer, page, head, token
 };
 
-// A lane: 16 elements of a row.  Places without a slot give zeros.
+// A lane: 16 elements of a row, one token's head in all of the block's layers.  Places without a slot give zeros.
 template <typename T, bool WIDE, bool PACKED>
 __global__ void __launch_bounds__(ROT_THREADS) kv_read_kernel(const __grid_constant__ ReadParams p) {
   pdl_trigger();
   pdl_wait();
-  __shared__ long long s_page[ROT_TOKENS];  // -1: no slot
-  __shared__ int s_token[ROT_TOKENS];
   const int tid = threadIdx.x, c = tid & (p.lanes - 1), group = tid / p.lanes, groups = ROT_THREADS / p.lanes;
-  const long long first = (long long)blockIdx.x * p.tokens;
-  const int tokens = p.places - first < p.tokens ? (int)(p.places - first) : p.tokens;
-  const int l0 = blockIdx.y * p.layers_block, layers = p.layers - l0 < p.layers_block ? p.layers - l0 : p.layers_block;
-  if (tid < tokens) {
-    const long long slot = p.slots[first + tid], page = slot >= 0 && slot < p.n_slots ? slot / p.page : -1;
-    s_page[tid] = page;
-    s_token[tid] = (int)(slot - page * p.page);
-  }
-  __syncthreads();
   if (c * ROT_E >= p.dim) return;
-  const int heads = 2 * p.heads, rows = tokens * layers * heads;
-  const Step step(groups, heads, layers);
-  Step at(group, heads, layers);
-  for (int r = group; r < rows; r += groups, at.add(step, heads, layers)) {
-    const long long place = first + at.t, page = s_page[at.t];
-    const int l = l0 + at.l;
-    const bool is_v = at.h >= p.heads;
-    const int h = is_v ? at.h - p.heads : at.h;
-    T* out = reinterpret_cast<T*>(is_v ? p.v_out : p.k_out) + ((l * p.places + place) * p.heads + h) * p.dim + c * ROT_E;
+  const int l0 = blockIdx.y * p.layers_block, layers = p.layers - l0 < p.layers_block ? p.layers - l0 : p.layers_block;
+  const long long r = (long long)blockIdx.x * groups + group, place = r / (2 * p.heads);
+  if (place >= p.places) return;
+  const bool is_v = r - place * 2 * p.heads >= p.heads;
+  const int h = (int)(r - place * 2 * p.heads) - (is_v ? p.heads : 0);
+  const long long slot = p.slots[place], page = slot >= 0 && slot < p.n_slots ? slot / p.page : -1;
+  const int token = (int)(slot - page * p.page);
+  T* out = reinterpret_cast<T*>(is_v ? p.v_out : p.k_out) + ((l0 * p.places + place) * p.heads + h) * p.dim + c * ROT_E;
+  const long long out_next = p.places * p.heads * p.dim;
+  const char* from = (is_v ? p.cache_v : p.cache_k) + l0 * p.from[0] + (page < 0 ? 0 : page * p.from[1]) + h * p.from[2];
+  const int at = PACKED ? token * (p.dim / 2) + c * 8 : 0, scale_at = PACKED ? p.page * (p.dim / 2) + token * (p.dim / 16) + c : 0;
+  const long long row_at = PACKED ? 0 : token * p.from[3] + c * ROT_E * (long long)sizeof(T);
+#pragma unroll 4
+  for (int l = 0; l < layers; ++l, out += out_next, from += p.from[0]) {
+    if constexpr (PACKED && WIDE && sizeof(T) == 2) {
+      constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
+      uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+      if (page >= 0) {
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(from + at));
+        const PkScale<BF16> s(__ldg(reinterpret_cast<const unsigned char*>(from + scale_at)));
+        v[0] = pk_word<BF16>(w.x, s), v[1] = pk_word<BF16>(w.y, s);
+      }
+      reinterpret_cast<uint4*>(out)[0] = v[0];
+      reinterpret_cast<uint4*>(out)[1] = v[1];
+      continue;
+    }
     float y[ROT_E] = {};
     if (page >= 0) {
-      const int token = s_token[at.t];
-      const char* from = (is_v ? p.cache_v : p.cache_k) + l * p.from[0] + page * p.from[1] + h * p.from[2];
       if constexpr (PACKED) {
-        const uint2 w = *reinterpret_cast<const uint2*>(from + token * (p.dim / 2) + c * 8);
-        const float s = pk_scale((unsigned char)from[(long long)p.page * (p.dim / 2) + token * (p.dim / 16) + c]);
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(from + at));
+        const float s = pk_scale(__ldg(reinterpret_cast<const unsigned char*>(from + scale_at)));
         pk_values(w.x, s, y);
         pk_values(w.y, s, y + 8);
       } else {
-        const T* row = reinterpret_cast<const T*>(from + token * p.from[3]) + c * ROT_E;
+        const T* row = reinterpret_cast<const T*>(from + row_at);
         if (WIDE) {
           load_vec<T, 16>(row, y);
         } else {
@@ -362,14 +366,16 @@ template <typename T> int launch_rotate(RotateParams& p, int ve, cudaStream_t st
 
 template <typename T, int VE> int launch_append(AppendParams& p, bool packed, cudaStream_t st) {
   turn_units(p.t, VE);
-  // A token's angles are worked out once for all layers of a block: few blocks per token, but enough to fill the GPU.
-  const int groups = ROT_THREADS / p.t.lanes, rows = 2 * p.heads;
+  // Tokens enough that each group of lanes has a row (16 at most), and as many layers as leave enough blocks to fill the GPU: a token's angles are
+  // worked out once for all layers of a block.
+  const int groups = ROT_THREADS / p.t.lanes;
+  p.tokens = groups / p.heads < 1 ? 1 : (groups / p.heads > ROT_TOKENS ? ROT_TOKENS : groups / p.heads);
+  while (p.tokens > 1 && p.places <= p.tokens / 2) p.tokens /= 2;
+  const long long across = (p.places + p.tokens - 1) / p.tokens;
   int lpb = p.layers;
-  while (lpb > 1 && lpb * rows > 2 * groups && p.places * ((p.layers + lpb - 1) / lpb) < 4 * 148) lpb = (lpb + 1) / 2;
+  while (lpb > 1 && across * ((p.layers + lpb - 1) / lpb) < 6 * 148) lpb = (lpb + 1) / 2;
   p.layers_block = lpb;
-  p.tokens = tokens_per_block(p.places, rows * lpb, p.t.lanes);
-  p.step = Step(groups, p.heads, lpb);
-  const dim3 grid((unsigned)((p.places + p.tokens - 1) / p.tokens), (unsigned)((p.layers + lpb - 1) / lpb));
+  const dim3 grid((unsigned)across, (unsigned)((p.layers + lpb - 1) / lpb));
   p.table_floats = p.tokens * 2 * turn_floats<VE>(p.t.columns);
   const size_t smem = p.table_floats * sizeof(float) + (packed ? (size_t)groups * p.t.dim * sizeof(T) : 0);
   if (packed) return launch_dependent(kv_append_kernel<T, VE, true>, grid, ROT_THREADS, st, p, smem);
@@ -490,12 +496,13 @@ int stand_kv_read(const stand_kv_rows* c, const void* dev_cache_k, const void* d
   p.places = (long long)c->B * c->width; p.n_slots = (long long)c->pages * c->page_size;
   const bool wide = p.dim % ROT_E == 0 && (((uintptr_t)dev_k | (uintptr_t)dev_v) & 15) == 0 &&
                     (c->packed || ((bits_of(dev_cache_k, p.from, 4, 1) | bits_of(dev_cache_v, p.from, 4, 1)) & 15) == 0);
-  const int groups = ROT_THREADS / p.lanes, rows = 2 * p.heads;
+  const int groups = ROT_THREADS / p.lanes;
+  const long long across = (p.places * 2 * p.heads + groups - 1) / groups;
+  if (across > 0x7FFFFFFFll) return STAND_E_ARG;
   int lpb = p.layers;
-  while (lpb > 1 && lpb * rows > 4 * groups) lpb = (lpb + 1) / 2;
+  while (lpb > 1 && across * ((p.layers + lpb - 1) / lpb) < 8 * 148) lpb = (lpb + 1) / 2;
   p.layers_block = lpb;
-  p.tokens = tokens_per_block(p.places, rows * lpb, p.lanes);
-  const dim3 grid((unsigned)((p.places + p.tokens - 1) / p.tokens), (unsigned)((p.layers + lpb - 1) / lpb));
+  const dim3 grid((unsigned)across, (unsigned)((p.layers + lpb - 1) / lpb));
   cudaStream_t st = (cudaStream_t)cu_stream;
   if (c->dtype == STAND_DTYPE_F32) return launch_read<float>(p, wide, c->packed, grid, st);
   if (c->dtype == STAND_DTYPE_BF16) return launch_read<__nv_bfloat16>(p, wide, c->packed, grid, st);

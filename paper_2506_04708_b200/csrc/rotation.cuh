@@ -153,16 +153,26 @@ template <typename T, int VE> struct RowLane {
       if (!has_b[k]) b[k] = 0;
     }
   }
-  // A row, read, normalised (weighted: by what weights(w, k) gives for unit k), turned by the table cs and, if it is there (in; else any row that
-  // may be read), given to put(y, a, b, whether there is a second vector) unit by unit.  All lanes of the warp.
-  template <typename W, typename F>
-  __device__ __forceinline__ void row(const Turn& t, const T* from, bool weighted, W weights, const float* cs, bool in, bool norm, F put) const {
-    float y[K][2 * VE];
+  // A row's elements as they lie.
+  struct Raw {
+    alignas(16) T e[K][2 * VE];
+  };
+  __device__ __forceinline__ void read(const T* from, Raw& raw) const {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      load_vec<T, VE>(from + a[k], y[k]);
-      load_vec<T, VE>(from + b[k], y[k] + VE);
+      copy_vec<T, VE>(raw.e[k], from + a[k]);
+      copy_vec<T, VE>(raw.e[k] + VE, from + b[k]);
     }
+  }
+  // The row normalised (weighted: by what weights(w, k) gives for unit k), turned by the table cs and, if it is there (in; else any row was read),
+  // given to put(y, a, b, whether there is a second vector) unit by unit.  All lanes of the warp.
+  template <typename W, typename F>
+  __device__ __forceinline__ void row(const Turn& t, const Raw& raw, bool weighted, W weights, const float* cs, bool in, bool norm, F put) const {
+    float y[K][2 * VE];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < 2 * VE; ++i) y[k][i] = to_float(raw.e[k][i]);
     if (norm) {
       float sum = 0.0f;
 #pragma unroll
