@@ -499,7 +499,7 @@ int stand_kv_read(const stand_kv_rows* c, const void* dev_cache_k, const void* d
   const int groups = ROT_THREADS / p.lanes;
   const long long across = (p.places * 2 * p.heads + groups - 1) / groups;
   if (across > 0x7FFFFFFFll) return STAND_E_ARG;
-  int lpb = p.layers;
+  int lpb = p.layers < 4 ? p.layers : 4;  // more in a row are slower: the layers lie far apart (4, 8, 32: 55, 57, 62 us for prompts of 32 layers)
   while (lpb > 1 && across * ((p.layers + lpb - 1) / lpb) < 8 * 148) lpb = (lpb + 1) / 2;
   p.layers_block = lpb;
   const dim3 grid((unsigned)across, (unsigned)((p.layers + lpb - 1) / lpb));
