@@ -46,7 +46,7 @@ extern "C" {
 
 #define STAND_DTYPE_F32 0
 #define STAND_DTYPE_BF16 1
-#define STAND_DTYPE_F16 2 /* stand_tree_attention and stand_kv_commit only */
+#define STAND_DTYPE_F16 2 /* attention, cached rows and head rotation only */
 
 #define STAND_OK 0
 #define STAND_E_ARG (-1)       /* invalid argument or configuration */

@@ -45,7 +45,7 @@ template <int DP, int NB> struct PrShape {
   static constexpr int X = PR_WARPS * ROWS * PITCH * 4;      // exchange between the warps, in the same place once those are done with
   static constexpr int SMEM = STAGES * SLOT + X;
   static_assert(X >= TREE + 16 * ROWS * 4 + ROWS * DP * 2, "the tree, its weights and rows");
-  static_assert(CTAS * (SMEM + 3072) <= 228 * 1024, "shared memory");
+  static_assert(CTAS * (SMEM + 3 * 1024) <= 228 * 1024, "shared memory");
 };
 
 struct PrParams {
@@ -560,7 +560,9 @@ inline bool rows_takes(const AttnParams& a, int dtype) {
 template <int DP, int NB, bool BF16> int launch_packed_rows(const AttnParams& a, void* scratch, int sms, unsigned wait_limit, cudaStream_t st) {
   using Sh = PrShape<DP, NB>;
   PrParams p;
-  ta_split(p.s, a, a.N * a.group, DP, sms, Sh::CTAS, 4, scratch);
+  // A piece's beginning and join as 8 tiles.  As 4 / 6 / 8 / 12: 64 sequences of 4 nodes over 500 - 8,000, 32 / 8 heads of 128: 155 / 144 / 136 / 137 us;
+  // 64 single tokens 93 / 93 / 94 / 98; 256 over 130 - 4,100 186 / 183 / 186 / 192.
+  ta_split(p.s, a, a.N * a.group, DP, sms, Sh::CTAS, 8, scratch);
   p.wait_limit = wait_limit;
   static SmemLimit limit;
   int rc = limit.raise(packed_rows_kernel<DP, NB, BF16>, Sh::SMEM);

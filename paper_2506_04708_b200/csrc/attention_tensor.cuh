@@ -285,7 +285,7 @@ template <int DP, int C, bool BF16, bool PACKED>
 __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
   using Sh = TaShape<DP, C, PACKED>;
   constexpr int TA_THREADS = TA_THREADS_OF<PACKED>;
-  constexpr int MMA_WARP = PACKED ? 8 : 5;  // packed: warps 4 - 7 unpack, one for each scheduler as the softmax warps are (two of them beside one: 420 us became 400)
+  constexpr int MMA_WARP = PACKED ? 8 : 5;  // packed: warps 4 - 7 unpack, one for each scheduler as the softmax warps are (with two of those beside one: 387 us rather than 378)
   constexpr int KT = TA_KT, HALVES = DP / 64, SLOTS = Sh::SLOTS, K_SLOTS = Sh::K_SLOTS, V_SLOTS = Sh::V_SLOTS;
   constexpr int PART_ROWS = TA_ROWS / C, W = KT / C, CH = W < 32 ? W : 32;  // rows of a part; keys of a tile that it takes
   extern __shared__ __align__(1024) char ta_smem[];

@@ -23,8 +23,6 @@ constexpr uint32_t PK_BAD = 0xF8;         // scales from here on are not finite
 constexpr uint32_t PK_LAST = 0xF7;        // the largest scale: 61440
 constexpr float PK_MOST = 7.0f * 61440.0f;
 
-__host__ __device__ __forceinline__ long long pk_block_bytes(int page, int dim) { return (long long)page * dim / 2 + (long long)page * dim / 16; }
-
 __device__ __forceinline__ float pk_scale(uint32_t byte) {
   return byte >= PK_BAD ? __uint_as_float(0x7FC00000u) : __half2float(__ushort_as_half((unsigned short)(byte << 7)));
 }
