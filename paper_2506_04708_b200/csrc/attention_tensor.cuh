@@ -29,6 +29,16 @@
 // overlaps the chain named below).  Prompts without a cache, 32 / 8 heads of 128: 4 x 4,096 rows 1,360 us, 1 x 16,384 4,950 us = 0.40 -
 // 0.44 PFLOP/s of the visible half.  In the first case no unit is near its limit (tensor pipe 35 %, exponentials 27 %, issue 29 %, memory 82 % of
 // a copy): what bounds a tile is the chain scores - maximum - exponentials - product, about 2,200 cycles, which two CTAs overlap.
+//
+// PACKED: the cache is in 4 bits.  Ten warps: 0-3 as above; 4, 5 make a tile's keys and 6, 7 its values from codes, each half a tile, in the places
+// that TMA fills otherwise; 8 issues the products; 9 copies codes and scales, tiles ahead, into stages of 9 bytes for 16 elements (and has TMA fetch the
+// tree's own).  What the unpacking warps write and the products read meets at the same barriers, after a fence between the two kinds of access.  A key's values
+// are exact in 16 bits, so the products are those of the definition.
+// Measured: 256 x 24 nodes as above: 378 us in short bursts, 440 in loops of seconds (floor 128: products; with a cache of 16 bits 400 and 469); 64 nodes over
+// 32,001: 60 us (floor 18); 16 x 32 nodes, 16 / 16 heads of 64, half, 1 - 8,190: 62 us; 64 x 24 of 16 / 4 heads of 256: 127 us.  Memory is no longer the
+// bound (0.3 of a copy), the chain of a tile is, of 2,100 - 2,600 cycles with 96 registers a thread: tensor pipe 31 %, exponentials 24 %, logic unit 41 %,
+// issue 50 %, shared memory 57 %.  Codes read by the unpacking warps straight from memory took 664 us, bulk copies by one lane 387 (950 - 1,480 cycles
+// a tile to issue them); weights by the maximum of the tile before, in one pass over the scores, 495; scores kept in registers between the two passes 452.
 #pragma once
 #include <cuda.h>
 
