@@ -227,8 +227,8 @@ class HeadRotation(_Op):
         pqo, pko = self._floats(q_out, self._q, "q_out"), self._floats(k_out, self._k, "k_out")
         strides = q.stride(), k.stride(), q_out.stride(), k_out.stride()
         if strides != self._strides:
-            c.q_stride[:], c.k_stride[:] = _steps(q, "q"), _steps(k, "k")
-            c.q_out_stride[:], c.k_out_stride[:] = _steps(q_out, "q_out"), _steps(k_out, "k_out")
+            qs, ks, qo, ko = _steps(q, "q"), _steps(k, "k"), _steps(q_out, "q_out"), _steps(k_out, "k_out")
+            c.q_stride[:], c.k_stride[:], c.q_out_stride[:], c.k_out_stride[:] = qs, ks, qo, ko
             self._strides = strides
         r = self._turn
         pb = self._opt(base, self.torch.int64, self._b, "base")

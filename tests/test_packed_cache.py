@@ -974,3 +974,18 @@ def test_rotation_offsets_pass_32_bits():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     op(x, x, q_out=rows, k_out=rows)
     assert torch.equal(rows, want[0]) and not big[2**20:2**31 - 2**20].any()
+
+
+@pytest.mark.gpu
+def test_a_refused_rotation_leaves_the_next_call_as_it_was():
+    """Strides of a call whose last argument is refused are forgotten with it."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    x = torch.randn((2, 3, 4, 64), device=DEV)
+    op = serving.HeadRotation(2, 3, 4, 4, 64, torch.float32, freq=torch.ones(32, device=DEV))
+    want = [t.clone() for t in op(x, x)]
+    wide = torch.randn((2, 3, 8, 64), device=DEV)[:, :, ::2]
+    with pytest.raises(binding.StandError):
+        op(wide, x, k_out=torch.zeros((2, 3, 64, 4), device=DEV).transpose(2, 3))
+    got = op(x, x)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
