@@ -490,7 +490,7 @@ typedef struct {
  *   (a, b) of pair i becomes (a cos t - b sin t, a sin t + b cos t),  t = (dev_base[b] + dev_offset[b, n]) * dev_freq[i]
  * with the angle worked out in 64 bits (positions up to 2^31 in magnitude).  dev_weight_q, dev_weight_k [dim] of the rows' type (NULL: ones).
  * dev_freq [rotary_dim / 2] float.  dev_base [B] int64 (NULL: 0) is what a sequence's positions begin with, dev_offset int32 what a node adds:
- * [N] or [B, N] (NULL: its number n).  Outputs may be the inputs themselves (same pointer and strides); they must not
+ * [N] or [B, N] (NULL: its number n).  Outputs have no stride of 0 (dimensions of one aside); they may be the inputs themselves (same pointer and strides) and must not
  * overlap them otherwise. */
 int stand_rotate_heads(const stand_rotation* shape, const void* dev_q, const void* dev_k, const void* dev_weight_q,
                        const void* dev_weight_k, const float* dev_freq, const int64_t* dev_base, const int32_t* dev_offset,

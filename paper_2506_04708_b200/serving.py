@@ -39,6 +39,11 @@ def _steps(x, what):
     return [s if n > 1 else 0 for n, s in zip(shape[:-1], strides)]
 
 
+def _apart(x, what):
+    """Refuses tensors to write whose rows share memory by a stride of 0 (expanded ones)."""
+    _need(not any(s == 0 and n > 1 for s, n in zip(x.stride(), x.shape)), f"{what}: wants rows of its own for every place")
+
+
 class _Op:
     """Device, stream and workspace handling of the operators."""
 
@@ -227,6 +232,7 @@ class HeadRotation(_Op):
         pqo, pko = self._floats(q_out, self._q, "q_out"), self._floats(k_out, self._k, "k_out")
         strides = q.stride(), k.stride(), q_out.stride(), k_out.stride()
         if strides != self._strides:
+            _apart(q_out, "q_out"), _apart(k_out, "k_out")
             qs, ks, qo, ko = _steps(q, "q"), _steps(k, "k"), _steps(q_out, "q_out"), _steps(k_out, "k_out")
             c.q_stride[:], c.k_stride[:], c.q_out_stride[:], c.k_out_stride[:] = qs, ks, qo, ko
             self._strides = strides
@@ -292,6 +298,7 @@ class KvAppend(_Op):
             pck, pcv = self._floats(cache_k, self._cache, "cache_k"), self._floats(cache_v, self._cache, "cache_v")
         strides = k.stride(), v.stride(), cache_k.stride(), cache_v.stride()
         if strides != self._strides:
+            _apart(cache_k, "cache_k"), _apart(cache_v, "cache_v")
             ks, vs, cs = _steps(k, "k"), _steps(v, "v"), _steps(cache_k, "cache_k")
             _need(_steps(cache_v, "cache_v") == cs, "KvAppend: both caches have the same strides")
             c.k_stride[:], c.v_stride[:], c.cache_stride[:] = ks, vs, cs + [0] * (4 - len(cs))

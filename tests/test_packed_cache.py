@@ -989,3 +989,25 @@ def test_a_refused_rotation_leaves_the_next_call_as_it_was():
         op(wide, x, k_out=torch.zeros((2, 3, 64, 4), device=DEV).transpose(2, 3))
     got = op(x, x)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.gpu
+def test_expanded_tensors_are_read_but_not_written():
+    import torch
+    from paper_2506_04708_b200 import serving
+    x = torch.randn((2, 1, 1, 64), device=DEV)
+    many = x.expand(2, 3, 4, 64)
+    op = serving.HeadRotation(2, 3, 4, 4, 64, torch.float32, freq=torch.ones(32, device=DEV))
+    want = [t.clone() for t in op(many.contiguous(), many.contiguous())]
+    got = op(many, many)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for bad in (dict(q_out=many), dict(k_out=many)):
+        with pytest.raises(binding.StandError):
+            op(many, many, **bad)
+    slots = torch.arange(6, device=DEV).view(2, 3)
+    for packed, shape, dtype in ((False, (1, 1, 64, 64), torch.float32), (True, (1, 1, 2304), torch.uint8)):
+        add = serving.KvAppend(1, 2, 3, 4, 64, torch.float32, 64, 1, 3, packed=packed)
+        cache = torch.zeros((1,) + shape, dtype=dtype, device=DEV).expand((1, 1, 4) + shape[2:])
+        with pytest.raises(binding.StandError):
+            add(many[None], many[None], slots, cache, cache.clone(memory_format=torch.contiguous_format))
+        assert not cache.any()
