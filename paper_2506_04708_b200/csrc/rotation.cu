@@ -147,7 +147,7 @@ struct AppendParams {
 };
 
 // As above, with a token's place in the cache and angles worked out once for all layers of a block.  1,100 tokens of three prompts in 32 layers, 8 heads of
-// 128 in bfloat16, norm and turn, to 4 bits: 66 us (floor 27), to a cache of their own type 56 us (floor 43); layer after layer in blocks of their own
+// 128 in bfloat16, norm and turn, to 4 bits: 55 us (floor 27), to a cache of their own type 55 us (floor 43); layer after layer in blocks of their own
 // it took 81 and 65.  In 4 bits the kernel is bound by issue (69 % of its slots, logic unit 48 %): the maximum of 16, a scale, 16 codes and their
 // place in two words cost about as much again as norm and turn.
 // Packed: a lane takes a group of 16 elements.  Where units are such groups they stay in registers; else (halves that are turned, short units) the
@@ -161,6 +161,7 @@ __global__ void __launch_bounds__(ROT_THREADS, sizeof(T) == 2 ? 4 : 3) kv_append
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, lanes = p.t.lanes, c = tid & (lanes - 1), group = tid / lanes, groups = ROT_THREADS / lanes;
+  const bool keys = blockIdx.z == 0;
   const long long first = (long long)blockIdx.x * p.tokens;
   const int tokens = p.places - first < p.tokens ? (int)(p.places - first) : p.tokens;
   const int l0 = blockIdx.y * p.layers_block, layers = p.layers - l0 < p.layers_block ? p.layers - l0 : p.layers_block;
@@ -178,12 +179,12 @@ __global__ void __launch_bounds__(ROT_THREADS, sizeof(T) == 2 ? 4 : 3) kv_append
     s_at[tid] = page < 0 ? 0 : turn_position(p.t, b, node);
   }
   __syncthreads();
-  if (p.t.freq) {
+  if (keys && p.t.freq) {
     turn_tables<VE>(p.t, rot_cs, tokens, [&](int tok) { return s_at[tok]; });
     __syncthreads();
   }
   T* const mine = reinterpret_cast<T*>(rot_cs + p.table_floats) + group * dim;
-  // Keys, then values: strides and what is done are the same for all lanes.  A group of lanes has one token's head in all of the block's layers, the
+  // Keys and values have blocks of their own: strides and what is done are the same for all lanes.  A group of lanes has one token's head in all of the block's layers, the
   // next layer's row on its way while one is worked on.
   auto kind = [&](const void* src, const long long (&in_s)[4], const long long* from, char* cache, auto are_keys) {
     constexpr bool KEYS = decltype(are_keys)::value;
@@ -249,8 +250,8 @@ __global__ void __launch_bounds__(ROT_THREADS, sizeof(T) == 2 ? 4 : 3) kv_append
       }
     }
   };
-  kind(p.k, p.k_in, s_from[0], p.cache_k, std::true_type{});
-  kind(p.v, p.v_in, s_from[1], p.cache_v, std::false_type{});
+  if (keys) kind(p.k, p.k_in, s_from[0], p.cache_k, std::true_type{});
+  else kind(p.v, p.v_in, s_from[1], p.cache_v, std::false_type{});
 }
 
 struct ReadParams {
@@ -377,15 +378,16 @@ template <typename T> int launch_rotate(RotateParams& p, int ve, cudaStream_t st
 template <typename T, int VE> int launch_append(AppendParams& p, bool packed, cudaStream_t st) {
   turn_units(p.t, VE);
   // Tokens enough that each group of lanes has a row (16 at most), and as many layers as leave enough blocks to fill the GPU: a token's angles are
-  // worked out once for all layers of a block.
+  // worked out once for all layers of a block.  With 2, 4, 8 (times 148 blocks each of keys and values): prompts of 32 layers 72, 55, 58 us, accepted paths of
+  // 28 layers 9.2, 9.5, 13.6; keys and values one after the other in one block at best 67 and 10.4.
   const int groups = ROT_THREADS / p.t.lanes;
   p.tokens = groups / p.heads < 1 ? 1 : (groups / p.heads > ROT_TOKENS ? ROT_TOKENS : groups / p.heads);
   while (p.tokens > 1 && p.places <= p.tokens / 2) p.tokens /= 2;
   const long long across = (p.places + p.tokens - 1) / p.tokens;
   int lpb = p.layers;
-  while (lpb > 1 && across * ((p.layers + lpb - 1) / lpb) < 6 * 148) lpb = (lpb + 1) / 2;
+  while (lpb > 1 && across * ((p.layers + lpb - 1) / lpb) < 4 * 148) lpb = (lpb + 1) / 2;
   p.layers_block = lpb;
-  const dim3 grid((unsigned)across, (unsigned)((p.layers + lpb - 1) / lpb));
+  const dim3 grid((unsigned)across, (unsigned)((p.layers + lpb - 1) / lpb), 2);
   p.table_floats = p.tokens * 2 * turn_floats<VE>(p.t.columns);
   const size_t smem = p.table_floats * sizeof(float) + (packed ? (size_t)groups * p.t.dim * sizeof(T) : 0);
   if (packed) return launch_dependent(kv_append_kernel<T, VE, true>, grid, ROT_THREADS, st, p, smem);
