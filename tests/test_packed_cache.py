@@ -1011,3 +1011,30 @@ def test_expanded_tensors_are_read_but_not_written():
         with pytest.raises(binding.StandError):
             add(many[None], many[None], slots, cache, cache.clone(memory_format=torch.contiguous_format))
         assert not cache.any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("packed", [False, True])
+def test_rows_at_multiples_of_16_bytes_that_are_none_of_32(packed):
+    """Sources and results whose rows begin 16 bytes behind a multiple of 32 (accesses are narrower there) give the same."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    dt, L, B, N, H, D = torch.bfloat16, 3, 2, 5, 2, 64
+    shape, slots = (L, B, N, H, D), torch.arange(10, device=DEV).view(B, N)
+
+    def shifted(x=None):
+        t = torch.empty(L * B * N * H * D + 8, dtype=dt, device=DEV)[8:].view(shape)
+        return t if x is None else t.copy_(x)
+
+    k, v = (torch.randn(shape, device=DEV).to(dt) for _ in range(2))
+    add = serving.KvAppend(L, B, N, H, D, dt, 16, 1, N, packed=packed)
+    back = serving.KvRead(L, B, H, D, dt, 16, 1, N, packed=packed)
+    cache = [torch.zeros((L, 1, H, 576) if packed else (L, 1, H, 16, D), dtype=torch.uint8 if packed else dt, device=DEV) for _ in range(4)]
+    add(k, v, slots, *cache[:2])
+    add(shifted(k), shifted(v), slots, *cache[2:])
+    assert torch.equal(cache[0], cache[2]) and torch.equal(cache[1], cache[3])
+    want = [t.clone() for t in back(slots, *cache[:2])]
+    got = back(slots, *cache[:2], k=shifted(), v=shifted())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    if not packed:
+        assert torch.equal(got[0], k) and torch.equal(got[1], v)
