@@ -176,6 +176,10 @@ __device__ __forceinline__ void ta_begin(const TaSplit& p, TaWalk& walk, TaRange
       at += n;
     }
   }
+  if (tid == 0) {  // for whoever keeps the record: read behind the barrier
+    sh.total = total;
+    sh.groups = (int)groups;
+  }
   before();
   __syncthreads();
   after();
@@ -185,10 +189,6 @@ __device__ __forceinline__ void ta_begin(const TaSplit& p, TaWalk& walk, TaRange
   walk.b_start = sh.b_start;
   walk.first = true;
   walk.cost = cost;
-  if (tid == 0) {
-    sh.total = total;
-    sh.groups = (int)groups;
-  }
 }
 
 // ---- packed tiles ---------------------------------------------------------------------
