@@ -30,7 +30,8 @@ struct Turn {
 };
 
 // A token's table: cos, then sin, of angle c * VE + j (pair j of unit c) at ((j / 4) * columns + c) * 4 + j % 4, so that the lanes of a row read 16
-// bytes each without conflict (VE = 1: one after the other).  Places past the last pair hold 1 and 0.
+// bytes each without conflict (VE = 1: one after the other).  Places past the last pair hold
+// 1 and 0 and turn nothing.
 template <int VE> __host__ __device__ __forceinline__ int turn_floats(int columns) { return (columns * VE + 3) & ~3; }  // cos alone
 template <int VE> __device__ __forceinline__ int turn_at(int columns, int i) {
   const int c = i / VE, j = i % VE;
@@ -108,11 +109,14 @@ template <int VE> __device__ __forceinline__ void turn_unit(const Turn& t, const
     s[0] = sn[u];
   }
   if (t.pairs) {
+    // A last unit may have fewer pairs than vectors have room for; what is not turned stays as it is (a turn by nothing would
+    // multiply it by 0, and its neighbour need not be finite).
+    const int left = t.half - u * VE;
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
       const float a = y[2 * i], b = y[2 * i + 1];
-      y[2 * i] = fmaf(a, c[i], -b * s[i]);
-      y[2 * i + 1] = fmaf(a, s[i], b * c[i]);
+      y[2 * i] = i < left ? fmaf(a, c[i], -b * s[i]) : a;
+      y[2 * i + 1] = i < left ? fmaf(a, s[i], b * c[i]) : b;
     }
   } else {
     if constexpr (VE >= 4) {

@@ -46,3 +46,85 @@ def test_what_a_block_shares_of_its_range_is_written_before_its_last_barrier():
     written = {m.group(1): m.start() for m in re.finditer(r"\bsh\.(\w+)(?:\[[^\]]*\])?\s*=[^=]", body)}
     assert set(written) == {"sum", "b", "b_start", "total", "groups"}
     assert all(at < last for at in written.values()), written
+
+
+# ---------------------------------------------------------------- elements past the turned ones
+def _bits_of(t):
+    """The bits of a tensor's elements, all NaN alike."""
+    import torch
+    return torch.where(torch.isnan(t), float("nan"), t).contiguous().view(torch.int32 if t.dtype == torch.float32 else torch.int16)
+
+
+def _rows_with_odd_values(dtype, dim, rotary, pairs, seed=0):
+    """Rows [1, 1, 9, 1, dim]: ordinary ones, then with values that are not finite on both sides of where the turned elements end, and with a zero
+    below zero; per row the elements that the turn makes of those."""
+    import torch
+    x = torch.from_numpy(np.random.default_rng(seed).standard_normal((1, 1, 9, 1, dim)).astype(np.float32)).to(ts._dtype(dtype))
+    hit = np.zeros((9, dim), bool)
+    inf, nan = float("inf"), float("nan")
+    for row, (at, value) in enumerate([(rotary, inf), (rotary + 1, nan), (rotary + 2, -inf), (dim - 1, nan), (dim - 2, inf), (rotary - 1, inf), (0, nan),
+                                       (rotary + 1, -0.0)], 1):
+        if at >= dim:
+            continue
+        x[0, 0, row, 0, at] = value
+        if value != 0:
+            hit[row, at] = True
+            if at < rotary:
+                hit[row, at ^ 1 if pairs else (at + rotary // 2) % rotary] = True
+    return x, hit
+
+
+def _moved(x, shift):
+    """The same rows, `shift` elements behind a boundary of 16 bytes."""
+    import torch
+    out = torch.empty(x.shape[:-1] + (x.shape[-1] + 16,), dtype=x.dtype, device=DEV)[..., shift:shift + x.shape[-1]]
+    return out.copy_(x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("pairs", [True, False])
+@pytest.mark.parametrize("shift", [0, 4, 1])
+@pytest.mark.parametrize("dim,rotary", [(80, 40), (100, 36), (64, 2), (128, 20), (48, 46), (128, 64), (31, 30), (16, 10)])
+def test_elements_past_the_turned_ones_stay_as_they_are(dtype, pairs, shift, dim, rotary):
+    """Bit by bit, whatever their neighbours hold; turned ones as defined, except what a value that is not finite is turned with.  The rows of a cache of
+    their own type are the same."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    x, hit = _rows_with_odd_values(dtype, dim, rotary, pairs)
+    n = x.shape[2]
+    freq = (1000.0 ** (-np.arange(rotary // 2) / (rotary // 2))).astype(np.float32)
+    offset = torch.arange(5, 5 + n, dtype=torch.int32, device=DEV)
+    rows = _moved(x[0], shift)
+    plan = serving.HeadRotation(1, n, 1, 1, dim, x.dtype, freq=tp._dev(freq), offset=offset, interleaved=pairs)
+    q, k = plan(rows, rows, q_out=_moved(x[0], shift), k_out=_moved(x[0], shift))
+    assert torch.equal(_bits_of(q), _bits_of(k))
+    assert torch.equal(_bits_of(q[..., rotary:]), _bits_of(rows[..., rotary:]))
+    got = q.double().cpu().numpy()[0, :, 0]
+    assert np.array_equal(~np.isfinite(got), hit)
+    fine = np.where(np.isfinite(x.double().numpy()[0, 0, :, 0]), x.double().numpy()[0, 0, :, 0], 0.0)
+    want, size = pref.rotate(fine, np.arange(5, 5 + n), freq, pairs)
+    tp._near(np.where(hit, 0.0, got), np.where(hit, 0.0, want), size, dtype, False)
+    cache, other = (torch.zeros((1, 1, 1, 16, dim + 16), dtype=x.dtype, device=DEV)[..., shift:shift + dim] for _ in range(2))
+    add = serving.KvAppend(1, 1, n, 1, dim, x.dtype, 16, 1, n, freq=tp._dev(freq), offset=offset, interleaved=pairs)
+    add(rows[None], rows[None], torch.arange(n, device=DEV)[None], cache, other)
+    assert torch.equal(_bits_of(cache[0, 0, 0, :n]), _bits_of(k[0, :, 0]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("dim,rotary", [(80, 40), (128, 20)])
+def test_in_4_bits_a_value_that_is_not_finite_spoils_its_group_alone(dtype, dim, rotary):
+    import torch
+    from paper_2506_04708_b200 import serving
+    x, hit = _rows_with_odd_values(dtype, dim, rotary, True)
+    n = x.shape[2]
+    freq = torch.ones(rotary // 2, device=DEV)
+    cache = [torch.zeros((1, 1, 1, serving.packed_block_bytes(16, dim)), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    slots = torch.arange(n, device=DEV)[None]
+    add = serving.KvAppend(1, 1, n, 1, dim, x.dtype, 16, 1, n, packed=True, freq=freq, interleaved=True)
+    add(x.to(DEV), x.to(DEV), slots, *cache)
+    k, v = serving.KvRead(1, 1, 1, dim, torch.float32, 16, 1, n, packed=True)(slots, *cache)
+    group = lambda h: np.repeat(h.reshape(n, dim // 16, 16).any(-1), 16, -1)  # noqa: E731
+    assert np.array_equal(np.isnan(k.cpu().numpy()[0, 0, :, 0]), group(hit))
+    assert np.array_equal(np.isnan(v.cpu().numpy()[0, 0, :, 0]), group(~np.isfinite(x.double().numpy()[0, 0, :, 0])))
