@@ -295,6 +295,11 @@ template <int DP, int C, bool BF16, bool PACKED>
 __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>::CTAS) tensor_attention_kernel(const __grid_constant__ TaParams p) {
   using Sh = TaShape<DP, C, PACKED>;
   constexpr int TA_THREADS = TA_THREADS_OF<PACKED>;
+  // Halves do not hold all that codes stand for: there cached keys and values lie in the slots as 1 / 8 of themselves.  The text's scores are
+  // brought back by their scale, its part of O by weights 2^3 larger than the tree's; so that these still fit, the maximum is raised that much earlier.
+  // All of it by powers of two, so no bit changes but those of weights that were too small for a half.
+  constexpr bool SHARED = PACKED && !BF16;
+  constexpr float SHARE = SHARED ? 8.0f : 1.0f, SHARE_LOG = SHARED ? 3.0f : 0.0f, SLACK = TA_SLACK - SHARE_LOG;
   constexpr int MMA_WARP = PACKED ? 8 : 5;  // packed: warps 4 - 7 unpack, one for each scheduler as the softmax warps are (with two of those beside one: 387 us rather than 378)
   constexpr int KT = TA_KT, HALVES = DP / 64, SLOTS = Sh::SLOTS, K_SLOTS = Sh::K_SLOTS, V_SLOTS = Sh::V_SLOTS;
   constexpr int PART_ROWS = TA_ROWS / C, W = KT / C, CH = W < 32 ? W : 32;  // rows of a part; keys of a tile that it takes
@@ -440,8 +445,8 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
               const int row = row0 + (i0 + i) * KEYS;
-              const PkScale<BF16> scale(byte[i]);
-              const uint4 v0 = pk_word<BF16>(swap ? w[i].y : w[i].x, scale), v1 = pk_word<BF16>(swap ? w[i].x : w[i].y, scale);
+              const PkScale<BF16, SHARED> scale(byte[i]);
+              const uint4 v0 = pk_word(swap ? w[i].y : w[i].x, scale), v1 = pk_word(swap ? w[i].x : w[i].y, scale);
               *reinterpret_cast<uint4*>(to + (i0 + i) * KEYS * 128 + ((piece ^ (row & 7)) << 4)) = v0;
               *reinterpret_cast<uint4*>(to + (i0 + i) * KEYS * 128 + ((piece ^ 1 ^ (row & 7)) << 4)) = v1;
             }
@@ -632,6 +637,7 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
         const bool tree = j >= s.p_tiles;
         const int left = s.len - j * KT;  // cached tokens from this tile on
         const bool partial = !tree && left < KT;
+        const float by = SHARED && !tree ? scale2 * SHARE : scale2;
         ok = wait_warp(bar_s + 8 * (n & 1), (n >> 1) & 1u);
         if (!ok) break;
         tc_fence_after();
@@ -665,11 +671,11 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
               top1 = max3(top1, __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
             }
           }
-          top = fmaxf(top, top1) * scale2;
+          top = fmaxf(top, top1) * by;
           // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores pass
           // it by TA_SLACK, so that o is seldom read, scaled and written (TA_LIFT keeps the weights within their type).  The warp's rows move together, as live rows want it: what lies in the lanes of others is
           // left from earlier kernels or belongs to nodes that were not drafted, and would enter the roundings of the weights.
-          if (__any_sync(FULL, live && top > m + TA_SLACK)) {
+          if (__any_sync(FULL, live && top > m + SLACK)) {
             const float raised = fmaxf(m, top);
             const float keep = raised == -INFINITY ? 1.0f : ta_ex2(m - raised);
             m = raised;
@@ -689,8 +695,8 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
               }
             }
           }
-          const float base = (m == -INFINITY ? 0.0f : m) - TA_LIFT<BF16>;
-          const unsigned long long scale_2 = pack2(scale2, scale2), base_2 = pack2(-base, -base);
+          const float base = (m == -INFINITY ? 0.0f : m) - (TA_LIFT<BF16> + (tree ? 0.0f : SHARE_LOG));
+          const unsigned long long scale_2 = pack2(by, by), base_2 = pack2(-base, -base);
           unsigned long long sum_2 = pack2(0.0f, 0.0f);
 #pragma unroll 1
           for (int c = 0; c < W / CH; ++c) {
@@ -715,7 +721,8 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
           }
           float sum0, sum1;
           unpack2(sum_2, sum0, sum1);
-          l += sum0 + sum1;
+          if constexpr (SHARED) l = fmaf(sum0 + sum1, tree ? 1.0f : 1.0f / SHARE, l);
+          else l += sum0 + sum1;
           tc_wait_st();
         }
         if (tree || (partial && !PACKED)) {

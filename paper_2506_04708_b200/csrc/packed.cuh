@@ -2,7 +2,7 @@
 //
 // A row's elements in groups of 16: a scale s of 8 bits - 5 exponent bits (bias 15), 3 fraction bits, no sign, subnormals, the
 // bits of a half between its sign and its last seven - and 16 whole numbers k of -8 .. 7 as k + 8 in 4 bits; an element is k s.
-// That has at most 7 significant bits: exact in bfloat16 and in half, so products of values are those of the definition.
+// That has at most 7 significant bits: exact in bfloat16 and, within its range, in half, so products of values are those of the definition.
 // s is the smallest with 7 s >= the group's largest magnitude, k the nearest whole number (even in a tie).  Exponent 31: not finite,
 // the whole group reads as NaN.
 // Four bytes hold 8 elements: the even ones in the low half, the odd ones in the high half, each from the low bits on, so that one
@@ -106,9 +106,10 @@ __device__ __forceinline__ uint32_t pk_two(float f) {  // twice, as bfloat16
   return r;
 }
 // A word of 8 codes as 8 values of the call's type (16 bytes), with the scale of its group.  bfloat16: a code n in bits 1 - 4 of a bfloat16
-// that begins at 64 is 64 + n, and (64 + n) s - 72 s is exact, 72 s having 7 significant bits; an infinite scale gives infinity less infinity.
-// Half: 1024 + n, less 1032, times s.
-template <bool BF16> struct PkScale {
+// that begins at 64 is 64 + n, and (64 + n) s - 72 s is exact, 72 s having at most 8 significant bits (9 x 15); an infinite scale gives infinity less infinity.
+// Half: 1024 + n, less 1032, times s.  SHARED (half): an eighth of each value, 128 + n / 8 less 129, times s.  A half ends at 65,504 and k s at 8 * 61,440; k s / 8 is
+// exact for every scale and code.
+template <bool BF16, bool SHARED = false> struct PkScale {
   uint32_t s, c;
   __device__ __forceinline__ explicit PkScale(uint32_t byte) {
     if constexpr (BF16) {
@@ -126,7 +127,7 @@ __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t b
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(x), "r"(mask), "r"(bits));
   return r;
 }
-template <bool BF16> __device__ __forceinline__ uint4 pk_word(uint32_t w, const PkScale<BF16>& p) {
+template <bool BF16, bool SHARED> __device__ __forceinline__ uint4 pk_word(uint32_t w, const PkScale<BF16, SHARED>& p) {
   uint32_t v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -134,9 +135,9 @@ template <bool BF16> __device__ __forceinline__ uint4 pk_word(uint32_t w, const 
       const uint32_t x = and_or(i == 0 ? w << 1 : w >> (4 * i - 1), 0x001E001Eu, 0x42804280u);
       asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(v[i]) : "r"(x), "r"(p.s), "r"(p.c));
     } else {
-      const uint32_t x = and_or(w >> (4 * i), 0x000F000Fu, 0x64006400u);
+      const uint32_t from = SHARED ? 0x58005800u : 0x64006400u, x = and_or(w >> (4 * i), 0x000F000Fu, from);
       uint32_t k;
-      asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(k) : "r"(x), "r"(0x64086408u));
+      asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(k) : "r"(x), "r"(from + 0x00080008u));
       asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(v[i]) : "r"(k), "r"(p.s));
     }
   }

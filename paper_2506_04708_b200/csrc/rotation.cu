@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(ROT_THREADS) kv_read_kernel(const __grid_const
       if (page >= 0) {
         const uint2 w = __ldg(reinterpret_cast<const uint2*>(from + at));
         const PkScale<BF16> s(__ldg(reinterpret_cast<const unsigned char*>(from + scale_at)));
-        v[0] = pk_word<BF16>(w.x, s), v[1] = pk_word<BF16>(w.y, s);
+        v[0] = pk_word(w.x, s), v[1] = pk_word(w.y, s);
       }
       if constexpr (WIDE == 2) {
         store_32(out, v[0], v[1]);

@@ -128,3 +128,45 @@ def test_in_4_bits_a_value_that_is_not_finite_spoils_its_group_alone(dtype, dim,
     group = lambda h: np.repeat(h.reshape(n, dim // 16, 16).any(-1), 16, -1)  # noqa: E731
     assert np.array_equal(np.isnan(k.cpu().numpy()[0, 0, :, 0]), group(hit))
     assert np.array_equal(np.isnan(v.cpu().numpy()[0, 0, :, 0]), group(~np.isfinite(x.double().numpy()[0, 0, :, 0])))
+
+
+# ---------------------------------------------------------------- values beyond a half
+def _beyond_a_half(seed, dtype, lens, N, hq, hkv, dim):
+    """A packed case whose keys and values reach 8 * 61,440 where texts are long enough to bring results back below 65,504."""
+    c = tp._packed_case(seed, dtype, lens, N, hq, hkv, dim, 16, parent=inputs.topology(N, min(N - 1, 3), 4), nan=False, spare=0)
+    rng = np.random.default_rng(seed)
+    for name, rate in (("ck", 0.3), ("cv", 0.02)):
+        blocks = c[name + "_packed"].numpy()
+        codes, scales = blocks[..., : 16 * dim // 2], blocks[..., 16 * dim // 2:].reshape(blocks.shape[:2] + (16, dim // 16))
+        codes[rng.random(codes.shape) < 0.02] &= 0xF0  # a code of -8, which nothing stores, reads as one
+        large = rng.random(scales.shape) < rate
+        if name == "cv":
+            for b, n in enumerate(lens):
+                if n < 300:
+                    large[c["table"][b, : -(-n // 16)]] = False
+        scales[large] = rng.integers(0xE8, 0xF8, large.sum())
+        import torch
+        c[name] = torch.from_numpy(pref.block_values(blocks, 16, dim))
+    return c
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("lens", [[0, 5, 300, 700, 130], [6000]])
+@pytest.mark.parametrize("N,hq,hkv,dim,odd", [(1, 8, 2, 128, False), (3, 4, 2, 64, False), (9, 4, 2, 64, False), (24, 4, 2, 64, False), (64, 4, 2, 64, False),
+                                              (24, 8, 2, 128, False), (3, 2, 1, 256, False), (5, 4, 2, 80, False), (24, 8, 2, 128, True)])
+def test_packed_attention_over_values_beyond_a_half(dtype, lens, N, hq, hkv, dim, odd):
+    """A cache may hold 491,520 and a half ends at 65,504: every kernel takes what the codes stand for, whatever the call's type."""
+    import torch
+    if len(lens) == 1:
+        lens = [lens[0] + N] if N > 30 else lens * 2
+    c = _beyond_a_half(dim + 2 * N, dtype, lens, N, hq, hkv, dim)
+    scale = 2.0**-21
+    want = ts._reference(c, scale)
+    assert np.abs(c["ck"].numpy()).max() > 400000 and np.abs(c["cv"].numpy()).max() > 400000 and np.abs(want[0]).max() < 60000
+
+    def move(q, k, v, ck, cv):
+        shift = lambda x: torch.empty(x.numel() + 1, dtype=x.dtype, device=DEV)[1:].view(x.shape).copy_(x)  # noqa: E731
+        return (shift(q), shift(k), shift(v), ck, cv) if odd else (q, k, v, ck, cv)
+
+    tp._check(c, tp._run_packed(c, scale=scale, move=move), want=want)
