@@ -200,9 +200,10 @@ __global__ void __launch_bounds__(PR_THREADS, PrShape<DP, NB>::CTAS) packed_rows
           for (int e = 0; e < 2; ++e) most = max(most, max(q[n][i][e] & 0x7F80u, q[n][i][e] >> 16 & 0x7F80u));
 #pragma unroll
         for (int d = 1; d < 4; d *= 2) most = max(most, __shfl_xor_sync(FULL, most, d));
-        // the row's largest power of two becomes 2^14: what is below 2^-29 of it loses bits, none is lost above 2^-38
+        // the row's largest power of two becomes 2^14: what is below 2^-29 of it loses bits, none is lost above 2^-38.  (Rows below 2^-112 are brought up by
+        // 2^126, the most that a float has together with its inverse; what is least in the type then is 2^-7.)
         int up = 14 + 127 - (int)(most >> 7);
-        up = most >= 0x7F80u ? 0 : (up > 100 ? 100 : up);
+        up = most >= 0x7F80u ? 0 : (up > 126 ? 126 : up);
         const float by = __int_as_float((127 + up) << 23);
         share = __int_as_float((127 - up) << 23);
 #pragma unroll
@@ -214,7 +215,8 @@ __global__ void __launch_bounds__(PR_THREADS, PrShape<DP, NB>::CTAS) packed_rows
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int row = n * 8 + 2 * t + c;
-        factor[n][c] = __shfl_sync(FULL, share, (2 * t + c) * 4) * (PK_SHARE * a.scale2);
+        // (not zero, which would make NaN of the masked scores' -inf; 2^-126 makes nothing of any product here as well)
+        factor[n][c] = fmaxf(__shfl_sync(FULL, share, (2 * t + c) * 4) * PK_SHARE * a.scale2, 0x1p-126f);
         node[n][c] = row / a.group;
         live[n][c] = row < p.s.rows && !(a.tree && a.tree[(long long)s.b * a.N + node[n][c]] < 0);
       }

@@ -170,3 +170,14 @@ def test_packed_attention_over_values_beyond_a_half(dtype, lens, N, hq, hkv, dim
         return (shift(q), shift(k), shift(v), ck, cv) if odd else (q, k, v, ck, cv)
 
     tp._check(c, tp._run_packed(c, scale=scale, move=move), want=want)
+
+
+# ---------------------------------------------------------------- queries at the ends of their range
+@pytest.mark.gpu
+@pytest.mark.parametrize("size,scale", [(2.0**-120, 2.0**117), (2.0**-126, 2.0**122), (2.0**-118, 2.0**-40), (2.0**-100, 2.0**-60), (2.0**118, 2.0**-121), (0.0, 2.0**-100)])
+@pytest.mark.parametrize("N,hq,dim", [(1, 4, 128), (1, 4, 64), (3, 8, 128), (24, 8, 64)])
+def test_packed_queries_at_the_ends_of_the_range(size, scale, N, hq, dim):
+    """bfloat16 rows as small and as large as the type has them, under scales that make ordinary scores of them or nothing at all."""
+    c = tp._packed_case(93, "bf16", [300, 5, 0, 77], N, hq, 2, dim, 16, parent=inputs.topology(N, min(3, N - 1), 3), nan=False)
+    c["qkv"][:, :, :hq] = (c["qkv"][:, :, :hq].double() * size).to(c["qkv"].dtype)
+    tp._check(c, tp._run_packed(c, scale=scale), want=ts._reference(c, scale))
