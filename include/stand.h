@@ -326,7 +326,7 @@ typedef struct {
   int32_t dim;        /* 1..256 */
   int32_t dtype;      /* STAND_DTYPE_* of q, k, v, cache and out */
   int32_t page_size;  /* a multiple of 16, up to 4096 */
-  int32_t pages;      /* pages in the pool, >= 0 */
+  int32_t pages;      /* pages in the pool, >= 0 (0: the caches may be NULL) */
   int32_t max_pages;  /* columns of the block table, >= 0; max_pages * page_size <= 2^30 */
   float scale;        /* scores are scale * q . k; > 0 */
   int64_t q_stride[3];      /* sequence, node, head */
@@ -501,7 +501,7 @@ typedef struct {
   int32_t layers, B, N;    /* N nodes per sequence in the source; layers up to 4096 */
   int32_t heads, dim;      /* up to 4096; 1..256 */
   int32_t dtype;           /* of the rows, and of a cache that is not packed */
-  int32_t page_size, pages; /* page_size up to 4096 */
+  int32_t page_size, pages; /* page_size up to 4096; pages >= 0 (0: the caches may be NULL) */
   int32_t width;           /* columns of dev_slots and dev_path */
   int32_t packed;          /* 1: the caches are in the 4-bit form */
   int32_t rotary_dim, interleaved, norm;  /* of the keys, as in stand_rotation */

@@ -57,7 +57,7 @@ int attention_call(const stand_attention* c, bool packed, const void* dev_q, con
                          int64_t mask_stride, const int32_t* dev_tree_tokens, void* dev_scratch, size_t scratch_bytes, void* dev_out,
                          float* dev_lse, void* cu_stream) {
   if (!attention_valid(c) || !dev_q || !dev_k || !dev_v || !dev_len || !dev_out) return STAND_E_ARG;
-  if (c->max_pages > 0 && (!dev_table || !dev_cache_k || !dev_cache_v)) return STAND_E_ARG;
+  if (c->max_pages > 0 && (!dev_table || (c->pages > 0 && (!dev_cache_k || !dev_cache_v)))) return STAND_E_ARG;
   if (packed && (c->dim % PK_GROUP != 0 || c->cache_stride[2] != 0 || ((c->cache_stride[0] | c->cache_stride[1]) & 15) != 0 || !aligned(16, dev_cache_k, dev_cache_v)))
     return STAND_E_ARG;
   if (!aligned(c->dtype == STAND_DTYPE_F32 ? 4 : 2, dev_q, dev_k, dev_v, dev_cache_k, dev_cache_v, dev_out) || !aligned(8, dev_len) ||
@@ -77,6 +77,10 @@ int attention_call(const stand_attention* c, bool packed, const void* dev_q, con
     p.k_stride[i] = c->kv_stride[i];
     p.v_stride[i] = c->own_v_stride ? c->v_stride[i] : c->kv_stride[i];
     p.cache_stride[i] = c->cache_stride[i];
+  }
+  if (p.pages == 0) {  // no page is read, but copies of nothing still name an address: one that is there
+    p.cache_k = p.cache_v = (const char*)dev_scratch;
+    for (int i = 0; i < 3; ++i) p.cache_stride[i] = 0;
   }
   cudaStream_t st = (cudaStream_t)cu_stream;
   int dev = -1, sms = 0;

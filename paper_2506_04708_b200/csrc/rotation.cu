@@ -473,7 +473,7 @@ int stand_rotate_heads(const stand_rotation* c, const void* dev_q, const void* d
 int stand_kv_append(const stand_kv_rows* c, const void* dev_k, const void* dev_v, const void* dev_weight_k, const float* dev_freq,
                     const int64_t* dev_base, const int32_t* dev_offset, const int32_t* dev_path, const int64_t* dev_slots, void* dev_cache_k,
                     void* dev_cache_v, void* cu_stream) {
-  if (!c || !dev_k || !dev_v || !dev_slots || !dev_cache_k || !dev_cache_v) return STAND_E_ARG;
+  if (!c || !dev_k || !dev_v || !dev_slots || (c->pages != 0 && (!dev_cache_k || !dev_cache_v))) return STAND_E_ARG;
   if (c->layers < 1 || c->layers > ROW_COUNT || c->B < 1 || c->N < 1 || c->heads < 1 || c->heads > ROW_COUNT || c->width < 1) return STAND_E_ARG;
   if (c->page_size < 1 || c->page_size > 4096 || c->pages < 0 || !type_valid(c->dtype) || (c->packed != 0 && c->packed != 1) || (c->reserved | c->reserved2) != 0) return STAND_E_ARG;
   if ((long long)c->B * c->width > 0x7FFFFFFFll) return STAND_E_ARG;
@@ -504,7 +504,7 @@ int stand_kv_append(const stand_kv_rows* c, const void* dev_k, const void* dev_v
 
 int stand_kv_read(const stand_kv_rows* c, const void* dev_cache_k, const void* dev_cache_v, const int64_t* dev_slots, void* dev_k, void* dev_v,
                   void* cu_stream) {
-  if (!c || !dev_k || !dev_v || !dev_slots || !dev_cache_k || !dev_cache_v) return STAND_E_ARG;
+  if (!c || !dev_k || !dev_v || !dev_slots || (c->pages != 0 && (!dev_cache_k || !dev_cache_v))) return STAND_E_ARG;
   if (c->layers < 1 || c->layers > ROW_COUNT || c->B < 1 || c->heads < 1 || c->heads > ROW_COUNT || c->width < 1 || c->dim < 1 || c->dim > ROT_DIM_MAX) return STAND_E_ARG;
   if (c->page_size < 1 || c->page_size > 4096 || c->pages < 0 || !type_valid(c->dtype) || (c->packed != 0 && c->packed != 1) || (c->reserved | c->reserved2) != 0) return STAND_E_ARG;
   if (c->rotary_dim != 0 || c->norm != 0 || (long long)c->B * c->width > 0x7FFFFFFFll) return STAND_E_ARG;

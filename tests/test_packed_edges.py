@@ -181,3 +181,40 @@ def test_packed_queries_at_the_ends_of_the_range(size, scale, N, hq, dim):
     c = tp._packed_case(93, "bf16", [300, 5, 0, 77], N, hq, 2, dim, 16, parent=inputs.topology(N, min(3, N - 1), 3), nan=False)
     c["qkv"][:, :, :hq] = (c["qkv"][:, :, :hq].double() * size).to(c["qkv"].dtype)
     tp._check(c, tp._run_packed(c, scale=scale), want=ts._reference(c, scale))
+
+
+# ---------------------------------------------------------------- pools without pages
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ts.ALL_TYPES)
+@pytest.mark.parametrize("packed", [False, True])
+def test_a_pool_without_pages(dtype, packed):
+    """Appends skip every place, reads give zeros, attention takes every page as one of zeros."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    dt = ts._dtype(dtype)
+    L, B, N, H, dim, page = 2, 3, 4, 2, 64, 16
+    shape = (0, H, serving.packed_block_bytes(page, dim)) if packed else (0, H, page, dim)
+    cache = torch.empty((L,) + shape, dtype=torch.uint8 if packed else dt, device=DEV)
+    x = torch.randn((L, B, N, H, dim), device=DEV).to(dt)
+    slots = torch.tensor([[0, 1, -1, 7]], device=DEV).expand(B, N).contiguous()
+    serving.KvAppend(L, B, N, H, dim, dt, page, 0, N, packed=packed)(x, x, slots, cache, cache)
+    for got in serving.KvRead(L, B, H, dim, dt, page, 0, N, packed=packed)(slots, cache, cache, k=x.clone(), v=x.clone()):
+        assert not got.any()
+    kind = serving.PackedTreeAttention if packed else serving.TreeAttention
+    for nodes, hq in ((1, 2), (4, 2), (9, 8)):
+        q = torch.randn((B, nodes, hq + 2 * H, dim), device=DEV).to(dt)
+        args = q[:, :, :hq], q[:, :, hq:hq + H], q[:, :, hq + H:]
+        table, length = torch.tensor([[0, -1, 5]] * B, dtype=torch.int32, device=DEV), torch.tensor([0, 20, 48], device=DEV)
+        out, lse = kind(B, nodes, hq, H, dim, dt, page, 0, 3)(*args, cache[0], cache[0], table, length)
+        zeros = torch.zeros((B * 3, H, page, dim), dtype=torch.float64)
+        c = dict(qkv=q.cpu(), ck=zeros, cv=zeros, table=table.cpu().numpy(), len=length.cpu().numpy(), tree=None, parent=None, mask=None, hq=hq, hkv=H, dim=dim,
+                 page=page, N=nodes, dtype=dtype)
+        tp._check(c, (out.double().cpu().numpy(), lse.double().cpu().numpy()))
+
+
+def test_caches_may_be_missing_only_where_there_are_no_pages(lib):
+    A, B2 = C.c_void_p(0x100000), C.c_void_p(0x200000)  # never touched: every call here is refused before a launch
+    for packed in (0, 1):
+        for pages in (1, 5):
+            assert lib.stand_kv_append(C.byref(tp._rows(packed=packed, pages=pages)), A, A, A, A, A, A, A, A, None, B2, None) == -1
+            assert lib.stand_kv_read(C.byref(tp._rows(packed=packed, pages=pages, N=0, rotary_dim=0, norm=0, eps=0.0)), B2, None, A, A, A, None) == -1
