@@ -491,7 +491,7 @@ typedef struct {
  * with the angle worked out in 64 bits (positions up to 2^31 in magnitude).  dev_weight_q, dev_weight_k [dim] of the rows' type (NULL: ones).
  * dev_freq [rotary_dim / 2] float.  dev_base [B] int64 (NULL: 0) is what a sequence's positions begin with, dev_offset int32 what a node adds:
  * [N] or [B, N] (NULL: its number n).  Outputs have no stride of 0 (dimensions of one aside); they may be the inputs themselves (same pointer and strides) and must not
- * overlap them otherwise. */
+ * overlap them, nor one another, otherwise (STAND_E_ARG, as below, where strides from the largest down cover the smaller ones). */
 int stand_rotate_heads(const stand_rotation* shape, const void* dev_q, const void* dev_k, const void* dev_weight_q,
                        const void* dev_weight_k, const float* dev_freq, const int64_t* dev_base, const int32_t* dev_offset,
                        void* dev_q_out, void* dev_k_out, void* cu_stream);
@@ -516,13 +516,13 @@ typedef struct {
  * normalised and turned as by stand_rotate_heads, dev_weight_k [layers, dim] - and of dev_v goes to slot dev_slots[b, j].  A packed
  * cache gets what a cache of the rows' type would hold, in 4 bits.  dev_path NULL: node j.  Places with a slot
  * outside [0, pages * page_size) or a node outside [0, N) are skipped.  Slots of one call must be distinct; the
- * source must not overlap the caches.  Nothing but the slots' own bytes is written. */
+ * source must not overlap the caches, whose strides are not 0 (dimensions of one aside).  Nothing but the slots' own bytes is written. */
 int stand_kv_append(const stand_kv_rows* shape, const void* dev_k, const void* dev_v, const void* dev_weight_k,
                     const float* dev_freq, const int64_t* dev_base, const int32_t* dev_offset, const int32_t* dev_path,
                     const int64_t* dev_slots, void* dev_cache_k, void* dev_cache_v, void* cu_stream);
 
 /* Rows of the cache as values of type dtype (any for a packed cache): dev_k, dev_v [layers, B, width, heads, dim], contiguous.
- * Places with a slot outside the pool give zeros.  The fields of the source rows and of norm and rotation are not used: 0. */
+ * Places with a slot outside the pool give zeros.  Results must not overlap the caches nor one another.  The fields of the source rows and of norm and rotation are not used: 0. */
 int stand_kv_read(const stand_kv_rows* shape, const void* dev_cache_k, const void* dev_cache_v, const int64_t* dev_slots,
                   void* dev_k, void* dev_v, void* cu_stream);
 

@@ -6,9 +6,11 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
 #include <type_traits>
 
 #include "launch.cuh"
+#include "overlap.cuh"
 #include "packed.cuh"
 #include "rotation.cuh"
 
@@ -433,6 +435,24 @@ bool make_turn(Turn& t, int dim, int rotary, int interleaved, int norm, float ep
   return true;
 }
 
+RowSet heads_of(const void* p, int B, int N, int heads, const long long (&stride)[3], int dim, int es) {
+  return {p, (int64_t)dim * es, 3, {B, N, heads, 1}, {stride[0] * es, stride[1] * es, stride[2] * es, 0}};
+}
+RowSet rows_of(const void* p, int layers, int B, int N, int heads, const long long (&stride)[4], int dim, int es) {
+  return {p, (int64_t)dim * es, 4, {layers, B, N, heads}, {stride[0] * es, stride[1] * es, stride[2] * es, stride[3] * es}};
+}
+// (strides in bytes; a packed cache's rows are its blocks)
+RowSet cache_of(const stand_kv_rows* c, const void* p, const long long (&stride)[4], int es) {
+  const int64_t bytes = c->packed ? (int64_t)STAND_PACKED_BLOCK_BYTES(c->page_size, c->dim) : (int64_t)c->dim * es;
+  return {p, bytes, 4, {c->layers, c->pages, c->heads, c->packed ? 1 : c->page_size}, {stride[0], stride[1], stride[2], stride[3]}};
+}
+// Rows to write that lie over one another by a stride of 0 (where there are any rows).
+bool stacked(const RowSet& r) {
+  bool any = true, zero = false;
+  for (int i = 0; i < r.dims; ++i) any = any && r.count[i] > 0, zero = zero || (r.stride[i] == 0 && r.count[i] > 1);
+  return any && zero;
+}
+
 bool packed_strides(const void* a, const void* b, const int64_t (&stride)[4]) {
   if (stride[3] != 0) return false;
   return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)stride[0] | (uintptr_t)stride[1] | (uintptr_t)stride[2]) & 15) == 0;
@@ -457,6 +477,12 @@ int stand_rotate_heads(const stand_rotation* c, const void* dev_q, const void* d
     p.q_in[i] = c->q_stride[i], p.k_in[i] = c->k_stride[i], p.q_to[i] = c->q_out_stride[i], p.k_to[i] = c->k_out_stride[i];
     if (p.q_in[i] < 0 || p.k_in[i] < 0 || p.q_to[i] < 0 || p.k_to[i] < 0) return STAND_E_ARG;
   }
+  const RowSet q = heads_of(dev_q, c->B, c->N, c->heads_q, p.q_in, c->dim, es), k = heads_of(dev_k, c->B, c->N, c->heads_kv, p.k_in, c->dim, es);
+  const RowSet qo = heads_of(dev_q_out, c->B, c->N, c->heads_q, p.q_to, c->dim, es), ko = heads_of(dev_k_out, c->B, c->N, c->heads_kv, p.k_to, c->dim, es);
+  if (stacked(qo) || stacked(ko) || (rows_meet(qo, q) && !same_rows(qo, q)) || (rows_meet(ko, k) && !same_rows(ko, k)) || rows_meet(qo, k) || rows_meet(ko, q))
+    return STAND_E_ARG;
+  // the same rows twice, to the same place: each is written twice alike
+  if (rows_meet(qo, ko) && !(same_rows(qo, ko) && same_rows(q, k) && dev_weight_q == dev_weight_k)) return STAND_E_ARG;
   p.q = dev_q; p.k = dev_k; p.q_out = dev_q_out; p.k_out = dev_k_out; p.weight_q = dev_weight_q; p.weight_k = dev_weight_k;
   p.B = c->B; p.N = c->N; p.heads_q = c->heads_q; p.heads = c->heads_q + c->heads_kv;
   // (a step past the last row is at most 256 rows, of heads or tokens, further)
@@ -489,6 +515,10 @@ int stand_kv_append(const stand_kv_rows* c, const void* dev_k, const void* dev_v
     p.k_in[i] = c->k_stride[i], p.v_in[i] = c->v_stride[i], p.to[i] = c->cache_stride[i] * (c->packed ? 1 : es);
     if (p.k_in[i] < 0 || p.v_in[i] < 0 || p.to[i] < 0) return STAND_E_ARG;
   }
+  const RowSet ck = cache_of(c, dev_cache_k, p.to, es), cv = cache_of(c, dev_cache_v, p.to, es);
+  for (const RowSet& from : {rows_of(dev_k, c->layers, c->B, c->N, c->heads, p.k_in, c->dim, es), rows_of(dev_v, c->layers, c->B, c->N, c->heads, p.v_in, c->dim, es)})
+    if (rows_meet(from, ck) || rows_meet(from, cv)) return STAND_E_ARG;
+  if (stacked(ck)) return STAND_E_ARG;
   p.k = dev_k; p.v = dev_v; p.weight = dev_weight_k; p.path = dev_path; p.slots = (const long long*)dev_slots;
   p.cache_k = (char*)dev_cache_k; p.cache_v = (char*)dev_cache_v;
   p.layers = c->layers; p.N = c->N; p.width = c->width; p.heads = c->heads; p.page = c->page_size; p.places = (long long)c->B * c->width;
@@ -518,6 +548,11 @@ int stand_kv_read(const stand_kv_rows* c, const void* dev_cache_k, const void* d
     p.from[i] = c->cache_stride[i] * (c->packed ? 1 : es);
     if (p.from[i] < 0) return STAND_E_ARG;
   }
+  const RowSet ck = cache_of(c, dev_cache_k, p.from, es), cv = cache_of(c, dev_cache_v, p.from, es);
+  const int64_t all = (int64_t)c->layers * c->B * c->width * c->heads * c->dim * es;
+  const RowSet k = {dev_k, all, 0, {}, {}}, v = {dev_v, all, 0, {}, {}};
+  if (rows_meet(k, ck) || rows_meet(k, cv) || rows_meet(v, ck) || rows_meet(v, cv)) return STAND_E_ARG;
+  if (rows_meet(k, v) && !(dev_k == dev_v && same_rows(ck, cv))) return STAND_E_ARG;
   p.cache_k = (const char*)dev_cache_k; p.cache_v = (const char*)dev_cache_v; p.slots = (const long long*)dev_slots; p.k_out = dev_k; p.v_out = dev_v;
   p.layers = c->layers; p.heads = c->heads; p.dim = c->dim; p.page = c->page_size; p.lanes = row_lanes(c->dim);
   p.places = (long long)c->B * c->width; p.n_slots = (long long)c->pages * c->page_size;

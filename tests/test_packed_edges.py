@@ -6,6 +6,7 @@ Oracles and tolerances are those of test_packed_cache.py and test_serving.py, wh
 import ctypes as C
 import os
 import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -218,3 +219,133 @@ def test_caches_may_be_missing_only_where_there_are_no_pages(lib):
         for pages in (1, 5):
             assert lib.stand_kv_append(C.byref(tp._rows(packed=packed, pages=pages)), A, A, A, A, A, A, A, A, None, B2, None) == -1
             assert lib.stand_kv_read(C.byref(tp._rows(packed=packed, pages=pages, N=0, rotary_dim=0, norm=0, eps=0.0)), B2, None, A, A, A, None) == -1
+
+
+# ---------------------------------------------------------------- rows laid over others
+def _bytes_of(at, row, dims):
+    """Every byte of rows, once for each time that it is one."""
+    a = np.array([at], np.int64)
+    for count, stride in dims:
+        a = (a[:, None] + np.arange(count) * stride).ravel()
+    return (a[:, None] + np.arange(row)).ravel()
+
+
+def test_rows_that_meet_are_found(tmp_path):
+    """Against the bytes themselves: dimensions inside one another, in any order, of equal and of other strides, rows between other rows."""
+    exe = str(tmp_path / "rows_meet")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-o", exe, os.path.join(ROOT, "tests", "rows_meet.cpp")], check=True)
+    rng = np.random.default_rng(0)
+    lines, want, met = [], [], 0
+
+    def layout(row):
+        """A nested layout of 0 .. 4 dimensions, in any order."""
+        size, out = row, []
+        for _ in range(rng.integers(0, 5)):
+            count = int(rng.integers(1, 5))
+            stride = size + int(rng.choice([0, 0, 1, size, 2 * size, 7]))
+            out.append((count, stride))
+            size = stride * count
+        return [out[i] for i in rng.permutation(len(out))]
+
+    for i in range(6000):
+        row = int(rng.integers(1, 9))
+        x = layout(row)
+        kind = rng.integers(0, 3)
+        y = [(int(rng.integers(1, c + 1)), s) for c, s in x] if kind == 0 else (x if kind == 1 else layout(row))  # slices of one tensor, the same shape, another one
+        other = row if kind else int(rng.integers(1, row + 1))
+        far = 1 + sum((c - 1) * s for c, s in x) + row
+        at = 10**6, 10**6 + int(rng.integers(-far, far + 1)) * int(rng.random() < 0.95)
+        for a, r, dims in ((at[0], row, x), (at[1], other, y)):
+            lines.append(f"{a} {r} {len(dims)} " + " ".join(f"{c} {s}" for c, s in dims))
+        meet = bool(np.intersect1d(_bytes_of(at[0], row, x), _bytes_of(at[1], other, y)).size)
+        met += meet
+        alike = at[0] == at[1] and row == other and len(x) == len(y) and all(c == d and (c == 1 or s == t) for (c, s), (d, t) in zip(x, y))
+        want.append((meet, alike))
+    # far apart, long and with strides of 0; layouts that are not decided (three strides of no order among one another) are not said to meet
+    for a, b, meet in (("4096 256 3 64 1048576 4096 2048 40 256", "14336 256 3 64 1048576 4096 2048 8 256", True), ("0 256 2 2147483647 10240 32 256", "8192 256 2 2147483647 10240 8 256", False),
+                       ("0 256 2 2147483647 10240 33 256", "8192 256 2 2147483647 10240 8 256", True), ("0 8 1 5 0", "4 8 0", True), ("0 8 2 0 64 5 8", "0 8 0", False),
+                       ("0 1 3 1000 1000003 1000 1000033 1000 1000037", "7 1 3 1000 1000081 1000 1000099 1000 1000117", None)):
+        lines += [a, b]
+        want.append((meet, False))
+    got = subprocess.run([exe], input="\n".join(lines), check=True, capture_output=True, text=True).stdout.split()
+    assert len(got) == len(want) and 1000 < met < 5000
+    for i, (g, (meet, alike)) in enumerate(zip(got, want)):
+        assert (meet is None or g[0] == str(int(meet))) and g[1] == str(int(alike)), (i, lines[2 * i:2 * i + 2], g, meet, alike)
+
+
+def test_rows_laid_over_others_are_refused(lib):
+    """At the C interface; no call here gets as far as a launch."""
+    at = lambda n: C.c_void_p(0x1000000 + 2 * n)  # noqa: E731  (elements of 16 bits)
+    far = C.c_void_p(0x9000000)
+    one = dict(B=2, N=3, heads_q=4, heads_kv=2, dim=64, rotary_dim=64, norm=0, eps=0.0)
+    side = (3 * 8 * 64, 8 * 64, 64)  # a projection of 4 + 2 + 2 heads
+    own = {4: (768, 256, 64), 2: (384, 128, 64)}
+
+    def rotate(q, k, qo, ko, qs=side, ks=side, qos=side, kos=side, **kw):
+        s = tp._rotation(**dict(one, **kw), q_stride=qs, k_stride=ks, q_out_stride=qos, k_out_stride=kos)
+        return lib.stand_rotate_heads(C.byref(s), q, k, None, None, far, None, None, qo, ko, None)
+
+    q, k, v = at(0), at(256), at(384)
+    apart = dict(qos=own[4], kos=own[2])
+    for bad in (dict(qo=k, ko=far, kos=own[2]), dict(qo=far, qos=own[4], ko=q), dict(qo=at(64), ko=far, kos=own[2]), dict(qo=q, qos=own[4], ko=far, kos=own[2]),
+                dict(qo=at(32), ko=far, kos=own[2]), dict(qo=v, ko=v), dict(qo=q, ko=at(320)), dict(qo=at(3 * 8 * 64), ko=far, kos=own[2]),
+                dict(qo=far, qos=own[4], ko=C.c_void_p(0x9000000 + 128), kos=own[2]), dict(qo=far, qos=(0, 256, 64), ko=q, kos=side),
+                dict(qo=far, qos=(768, 256, 0), ko=at(4096), kos=own[2]), dict(qo=at(4096), qos=own[4], ko=far, kos=(0, 128, 64))):
+        assert rotate(**dict(dict(q=q, k=k), **bad)) == -1, bad
+    assert rotate(q=q, k=q, qo=q, ko=far, kos=own[2]) == -1  # in place, but the keys are the same rows
+    # keys written twice from rows that are not the same
+    assert rotate(q=q, k=at(128), qo=far, ko=far, heads_q=2, qos=own[2], kos=own[2]) == -1
+
+    rows = dict(layers=2, B=2, N=3, heads=2, dim=64, page_size=16, pages=5, norm=0, rotary_dim=0, eps=0.0)
+    src = (2 * 3 * 2 * 64, 3 * 2 * 64, 2 * 64, 64)
+    for packed, stride, size in ((0, (5 * 2 * 16 * 64, 2 * 16 * 64, 16 * 64, 64), 2 * 5 * 2 * 16 * 64), (1, (5 * 2 * 576, 2 * 576, 576, 0), 2 * 5 * 288)):
+
+        def append(k, v, ck, cv, cache=stride):
+            s = tp._rows(**dict(rows, packed=packed), k_stride=src, v_stride=src, cache_stride=cache)
+            return lib.stand_kv_append(C.byref(s), k, v, None, None, None, None, None, A, ck, cv, None)
+
+        A = C.c_void_p(0x8000000)
+        for bad in (dict(k=at(0), v=far, ck=at(0), cv=A), dict(k=far, v=at(64), ck=A, cv=at(0)), dict(k=at(size - 64), v=far, ck=A, cv=at(0)), dict(k=far, v=at(0), ck=at(768), cv=A),
+                    dict(k=far, v=far, ck=at(0), cv=at(0), cache=(0,) + stride[1:]), dict(k=far, v=far, ck=at(0), cv=at(0), cache=stride[:2] + (0,) + stride[3:])):
+            assert append(**bad) == -1, bad
+
+        def read(k, v, ck, cv):
+            s = tp._rows(**dict(rows, packed=packed, N=0), cache_stride=stride)
+            return lib.stand_kv_read(C.byref(s), ck, cv, A, k, v, None)
+
+        for bad in (dict(k=at(0), v=far, ck=at(0), cv=A), dict(k=far, v=at(size - 8), ck=A, cv=at(0)), dict(k=far, v=C.c_void_p(0x9000000 + 128), ck=at(0), cv=at(0)),
+                    dict(k=far, v=far, ck=at(0), cv=at(65536))):
+            assert read(**bad) == -1, bad
+
+
+@pytest.mark.gpu
+def test_rows_between_others_are_written():
+    """Results beside inputs in one tensor, row by row; in place; the same rows to the same place twice."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    B, N, hq, hkv, dim = 3, 5, 4, 2, 64
+    buf = torch.randn((B, N, 2 * (hq + hkv), dim), device=DEV).bfloat16()
+    q, k, qo, ko = buf.split([hq, hkv, hq, hkv], 2)
+    op = serving.HeadRotation(B, N, hq, hkv, dim, torch.bfloat16, freq=torch.ones(32, device=DEV))
+    want = [t.clone() for t in op(q.contiguous(), k.contiguous())]
+    before = q.clone(), k.clone()
+    op(q, k, q_out=qo, k_out=ko)
+    assert torch.equal(qo, want[0]) and torch.equal(ko, want[1]) and torch.equal(q, before[0]) and torch.equal(k, before[1])
+    op(q, k, q_out=qo, k_out=k)  # one in place
+    assert torch.equal(qo, want[0]) and torch.equal(k, want[1])
+    with pytest.raises(binding.StandError):
+        op(q, k, q_out=buf[:, :, 1:1 + hq], k_out=ko)
+    same = serving.HeadRotation(B, N, hkv, hkv, dim, torch.bfloat16, freq=torch.ones(32, device=DEV))
+    one = same(before[1], before[1], q_out=ko, k_out=ko)[0]
+    assert torch.equal(one, want[1])
+    # a layer's rows between the pages of a cache that they go to
+    arena = torch.zeros((1, 4, 2, 16 * dim + dim), dtype=torch.bfloat16, device=DEV)
+    cache, rows = arena[..., :16 * dim].unflatten(-1, (16, dim)), arena[..., 16 * dim:][:, :, None]
+    rows.copy_(torch.randn(rows.shape, device=DEV))
+    other = torch.zeros((1, 4, 2, 17 * dim), dtype=torch.bfloat16, device=DEV)[..., :16 * dim].unflatten(-1, (16, dim))
+    slots = torch.tensor([[3], [40], [17], [50]], device=DEV)
+    serving.KvAppend(1, 4, 1, 2, dim, torch.bfloat16, 16, 4, 1)(rows, rows, slots, cache, other)
+    for b, s in enumerate((3, 40, 17, 50)):
+        assert torch.equal(cache[0, s // 16, :, s % 16], rows[0, b, 0]) and torch.equal(other[0, s // 16, :, s % 16], rows[0, b, 0])
+    with pytest.raises(binding.StandError):
+        serving.KvRead(1, 4, 2, dim, torch.bfloat16, 16, 4, 1)(slots, cache, cache, k=arena.flatten()[:512].view(1, 4, 1, 2, dim))
