@@ -489,7 +489,7 @@ typedef struct {
  *   y = norm ? x / sqrt(mean(x^2) + eps) * weight : x
  *   (a, b) of pair i becomes (a cos t - b sin t, a sin t + b cos t),  t = (dev_base[b] + dev_offset[b, n]) * dev_freq[i]
  * with the angle worked out in 64 bits (positions up to 2^31 in magnitude).  dev_weight_q, dev_weight_k [dim] of the rows' type (NULL: ones).
- * dev_freq [rotary_dim / 2] float.  dev_base [B] int64 (NULL: 0) is what a sequence's positions begin with, dev_offset int32 what a node adds:
+ * A row whose squares go beyond 32-bit floats comes out as zeros.  dev_freq [rotary_dim / 2] float.  dev_base [B] int64 (NULL: 0) is what a sequence's positions begin with, dev_offset int32 what a node adds:
  * [N] or [B, N] (NULL: its number n).  Outputs have no stride of 0 (dimensions of one aside); they may be the inputs themselves (same pointer and strides) and must not
  * overlap them, nor one another, otherwise (STAND_E_ARG, as below, where strides from the largest down cover the smaller ones). */
 int stand_rotate_heads(const stand_rotation* shape, const void* dev_q, const void* dev_k, const void* dev_weight_q,
@@ -528,8 +528,10 @@ int stand_kv_read(const stand_kv_rows* shape, const void* dev_cache_k, const voi
 
 /* stand_tree_attention over packed caches: the same shapes, arguments, scratch and results, with cached keys and values what
  * their codes stand for.  dim is a multiple of 16; cache_stride: page and head in bytes (multiples of 16), then 0; caches
- * begin at multiples of 16 bytes.  The nodes' own keys and values are of type dtype.  In 16-bit calls the softmax weights of cached
- * tokens are halves where they multiply the values: those below 2^-32 of a row's largest may count as 0. */
+ * begin at multiples of 16 bytes.  The nodes' own keys and values are of type dtype.  In 16-bit calls the softmax weights are rounded to 16 bits where
+ * they multiply the values, as there: to the call's type, but to halves for cached tokens where a key head has at most 16 rows (nodes times its
+ * query heads) and dim is 64 or 128; halves below 2^-32 of a row's largest weight may count as 0.  In those calls elements of bfloat16
+ * queries lose bits below 2^-29 of their row's largest, and those below 2^-39 may count as 0. */
 int stand_packed_tree_attention(const stand_attention* shape, const void* dev_q, const void* dev_k, const void* dev_v,
                                 const void* dev_cache_k, const void* dev_cache_v, const int32_t* dev_table,
                                 const int64_t* dev_len, const uint32_t* dev_mask, int64_t mask_stride,

@@ -18,9 +18,9 @@
 // a power of two of their own; weights are halves with the lift that TA_LIFT describes.  The nodes' own keys and values are of the call's type, and so are the
 // products with them.
 //
-// Measured, 32 / 8 heads of 128, bfloat16: 64 single tokens over 500 - 8,000 94 us = 3.3 TB/s (floor 48), 256 over 130 - 4,100 186 us, 64 sequences of 4 nodes
-// 136 us, one token over 700 9.7 us; heads of 64 in half 61 us for 64 tokens.  Bound by issue: the logic unit at 45 % and the half products at 48 % share
-// it, and with all pages in L2 the first case takes 88 us.  Products of two or three tiles interleaved, and sums beside the next scores: no change.
+// Measured, 32 / 8 heads of 128, bfloat16: 64 single tokens over 500 - 8,000 91 us = 3.4 TB/s (floor 48), 256 over 130 - 4,100 182 us, 64 sequences of 4 nodes
+// 136 us, one token over 700 9.7 us; heads of 64 in half 60 us for 64 tokens.  Bound by issue: the logic unit at 45 % and the half products at 48 % share
+// it, and with all pages in L2 the first case took 88 us where it took 94 without.  Products of two or three tiles interleaved, and sums beside the next scores: no change.
 #pragma once
 #include "async.cuh"
 #include "attention_plain.cuh"

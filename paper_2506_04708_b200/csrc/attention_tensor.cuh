@@ -33,9 +33,9 @@
 // PACKED: the cache is in 4 bits.  Ten warps: 0-3 as above; 4, 5 make a tile's keys and 6, 7 its values from codes, each half a tile, in the places
 // that TMA fills otherwise; 8 issues the products; 9 copies codes and scales, tiles ahead, into stages of 9 bytes for 16 elements (and has TMA fetch the
 // tree's own).  What the unpacking warps write and the products read meets at the same barriers, after a fence between the two kinds of access.  A key's values
-// are exact in 16 bits, so the products are those of the definition.
-// Measured: 256 x 24 nodes as above: 378 us in short bursts, 440 in loops of seconds (floor 128: products; with a cache of 16 bits 400 and 469); 64 nodes over
-// 32,001: 60 us (floor 18); 16 x 32 nodes, 16 / 16 heads of 64, half, 1 - 8,190: 62 us; 64 x 24 of 16 / 4 heads of 256: 127 us.  Memory is no longer the
+// (in half: an eighth of them) are exact in 16 bits, so the products are those of the definition.
+// Measured: 256 x 24 nodes as above: 380 us in short bursts, 438 in loops of seconds (floor 128: products; with a cache of 16 bits 400 and 469), in half 388 - 396; 64 nodes over
+// 32,001: 61 us (floor 18; 16 bits 52); 16 x 32 nodes, 16 / 16 heads of 64, half, 1 - 8,190: 63 us (16 bits 59); 64 x 24 of 16 / 4 heads of 256: 129 us (118).  Memory is no longer the
 // bound (0.3 of a copy), the chain of a tile is, of 2,100 - 2,600 cycles with 96 registers a thread: tensor pipe 31 %, exponentials 24 %, logic unit 41 %,
 // issue 50 %, shared memory 57 %.  Codes read by the unpacking warps straight from memory took 664 us, bulk copies by one lane 387 (950 - 1,480 cycles
 // a tile to issue them); weights by the maximum of the tile before, in one pass over the scores, 495; scores kept in registers between the two passes 452.
@@ -53,7 +53,7 @@ constexpr int TA_ROWS = 128;              // rows of a CTA: lanes of tensor memo
 template <bool PACKED> constexpr int TA_THREADS_OF = PACKED ? 320 : 224;
 constexpr float TA_SLACK = 8.0f;          // the maximum is raised only when scores pass it by 2^8 (below)
 // Weights of the second product are rounded to the input's type, since both operands of a 16-bit product have one type: each
-// is off by 2^-9 (bfloat16) or 2^-12 (half) of itself at most, independently, which is what rounding the result costs anyway;
+// is off by 2^-8 (bfloat16) or 2^-11 (half) of itself at most, independently, which is what rounding the result costs anyway;
 // their sum l is taken before the rounding, in fp32.  Half has few exponents: there weights are 2^7 times larger (at most 2^15,
 // with the slack), as are l and o, so that those down to 2^-21 of the largest keep all bits and none above 2^-32 is lost
 // (unlifted, 40,000 keys of 2^-26 beside a dominant one were lost from o while they stayed in l).  Bfloat16 has the exponents of
@@ -673,7 +673,7 @@ __global__ void __launch_bounds__(TA_THREADS_OF<PACKED>, TaShape<DP, C, PACKED>:
           }
           top = fmaxf(top, top1) * by;
           // Any m near the maximum will do, since o and l carry the same factor: it is left where it is until scores pass
-          // it by TA_SLACK, so that o is seldom read, scaled and written (TA_LIFT keeps the weights within their type).  The warp's rows move together, as live rows want it: what lies in the lanes of others is
+          // it by SLACK, so that o is seldom read, scaled and written (TA_LIFT keeps the weights within their type).  The warp's rows move together, as live rows want it: what lies in the lanes of others is
           // left from earlier kernels or belongs to nodes that were not drafted, and would enter the roundings of the weights.
           if (__any_sync(FULL, live && top > m + SLACK)) {
             const float raised = fmaxf(m, top);

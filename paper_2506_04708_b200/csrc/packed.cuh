@@ -6,7 +6,8 @@
 // s is the smallest with 7 s >= the group's largest magnitude, k the nearest whole number (even in a tie).  Exponent 31: not finite,
 // the whole group reads as NaN.
 // Four bytes hold 8 elements: the even ones in the low half, the odd ones in the high half, each from the low bits on, so that one
-// mask brings two neighbours into the two halves of a word.
+// mask brings two neighbours into the two halves of a word.  (Codes in the last bits of a float that begins at a power of two, less that power: published for
+// weights of 4 bits by Kim, Henry, Fahim and Awadalla, arXiv 2211.10017.  Layout, powers and scales are this form's.)
 // A block is one head's tokens of one page: the codes of all tokens (dim / 2 bytes each), then their scales (dim / 16 each).
 #pragma once
 #include <cuda_bf16.h>

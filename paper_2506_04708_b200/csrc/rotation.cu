@@ -149,7 +149,7 @@ struct AppendParams {
 };
 
 // As above, with a token's place in the cache and angles worked out once for all layers of a block.  1,100 tokens of three prompts in 32 layers, 8 heads of
-// 128 in bfloat16, norm and turn, to 4 bits: 55 us (floor 27), to a cache of their own type 55 us (floor 43); layer after layer in blocks of their own
+// 128 in bfloat16, norm and turn, to 4 bits: 54 us (floor 27), to a cache of their own type 54 us (floor 43); layer after layer in blocks of their own
 // it took 81 and 65.  In 4 bits the kernel is bound by issue (69 % of its slots, logic unit 48 %): the maximum of 16, a scale, 16 codes and their
 // place in two words cost about as much again as norm and turn.
 // Packed: a lane takes a group of 16 elements.  Where units are such groups they stay in registers; else (halves that are turned, short units) the

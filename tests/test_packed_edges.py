@@ -349,3 +349,23 @@ def test_rows_between_others_are_written():
         assert torch.equal(cache[0, s // 16, :, s % 16], rows[0, b, 0]) and torch.equal(other[0, s // 16, :, s % 16], rows[0, b, 0])
     with pytest.raises(binding.StandError):
         serving.KvRead(1, 4, 2, dim, torch.bfloat16, 16, 4, 1)(slots, cache, cache, k=arena.flatten()[:512].view(1, 4, 1, 2, dim))
+
+
+# ---------------------------------------------------------------- rows beyond the range of sums
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_whose_squares_pass_the_range_come_out_as_zeros(dtype):
+    """As the contract says; the other rows are what they are without them, and rows just within it are normalised."""
+    import torch
+    from paper_2506_04708_b200 import serving
+    x = torch.from_numpy(np.random.default_rng(2).standard_normal((1, 6, 2, 64)).astype(np.float32)).to(ts._dtype(dtype)).to(DEV)
+    op = serving.HeadRotation(1, 6, 2, 2, 64, x.dtype, freq=torch.ones(32, device=DEV), norm=True)
+    clean = op(x, x)[0].clone()
+    x[0, 1, 0] *= 2.0**100
+    x[0, 2, 1] *= 2.0**50  # squares of up to 2^104, 64 of them
+    got = op(x, x)[0].clone()
+    assert not got[0, 1, 0].any()
+    want, size = pref.rotate(x[0, 2, 1].double().cpu().numpy()[None], np.array([2]), np.ones(32, np.float32), False, None, 1e-6)
+    tp._near(got[0, 2, 1].double().cpu().numpy()[None], want, size, dtype, True)
+    got[0, 1, 0], got[0, 2, 1] = clean[0, 1, 0], clean[0, 2, 1]
+    assert torch.equal(got, clean)
